@@ -301,6 +301,125 @@ int dd_sparse_decode_attn_static(int batch, int n_q_heads, int n_kv_heads, int h
                                  int k_pages, int n_q_tokens, int n_splits, const void* q, const void* slot,
                                  const int* idx, const int* ctx_len, void* out, float* out_lse, void* stream);
 
+/* ---- the paged key-value cache: rotary positions, writing, reading back, attention over all of it -------------- */
+
+/* These calls need no context: the method's path reads a store of final keys and values; what follows puts keys and
+ * values into such a store (or any paged cache), brings pages back, and attends to every cached token where a layer is
+ * not sparse. Asynchronous on `stream`; nothing is allocated; every pointer is checked on the host before a launch and
+ * has to belong to the current device. Errors: DD_ERR_INVALID_ARG / DD_ERR_NOT_PINNED / DD_ERR_CUDA, the text from
+ * dd_last_error_message(NULL) on the calling thread. head_dim 64 or 128. */
+
+#define DD_BF16 0
+#define DD_FP16 1
+
+#define DD_CACHE_BF16 0
+#define DD_CACHE_FP16 1
+#define DD_CACHE_E4M3 2   /* 8-bit floating point, one power-of-two scale per token and head */
+
+#define DD_ROPE_HALF        0   /* element i turns with element i + rot_dim/2 */
+#define DD_ROPE_INTERLEAVED 1   /* element 2i turns with element 2i + 1 */
+
+#define DD_ROPE_NONE     0
+#define DD_ROPE_LINEAR   1      /* every frequency divided by factor */
+#define DD_ROPE_NTK      2      /* base multiplied by factor^(r / (r - 2)), r = rot_dim */
+#define DD_ROPE_BY_PARTS 3      /* by the whole turns a pair makes within original_len positions */
+
+/* Rows of a tensor [tokens][heads][head_dim]: the head_dim elements of a row are adjacent, token and head strides are free
+ * (in elements, multiples of 8, not negative), so slices of a fused projection's output need no copy. */
+typedef struct dd_rows {
+  void* data;                 /* dev, 16-byte aligned: row (token 0, head 0) */
+  int dtype;                  /* DD_BF16 or DD_FP16 */
+  int n_heads;
+  long long token_stride, head_stride;
+} dd_rows;
+
+/* Rotary positions: pair i of a row at position p is turned by p * turns[i] whole turns and multiplied by amplitude;
+ * elements from rot_dim on are copied. rot_dim is a multiple of 16, at most head_dim. */
+typedef struct dd_rope {
+  const double* turns;        /* dev [rot_dim / 2], 8-byte aligned; filled from dd_rope_turns */
+  int rot_dim;
+  int layout;                 /* DD_ROPE_HALF or DD_ROPE_INTERLEAVED */
+  float amplitude;
+} dd_rope;
+
+/* A pool of pages and the block tables of the requests that live in it. A page holds page_tokens tokens of one KV head:
+ *   DD_CACHE_BF16 / FP16   K [page_tokens][head_dim], then V [page_tokens][head_dim]
+ *   DD_CACHE_E4M3          the codes of K, the codes of V (same order, one byte each), the exponent bytes of K
+ *                          [page_tokens], the exponent bytes of V; a value is code * 2^(byte - 127)
+ * Page (block, head) starts at data + block * block_stride + head * head_stride (bytes, multiples of 16). A layer of the
+ * method's store [B][Hkv][P][page] is such a pool: block = b * Hkv * P + p with block_stride = page bytes, head_stride =
+ * P * page bytes, n_blocks = (B - 1) * Hkv * P + P. */
+typedef struct dd_cache {
+  void* data;                 /* dev; dd_cache_append and dd_cache_read also take page-locked host memory */
+  int format;                 /* DD_CACHE_* */
+  int n_kv_heads;
+  int head_dim;               /* 64 or 128 */
+  int page_tokens;            /* 16, 32, 64, 128 or 256 */
+  int n_blocks;
+  long long block_stride, head_stride;
+  const int* block_table;     /* dev int32 [batch][table_stride]: block of every page of every request */
+  int batch;
+  int max_pages;              /* entries of a table row that may be used */
+  long long table_stride;     /* elements between table rows, >= max_pages */
+  int* status;                /* dev int32 [2] or NULL. {DD_ERR_INDEX_RANGE, value} once a kernel has met a block, page,
+                                 request or length out of range; the caller clears it */
+} dd_cache;
+
+/* Bytes of one page, 0 for a combination that is not supported. */
+size_t dd_cache_page_bytes(int format, int page_tokens, int head_dim);
+
+/* Turns per position of every pair, on the host in 64 bits: turns[i] = f_i / 2 pi with f_i = base^(-2i / rot_dim), scaled for
+ * longer contexts. DD_ROPE_BY_PARTS: a pair that makes at most low_turns turns within original_len positions is slowed
+ * by factor, one that makes at least high_turns is kept, linear in the number of turns between. factor, original_len,
+ * low_turns and high_turns are used by the scalings that name them. */
+int dd_rope_turns(int rot_dim, double base, int scaling, double factor, double original_len, double low_turns,
+                  double high_turns, double* turns);
+
+/* Turns the rows of q and of k (either may be NULL, with its output) of n_tokens tokens:
+ *   out[n, h, :] = amplitude * R(positions[n]) in[n, h, :]
+ * in 32 bits, the angles in 64, rounded once. An output may be its own input. backward = 1 applies the transpose: the
+ * gradient of the call with backward = 0. A token with a negative position is padding: its output rows stay as they are.
+ *   positions  dev int32 [n_tokens] */
+int dd_rope_apply(const dd_rope* rope, int head_dim, int n_tokens, const int* positions, const dd_rows* q, const dd_rows* k,
+                  const dd_rows* q_out, const dd_rows* k_out, int backward, void* stream);
+
+/* Writes the K and V rows of n_tokens new tokens into their pages: token n belongs to request requests[n] and lands at
+ * position positions[n] of it. DD_CACHE_E4M3: the exponent of a row is the smallest e >= -127 with which its largest
+ * finite magnitude is at most 448 * 2^e, a code is the value times 2^-e (exact) rounded to nearest even; infinities and
+ * NaN become the NaN code. With `rope` the keys are turned on the way (32 bits, rounded once, into the page), and with q /
+ * q_out the queries of the same tokens are turned in the same launch. A negative position is padding: nothing of that
+ * token is written. A request, page or block out of range is reported in status and the token skipped. Two tokens of one
+ * call must not name the same place: which of them the page then holds (in parts) is not defined.
+ *   positions, requests  dev int32 [n_tokens]; requests NULL = n_tokens / batch tokens of each request in turn
+ *   k, v                 dev [n_tokens][n_kv_heads][head_dim]; 16-bit caches take rows of their own type */
+int dd_cache_append(const dd_cache* cache, int n_tokens, const int* positions, const int* requests, const dd_rows* k,
+                    const dd_rows* v, const dd_rope* rope, const dd_rows* q, const dd_rows* q_out, void* stream);
+
+/* Reads pages back in attention layout (the layout of a ring slot):
+ *   out[b][g][0|1][j * page_tokens + i][:] = K | V of token i of page idx[b][g][j] of request b, KV head g
+ * A page that is out of range (or whose table entry is) is reported in status and reads as zeros.
+ *   idx  dev int32 [batch][n_kv_heads][k_pages]
+ *   out  dev [batch][n_kv_heads][2][k_pages * page_tokens][head_dim], out_dtype; 16-bit caches give their own type */
+int dd_cache_read(const dd_cache* cache, const int* idx, int k_pages, void* out, int out_dtype, void* stream);
+
+/* Attention of the last n_q_tokens tokens of every request over all of its cached tokens (their own keys and values are in
+ * the cache already): query token t of request b stands at position ctx_len[b] - n_q_tokens + t and sees the positions up
+ * to its own, with window > 0 only the last `window` of them.
+ *   z[n]   = <q[b*n_q_tokens + t, h, :], K[n, h / G, :]> * scale        scale 0 = 1 / sqrt(head_dim)
+ *   out    = sum softmax(z) * V;  out_lse = ln sum exp(z)
+ * A query token before the request's beginning (ctx_len < n_q_tokens; empty requests) gives zeros and -inf. What lies in
+ * the pages behind ctx_len is never used, whatever its bits. Any number of query heads per KV head, any ctx_len up to
+ * max_pages * page_tokens (more is reported in status and cut; a negative one counts as 0); a table entry out of range is
+ * reported and its page reads as zeros. Only entries of pages that hold a visible token are read.
+ *   q, out     dev [batch * n_q_tokens][n_q_heads][head_dim], one dtype (that of a 16-bit cache)
+ *   ctx_len    dev int32 [batch]
+ *   out_lse    dev fp32 [batch * n_q_tokens][n_q_heads] or NULL
+ *   workspace  dev, dd_cache_decode_attn_workspace() bytes, 16-byte aligned, contents irrelevant. Calls that may run at
+ *              the same time (other streams, other graphs) need one each. */
+size_t dd_cache_decode_attn_workspace(int n_q_heads, int n_kv_heads, int head_dim, int n_q_tokens);
+int dd_cache_decode_attn(const dd_cache* cache, int n_q_tokens, const dd_rows* q, const int* ctx_len, const dd_rows* out,
+                         float* out_lse, int window, float scale, void* workspace, size_t workspace_bytes, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

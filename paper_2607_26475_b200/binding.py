@@ -35,6 +35,17 @@ DD_ATTN_STREAM = 2
 DD_ATTN_TC = 3
 DD_SELECT_AUTO = 0
 DD_SELECT_TWO_KERNELS = 1
+DD_BF16 = 0
+DD_FP16 = 1
+DD_CACHE_BF16 = 0
+DD_CACHE_FP16 = 1
+DD_CACHE_E4M3 = 2
+DD_ROPE_HALF = 0
+DD_ROPE_INTERLEAVED = 1
+DD_ROPE_NONE = 0
+DD_ROPE_LINEAR = 1
+DD_ROPE_NTK = 2
+DD_ROPE_BY_PARTS = 3
 
 EXPORTS = [
     "dd_create", "dd_destroy", "dd_slot_bytes", "dd_ring_bytes", "dd_scratch_bytes", "dd_slot_ptr",
@@ -45,6 +56,8 @@ EXPORTS = [
     "dd_fetch_missing_from_host", "dd_get_merged_indices", "dd_miss_stats", "dd_probe_attn_loads", "dd_probe_select_loads",
     "dd_trace_begin", "dd_trace_end", "dd_trace_read", "dd_decode_step_host", "dd_last_device_error",
     "dd_gather_stats", "dd_set_bulk_wait", "dd_test_pick_cluster", "dd_test_stage_plan", "dd_test_attn_split",
+    "dd_cache_page_bytes", "dd_rope_turns", "dd_rope_apply", "dd_cache_append", "dd_cache_read",
+    "dd_cache_decode_attn_workspace", "dd_cache_decode_attn",
 ]
 
 
@@ -60,6 +73,25 @@ class DDConfig(C.Structure):
         ("landmark_chunk_tokens", C.c_int), ("miss_correction", C.c_int), ("urgent_stream", C.c_void_p),
         ("select_stream", C.c_void_p), ("stage_min_run_pages", C.c_int), ("stage_block_pages", C.c_int), ("attn_mode", C.c_int),
     ]
+
+
+class DDRows(C.Structure):
+    """Mirror of `dd_rows`."""
+    _fields_ = [("data", C.c_void_p), ("dtype", C.c_int), ("n_heads", C.c_int), ("token_stride", C.c_longlong),
+                ("head_stride", C.c_longlong)]
+
+
+class DDRope(C.Structure):
+    """Mirror of `dd_rope`."""
+    _fields_ = [("turns", C.c_void_p), ("rot_dim", C.c_int), ("layout", C.c_int), ("amplitude", C.c_float)]
+
+
+class DDCache(C.Structure):
+    """Mirror of `dd_cache`."""
+    _fields_ = [("data", C.c_void_p), ("format", C.c_int), ("n_kv_heads", C.c_int), ("head_dim", C.c_int),
+                ("page_tokens", C.c_int), ("n_blocks", C.c_int), ("block_stride", C.c_longlong), ("head_stride", C.c_longlong),
+                ("block_table", C.c_void_p), ("batch", C.c_int), ("max_pages", C.c_int), ("table_stride", C.c_longlong),
+                ("status", C.c_void_p)]
 
 
 class DDError(RuntimeError):
@@ -123,6 +155,16 @@ def _load() -> C.CDLL:
     lib.dd_static_scratch_capacity.argtypes = []
     lib.dd_static_scratch_capacity.restype = C.c_size_t
     lib.dd_sparse_decode_attn_static.argtypes = [ip] * 8 + [vp] * 7
+    rows, rope, cache = C.POINTER(DDRows), C.POINTER(DDRope), C.POINTER(DDCache)
+    lib.dd_cache_page_bytes.argtypes = [ip, ip, ip]
+    lib.dd_cache_page_bytes.restype = C.c_size_t
+    lib.dd_rope_turns.argtypes = [ip, C.c_double, ip, C.c_double, C.c_double, C.c_double, C.c_double, C.POINTER(C.c_double)]
+    lib.dd_rope_apply.argtypes = [rope, ip, ip, vp, rows, rows, rows, rows, ip, vp]
+    lib.dd_cache_append.argtypes = [cache, ip, vp, vp, rows, rows, rope, rows, rows, vp]
+    lib.dd_cache_read.argtypes = [cache, vp, ip, vp, ip, vp]
+    lib.dd_cache_decode_attn_workspace.argtypes = [ip, ip, ip, ip]
+    lib.dd_cache_decode_attn_workspace.restype = C.c_size_t
+    lib.dd_cache_decode_attn.argtypes = [cache, ip, rows, vp, rows, vp, ip, C.c_float, vp, C.c_size_t, vp]
     return lib
 
 
@@ -171,6 +213,188 @@ def sparse_decode_attn_static(q, slot, idx, ctx_len, out, out_lse=None, *, n_spl
                                           _ptr(ctx_len), _ptr(out), _ptr(out_lse), _stream(stream))
     if rc != DD_OK:
         raise DDError(rc, lib.dd_last_error_message(None).decode())
+
+
+_ROW_TYPES = {torch.bfloat16: DD_BF16, torch.float16: DD_FP16}
+
+
+def _invalid(message: str) -> DDError:
+    return DDError(DD_ERR_INVALID_ARG, message)
+
+
+def _rows(t, name: str, head_dim: int, tokens: int | None = None):
+    """`dd_rows` of a tensor [tokens, heads, head_dim] whose rows are dense (slices of a larger tensor are fine)."""
+    if t is None:
+        return None
+    kind = _ROW_TYPES.get(t.dtype)
+    if kind is None:
+        raise _invalid(f"{name} must be bfloat16 or float16, not {t.dtype}")
+    if t.dim() != 3 or t.shape[2] != head_dim or (tokens is not None and t.shape[0] != tokens):
+        raise _invalid(f"{name} must be [{'tokens' if tokens is None else tokens}, heads, {head_dim}], not {tuple(t.shape)}")
+    token, head, one = t.stride()
+    if one != 1:
+        raise _invalid(f"the elements of a row of {name} must be adjacent")
+    # a stride that is never stepped over may be anything: hand on one that passes
+    return DDRows(t.data_ptr(), kind, t.shape[1], token if t.shape[0] > 1 else head_dim * t.shape[1], head if t.shape[1] > 1 else head_dim)
+
+
+def _ints(t, name: str, shape=None):
+    if t.dtype != torch.int32 or not t.is_contiguous() or (shape is not None and tuple(t.shape) != tuple(shape)):
+        raise _invalid(f"{name} must be a dense int32 tensor{'' if shape is None else ' of shape ' + str(tuple(shape))}, "
+                       f"not {t.dtype} {tuple(t.shape)}")
+    return t.data_ptr()
+
+
+def _raise_last(rc: int):
+    if rc != DD_OK:
+        raise DDError(rc, lib.dd_last_error_message(None).decode())
+
+
+class Rope:
+    """Rotary positions of one model: the turns per position of every pair (64 bits, on the device), the pair layout and the
+    amplitude. See `dd_rope_turns` for the scalings."""
+
+    def __init__(self, *, head_dim=128, rot_dim=None, base=10000.0, layout=DD_ROPE_HALF, scaling=DD_ROPE_NONE, factor=1.0,
+                 original_len=0.0, low_turns=1.0, high_turns=32.0, amplitude=1.0, device="cuda"):
+        self.head_dim, self.rot_dim = head_dim, head_dim if rot_dim is None else rot_dim
+        n = max(1, self.rot_dim // 2)
+        host = (C.c_double * n)()
+        _raise_last(lib.dd_rope_turns(self.rot_dim, base, scaling, factor, original_len, low_turns, high_turns, host))
+        self.turns_host = torch.tensor(list(host), dtype=torch.float64)
+        self.turns = self.turns_host.to(device)
+        self.c = DDRope(self.turns.data_ptr(), self.rot_dim, layout, amplitude)
+
+    def apply(self, positions, q, k, q_out=None, k_out=None, *, backward=False, stream=None):
+        """Turns q [N, Hq, d] and k [N, Hkv, d] (either may be None) by their positions [N] into q_out and k_out; without
+        an output, in place. backward: the transpose, i.e. the gradient with respect to the inputs."""
+        n = positions.shape[0]
+        rq, rk = _rows(q, "q", self.head_dim, n), _rows(k, "k", self.head_dim, n)
+        oq = _rows(q_out, "q_out", self.head_dim, n) if q_out is not None else rq
+        ok = _rows(k_out, "k_out", self.head_dim, n) if k_out is not None else rk
+        rc = lib.dd_rope_apply(self.c, self.head_dim, n, _ints(positions, "positions", (n,)), rq, rk, oq, ok,
+                               1 if backward else 0, _stream(stream))
+        _raise_last(rc)
+
+
+class PagedCache:
+    """A pool of KV pages and the block tables of the requests that live in it (`dd_cache`). Owns nothing but an error word.
+
+    data         [n_blocks, Hkv, ...]: each (block, head) one dense page of dd_cache_page_bytes() bytes; on the device, or
+                 page-locked host memory (append and read only)
+    block_table  [batch, max_pages] int32 on the device
+    """
+
+    def __init__(self, data, block_table, *, cache_format=DD_CACHE_BF16, head_dim=128, page_tokens=16, n_blocks=None,
+                 block_stride=None, head_stride=None, n_kv_heads=None):
+        page = lib.dd_cache_page_bytes(cache_format, page_tokens, head_dim)
+        if page == 0:
+            raise _invalid(f"format {cache_format} with {page_tokens} tokens of {head_dim} elements a page is not supported")
+        size = data.element_size()
+        if n_blocks is None:
+            if data.dim() < 3 or data[0, 0].numel() * size != page or not data[0, 0].is_contiguous():
+                raise _invalid(f"data must be [n_blocks, n_kv_heads, ...] with dense pages of {page} bytes, not {tuple(data.shape)}")
+            n_blocks, n_kv_heads = data.shape[0], data.shape[1]
+            block_stride = data.stride(0) * size if n_blocks > 1 else page * n_kv_heads
+            head_stride = data.stride(1) * size if n_kv_heads > 1 else page
+        if block_table.dtype != torch.int32 or block_table.dim() != 2 or (block_table.shape[1] > 1 and block_table.stride(1) != 1):
+            raise _invalid("block_table must be int32 [batch, max_pages] with dense rows")
+        batch, max_pages = block_table.shape
+        if batch < 1 or max_pages < 1:
+            raise _invalid("block_table is empty")
+        self.data, self.block_table = data, block_table
+        self.head_dim, self.page_tokens, self.cache_format = head_dim, page_tokens, cache_format
+        self.status = torch.zeros(2, dtype=torch.int32, device=block_table.device)
+        self.c = DDCache(data.data_ptr(), cache_format, n_kv_heads, head_dim, page_tokens, n_blocks, block_stride, head_stride,
+                         block_table.data_ptr(), batch, max_pages, block_table.stride(0) if batch > 1 else max_pages,
+                         self.status.data_ptr())
+        self._workspace_bytes = {}
+
+    @classmethod
+    def of_store(cls, kv_layer, *, cache_format=DD_CACHE_BF16, head_dim=128, page_tokens=16, device="cuda"):
+        """A layer of the method's store, [B, Hkv, P, ...] dense, seen as a cache: page p of request b is its page p."""
+        if kv_layer.dim() < 4 or not kv_layer.is_contiguous():
+            raise _invalid("kv_layer must be a dense [batch, n_kv_heads, max_pages, ...] tensor")
+        B, H, P = kv_layer.shape[:3]
+        page = lib.dd_cache_page_bytes(cache_format, page_tokens, head_dim)
+        if kv_layer[0, 0, 0].numel() * kv_layer.element_size() != page:
+            raise _invalid(f"the pages of kv_layer must hold {page} bytes")
+        table = (torch.arange(B, dtype=torch.int32).view(-1, 1) * (H * P) + torch.arange(P, dtype=torch.int32)).to(device)
+        return cls(kv_layer, table, cache_format=cache_format, head_dim=head_dim, page_tokens=page_tokens,
+                   n_blocks=(B - 1) * H * P + P, block_stride=page, head_stride=P * page, n_kv_heads=H)
+
+    def append(self, k, v, positions, requests=None, *, rope=None, q=None, q_out=None, stream=None):
+        """Writes k and v [N, Hkv, d] of N new tokens to position positions[n] of request requests[n] (None: N / batch tokens
+        of each request in turn); with `rope`, k is turned on the way and q [N, Hq, d] into q_out (None: in place)."""
+        n = positions.shape[0]
+        if rope is not None and rope.head_dim != self.head_dim:
+            raise _invalid("rope and cache differ in head_dim")
+        rq = _rows(q, "q", self.head_dim, n)
+        oq = _rows(q_out, "q_out", self.head_dim, n) if q_out is not None else rq
+        rc = lib.dd_cache_append(self.c, n, _ints(positions, "positions", (n,)),
+                                 None if requests is None else _ints(requests, "requests", (n,)),
+                                 _rows(k, "k", self.head_dim, n), _rows(v, "v", self.head_dim, n),
+                                 rope.c if rope is not None else None, rq, oq, _stream(stream))
+        _raise_last(rc)
+
+    def read(self, idx, out, stream=None):
+        """Pages idx [batch, Hkv, k] (numbers within each request) in attention layout into out
+        [batch, Hkv, 2, k * page_tokens, d], dense bfloat16 or float16."""
+        kind = _ROW_TYPES.get(out.dtype)
+        c = self.c
+        if idx.dim() != 3 or idx.shape[0] != c.batch or idx.shape[1] != c.n_kv_heads:
+            raise _invalid(f"idx must be [{c.batch}, {c.n_kv_heads}, k], not {tuple(idx.shape)}")
+        k = idx.shape[2]
+        if kind is None or not out.is_contiguous() or tuple(out.shape) != (c.batch, c.n_kv_heads, 2, k * self.page_tokens, self.head_dim):
+            raise _invalid(f"out must be a dense 16-bit tensor {(c.batch, c.n_kv_heads, 2, k * self.page_tokens, self.head_dim)}")
+        _raise_last(lib.dd_cache_read(c, _ints(idx, "idx"), k, out.data_ptr(), kind, _stream(stream)))
+
+    def decode_attn(self, q, ctx_len, out, out_lse=None, *, window=0, scale=0.0, workspace=None, stream=None):
+        """Attention of the last Tq tokens of every request over its cached tokens. q, out [batch, Tq, Hq, d]; ctx_len
+        [batch] int32; out_lse [batch, Tq, Hq] float32. Without a workspace the call takes one from torch's allocator on
+        the stream it runs on (safe for several streams and for graph capture)."""
+        c = self.c
+        if q.dim() != 4 or q.shape[0] != c.batch or out.shape != q.shape:
+            raise _invalid(f"q and out must be [{c.batch}, tokens, heads, {self.head_dim}], not {tuple(q.shape)} and {tuple(out.shape)}")
+        B, Tq, Hq, _ = q.shape
+        rq, ro = _rows4(q, "q", self.head_dim), _rows4(out, "out", self.head_dim)
+        if out_lse is not None and (out_lse.dtype != torch.float32 or not out_lse.is_contiguous() or tuple(out_lse.shape) != (B, Tq, Hq)):
+            raise _invalid(f"out_lse must be a dense float32 tensor {(B, Tq, Hq)}")
+        need = self._workspace_bytes.get((Hq, Tq))
+        if need is None:
+            need = lib.dd_cache_decode_attn_workspace(Hq, c.n_kv_heads, self.head_dim, Tq)
+            self._workspace_bytes[(Hq, Tq)] = need
+        if workspace is None:
+            workspace = _scratch(max(need, 16), stream)
+        rc = lib.dd_cache_decode_attn(c, Tq, rq, _ints(ctx_len, "ctx_len", (B,)), ro, _ptr(out_lse), window, scale,
+                                      workspace.data_ptr(), workspace.numel() * workspace.element_size(), _stream(stream))
+        _raise_last(rc)
+
+    def workspace(self, n_q_heads: int, n_q_tokens: int = 1) -> torch.Tensor:
+        """A workspace for decode_attn calls of this shape."""
+        return torch.empty(max(16, lib.dd_cache_decode_attn_workspace(n_q_heads, self.c.n_kv_heads, self.head_dim, n_q_tokens)),
+                           dtype=torch.uint8, device=self.block_table.device)
+
+    def device_error(self):
+        """(code, detail) of the first index that a kernel found out of range; synchronises and clears it."""
+        code, detail = self.status.tolist()
+        self.status.zero_()
+        return code, detail
+
+
+def _rows4(t, name: str, head_dim: int):
+    """`dd_rows` of [batch, tokens, heads, head_dim] as batch * tokens rows with one stride."""
+    B, Tq = t.shape[0], t.shape[1]
+    if B > 1 and Tq > 1 and t.stride(0) != Tq * t.stride(1):
+        raise _invalid(f"the tokens of {name} must lie at one stride: [batch, tokens] has to fold into one dimension")
+    step = t.stride(1) if Tq > 1 else t.stride(0)
+    return _rows(t.as_strided((B * Tq, t.shape[2], t.shape[3]), (step, t.stride(2), t.stride(3))), name, head_dim)
+
+
+def _scratch(n_bytes: int, stream) -> torch.Tensor:
+    if stream is None:
+        return torch.empty(n_bytes, dtype=torch.uint8, device="cuda")
+    with torch.cuda.stream(torch.cuda.ExternalStream(stream) if isinstance(stream, int) else stream):
+        return torch.empty(n_bytes, dtype=torch.uint8, device="cuda")
 
 
 class Context:

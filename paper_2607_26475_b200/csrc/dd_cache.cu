@@ -1,0 +1,237 @@
+// The paged key-value cache: argument checks shared by its calls, and the kernel that reads pages back.
+#include "dd_cache.cuh"
+
+// ---------------------------------------------------------------------------------------------
+// checks
+// ---------------------------------------------------------------------------------------------
+// The current device, or -1 where there is none: the checks that need no device come first then, and the pointer checks fail.
+int dd_current_device() {
+  int device = -1;
+  if (cudaGetDevice(&device) != cudaSuccess) {
+    cudaGetLastError();
+    return -1;
+  }
+  return device;
+}
+
+int dd_check_ptr(const void* p, const char* who, const char* what, int align, int device) {
+  if (!p) return dd_fail(nullptr, DD_ERR_INVALID_ARG, "%s: %s is NULL", who, what);
+  if (((uintptr_t)p) & (uintptr_t)(align - 1))
+    return dd_fail(nullptr, DD_ERR_INVALID_ARG, "%s: %s is not %d-byte aligned", who, what, align);
+  cudaPointerAttributes a;
+  cudaError_t e = cudaPointerGetAttributes(&a, p);
+  if (e != cudaSuccess) {
+    cudaGetLastError();
+    return dd_fail(nullptr, DD_ERR_INVALID_ARG, "%s: %s: %s", who, what, cudaGetErrorString(e));
+  }
+  if (a.type != cudaMemoryTypeDevice && a.type != cudaMemoryTypeManaged)
+    return dd_fail(nullptr, DD_ERR_INVALID_ARG, "%s: %s is not device memory", who, what);
+  if (a.type == cudaMemoryTypeDevice && a.device != device)
+    return dd_fail(nullptr, DD_ERR_INVALID_ARG, "%s: %s lives on device %d, the current one is %d", who, what, a.device, device);
+  return DD_OK;
+}
+
+int dd_check_rows(const dd_rows* r, const char* who, const char* what, int head_dim, bool is_output) {
+  if (!r) return dd_fail(nullptr, DD_ERR_INVALID_ARG, "%s: %s is NULL", who, what);
+  if (r->dtype != DD_BF16 && r->dtype != DD_FP16) return dd_fail(nullptr, DD_ERR_INVALID_ARG, "%s: %s has an unknown dtype", who, what);
+  if (r->n_heads < 1) return dd_fail(nullptr, DD_ERR_INVALID_ARG, "%s: %s has no heads", who, what);
+  if (r->token_stride < 0 || r->head_stride < 0 || r->token_stride % 8 || r->head_stride % 8)
+    return dd_fail(nullptr, DD_ERR_INVALID_ARG, "%s: strides of %s must be non-negative multiples of 8 elements", who, what);
+  if (is_output && (r->token_stride < head_dim || (r->n_heads > 1 && r->head_stride < head_dim)))
+    return dd_fail(nullptr, DD_ERR_INVALID_ARG, "%s: rows of %s overlap", who, what);
+  if (!r->data) return dd_fail(nullptr, DD_ERR_INVALID_ARG, "%s: %s is NULL", who, what);
+  return DD_OK;
+}
+
+extern "C" size_t dd_cache_page_bytes(int format, int page_tokens, int head_dim) {
+  if (head_dim != 64 && head_dim != 128) return 0;
+  if (page_tokens < 16 || page_tokens > 256 || (page_tokens & (page_tokens - 1))) return 0;
+  if (format == DD_CACHE_BF16 || format == DD_CACHE_FP16) return (size_t)4 * page_tokens * head_dim;
+  if (format == DD_CACHE_E4M3) return (size_t)2 * page_tokens * head_dim + 2 * page_tokens;
+  return 0;
+}
+
+int dd_check_cache(const dd_cache* c, const char* who) {
+  if (!c) return dd_fail(nullptr, DD_ERR_INVALID_ARG, "%s: cache is NULL", who);
+  const long long page = (long long)dd_cache_page_bytes(c->format, c->page_tokens, c->head_dim);
+  if (!page)
+    return dd_fail(nullptr, DD_ERR_INVALID_ARG, "%s: format %d with %d tokens of %d elements a page is not supported "
+                   "(head_dim 64 or 128, page_tokens 16, 32, 64, 128 or 256)", who, c->format, c->page_tokens, c->head_dim);
+  if (c->n_kv_heads < 1 || c->n_blocks < 1 || c->batch < 1 || c->max_pages < 1)
+    return dd_fail(nullptr, DD_ERR_INVALID_ARG, "%s: sizes of the cache must be positive", who);
+  if ((long long)c->max_pages * c->page_tokens > 0x7fffffffLL - 16)
+    return dd_fail(nullptr, DD_ERR_INVALID_ARG, "%s: max_pages * page_tokens does not fit 31 bits", who);
+  if (c->table_stride < c->max_pages && c->batch > 1)
+    return dd_fail(nullptr, DD_ERR_INVALID_ARG, "%s: table_stride is below max_pages", who);
+  if (c->table_stride < 0) return dd_fail(nullptr, DD_ERR_INVALID_ARG, "%s: table_stride is negative", who);
+  if (c->block_stride % 16 || c->head_stride % 16 || c->block_stride < 0 || c->head_stride < 0)
+    return dd_fail(nullptr, DD_ERR_INVALID_ARG, "%s: page strides must be non-negative multiples of 16 bytes", who);
+  if ((c->n_blocks > 1 && c->block_stride < page) || (c->n_kv_heads > 1 && c->head_stride < page))
+    return dd_fail(nullptr, DD_ERR_INVALID_ARG, "%s: pages of %lld bytes overlap", who, page);
+  if (!c->data) return dd_fail(nullptr, DD_ERR_INVALID_ARG, "%s: cache->data is NULL", who);
+  if (((uintptr_t)c->data) & 15) return dd_fail(nullptr, DD_ERR_INVALID_ARG, "%s: cache->data is not 16-byte aligned", who);
+  if (!c->block_table) return dd_fail(nullptr, DD_ERR_INVALID_ARG, "%s: cache->block_table is NULL", who);
+  return DD_OK;
+}
+
+int dd_check_cache_memory(const dd_cache* c, const char* who, int device, bool allow_host, const char** data_dev, bool* on_host) {
+  DD_TRY(dd_check_ptr(c->block_table, who, "cache->block_table", 4, device));
+  if (c->status) DD_TRY(dd_check_ptr(c->status, who, "cache->status", 4, device));
+  cudaPointerAttributes a;
+  cudaError_t e = cudaPointerGetAttributes(&a, c->data);
+  if (e != cudaSuccess) {
+    cudaGetLastError();
+    return dd_fail(nullptr, DD_ERR_INVALID_ARG, "%s: cache->data: %s", who, cudaGetErrorString(e));
+  }
+  if (a.type == cudaMemoryTypeUnregistered)
+    return dd_fail(nullptr, DD_ERR_NOT_PINNED, "%s: cache->data is pageable host memory; page-lock it (cudaHostAlloc / cudaHostRegister)", who);
+  if (a.type == cudaMemoryTypeHost) {
+    if (!allow_host) return dd_fail(nullptr, DD_ERR_INVALID_ARG, "%s: cache->data must be device memory", who);
+    if (!a.devicePointer) return dd_fail(nullptr, DD_ERR_NOT_PINNED, "%s: cache->data is page-locked but not mapped into the device", who);
+    *data_dev = (const char*)a.devicePointer;
+    if (on_host) *on_host = true;
+    return DD_OK;
+  }
+  if (a.type == cudaMemoryTypeDevice && a.device != device)
+    return dd_fail(nullptr, DD_ERR_INVALID_ARG, "%s: cache->data lives on device %d, the current one is %d", who, a.device, device);
+  *data_dev = (const char*)c->data;
+  if (on_host) *on_host = false;
+  return DD_OK;
+}
+
+dd_cache_view dd_make_view(const dd_cache* c, const char* data_dev) {
+  dd_cache_view v;
+  v.data = const_cast<char*>(data_dev);
+  v.block_stride = c->block_stride;
+  v.head_stride = c->head_stride;
+  v.table = c->block_table;
+  v.table_stride = c->table_stride;
+  v.status = c->status;
+  v.n_blocks = c->n_blocks;
+  v.n_kv_heads = c->n_kv_heads;
+  v.batch = c->batch;
+  v.max_pages = c->max_pages;
+  v.page_shift = dd_log2i(c->page_tokens);
+  return v;
+}
+
+// ---------------------------------------------------------------------------------------------
+// reading pages back
+// ---------------------------------------------------------------------------------------------
+// One warp per 16 tokens of a page: K and V of a tile are two contiguous runs, read with 16-byte loads that are all in
+// flight before the first store (4 KiB a warp for e4m3 at head_dim 128, 8 KiB for 16-bit pages), and written as two
+// contiguous runs of 16-bit rows. Bound: HBM, or the host link for a page-locked pool. The exponents of a tile are 16
+// bytes for K and 16 for V: one byte per lane in one load, handed out by shuffles.
+constexpr int CR_THREADS = 256;
+
+template <int FMT, typename T, int D>
+__global__ void __launch_bounds__(CR_THREADS) dd_cache_read_kernel(dd_cache_view c, const int* __restrict__ idx,
+                                                                  char* __restrict__ out, int k_pages, long long n_tiles) {
+  constexpr int ES = FMT == DD_CACHE_E4M3 ? 1 : 2;
+  constexpr int NL = 16 * D * ES / 512;                // 16-byte loads per lane for the K (or V) part of a tile
+  const int lane = threadIdx.x & 31;
+  const int page_tokens = 1 << c.page_shift, tiles_per_page = page_tokens >> 4;
+  const long long n_warps = (long long)gridDim.x * (CR_THREADS / 32);
+  dd_grid_dependency_wait();
+  for (long long item = (long long)(threadIdx.x >> 5) * gridDim.x + blockIdx.x; item < n_tiles; item += n_warps) {
+    const long long entry = item / tiles_per_page;     // position in idx
+    const int tile = (int)(item - entry * tiles_per_page);
+    const long long bg = entry / k_pages;
+    const int j = (int)(entry - bg * k_pages);
+    const int b = (int)(bg / c.n_kv_heads), g = (int)(bg - (long long)b * c.n_kv_heads);
+    const int p = idx[entry];
+    int blk = -1;
+    if (p < 0 || p >= c.max_pages) {
+      if (lane == 0) dd_status(c.status, p);
+    } else {
+      blk = c.table[b * c.table_stride + p];
+      if (blk < 0 || blk >= c.n_blocks) {
+        if (lane == 0) dd_status(c.status, blk);
+        blk = -1;
+      }
+    }
+    uint4 r[2][NL];
+    int ex = 0;
+    if (blk >= 0) {
+      const char* page = c.data + blk * c.block_stride + g * c.head_stride;
+      const char* src = page + tile * (16 * D * ES) + lane * 16;
+#pragma unroll
+      for (int kv = 0; kv < 2; ++kv)
+#pragma unroll
+        for (int i = 0; i < NL; ++i) r[kv][i] = dd_ld_stream(src + kv * page_tokens * D * ES + i * 512);
+      if (ES == 1)
+        ex = *reinterpret_cast<const unsigned char*>(page + 2 * page_tokens * D + (lane >> 4) * page_tokens + tile * 16 + (lane & 15));
+    } else {
+#pragma unroll
+      for (int kv = 0; kv < 2; ++kv)
+#pragma unroll
+        for (int i = 0; i < NL; ++i) r[kv][i] = make_uint4(0u, 0u, 0u, 0u);
+    }
+#pragma unroll
+    for (int kv = 0; kv < 2; ++kv) {
+      // row of the output: unit bg, half kv, page j, tile
+      char* dst = out + ((((bg * 2 + kv) * k_pages + j) * tiles_per_page + tile) * 16LL) * (2 * D);
+#pragma unroll
+      for (int i = 0; i < NL; ++i) {
+        if (ES == 2) {
+          dd_st_v4(dst + i * 512 + lane * 16, r[kv][i]);
+        } else {
+          const int at = i * 512 + lane * 16;          // element of the tile
+          const float s = dd_two_to_byte(__shfl_sync(0xffffffffu, ex, kv * 16 + at / D));
+          const uint32_t w[4] = {r[kv][i].x, r[kv][i].y, r[kv][i].z, r[kv][i].w};
+          uint32_t o[8];
+#pragma unroll
+          for (int q = 0; q < 4; ++q) {
+            uint32_t lo, hi;
+            dd_e4m3x4_to_half(w[q], lo, hi);
+            const float2 a = dd_unpack2<__half>(lo), b2 = dd_unpack2<__half>(hi);
+            o[2 * q] = dd_pack2<T>(a.x * s, a.y * s);  // exact for bf16 but for results below its smallest normal
+            o[2 * q + 1] = dd_pack2<T>(b2.x * s, b2.y * s);
+          }
+          dd_st_v4(dst + at * 2, make_uint4(o[0], o[1], o[2], o[3]));
+          dd_st_v4(dst + at * 2 + 16, make_uint4(o[4], o[5], o[6], o[7]));
+        }
+      }
+    }
+  }
+}
+
+template <int D>
+static const void* cr_kernel_of(int format, int dtype) {
+  if (format != DD_CACHE_E4M3) return (const void*)dd_cache_read_kernel<DD_CACHE_BF16, __nv_bfloat16, D>;   // a copy of 16-bit words
+  return dtype == DD_BF16 ? (const void*)dd_cache_read_kernel<DD_CACHE_E4M3, __nv_bfloat16, D>
+                          : (const void*)dd_cache_read_kernel<DD_CACHE_E4M3, __half, D>;
+}
+
+extern "C" int dd_cache_read(const dd_cache* cache, const int* idx, int k_pages, void* out, int out_dtype, void* stream) {
+  const char* who = "dd_cache_read";
+  DD_TRY(dd_check_cache(cache, who));
+  if (k_pages < 0) return dd_fail(nullptr, DD_ERR_INVALID_ARG, "%s: k_pages is negative", who);
+  if (out_dtype != DD_BF16 && out_dtype != DD_FP16) return dd_fail(nullptr, DD_ERR_INVALID_ARG, "%s: unknown out_dtype", who);
+  if ((cache->format == DD_CACHE_BF16 && out_dtype != DD_BF16) || (cache->format == DD_CACHE_FP16 && out_dtype != DD_FP16))
+    return dd_fail(nullptr, DD_ERR_INVALID_ARG, "%s: a 16-bit cache is read in its own type", who);
+  if (k_pages == 0) return DD_OK;
+  const int device = dd_current_device();
+  const char* data = nullptr;
+  bool on_host = false;
+  DD_TRY(dd_check_cache_memory(cache, who, device, true, &data, &on_host));
+  DD_TRY(dd_check_ptr(idx, who, "idx", 4, device));
+  DD_TRY(dd_check_ptr(out, who, "out", 16, device));
+  long long n_tiles = (long long)cache->batch * cache->n_kv_heads * k_pages * (cache->page_tokens / 16);
+  long long blocks = (n_tiles + CR_THREADS / 32 - 1) / (CR_THREADS / 32);
+  if (on_host && blocks > 16) blocks = 16;             // as many as the host link needs; the other SMs stay free
+  if (blocks > 0x7fffffffLL) blocks = 0x7fffffffLL;
+  dd_cache_view v = dd_make_view(cache, data);
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3((unsigned)blocks);
+  cfg.blockDim = dim3(CR_THREADS);
+  cfg.stream = (cudaStream_t)stream;
+  cudaLaunchAttribute at;
+  dd_pdl_attr(&at);
+  cfg.attrs = &at;
+  cfg.numAttrs = 1;
+  void* args[] = {&v, &idx, &out, &k_pages, &n_tiles};
+  DD_CUDA_TRY(nullptr, cudaLaunchKernelExC(&cfg, cache->head_dim == 128 ? cr_kernel_of<128>(cache->format, out_dtype)
+                                                                        : cr_kernel_of<64>(cache->format, out_dtype), args));
+  return DD_OK;
+}
