@@ -5,11 +5,13 @@
 // are, and no pause at the border between two requests.
 //
 // Work split. The context of every (request, row tile, KV head) "unit" is cut into tiles of 16 tokens, and all tiles of
-// the launch form one flat list, request by request. Block x of a grid that fills the device once takes an equal run of
-// the list; lengths are read on the device, so the launch does not depend on them (a captured graph may be replayed with
-// other lengths). The warps of a block take the tiles of its run in turn. Each warp keeps a ring of half tiles (K or V) in
-// flight with 16-byte cp.async; a lane copies exactly the fragments it will use itself into its own slots of the ring, so
-// no barrier, no swizzle and no bank conflict is involved, and the ring runs on across the borders of units.
+// the launch form one flat list, request by request, with a few empty places behind each unit that stand for what a unit
+// costs besides its tiles. Every warp of a grid that fills the device once takes an equal run of the list; lengths are
+// read on the device, so the launch does not depend on them (a captured graph may be replayed with other lengths). A
+// warp works alone: it keeps a ring of half tiles (K or V) in flight with 16-byte cp.async, and the ring runs on across the
+// borders of units. A copy instruction takes 512 contiguous bytes (whole 128-byte lines; fragments fetched straight from
+// global memory touch half lines and ran at half the rate), and the chunks of a row are placed by row ^ chunk, so that
+// ldmatrix reads them without bank conflicts: K as it lies, V transposed.
 //
 // Arithmetic, with the up-to-8 query rows of a KV head as the N = 8 columns of the MMA (two column tiles for up to 16
 // rows, several row tiles beyond):
@@ -19,23 +21,24 @@
 // multiplies its scores; the scale of a value is added to the exponent of its weight: with w = z + log2(scale of v) the
 // running reference is the maximum of w, P = 2^(w - ref) <= 1 multiplies codes, and the denominator sums 2^(z - ref).
 // The reference moves only when a weight exceeds it by 2^8 (one vote per tile instead of a reduction), so P is at most
-// 2^14 after a factor 2^6 that keeps small weights out of the half's subnormals (a weight 2^-30 of the largest is still
+// 2^14 after a factor 2^6 that keeps small weights out of the half's subnormals (a weight 2^-20 of the reference is still
 // normal). Queries are multiplied by a power of two per row to fill the half's range: exact for every element above
 // 2^-28 of the row's largest.
 //
 // Rounding: P to bf16 (bf16 pages; off by 2^-8 relative at most: the MMA takes both operands in one type) or half (2^-11), q
 // as said, the output once. Scores, reference, denominators, accumulators and partial results are fp32.
 //
-// Joining. A unit inside one block is finished there. A unit cut across blocks leaves one fp32 partial per block in the
-// workspace, and a second small kernel adds them in block order (always the same order: the result does not depend on
-// timing); the block in which a cut unit begins writes down who takes part.
+// Joining. A unit inside one warp's run is finished there. The pieces of a cut unit that the warps of one block hold when
+// their runs end are added in shared memory; what is left (one fp32 partial per block, and the unit's last piece) goes to
+// the workspace, and a second small kernel adds those, always in the order of the list: the result does not depend on
+// timing. The warp in whose run a cut unit begins writes down where it ends.
 #include "dd_cache.cuh"
 
 namespace {
 
 constexpr int CA_WARPS = 8;
 constexpr int CA_THREADS = CA_WARPS * 32;
-constexpr int CA_MIN_SHARE = CA_WARPS;       // tiles per block at least: one per warp
+constexpr int CA_UNIT_COST = 1;              // empty places behind a unit in the flat list
 constexpr float CA_HEADROOM = 6.f;           // log2 of the factor on P
 constexpr float CA_LAZY = 8.f;               // how far (log2) a weight may exceed the reference
 
@@ -48,18 +51,25 @@ template <int FMT, int D, int NT>
 struct ca_geom {
   static constexpr bool FP8 = FMT >= 2;
   static constexpr int ES = FP8 ? 1 : 2;
-  static constexpr int HALF_BYTES = 16 * D * ES;                      // K (or V) of a tile
+  static constexpr int ROW = D * ES;                                  // bytes of a row: 64, 128 or 256
+  static constexpr int HALF_BYTES = 16 * ROW;                         // K (or V) of a tile
   static constexpr int SLOT_BYTES = HALF_BYTES + (FP8 ? 32 : 0);      // e4m3: + exponents of the tile (in K's slot)
+  static constexpr int COPIES = HALF_BYTES / 512;
   static constexpr int BLOCKS_PER_SM = NT == 1 ? 2 : 1;               // two column tiles need the registers of a whole SM
-  static constexpr int MERGE_BYTES = (CA_WARPS / 2) * 32 * (D / 4) * 4;
-  static constexpr int RING_BUDGET = (BLOCKS_PER_SM == 2 ? 97 : 194) * 1024;
+  static constexpr int RING_BUDGET = (BLOCKS_PER_SM == 2 ? 110 : 220) * 1024;
   static constexpr int STAGES_ = RING_BUDGET / (CA_WARPS * SLOT_BYTES);
   static constexpr int STAGES = STAGES_ > 12 ? 12 : STAGES_;
-  static constexpr int SMEM = CA_WARPS * STAGES * SLOT_BYTES + MERGE_BYTES;
+  static constexpr int WARP_BYTES = STAGES * SLOT_BYTES;
+  static constexpr int SMEM = CA_WARPS * WARP_BYTES;
   static constexpr int NACC = D / 4;                                  // accumulator registers per column tile
-  static constexpr int CH = FP8 ? 16 : 8;                             // channels per 16-byte chunk of a K row
-  static constexpr int K_CHUNKS = D / (4 * CH);                       // chunks per lane and row: D/32 (16-bit), D/64 (e4m3)
+  static_assert(WARP_BYTES >= NT * NACC * 128, "a warp's ring holds its accumulators at the end");
 };
+
+// Byte offset of 16-byte chunk c of row r in a half tile: a column of 8 rows covers all 32 banks.
+template <int ROW> __device__ __forceinline__ uint32_t ca_place(int r, int c) {
+  if (ROW >= 128) return r * ROW + ((c ^ (r & 7)) << 4);
+  return r * ROW + ((c ^ ((r >> 1) & 3)) << 4);                       // 64-byte rows: two of them make a line
+}
 
 struct ca_args {
   dd_cache_view c;
@@ -68,9 +78,9 @@ struct ca_args {
   long long q_token_stride, q_head_stride, out_token_stride, out_head_stride;   // bytes
   const int* ctx_len;
   float* lse;
-  float* part_o;       // [2 * blocks][NT][D / 4][32]
-  float2* part_ml;     // [2 * blocks][NT * 8]
-  int4* desc;          // [blocks]: (request, row tile * heads + head, blocks of the unit, 0) of the cut unit that begins in the block
+  float* part_o;       // [2 * warps][NT][D / 4][32]
+  float2* part_ml;     // [2 * warps][NT * 8]
+  int4* desc;          // [warps]: (request, row tile * heads + head, last warp of the unit + 1) of the cut unit that begins in a warp's run, or 0
   int n_q_heads, G, Tq, n_rows, row_tiles, window;
   float scale_log2;
 };
@@ -78,23 +88,16 @@ struct ca_args {
 __device__ __forceinline__ void ca_cp16(uint32_t dst, const void* src, uint32_t bytes) {
   asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(bytes) : "memory");
 }
-__device__ __forceinline__ void ca_cp8(uint32_t dst, const void* src, uint32_t bytes) {
-  asm volatile("cp.async.ca.shared.global [%0], [%1], 8, %2;" ::"r"(dst), "l"(src), "r"(bytes) : "memory");
-}
 __device__ __forceinline__ void ca_cp4(uint32_t dst, const void* src, uint32_t bytes) {
   asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(dst), "l"(src), "r"(bytes) : "memory");
 }
 __device__ __forceinline__ void ca_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
 template <int N> __device__ __forceinline__ void ca_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
-__device__ __forceinline__ uint4 ca_lds16(uint32_t a) {
-  uint4 v;
-  asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(a) : "memory");
-  return v;
+__device__ __forceinline__ void ca_ldsm(uint32_t (&r)[4], uint32_t at) {
+  asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0,%1,%2,%3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(at) : "memory");
 }
-__device__ __forceinline__ uint2 ca_lds8(uint32_t a) {
-  uint2 v;
-  asm volatile("ld.shared.v2.u32 {%0,%1}, [%2];" : "=r"(v.x), "=r"(v.y) : "r"(a) : "memory");
-  return v;
+__device__ __forceinline__ void ca_ldsm_trans(uint32_t (&r)[4], uint32_t at) {
+  asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0,%1,%2,%3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(at) : "memory");
 }
 __device__ __forceinline__ int ca_lds_byte(uint32_t a) {
   uint32_t v;
@@ -122,8 +125,6 @@ __device__ __forceinline__ float ca_exp2(float x) {
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
   return y;
 }
-__device__ __forceinline__ uint32_t ca_word(const uint4& v, int w) { return w == 0 ? v.x : (w == 1 ? v.y : (w == 2 ? v.z : v.w)); }
-
 // Tokens [first, end) of a request that any of its query tokens sees, as tiles of 16.
 struct ca_span {
   int end, first;      // tokens; first is the lowest visible one
@@ -148,52 +149,66 @@ __device__ __forceinline__ ca_span ca_span_of(const ca_args& a, int b, bool repo
   return s;
 }
 
-// A place in the flat list of tiles.
+// A place in the flat list: tile t of unit (b, sub), `left` places before the end of the run.
 struct ca_cursor {
-  int b, sub, t;       // request, row tile * heads + head, tile of the unit
+  int b, sub, t, left;   // sub = row tile * heads + head
   ca_span s;
 };
-__device__ __forceinline__ void ca_advance(const ca_args& a, ca_cursor& k, int by, int subs) {
-  k.t += by;
-  while (k.t >= k.s.tiles) {
-    k.t -= k.s.tiles;
-    if (++k.sub == subs) {
-      k.sub = 0;
-      do {
-        if (++k.b >= a.c.batch) { k.b = a.c.batch - 1; k.s.tiles = 0x7fffffff; return; }   // behind the last tile: never used
-        k.s = ca_span_of(a, k.b, false);
-      } while (k.s.tiles == 0);
-    }
+// To the first tile of the next unit.
+__device__ __forceinline__ void ca_next_unit(const ca_args& a, ca_cursor& k, int subs) {
+  k.t = 0;
+  if (++k.sub == subs) {
+    k.sub = 0;
+    do {
+      if (k.b + 1 >= a.c.batch) { k.left = 0; return; }
+      k.s = ca_span_of(a, ++k.b, false);
+    } while (k.s.tiles == 0);
+  }
+}
+__device__ __forceinline__ void ca_step(const ca_args& a, ca_cursor& k, int subs) {
+  --k.left;
+  if (++k.t >= k.s.tiles) {
+    k.left -= CA_UNIT_COST;
+    if (k.left > 0) ca_next_unit(a, k, subs);
   }
 }
 
-__device__ __forceinline__ int ca_channel(bool fp8, int D, int g, int m) {      // channel of accumulator row g of V product m
-  return fp8 ? (D / 8) * g + 2 * m : (m >> 2) * 64 + 8 * g + 2 * (m & 3);
-}
+// Channel of accumulator m at row g of the product (row g + 8: + ca_pair).
+__device__ __forceinline__ int ca_channel(bool fp8, int g, int m) { return 16 * m + (fp8 ? 2 * g : g); }
+__device__ __forceinline__ constexpr int ca_pair(bool fp8) { return fp8 ? 1 : 8; }
+
+__device__ __forceinline__ float ca_lse(float ref, float den) { return (ref - CA_HEADROOM + log2f(den)) * 0.6931471805599453f; }
 
 template <int FMT, int D, int NT>
 __global__ void __launch_bounds__(CA_THREADS, (ca_geom<FMT, D, NT>::BLOCKS_PER_SM)) dd_cache_attn_kernel(const ca_args a) {
   using geo = ca_geom<FMT, D, NT>;
   using TQ = typename ca_types<FMT>::Q;
+  using TP = typename ca_types<FMT == 0 ? 0 : 1>::Q;
   constexpr bool FP8 = geo::FP8;
   constexpr int NS = geo::STAGES;
-  extern __shared__ __align__(16) unsigned char ca_smem[];
+  extern __shared__ __align__(128) unsigned char ca_smem[];
   __shared__ long long sh_scan[CA_WARPS];
-  __shared__ int sh_start[3];
+  __shared__ int sh_start[CA_WARPS][3];
   __shared__ float2 sh_ml[CA_WARPS][NT * 8];
+  __shared__ int2 sh_key[CA_WARPS];
 
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int g = lane >> 2, t = lane & 3;
   const int subs = a.row_tiles * a.c.n_kv_heads;
   const int B = a.c.batch;
+  const long long n_warps = (long long)gridDim.x * CA_WARPS;
+  const int me = blockIdx.x * CA_WARPS + warp;
 
   dd_grid_dependency_wait();
 
-  // ---- this block's run of the flat list
+  // ---- the runs of this block's warps in the flat list
   long long mine = 0;
   const int chunk = (B + CA_THREADS - 1) / CA_THREADS;
   const int b_lo = min(B, (int)threadIdx.x * chunk), b_hi = min(B, b_lo + chunk);
-  for (int b = b_lo; b < b_hi; ++b) mine += (long long)ca_span_of(a, b, blockIdx.x == 0).tiles * subs;
+  for (int b = b_lo; b < b_hi; ++b) {
+    const int nt = ca_span_of(a, b, blockIdx.x == 0).tiles;
+    if (nt > 0) mine += (long long)(nt + CA_UNIT_COST) * subs;
+  }
   long long incl = mine;
 #pragma unroll
   for (int o = 1; o < 32; o <<= 1) {
@@ -201,6 +216,7 @@ __global__ void __launch_bounds__(CA_THREADS, (ca_geom<FMT, D, NT>::BLOCKS_PER_S
     if (lane >= o) incl += v;
   }
   if (lane == 31) sh_scan[warp] = incl;
+  if (threadIdx.x < CA_WARPS) sh_start[threadIdx.x][0] = -1;
   __syncthreads();
   long long total = 0, before = 0;
 #pragma unroll
@@ -208,20 +224,20 @@ __global__ void __launch_bounds__(CA_THREADS, (ca_geom<FMT, D, NT>::BLOCKS_PER_S
     if (w < warp) before += sh_scan[w];
     total += sh_scan[w];
   }
-  long long share = (total + gridDim.x - 1) / gridDim.x;
-  if (share < CA_MIN_SHARE) share = CA_MIN_SHARE;
-  const long long f0 = share * blockIdx.x;
-  const long long f1 = f0 + share < total ? f0 + share : total;
-  {
-    long long at = before + incl - mine;             // first tile of this thread's requests
-    if (f0 < total && f0 >= at && f0 < at + mine) {
+  const long long share = max(1LL, (total + n_warps - 1) / n_warps);
+  if (mine > 0) {
+    const long long lo = before + incl - mine;       // first place of this thread's requests
+    for (int w = 0; w < CA_WARPS; ++w) {
+      const long long f = share * ((long long)blockIdx.x * CA_WARPS + w);
+      if (f < lo || f >= lo + mine) continue;
+      long long at = lo;
       for (int b = b_lo; b < b_hi; ++b) {
         const int nt = ca_span_of(a, b, false).tiles;
-        const long long n = (long long)nt * subs;
-        if (f0 < at + n) {
-          sh_start[0] = b;
-          sh_start[1] = (int)((f0 - at) / nt);
-          sh_start[2] = (int)((f0 - at) % nt);
+        const long long n = nt > 0 ? (long long)(nt + CA_UNIT_COST) * subs : 0;
+        if (f < at + n) {
+          sh_start[w][0] = b;
+          sh_start[w][1] = (int)((f - at) / (nt + CA_UNIT_COST));
+          sh_start[w][2] = (int)((f - at) % (nt + CA_UNIT_COST));
           break;
         }
         at += n;
@@ -241,35 +257,42 @@ __global__ void __launch_bounds__(CA_THREADS, (ca_geom<FMT, D, NT>::BLOCKS_PER_S
       }
     }
   }
-  if (f0 >= total) {
-    if (threadIdx.x == 0) a.desc[blockIdx.x] = make_int4(0, 0, 0, 0);
-    return;
-  }
 
-  // ---- the issuing side: this warp's tiles are f0 + warp, + CA_WARPS, ...
-  const uint32_t ring = (uint32_t)__cvta_generic_to_shared(ca_smem) + warp * NS * geo::SLOT_BYTES;
-  float* merge = reinterpret_cast<float*>(ca_smem + CA_WARPS * NS * geo::SLOT_BYTES);
-  const int span = (int)(f1 - f0);
-  int left = span > warp ? (span - warp - 1) / CA_WARPS + 1 : 0;      // tiles not yet issued
+  // ---- the issuing side
+  const uint32_t ring = (uint32_t)__cvta_generic_to_shared(ca_smem) + warp * geo::WARP_BYTES;
   ca_cursor is;
-  is.b = sh_start[0]; is.sub = sh_start[1]; is.t = sh_start[2];
-  is.s = ca_span_of(a, is.b, false);
-  if (left > 0) ca_advance(a, is, warp, subs);
+  is.b = sh_start[warp][0];
+  is.left = 0;
+  if (is.b >= 0) {
+    is.sub = sh_start[warp][1];
+    is.t = sh_start[warp][2];
+    is.s = ca_span_of(a, is.b, false);
+    is.left = (int)share;
+    if (is.t >= is.s.tiles) {                        // the run begins in the empty places behind a unit
+      is.left -= is.s.tiles + CA_UNIT_COST - is.t;
+      if (is.left > 0) ca_next_unit(a, is, subs);
+    }
+  }
+  ca_cursor u = is;                                  // the using side starts at the same place
   const int page_mask = (1 << a.c.page_shift) - 1;
-
-  auto block_of = [&](const ca_cursor& k) {          // table entry of a tile, -1 if it names no block
-    const int blk = __ldg(a.c.table + k.b * a.c.table_stride + (((k.s.tile0 + k.t) << 4) >> a.c.page_shift));
-    return blk;
+  auto block_of = [&](const ca_cursor& k) {
+    return __ldg(a.c.table + k.b * a.c.table_stride + (((k.s.tile0 + k.t) << 4) >> a.c.page_shift));
   };
-  int next_blk = left > 0 ? block_of(is) : 0;
+  int next_blk = is.left > 0 ? block_of(is) : 0;
   const char* src = nullptr;                         // K of the tile being issued; V lies page_tokens rows behind
   int n_first = 0, n_valid = 0;                      // tokens [n_first, n_valid) of it exist (and are visible to some row)
   bool second = false;                               // the next half to issue is V
-  int put = 0;                                       // slot it goes to
+  uint32_t put = ring;                               // slot it goes to
 
+  auto copy_half = [&](const char* from) {
+#pragma unroll
+    for (int i = 0; i < geo::COPIES; ++i) {
+      const int r = i * (512 / geo::ROW) + lane / (geo::ROW / 16), c = lane % (geo::ROW / 16);
+      ca_cp16(put + ca_place<geo::ROW>(r, c), from + i * 512 + lane * 16, (r >= n_first && r < n_valid) ? 16u : 0u);
+    }
+  };
   auto issue = [&]() {
-    if (left > 0) {
-      const uint32_t dst = ring + put * geo::SLOT_BYTES;
+    if (is.left > 0) {
       if (!second) {
         const int tok0 = (is.s.tile0 + is.t) << 4;
         const int head = is.sub % a.c.n_kv_heads;
@@ -281,57 +304,49 @@ __global__ void __launch_bounds__(CA_THREADS, (ca_geom<FMT, D, NT>::BLOCKS_PER_S
           blk = 0;
           n_valid = 0;                               // reads as zeros
         }
-        src = a.c.data + blk * a.c.block_stride + head * a.c.head_stride + (long long)(tok0 & page_mask) * (D * geo::ES);
-        const uint32_t ok0 = (g >= n_first && g < n_valid) ? 16u : 0u, ok1 = (g + 8 >= n_first && g + 8 < n_valid) ? 16u : 0u;
-#pragma unroll
-        for (int s = 0; s < geo::K_CHUNKS; ++s) {
-          const char* p = src + g * (D * geo::ES) + (t + 4 * s) * 16;
-          ca_cp16(dst + (2 * s) * 512 + lane * 16, p, ok0);
-          ca_cp16(dst + (2 * s + 1) * 512 + lane * 16, p + 8 * D * geo::ES, ok1);
-        }
+        const int in_page = tok0 & page_mask;
+        const char* page = a.c.data + blk * a.c.block_stride + head * a.c.head_stride;
+        src = page + in_page * geo::ROW;
+        copy_half(src);
         if (FP8 && lane < 8) {
           // exponents: K's behind all the codes of the page, V's behind those
-          const int in_page = tok0 & page_mask;
-          const char* ex = src - in_page * D + (2 * D + (lane >= 4 ? 1 : 0)) * (page_mask + 1) + in_page + (lane & 3) * 4;
-          ca_cp4(dst + geo::HALF_BYTES + lane * 4, ex, n_valid > 0 ? 4u : 0u);
+          const char* ex = page + (2 * D + (lane >> 2)) * (page_mask + 1) + in_page + (lane & 3) * 4;
+          ca_cp4(put + geo::HALF_BYTES + lane * 4, ex, n_valid > 0 ? 4u : 0u);
         }
         second = true;
       } else {
-        const char* vp = src + (long long)(page_mask + 1) * (D * geo::ES);
-#pragma unroll
-        for (int k = 0; k < 4; ++k) {
-          const int tok = 2 * t + (k & 1) + (k >> 1) * 8;
-          const bool ok = tok >= n_first && tok < n_valid;
-          if (FP8 && D == 64) {
-            ca_cp8(dst + k * 256 + lane * 8, vp + tok * D + g * 8, ok ? 8u : 0u);
-          } else if (FP8) {
-            ca_cp16(dst + k * 512 + lane * 16, vp + tok * D + g * 16, ok ? 16u : 0u);
-          } else {
-#pragma unroll
-            for (int c = 0; c < D / 64; ++c)
-              ca_cp16(dst + (k * (D / 64) + c) * 512 + lane * 16, vp + tok * (2 * D) + c * 128 + g * 16, ok ? 16u : 0u);
-          }
-        }
+        copy_half(src + (page_mask + 1) * geo::ROW);
         second = false;
-        if (--left > 0) {
-          ca_advance(a, is, CA_WARPS, subs);
-          next_blk = block_of(is);
-        }
+        ca_step(a, is, subs);
+        if (is.left > 0) next_blk = block_of(is);
       }
     }
     ca_commit();
-    put = put + 1 == NS ? 0 : put + 1;
+    put = put + geo::SLOT_BYTES == ring + geo::WARP_BYTES ? ring : put + geo::SLOT_BYTES;
   };
 #pragma unroll 1
   for (int i = 0; i < NS; ++i) issue();
-  int take = 0;                                      // slot of the next half to use
+  uint32_t take = ring;                              // slot of the next half to use
+  auto use_up = [&]() {                              // everything of the slot is in registers: refill it
+    __syncwarp();
+    take = take + geo::SLOT_BYTES == ring + geo::WARP_BYTES ? ring : take + geo::SLOT_BYTES;
+    issue();
+  };
+  // ldmatrix addresses: K matrices (rows 0-7 | 8-15) x (chunk 2i | 2i+1), V matrices the same or with the two swapped
+  const int r8 = lane & 7, m1 = (lane >> 3) & 1, m2 = lane >> 4;
+  const uint32_t k_row = (r8 + 8 * m1) * geo::ROW, k_x = (ca_place<geo::ROW>(r8 + 8 * m1, 0) - k_row) ^ (m2 << 4);
+  const int v_r = FP8 ? r8 + 8 * m1 : r8 + 8 * m2, v_c = FP8 ? m2 : m1;
+  const uint32_t v_row = v_r * geo::ROW, v_x = (ca_place<geo::ROW>(v_r, 0) - v_row) ^ (v_c << 4);
 
   // ---- the using side, unit by unit
-  int b = sh_start[0], sub = sh_start[1], t0 = sh_start[2];
-  ca_span s = ca_span_of(a, b, false);
   int4 desc = make_int4(0, 0, 0, 0);
-  for (long long f = f0; f < f1;) {
-    const int n_here = (int)min((long long)(s.tiles - t0), f1 - f);   // tiles of the unit in this block
+  int2 key = make_int2(-1, 0);                       // the unit whose piece is left over at the end of the run
+  float acc[NT][D / 16][4];
+  float ref[NT][2], sum[NT][2];
+  while (u.left > 0) {
+    const int b = u.b, sub = u.sub, t0 = u.t;
+    const ca_span s = u.s;
+    const int n_here = min(s.tiles - t0, u.left);                     // tiles of the unit in this run
     if (n_here <= 0) break;                                           // lengths changed under the call: stop
     const int rt = sub / a.c.n_kv_heads, head = sub - rt * a.c.n_kv_heads;
     const int r0 = rt * NT * 8;                                       // first row of the tile
@@ -343,26 +358,31 @@ __global__ void __launch_bounds__(CA_THREADS, (ca_geom<FMT, D, NT>::BLOCKS_PER_S
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt) {
       const int row = r0 + nt * 8 + g;
-      uint2 w[D / 16];
       if (row < a.n_rows) {
         const int tok = row / a.G;
         const char* qr = a.q + ((long long)b * a.Tq + tok) * a.q_token_stride + (head * a.G + row - tok * a.G) * a.q_head_stride;
 #pragma unroll
         for (int ks = 0; ks < D / 16; ++ks) {
-          const int ch = (t + 4 * (ks / (geo::CH / 4))) * geo::CH + 4 * (ks % (geo::CH / 4));
-          w[ks] = *reinterpret_cast<const uint2*>(qr + 2 * ch);
+          if (FP8) {                                                  // k-slots 2t, 2t+1 | 2t+8, 2t+9: channels 4t .. 4t+3 of 16
+            const uint2 w = *reinterpret_cast<const uint2*>(qr + 2 * (16 * ks + 4 * t));
+            qf[nt][2 * ks] = w.x;
+            qf[nt][2 * ks + 1] = w.y;
+          } else {
+            qf[nt][2 * ks] = *reinterpret_cast<const uint32_t*>(qr + 2 * (16 * ks + 2 * t));
+            qf[nt][2 * ks + 1] = *reinterpret_cast<const uint32_t*>(qr + 2 * (16 * ks + 8 + 2 * t));
+          }
         }
       } else {
 #pragma unroll
-        for (int ks = 0; ks < D / 16; ++ks) w[ks] = make_uint2(0u, 0u);
+        for (int ks = 0; ks < D / 8; ++ks) qf[nt][ks] = 0u;
       }
       float back = 1.f;                                               // what the row was divided by
       if (FP8) {
         float amax = 0.f;
 #pragma unroll
-        for (int ks = 0; ks < D / 16; ++ks) {
-          const float2 u0 = dd_unpack2<TQ>(w[ks].x), u1 = dd_unpack2<TQ>(w[ks].y);
-          amax = fmaxf(amax, fmaxf(fmaxf(fabsf(u0.x), fabsf(u0.y)), fmaxf(fabsf(u1.x), fabsf(u1.y))));
+        for (int ks = 0; ks < D / 8; ++ks) {
+          const float2 w = dd_unpack2<TQ>(qf[nt][ks]);
+          amax = fmaxf(amax, fmaxf(fabsf(w.x), fabsf(w.y)));
         }
         amax = fmaxf(amax, __shfl_xor_sync(0xffffffffu, amax, 1));
         amax = fmaxf(amax, __shfl_xor_sync(0xffffffffu, amax, 2));
@@ -373,14 +393,11 @@ __global__ void __launch_bounds__(CA_THREADS, (ca_geom<FMT, D, NT>::BLOCKS_PER_S
         const float by = __uint_as_float((uint32_t)(127 - e) << 23);
         back = __uint_as_float((uint32_t)(127 + e) << 23);
 #pragma unroll
-        for (int ks = 0; ks < D / 16; ++ks) {
-          const float2 u0 = dd_unpack2<TQ>(w[ks].x), u1 = dd_unpack2<TQ>(w[ks].y);
-          w[ks].x = dd_pack2<__half>(u0.x * by, u0.y * by);
-          w[ks].y = dd_pack2<__half>(u1.x * by, u1.y * by);
+        for (int ks = 0; ks < D / 8; ++ks) {
+          const float2 w = dd_unpack2<TQ>(qf[nt][ks]);
+          qf[nt][ks] = dd_pack2<__half>(w.x * by, w.y * by);
         }
       }
-#pragma unroll
-      for (int ks = 0; ks < D / 16; ++ks) { qf[nt][2 * ks] = w[ks].x; qf[nt][2 * ks + 1] = w[ks].y; }
 #pragma unroll
       for (int c = 0; c < 2; ++c) {
         zs[nt][c] = a.scale_log2 * (FP8 ? __shfl_sync(0xffffffffu, back, (2 * t + c) * 4) : 1.f);
@@ -391,8 +408,6 @@ __global__ void __launch_bounds__(CA_THREADS, (ca_geom<FMT, D, NT>::BLOCKS_PER_S
     const int pos_lo = s.end - a.Tq + r0 / a.G;                       // positions of the first and last row of the tile
     const int pos_hi = s.end - a.Tq + (min(a.n_rows, r0 + NT * 8) - 1) / a.G;
 
-    float acc[NT][D / 16][4];
-    float ref[NT][2], sum[NT][2];
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt) {
 #pragma unroll
@@ -401,46 +416,45 @@ __global__ void __launch_bounds__(CA_THREADS, (ca_geom<FMT, D, NT>::BLOCKS_PER_S
       sum[nt][0] = sum[nt][1] = 0.f;
     }
 
-    int i = (warp - (int)((f - f0) % CA_WARPS) + CA_WARPS) % CA_WARPS;   // first tile of the segment that is this warp's
-    for (; i < n_here; i += CA_WARPS) {
+    for (int i = 0; i < n_here; ++i) {
       const int tok0 = (s.tile0 + t0 + i) << 4;
       // ---- scores
       float z[NT][4];
       int kex0 = 0, kex1 = 0, vex0 = 0, vex1 = 0;
       ca_wait<NS - 1>();
-      if (FP8) __syncwarp();
+      __syncwarp();
       {
-        const uint32_t slot = ring + take * geo::SLOT_BYTES;
         float z2[NT][4];                                              // two chains: the products of one depend on each other
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt)
           z[nt][0] = z[nt][1] = z[nt][2] = z[nt][3] = z2[nt][0] = z2[nt][1] = z2[nt][2] = z2[nt][3] = 0.f;
+        const uint32_t at = take + k_row;
+        if (FP8) {
 #pragma unroll
-        for (int c = 0; c < geo::K_CHUNKS; ++c) {
-          const uint4 lo = ca_lds16(slot + (2 * c) * 512 + lane * 16), hi = ca_lds16(slot + (2 * c + 1) * 512 + lane * 16);
-          if (FP8) {
+          for (int c = 0; c < D / 32; ++c) {
+            uint32_t r[4];                                            // four codes each: rows g, g + 8 of chunk 2c, of chunk 2c + 1
+            ca_ldsm(r, at + (k_x ^ (c << 5)));
 #pragma unroll
-            for (int w = 0; w < 4; ++w) {
+            for (int w = 0; w < 2; ++w) {
               uint32_t a0, a1, a2, a3;
-              dd_e4m3x4_to_half(ca_word(lo, w), a0, a2);
-              dd_e4m3x4_to_half(ca_word(hi, w), a1, a3);
+              dd_e4m3x4_to_half(r[2 * w], a0, a2);
+              dd_e4m3x4_to_half(r[2 * w + 1], a1, a3);
 #pragma unroll
-              for (int nt = 0; nt < NT; ++nt)
-                ca_mma<FMT>((w & 1) ? z2[nt] : z[nt], a0, a1, a2, a3, qf[nt][2 * (4 * c + w)], qf[nt][2 * (4 * c + w) + 1]);
-            }
-          } else {
-#pragma unroll
-            for (int nt = 0; nt < NT; ++nt) {
-              ca_mma<FMT>(z[nt], lo.x, hi.x, lo.y, hi.y, qf[nt][4 * c], qf[nt][4 * c + 1]);
-              ca_mma<FMT>(z2[nt], lo.z, hi.z, lo.w, hi.w, qf[nt][4 * c + 2], qf[nt][4 * c + 3]);
+              for (int nt = 0; nt < NT; ++nt) ca_mma<FMT>(w ? z2[nt] : z[nt], a0, a1, a2, a3, qf[nt][4 * c + 2 * w], qf[nt][4 * c + 2 * w + 1]);
             }
           }
-        }
-        if (FP8) {
-          kex0 = ca_lds_byte(slot + geo::HALF_BYTES + g);
-          kex1 = ca_lds_byte(slot + geo::HALF_BYTES + g + 8);
-          vex0 = ca_lds_byte(slot + geo::HALF_BYTES + 16 + g) - 127;
-          vex1 = ca_lds_byte(slot + geo::HALF_BYTES + 16 + g + 8) - 127;
+          kex0 = ca_lds_byte(take + geo::HALF_BYTES + g);
+          kex1 = ca_lds_byte(take + geo::HALF_BYTES + g + 8);
+          vex0 = ca_lds_byte(take + geo::HALF_BYTES + 16 + g) - 127;
+          vex1 = ca_lds_byte(take + geo::HALF_BYTES + 16 + g + 8) - 127;
+        } else {
+#pragma unroll
+          for (int c = 0; c < D / 16; ++c) {
+            uint32_t r[4];
+            ca_ldsm(r, at + (k_x ^ (c << 5)));
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt) ca_mma<FMT>((c & 1) ? z2[nt] : z[nt], r[0], r[1], r[2], r[3], qf[nt][2 * c], qf[nt][2 * c + 1]);
+          }
         }
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt)
@@ -450,9 +464,7 @@ __global__ void __launch_bounds__(CA_THREADS, (ca_geom<FMT, D, NT>::BLOCKS_PER_S
             if (FP8) z[nt][e] *= dd_two_to_byte(e < 2 ? kex0 : kex1);
           }
       }
-      if (FP8) __syncwarp();                                          // the exponents have been read: the slot may be refilled
-      take = take + 1 == NS ? 0 : take + 1;
-      issue();
+      use_up();
 
       // ---- masks: z[.][0..1] is token tok0 + g, z[.][2..3] token tok0 + g + 8
       const bool partial = tok0 + 15 > pos_lo || (a.window > 0 && tok0 <= pos_hi - a.window);
@@ -503,76 +515,76 @@ __global__ void __launch_bounds__(CA_THREADS, (ca_geom<FMT, D, NT>::BLOCKS_PER_S
             sum[nt][e & 1] += p[e];
           }
         }
-        using TP = typename ca_types<FMT == 0 ? 0 : 1>::Q;
         pb[nt][0] = ca_transpose(dd_pack2<TP>(p[0], p[1]));
         pb[nt][1] = ca_transpose(dd_pack2<TP>(p[2], p[3]));
       }
 
       // ---- weighted values
       ca_wait<NS - 1>();
-      {
-        const uint32_t slot = ring + take * geo::SLOT_BYTES;
-        // Tokens seen by some rows of the tile and not by others: a weight of zero does not keep an infinity or NaN of V
-        // out of the sum, so the products are taken query token by query token with the unseen values replaced by zeros.
-        const bool mixed = partial && a.Tq > 1;
-        for (int p = mixed ? pos_lo : pos_hi; p <= pos_hi; ++p) {
-          uint4 v[4][(D + 63) / 64];
+      __syncwarp();
+      // Registers of V^T: r[0], r[1] hold tokens 2t | 2t+1 (low | high half), r[2], r[3] tokens 2t+8 | 2t+9, for the channels of
+      // rows g and g + 8.
+      auto value_frag = [&](uint32_t (&r)[4], const uint32_t (&raw)[4], int half) {
+        if (FP8) {
+          // bytes of a register: two channels of token 2t, the same two of 2t+1; token pairs side by side, then as halves
+          dd_e4m3x4_to_half(__byte_perm(raw[2 * half], 0u, 0x3120u), r[0], r[1]);
+          dd_e4m3x4_to_half(__byte_perm(raw[2 * half + 1], 0u, 0x3120u), r[2], r[3]);
+        } else {
 #pragma unroll
-          for (int k = 0; k < 4; ++k) {
-            if (FP8 && D == 64) {
-              const uint2 h = ca_lds8(slot + k * 256 + lane * 8);
-              v[k][0] = make_uint4(h.x, h.y, 0u, 0u);
-            } else if (FP8) {
-              v[k][0] = ca_lds16(slot + k * 512 + lane * 16);
-            } else {
+          for (int e = 0; e < 4; ++e) r[e] = raw[e];
+        }
+      };
+      const uint32_t at = take + v_row;
+      if (!(partial && a.Tq > 1)) {
 #pragma unroll
-              for (int c = 0; c < D / 64; ++c) v[k][c] = ca_lds16(slot + (k * (D / 64) + c) * 512 + lane * 16);
-            }
-            if (mixed) {
-              const int tok = tok0 + 2 * t + (k & 1) + (k >> 1) * 8;
-              if (tok > p || (a.window > 0 && tok <= p - a.window)) {
+        for (int c = 0; c < D / (FP8 ? 32 : 16); ++c) {
+          uint32_t raw[4];
+          ca_ldsm_trans(raw, at + (v_x ^ (c << 5)));
 #pragma unroll
-                for (int c = 0; c < (D + 63) / 64; ++c) v[k][c] = make_uint4(0u, 0u, 0u, 0u);
-              }
-            }
+          for (int half = 0; half < (FP8 ? 2 : 1); ++half) {
+            uint32_t r[4];
+            value_frag(r, raw, half);
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt) ca_mma<FMT>(acc[nt][FP8 ? 2 * c + half : c], r[0], r[1], r[2], r[3], pb[nt][0], pb[nt][1]);
+          }
+        }
+      } else {
+        // Some tokens are seen by some rows of the tile and not by others: a weight of zero does not keep an infinity or NaN
+        // of V out of the sum, so the products are taken query token by query token with the unseen values made zero.
+#pragma unroll 1
+        for (int p = pos_lo; p <= pos_hi; ++p) {
+          uint32_t keep[2];                                           // tokens 2t | 2t+1 and 2t+8 | 2t+9
+#pragma unroll
+          for (int k = 0; k < 2; ++k) {
+            const int tok = tok0 + 2 * t + 8 * k, from = a.window > 0 ? p - a.window : -1;
+            keep[k] = ((tok <= p && tok > from) ? 0xffffu : 0u) | ((tok + 1 <= p && tok + 1 > from) ? 0xffff0000u : 0u);
           }
 #pragma unroll
-          for (int m = 0; m < D / 16; ++m) {
-            uint32_t a0, a1, a2, a3;
-            if (FP8) {
-              // bytes 2(m&1), 2(m&1)+1 of word m / 2: two channels; tokens 2t | 2t+1 side by side, then as halves
-              const uint32_t sel = (m & 1) ? 0x7362u : 0x5140u;
-              dd_e4m3x4_to_half(__byte_perm(ca_word(v[0][0], m >> 1), ca_word(v[1][0], m >> 1), sel), a0, a1);
-              dd_e4m3x4_to_half(__byte_perm(ca_word(v[2][0], m >> 1), ca_word(v[3][0], m >> 1), sel), a2, a3);
-            } else {
-              const int c = m >> 2, w = m & 3;
-              a0 = __byte_perm(ca_word(v[0][c], w), ca_word(v[1][c], w), 0x5410u);
-              a1 = __byte_perm(ca_word(v[0][c], w), ca_word(v[1][c], w), 0x7632u);
-              a2 = __byte_perm(ca_word(v[2][c], w), ca_word(v[3][c], w), 0x5410u);
-              a3 = __byte_perm(ca_word(v[2][c], w), ca_word(v[3][c], w), 0x7632u);
-            }
+          for (int c = 0; c < D / (FP8 ? 32 : 16); ++c) {
+            uint32_t raw[4];
+            ca_ldsm_trans(raw, at + (v_x ^ (c << 5)));
 #pragma unroll
-            for (int nt = 0; nt < NT; ++nt) {
-              if (!mixed) {
-                ca_mma<FMT>(acc[nt][m], a0, a1, a2, a3, pb[nt][0], pb[nt][1]);
-              } else {
+            for (int e = 0; e < 4; ++e) raw[e] &= keep[FP8 ? (e & 1) : (e >> 1)];
+#pragma unroll
+            for (int half = 0; half < (FP8 ? 2 : 1); ++half) {
+              uint32_t r[4];
+              value_frag(r, raw, half);
+#pragma unroll
+              for (int nt = 0; nt < NT; ++nt) {
                 float one[4] = {0.f, 0.f, 0.f, 0.f};
-                ca_mma<FMT>(one, a0, a1, a2, a3, pb[nt][0], pb[nt][1]);
+                ca_mma<FMT>(one, r[0], r[1], r[2], r[3], pb[nt][0], pb[nt][1]);
 #pragma unroll
                 for (int e = 0; e < 4; ++e)
-                  if (pos[nt][e & 1] == p) acc[nt][m][e] += one[e];
+                  if (pos[nt][e & 1] == p) acc[nt][FP8 ? 2 * c + half : c][e] += one[e];
               }
             }
           }
         }
       }
-      take = take + 1 == NS ? 0 : take + 1;
-      issue();
+      use_up();
     }
 
-    // ---- the block's result for the unit: warps merged pairwise, always in the same order
-    const bool whole = t0 == 0 && n_here == s.tiles;
-    const int slot_of_block = 2 * blockIdx.x + (t0 == 0 ? 1 : 0);
+    // ---- the end of the unit, or of the run
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
@@ -580,159 +592,162 @@ __global__ void __launch_bounds__(CA_THREADS, (ca_geom<FMT, D, NT>::BLOCKS_PER_S
         sum[nt][c] += __shfl_xor_sync(0xffffffffu, sum[nt][c], 4);
         sum[nt][c] += __shfl_xor_sync(0xffffffffu, sum[nt][c], 8);
         sum[nt][c] += __shfl_xor_sync(0xffffffffu, sum[nt][c], 16);
-        if (g == 0) sh_ml[warp][nt * 8 + 2 * t + c] = make_float2(ref[nt][c], sum[nt][c]);
       }
-    __syncthreads();
-    float top[NT][2], den[NT][2];
+    const bool ends = t0 + n_here == s.tiles;
+    if (ends && t0 == 0) {
 #pragma unroll
-    for (int nt = 0; nt < NT; ++nt)
+      for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-      for (int c = 0; c < 2; ++c) {
-        float M = -INFINITY, L = 0.f;
+        for (int c = 0; c < 2; ++c) {
+          const int r = r0 + nt * 8 + 2 * t + c;
+          if (r < a.n_rows) {
+            const int tok = r / a.G, h = head * a.G + r - tok * a.G;
+            const long long tn = (long long)b * a.Tq + tok;
+            const bool empty = pos[nt][c] < 0;
+            const float inv = empty ? 0.f : 1.f / sum[nt][c];
+            char* o = a.out + tn * a.out_token_stride + h * a.out_head_stride;
 #pragma unroll
-        for (int w = 0; w < CA_WARPS; ++w) M = fmaxf(M, sh_ml[w][nt * 8 + 2 * t + c].x);
-#pragma unroll
-        for (int w = 0; w < CA_WARPS; ++w) {
-          const float2 ml = sh_ml[w][nt * 8 + 2 * t + c];
-          L += ml.x == -INFINITY ? ml.y : ml.y * ca_exp2(ml.x - M);   // a warp without a finite weight still passes on a NaN
+            for (int m = 0; m < D / 16; ++m) {
+              const uint32_t w = empty ? 0u : dd_pack2<TQ>(acc[nt][m][c] * inv, acc[nt][m][2 + c] * inv);
+              if (FP8) {
+                *reinterpret_cast<uint32_t*>(o + 2 * ca_channel(FP8, g, m)) = w;
+              } else {
+                *reinterpret_cast<unsigned short*>(o + 2 * ca_channel(FP8, g, m)) = (unsigned short)w;
+                *reinterpret_cast<unsigned short*>(o + 2 * (ca_channel(FP8, g, m) + ca_pair(FP8))) = (unsigned short)(w >> 16);
+              }
+            }
+            if (a.lse && g == 0) a.lse[tn * a.n_q_heads + h] = empty ? -INFINITY : ca_lse(ref[nt][c], sum[nt][c]);
+          }
         }
-        top[nt][c] = M;
-        den[nt][c] = L;
-        const float fix = ref[nt][c] == -INFINITY ? 1.f : ca_exp2(ref[nt][c] - M);
+    } else if (ends) {
+      // the last piece of a unit that began in an earlier run: slot 2 me
+      float* po = a.part_o + 2LL * me * NT * geo::NACC * 32;
 #pragma unroll
-        for (int m = 0; m < D / 16; ++m) { acc[nt][m][c] *= fix; acc[nt][m][2 + c] *= fix; }
+      for (int nt = 0; nt < NT; ++nt) {
+#pragma unroll
+        for (int m = 0; m < D / 16; ++m)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) po[(nt * geo::NACC + m * 4 + e) * 32 + lane] = acc[nt][m][e];
+        if (g == 0) {
+          a.part_ml[2LL * me * NT * 8 + nt * 8 + 2 * t] = make_float2(ref[nt][0], sum[nt][0]);
+          a.part_ml[2LL * me * NT * 8 + nt * 8 + 2 * t + 1] = make_float2(ref[nt][1], sum[nt][1]);
+        }
       }
+    } else {
+      key = make_int2(b, sub);                                        // the run ends inside the unit
+    }
+    if (t0 == 0 && !ends)                                             // it begins here: its last tile lies in run ...
+      desc = make_int4(b, sub, (int)((share * me + (share - u.left) + s.tiles - 1) / share) + 1, 0);
+
+    // ---- the next unit
+    u.left -= n_here + CA_UNIT_COST;
+    if (u.left > 0) ca_next_unit(a, u, subs);
+  }
+  if (lane == 0) a.desc[me] = desc;
+  ca_wait<0>();
+  __syncwarp();
+
+  // ---- pieces left over at the ends of the runs: neighbouring warps inside the same unit become one partial, in slot
+  // 2 w + 1 of the first of them
+  if (lane == 0) sh_key[warp] = key;
+  if (key.x >= 0) {
+    float* own = reinterpret_cast<float*>(ca_smem + warp * geo::WARP_BYTES);
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt) {
 #pragma unroll
-      for (int half = CA_WARPS / 2; half >= 1; half >>= 1) {
-        if (warp >= half && warp < 2 * half) {
+      for (int m = 0; m < D / 16; ++m)
 #pragma unroll
-          for (int m = 0; m < D / 16; ++m)
-#pragma unroll
-            for (int e = 0; e < 4; ++e) merge[((warp - half) * geo::NACC + m * 4 + e) * 32 + lane] = acc[nt][m][e];
-        }
-        __syncthreads();
-        if (warp < half) {
-#pragma unroll
-          for (int m = 0; m < D / 16; ++m)
-#pragma unroll
-            for (int e = 0; e < 4; ++e) acc[nt][m][e] += merge[(warp * geo::NACC + m * 4 + e) * 32 + lane];
-        }
-        __syncthreads();
-      }
-    }
-    if (warp == 0) {
-      if (whole) {
-#pragma unroll
-        for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-          for (int c = 0; c < 2; ++c) {
-            const int r = r0 + nt * 8 + 2 * t + c;
-            if (r < a.n_rows) {
-              const int tok = r / a.G, h = head * a.G + r - tok * a.G;
-              const long long tn = (long long)b * a.Tq + tok;
-              const bool empty = pos[nt][c] < 0;
-              const float inv = empty ? 0.f : 1.f / den[nt][c];
-              char* o = a.out + tn * a.out_token_stride + h * a.out_head_stride;
-#pragma unroll
-              for (int k = 0; k < D / 64; ++k) {
-                uint32_t w[4];
-#pragma unroll
-                for (int q = 0; q < 4; ++q)
-                  w[q] = empty ? 0u : dd_pack2<TQ>(acc[nt][4 * k + q][c] * inv, acc[nt][4 * k + q][2 + c] * inv);
-                *reinterpret_cast<uint4*>(o + 2 * ca_channel(FP8, D, g, 4 * k)) = make_uint4(w[0], w[1], w[2], w[3]);
-              }
-              if (a.lse && g == 0)
-                a.lse[tn * a.n_q_heads + h] = empty ? -INFINITY : (top[nt][c] - CA_HEADROOM + log2f(den[nt][c])) * 0.6931471805599453f;
-            }
-          }
-      } else {
-        float* po = a.part_o + (long long)slot_of_block * NT * geo::NACC * 32;
-#pragma unroll
-        for (int nt = 0; nt < NT; ++nt) {
-#pragma unroll
-          for (int m = 0; m < D / 16; ++m)
-#pragma unroll
-            for (int e = 0; e < 4; ++e) po[(nt * geo::NACC + m * 4 + e) * 32 + lane] = acc[nt][m][e];
-          if (g == 0) {
-            a.part_ml[(long long)slot_of_block * NT * 8 + nt * 8 + 2 * t] = make_float2(top[nt][0], den[nt][0]);
-            a.part_ml[(long long)slot_of_block * NT * 8 + nt * 8 + 2 * t + 1] = make_float2(top[nt][1], den[nt][1]);
-          }
-        }
-      }
-    }
-    if (t0 == 0 && !whole)                                            // the last unit of the run, going on in the next blocks
-      desc = make_int4(b, sub, (int)((f + s.tiles - 1) / share - blockIdx.x) + 1, 0);
-
-    // ---- the next unit
-    f += n_here;
-    t0 = 0;
-    if (f < f1) {
-      if (++sub == subs) {
-        sub = 0;
-        do { s = ca_span_of(a, ++b, false); } while (s.tiles == 0 && b < B - 1);
+        for (int e = 0; e < 4; ++e) own[(nt * geo::NACC + m * 4 + e) * 32 + lane] = acc[nt][m][e];
+      if (g == 0) {
+        sh_ml[warp][nt * 8 + 2 * t] = make_float2(ref[nt][0], sum[nt][0]);
+        sh_ml[warp][nt * 8 + 2 * t + 1] = make_float2(ref[nt][1], sum[nt][1]);
       }
     }
   }
-  ca_wait<0>();
-  if (threadIdx.x == 0) a.desc[blockIdx.x] = desc;
+  __syncthreads();
+  for (int w0 = 0; w0 < CA_WARPS;) {
+    const int2 k0 = sh_key[w0];
+    int w1 = w0 + 1;
+    if (k0.x < 0) { w0 = w1; continue; }
+    while (w1 < CA_WARPS && sh_key[w1].x == k0.x && sh_key[w1].y == k0.y) ++w1;
+    const long long slot = 2LL * (blockIdx.x * CA_WARPS + w0) + 1;
+#pragma unroll
+    for (int k = 0; k < NT * geo::NACC * 32 / CA_THREADS; ++k) {
+      const int e = k * CA_THREADS + threadIdx.x;
+      const int row = e / (geo::NACC * 32) * 8 + 2 * (e & 3) + ((e >> 5) & 1);
+      float M = -INFINITY, L = 0.f, x = 0.f;
+      for (int w = w0; w < w1; ++w) M = fmaxf(M, sh_ml[w][row].x);
+      for (int w = w0; w < w1; ++w) {
+        const float2 ml = sh_ml[w][row];
+        const float sc = ml.x == -INFINITY ? 1.f : ca_exp2(ml.x - M);  // without a finite weight: zeros, or a NaN to pass on
+        L = fmaf(ml.y, sc, L);
+        x = fmaf(reinterpret_cast<const float*>(ca_smem + w * geo::WARP_BYTES)[e], sc, x);
+      }
+      a.part_o[slot * NT * geo::NACC * 32 + e] = x;
+      if (((e >> 2) & 7) == 0 && ((e >> 5) % geo::NACC) < 2) a.part_ml[slot * NT * 8 + row] = make_float2(M, L);
+    }
+    w0 = w1;
+  }
 }
 
-// Adds the partials of the unit that begins in block x of the attention kernel and goes on in the following ones.
-// Grid (blocks of the attention kernel, NT * D / 32): every thread owns one accumulator element.
+// Adds the partials of the cut units that begin in block x of the attention kernel. Grid (blocks of the attention kernel,
+// NT * D / 32): every thread owns one accumulator element. The partials of a unit from run w0 (where it begins) to run w1
+// (where it ends) are: one per block among the runs w0 .. w1 - 1, in the slot of the first of them, and the last piece.
 template <int FMT, int D, int NT>
-__global__ void __launch_bounds__(256) dd_cache_attn_join_kernel(const ca_args a, int max_parts) {
+__global__ void __launch_bounds__(256) dd_cache_attn_join_kernel(const ca_args a) {
   using TQ = typename ca_types<FMT>::Q;
   constexpr int NACC = D / 4;
   extern __shared__ float ja_scale[];                                 // [parts][8] of the column tile
   __shared__ float2 sh_ml[8];
   dd_grid_dependency_wait();
-  const int4 d = a.desc[blockIdx.x];
-  const int n = min(d.z, max_parts);
-  if (n == 0) return;
   const int e = blockIdx.y * 256 + threadIdx.x;                       // element: [nt][register][lane]
   const int nt = (blockIdx.y * 256) / (NACC * 32);
-  const long long first = 2LL * blockIdx.x + 1;                       // the unit's own block leaves its partial in its second slot
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  auto slot = [&](int i) { return i == 0 ? first : 2LL * (blockIdx.x + i); };
-  {
-    // warp w: the scales of row w of the column tile
-    const int row = nt * 8 + warp;
-    float M = -INFINITY;
-    for (int i = lane; i < n; i += 32) M = fmaxf(M, a.part_ml[slot(i) * NT * 8 + row].x);
-#pragma unroll
-    for (int o = 16; o; o >>= 1) M = fmaxf(M, __shfl_xor_sync(0xffffffffu, M, o));
-    float L = 0.f;
-    for (int i = lane; i < n; i += 32) {
-      const float2 ml = a.part_ml[slot(i) * NT * 8 + row];
-      const float sc = ml.x == -INFINITY ? 1.f : ca_exp2(ml.x - M);   // nothing but zeros (or NaN) there
-      ja_scale[i * 8 + warp] = sc;
-      L += ml.y * sc;
-    }
-#pragma unroll
-    for (int o = 16; o; o >>= 1) L += __shfl_xor_sync(0xffffffffu, L, o);
-    if (lane == 0) sh_ml[warp] = make_float2(M, L);
-  }
-  __syncthreads();
   const int reg = (e / 32) % NACC, m = reg >> 2, g = lane >> 2, t = lane & 3;
   const int col = 2 * t + (reg & 1);
-  float acc = 0.f;
+  for (int w0 = blockIdx.x * CA_WARPS; w0 < (blockIdx.x + 1) * CA_WARPS; ++w0) {
+    const int4 d = a.desc[w0];
+    if (d.z == 0) continue;
+    const int w1 = d.z - 1, first_block = w0 / CA_WARPS;
+    const int n = (w1 - 1) / CA_WARPS - first_block + 2;              // partials
+    auto slot = [&](int i) -> long long { return i == 0 ? 2LL * w0 + 1 : (i == n - 1 ? 2LL * w1 : 2LL * (first_block + i) * CA_WARPS + 1); };
+    __syncthreads();
+    {
+      // warp w: the scales of row w of the column tile
+      const int row = nt * 8 + warp;
+      float M = -INFINITY;
+      for (int i = lane; i < n; i += 32) M = fmaxf(M, a.part_ml[slot(i) * NT * 8 + row].x);
+#pragma unroll
+      for (int o = 16; o; o >>= 1) M = fmaxf(M, __shfl_xor_sync(0xffffffffu, M, o));
+      float L = 0.f;
+      for (int i = lane; i < n; i += 32) {
+        const float2 ml = a.part_ml[slot(i) * NT * 8 + row];
+        const float sc = ml.x == -INFINITY ? 1.f : ca_exp2(ml.x - M);
+        ja_scale[i * 8 + warp] = sc;
+        L += ml.y * sc;
+      }
+#pragma unroll
+      for (int o = 16; o; o >>= 1) L += __shfl_xor_sync(0xffffffffu, L, o);
+      if (lane == 0) sh_ml[warp] = make_float2(M, L);
+    }
+    __syncthreads();
+    float x = 0.f;
 #pragma unroll 8
-  for (int i = 0; i < n; ++i) acc = fmaf(a.part_o[slot(i) * (NT * NACC * 32) + e], ja_scale[i * 8 + col], acc);
-  const int rt = d.y / a.c.n_kv_heads, head = d.y - rt * a.c.n_kv_heads;
-  const int r = rt * NT * 8 + nt * 8 + col;
-  if (r >= a.n_rows) return;
-  const ca_span s = ca_span_of(a, d.x, false);
-  const int tok = r / a.G, h = head * a.G + r - tok * a.G;
-  const long long tn = (long long)d.x * a.Tq + tok;
-  const bool empty = s.end - a.Tq + tok < 0;
-  const float2 ml = sh_ml[col];
-  const int ch = ca_channel(FMT >= 2, D, g, m) + ((reg >> 1) & 1);
-  TQ* o = reinterpret_cast<TQ*>(a.out + tn * a.out_token_stride + h * a.out_head_stride);
-  const uint32_t w = dd_pack2<TQ>(empty ? 0.f : acc / ml.y, 0.f);
-  o[ch] = *reinterpret_cast<const TQ*>(&w);
-  if (a.lse && ch == 0) a.lse[tn * a.n_q_heads + h] = empty ? -INFINITY : (ml.x - CA_HEADROOM + log2f(ml.y)) * 0.6931471805599453f;
+    for (int i = 0; i < n; ++i) x = fmaf(a.part_o[slot(i) * (NT * NACC * 32) + e], ja_scale[i * 8 + col], x);
+    const int rt = d.y / a.c.n_kv_heads, head = d.y - rt * a.c.n_kv_heads;
+    const int r = rt * NT * 8 + nt * 8 + col;
+    if (r < a.n_rows) {
+      const ca_span s = ca_span_of(a, d.x, false);
+      const int tok = r / a.G, h = head * a.G + r - tok * a.G;
+      const long long tn = (long long)d.x * a.Tq + tok;
+      const bool empty = s.end - a.Tq + tok < 0;
+      const float2 ml = sh_ml[col];
+      const int ch = ca_channel(FMT >= 2, g, m) + (reg & 2 ? ca_pair(FMT >= 2) : 0);
+      const uint32_t w = dd_pack2<TQ>(empty ? 0.f : x / ml.y, 0.f);
+      *reinterpret_cast<unsigned short*>(a.out + tn * a.out_token_stride + h * a.out_head_stride + 2 * ch) = (unsigned short)w;
+      if (a.lse && ch == 0) a.lse[tn * a.n_q_heads + h] = empty ? -INFINITY : ca_lse(ml.x, ml.y);
+    }
+  }
 }
 
 struct ca_plan {
@@ -743,7 +758,7 @@ struct ca_plan {
 template <int FMT, int D, int NT> ca_plan ca_plan_of() {
   using geo = ca_geom<FMT, D, NT>;
   static_assert(geo::SMEM <= 227 * 1024, "shared memory of a block");
-  static_assert(geo::BLOCKS_PER_SM == 1 || geo::SMEM + 2048 <= 114 * 1024, "shared memory of two blocks");
+  static_assert(geo::BLOCKS_PER_SM == 1 || geo::SMEM + 1024 + 2048 <= 114 * 1024, "shared memory of two blocks");
   return {(const void*)dd_cache_attn_kernel<FMT, D, NT>, (const void*)dd_cache_attn_join_kernel<FMT, D, NT>, geo::SMEM, geo::BLOCKS_PER_SM, NT};
 }
 template <int FMT> ca_plan ca_pick(int d, int nt) {
@@ -766,11 +781,11 @@ int ca_column_tiles(int rows) { return rows <= 8 ? 1 : 2; }
 struct ca_sizes { size_t part_o, part_ml, desc; size_t total() const { return part_o + part_ml + desc; } };
 ca_sizes ca_size(int head_dim, int rows, int sms) {
   const int nt = ca_column_tiles(rows);
-  const size_t blocks = (size_t)sms * (nt == 1 ? 2 : 1);
+  const size_t warps = (size_t)sms * (nt == 1 ? 2 : 1) * CA_WARPS;
   ca_sizes z;
-  z.part_o = 2 * blocks * nt * 8 * head_dim * sizeof(float);
-  z.part_ml = 2 * blocks * nt * 8 * sizeof(float2);
-  z.desc = (blocks * sizeof(int4) + 255) & ~(size_t)255;
+  z.part_o = 2 * warps * nt * 8 * head_dim * sizeof(float);
+  z.part_ml = 2 * warps * nt * 8 * sizeof(float2);
+  z.desc = (warps * sizeof(int4) + 255) & ~(size_t)255;
   return z;
 }
 
@@ -857,11 +872,9 @@ extern "C" int dd_cache_decode_attn(const dd_cache* cache, int n_q_tokens, const
   cfg.dynamicSmemBytes = p.smem;
   void* args[] = {&a};
   DD_CUDA_TRY(nullptr, cudaLaunchKernelExC(&cfg, p.main_kernel, args));
-  int max_parts = blocks;
   cfg.gridDim = dim3((unsigned)blocks, (unsigned)(nt * cache->head_dim / 32));
   cfg.blockDim = dim3(256);
-  cfg.dynamicSmemBytes = (size_t)blocks * 8 * sizeof(float);
-  void* jargs[] = {&a, &max_parts};
-  DD_CUDA_TRY(nullptr, cudaLaunchKernelExC(&cfg, p.join_kernel, jargs));
+  cfg.dynamicSmemBytes = (size_t)(blocks + 1) * 8 * sizeof(float);     // at most one partial per block and the last piece
+  DD_CUDA_TRY(nullptr, cudaLaunchKernelExC(&cfg, p.join_kernel, args));
   return DD_OK;
 }
