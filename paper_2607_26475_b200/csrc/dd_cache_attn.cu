@@ -19,7 +19,7 @@
 //   O^T[d, n]    += V^T[d, token] P^T[token, n]   A = V^T, B = P^T
 // e4m3 pages: codes are exact as halves, so both products run as half MMAs on the codes. The power-of-two scale of a key
 // multiplies its scores; the scale of a value is added to the exponent of its weight: with w = z + log2(scale of v) the
-// running reference is the maximum of w, P = 2^(w - ref) <= 1 multiplies codes, and the denominator sums 2^(z - ref).
+// running reference is the maximum of w, P = 2^(w - ref) multiplies codes, and the denominator sums 2^(z - ref).
 // The reference moves only when a weight exceeds it by 2^8 (one vote per tile instead of a reduction), so P is at most
 // 2^14 after a factor 2^6 that keeps small weights out of the half's subnormals (a weight 2^-20 of the reference is still
 // normal). Queries are multiplied by a power of two per row to fill the half's range: exact for every element above
@@ -41,6 +41,7 @@ constexpr int CA_THREADS = CA_WARPS * 32;
 constexpr int CA_UNIT_COST = 1;              // empty places behind a unit in the flat list
 constexpr float CA_HEADROOM = 6.f;           // log2 of the factor on P
 constexpr float CA_LAZY = 8.f;               // how far (log2) a weight may exceed the reference
+constexpr float CA_NONE = -3.0e38f;          // reference before any token: every finite score exceeds it
 
 // formats: 0 bf16 pages and queries, 1 half pages and queries, 2 / 3 e4m3 pages with bf16 / half queries
 template <int FMT> struct ca_types { using Q = __nv_bfloat16; };
@@ -53,16 +54,20 @@ struct ca_geom {
   static constexpr int ES = FP8 ? 1 : 2;
   static constexpr int ROW = D * ES;                                  // bytes of a row: 64, 128 or 256
   static constexpr int HALF_BYTES = 16 * ROW;                         // K (or V) of a tile
-  static constexpr int SLOT_BYTES = HALF_BYTES + (FP8 ? 32 : 0);      // e4m3: + exponents of the tile (in K's slot)
+  // What one copy group of a warp brings: a whole tile where that is at most 4 KiB, else K or V of a tile in turn.
+  static constexpr bool WHOLE = 2 * HALF_BYTES <= 4096;
+  static constexpr int EXP_AT = 2 * HALF_BYTES;                       // e4m3: exponents of the tile, 16 of K and 16 of V
+  static constexpr int SLOT_BYTES = (WHOLE ? 2 : 1) * HALF_BYTES + (FP8 ? 32 : 0);
   static constexpr int COPIES = HALF_BYTES / 512;
   static constexpr int BLOCKS_PER_SM = NT == 1 ? 2 : 1;               // two column tiles need the registers of a whole SM
   static constexpr int RING_BUDGET = (BLOCKS_PER_SM == 2 ? 110 : 220) * 1024;
   static constexpr int STAGES_ = RING_BUDGET / (CA_WARPS * SLOT_BYTES);
-  static constexpr int STAGES = STAGES_ > 12 ? 12 : STAGES_;
+  static constexpr int STAGES = STAGES_ > 8 ? 8 : STAGES_;
   static constexpr int WARP_BYTES = STAGES * SLOT_BYTES;
   static constexpr int SMEM = CA_WARPS * WARP_BYTES;
   static constexpr int NACC = D / 4;                                  // accumulator registers per column tile
   static_assert(WARP_BYTES >= NT * NACC * 128, "a warp's ring holds its accumulators at the end");
+  static_assert(!FP8 || WHOLE, "exponents travel with a whole tile");
 };
 
 // Byte offset of 16-byte chunk c of row r in a half tile: a column of 8 rows covers all 32 banks.
@@ -125,6 +130,17 @@ __device__ __forceinline__ float ca_exp2(float x) {
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
   return y;
 }
+__device__ __forceinline__ void ca_cp16_all(uint32_t dst, const void* src) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
+}
+// What adding the rows of i copies of 512 bytes changes in ca_place's xor.
+template <int ROW> __device__ __forceinline__ constexpr uint32_t ca_twist(int i) {
+  return ROW >= 128 ? ((i * (512 / ROW)) & 7) << 4 : 0;              // 64-byte rows: 8 rows a copy, nothing changes
+}
+__device__ __forceinline__ long long ca_div(long long x, int y) {    // x >= 0, y > 0
+  return (x >> 32) == 0 ? (long long)((uint32_t)x / (uint32_t)y) : x / y;
+}
+
 // Tokens [first, end) of a request that any of its query tokens sees, as tiles of 16.
 struct ca_span {
   int end, first;      // tokens; first is the lowest visible one
@@ -177,7 +193,7 @@ __device__ __forceinline__ void ca_step(const ca_args& a, ca_cursor& k, int subs
 __device__ __forceinline__ int ca_channel(bool fp8, int g, int m) { return 16 * m + (fp8 ? 2 * g : g); }
 __device__ __forceinline__ constexpr int ca_pair(bool fp8) { return fp8 ? 1 : 8; }
 
-__device__ __forceinline__ float ca_lse(float ref, float den) { return (ref - CA_HEADROOM + log2f(den)) * 0.6931471805599453f; }
+__device__ __forceinline__ float ca_lse(float from, float den) { return (from + log2f(den)) * 0.6931471805599453f; }
 
 template <int FMT, int D, int NT>
 __global__ void __launch_bounds__(CA_THREADS, (ca_geom<FMT, D, NT>::BLOCKS_PER_SM)) dd_cache_attn_kernel(const ca_args a) {
@@ -187,8 +203,6 @@ __global__ void __launch_bounds__(CA_THREADS, (ca_geom<FMT, D, NT>::BLOCKS_PER_S
   constexpr bool FP8 = geo::FP8;
   constexpr int NS = geo::STAGES;
   extern __shared__ __align__(128) unsigned char ca_smem[];
-  __shared__ long long sh_scan[CA_WARPS];
-  __shared__ int sh_start[CA_WARPS][3];
   __shared__ float2 sh_ml[CA_WARPS][NT * 8];
   __shared__ int2 sh_key[CA_WARPS];
 
@@ -196,107 +210,102 @@ __global__ void __launch_bounds__(CA_THREADS, (ca_geom<FMT, D, NT>::BLOCKS_PER_S
   const int g = lane >> 2, t = lane & 3;
   const int subs = a.row_tiles * a.c.n_kv_heads;
   const int B = a.c.batch;
-  const long long n_warps = (long long)gridDim.x * CA_WARPS;
   const int me = blockIdx.x * CA_WARPS + warp;
 
   dd_grid_dependency_wait();
 
-  // ---- the runs of this block's warps in the flat list
-  long long mine = 0;
-  const int chunk = (B + CA_THREADS - 1) / CA_THREADS;
-  const int b_lo = min(B, (int)threadIdx.x * chunk), b_hi = min(B, b_lo + chunk);
-  for (int b = b_lo; b < b_hi; ++b) {
-    const int nt = ca_span_of(a, b, blockIdx.x == 0).tiles;
-    if (nt > 0) mine += (long long)(nt + CA_UNIT_COST) * subs;
-  }
-  long long incl = mine;
+  // ---- this warp's run of the flat list: every warp adds up the list by itself, 32 requests at a time
+  ca_cursor is;
+  is.b = is.sub = is.t = is.left = 0;
+  is.s = ca_span_of(a, min(lane, B - 1), blockIdx.x == 0 && warp == 0 && lane < B);
+  auto places = [&](const ca_span& sp) -> long long { return sp.tiles > 0 ? (long long)(sp.tiles + CA_UNIT_COST) * subs : 0; };
+  const long long cost0 = lane < B ? places(is.s) : 0;               // of the first 32 requests
+  long long total = cost0;
+  for (int b = lane + 32; b < B; b += 32) total += places(ca_span_of(a, b, blockIdx.x == 0 && warp == 0));
 #pragma unroll
-  for (int o = 1; o < 32; o <<= 1) {
-    const long long v = __shfl_up_sync(0xffffffffu, incl, o);
-    if (lane >= o) incl += v;
-  }
-  if (lane == 31) sh_scan[warp] = incl;
-  if (threadIdx.x < CA_WARPS) sh_start[threadIdx.x][0] = -1;
-  __syncthreads();
-  long long total = 0, before = 0;
-#pragma unroll
-  for (int w = 0; w < CA_WARPS; ++w) {
-    if (w < warp) before += sh_scan[w];
-    total += sh_scan[w];
-  }
-  const long long share = max(1LL, (total + n_warps - 1) / n_warps);
-  if (mine > 0) {
-    const long long lo = before + incl - mine;       // first place of this thread's requests
-    for (int w = 0; w < CA_WARPS; ++w) {
-      const long long f = share * ((long long)blockIdx.x * CA_WARPS + w);
-      if (f < lo || f >= lo + mine) continue;
-      long long at = lo;
-      for (int b = b_lo; b < b_hi; ++b) {
-        const int nt = ca_span_of(a, b, false).tiles;
-        const long long n = nt > 0 ? (long long)(nt + CA_UNIT_COST) * subs : 0;
-        if (f < at + n) {
-          sh_start[w][0] = b;
-          sh_start[w][1] = (int)((f - at) / (nt + CA_UNIT_COST));
-          sh_start[w][2] = (int)((f - at) % (nt + CA_UNIT_COST));
-          break;
-        }
-        at += n;
+  for (int o = 16; o; o >>= 1) total += __shfl_xor_sync(0xffffffffu, total, o);
+  const long long share = max(1LL, ca_div(total + (long long)gridDim.x * CA_WARPS - 1, (int)gridDim.x * CA_WARPS));
+  const long long f0 = share * me;
+  if (f0 < total) {
+    long long at = 0;                                                 // first place of the 32 requests looked at
+    for (int b0 = 0;; b0 += 32) {
+      ca_span sp = is.s;
+      long long cost = cost0;
+      if (b0 > 0) {
+        sp = ca_span_of(a, min(b0 + lane, B - 1), false);
+        cost = b0 + lane < B ? places(sp) : 0;
       }
+      long long incl = cost;
+#pragma unroll
+      for (int o = 1; o < 32; o <<= 1) {
+        const long long v = __shfl_up_sync(0xffffffffu, incl, o);
+        if (lane >= o) incl += v;
+      }
+      const unsigned in = __ballot_sync(0xffffffffu, f0 >= at + incl - cost && f0 < at + incl);
+      if (in) {
+        const int l = __ffs(in) - 1;
+        is.b = b0 + l;
+        is.s.end = __shfl_sync(0xffffffffu, sp.end, l);
+        is.s.first = __shfl_sync(0xffffffffu, sp.first, l);
+        is.s.tile0 = __shfl_sync(0xffffffffu, sp.tile0, l);
+        is.s.tiles = __shfl_sync(0xffffffffu, sp.tiles, l);
+        const long long off = f0 - (at + __shfl_sync(0xffffffffu, incl - cost, l));
+        is.sub = (int)ca_div(off, is.s.tiles + CA_UNIT_COST);
+        is.t = (int)(off - (long long)is.sub * (is.s.tiles + CA_UNIT_COST));
+        is.left = (int)min(share, 0x7fffffffLL);
+        break;
+      }
+      at += __shfl_sync(0xffffffffu, incl, 31);
+      if (b0 + 32 >= B) break;                                        // lengths changed under the call
     }
-  }
-  __syncthreads();
-
-  // ---- units without a token: zeros and -inf, shared out over the blocks
-  for (int b = blockIdx.x; b < B; b += gridDim.x) {
-    if (ca_span_of(a, b, false).tiles == 0) {
-      for (int i = threadIdx.x; i < a.Tq * a.n_q_heads * (D / 8); i += CA_THREADS) {
-        const int row = i / (D / 8), tok = row / a.n_q_heads, h = row - tok * a.n_q_heads;
-        char* o = a.out + ((long long)b * a.Tq + tok) * a.out_token_stride + h * a.out_head_stride;
-        *reinterpret_cast<uint4*>(o + (i % (D / 8)) * 16) = make_uint4(0u, 0u, 0u, 0u);
-        if (a.lse && i % (D / 8) == 0) a.lse[((long long)b * a.Tq + tok) * a.n_q_heads + h] = -INFINITY;
-      }
+    if (is.left > 0 && is.t >= is.s.tiles) {                          // the run begins in the empty places behind a unit
+      is.left -= is.s.tiles + CA_UNIT_COST - is.t;
+      if (is.left > 0) ca_next_unit(a, is, subs);
     }
   }
 
   // ---- the issuing side
   const uint32_t ring = (uint32_t)__cvta_generic_to_shared(ca_smem) + warp * geo::WARP_BYTES;
-  ca_cursor is;
-  is.b = sh_start[warp][0];
-  is.left = 0;
-  if (is.b >= 0) {
-    is.sub = sh_start[warp][1];
-    is.t = sh_start[warp][2];
-    is.s = ca_span_of(a, is.b, false);
-    is.left = (int)share;
-    if (is.t >= is.s.tiles) {                        // the run begins in the empty places behind a unit
-      is.left -= is.s.tiles + CA_UNIT_COST - is.t;
-      if (is.left > 0) ca_next_unit(a, is, subs);
-    }
-  }
   ca_cursor u = is;                                  // the using side starts at the same place
   const int page_mask = (1 << a.c.page_shift) - 1;
-  auto block_of = [&](const ca_cursor& k) {
-    return __ldg(a.c.table + k.b * a.c.table_stride + (((k.s.tile0 + k.t) << 4) >> a.c.page_shift));
+  // Table entries of the next 32 tiles of the unit, one per lane.
+  int blocks = 0, blocks_from = 0;
+  const char* head_at = nullptr;                     // page 0 of the unit's head
+  auto look_up = [&]() {
+    blocks_from = is.t;
+    const int i = min(is.t + lane, is.s.tiles - 1);
+    blocks = __ldg(a.c.table + is.b * a.c.table_stride + (((is.s.tile0 + i) << 4) >> a.c.page_shift));
   };
-  int next_blk = is.left > 0 ? block_of(is) : 0;
+  auto enter_unit = [&]() {
+    head_at = a.c.data + (is.sub % a.c.n_kv_heads) * a.c.head_stride;
+    look_up();
+  };
+  if (is.left > 0) enter_unit();
   const char* src = nullptr;                         // K of the tile being issued; V lies page_tokens rows behind
   int n_first = 0, n_valid = 0;                      // tokens [n_first, n_valid) of it exist (and are visible to some row)
   bool second = false;                               // the next half to issue is V
   uint32_t put = ring;                               // slot it goes to
+  const uint32_t place0 = ca_place<geo::ROW>(lane / (geo::ROW / 16), lane % (geo::ROW / 16));
 
-  auto copy_half = [&](const char* from) {
+  // Copy i of a half takes bytes [512 i, 512 i + 512): 8, 4 or 2 rows; its row numbers change the swizzle by a constant.
+  auto copy_half = [&](uint32_t to, const char* from) {
+    if (n_first <= 0 && n_valid >= 16) {
 #pragma unroll
-    for (int i = 0; i < geo::COPIES; ++i) {
-      const int r = i * (512 / geo::ROW) + lane / (geo::ROW / 16), c = lane % (geo::ROW / 16);
-      ca_cp16(put + ca_place<geo::ROW>(r, c), from + i * 512 + lane * 16, (r >= n_first && r < n_valid) ? 16u : 0u);
+      for (int i = 0; i < geo::COPIES; ++i)
+        ca_cp16_all(to + (place0 ^ ca_twist<geo::ROW>(i)) + i * 512, from + i * 512 + lane * 16);
+    } else {
+#pragma unroll
+      for (int i = 0; i < geo::COPIES; ++i) {
+        const int r = i * (512 / geo::ROW) + lane / (geo::ROW / 16);
+        ca_cp16(to + (place0 ^ ca_twist<geo::ROW>(i)) + i * 512, from + i * 512 + lane * 16, (r >= n_first && r < n_valid) ? 16u : 0u);
+      }
     }
   };
   auto issue = [&]() {
     if (is.left > 0) {
-      if (!second) {
+      if (geo::WHOLE || !second) {
         const int tok0 = (is.s.tile0 + is.t) << 4;
-        const int head = is.sub % a.c.n_kv_heads;
-        int blk = next_blk;
+        int blk = __shfl_sync(0xffffffffu, blocks, is.t - blocks_from);
         n_first = is.s.first - tok0;
         n_valid = is.s.end - tok0;
         if ((unsigned)blk >= (unsigned)a.c.n_blocks) {
@@ -305,28 +314,31 @@ __global__ void __launch_bounds__(CA_THREADS, (ca_geom<FMT, D, NT>::BLOCKS_PER_S
           n_valid = 0;                               // reads as zeros
         }
         const int in_page = tok0 & page_mask;
-        const char* page = a.c.data + blk * a.c.block_stride + head * a.c.head_stride;
+        const char* page = head_at + blk * a.c.block_stride;
         src = page + in_page * geo::ROW;
-        copy_half(src);
+        copy_half(put, src);
         if (FP8 && lane < 8) {
           // exponents: K's behind all the codes of the page, V's behind those
           const char* ex = page + (2 * D + (lane >> 2)) * (page_mask + 1) + in_page + (lane & 3) * 4;
-          ca_cp4(put + geo::HALF_BYTES + lane * 4, ex, n_valid > 0 ? 4u : 0u);
+          ca_cp4(put + geo::EXP_AT + lane * 4, ex, n_valid > 0 ? 4u : 0u);
         }
-        second = true;
-      } else {
-        copy_half(src + (page_mask + 1) * geo::ROW);
-        second = false;
-        ca_step(a, is, subs);
-        if (is.left > 0) next_blk = block_of(is);
       }
+      if (geo::WHOLE || second) {
+        copy_half(put + (geo::WHOLE ? geo::HALF_BYTES : 0), src + (page_mask + 1) * geo::ROW);
+        ca_step(a, is, subs);
+        if (is.left > 0) {
+          if (is.t == 0) enter_unit();
+          else if (is.t - blocks_from == 32) look_up();
+        }
+      }
+      second = !second;
     }
     ca_commit();
     put = put + geo::SLOT_BYTES == ring + geo::WARP_BYTES ? ring : put + geo::SLOT_BYTES;
   };
 #pragma unroll 1
   for (int i = 0; i < NS; ++i) issue();
-  uint32_t take = ring;                              // slot of the next half to use
+  uint32_t take = ring;                              // slot of the next copy group to use
   auto use_up = [&]() {                              // everything of the slot is in registers: refill it
     __syncwarp();
     take = take + geo::SLOT_BYTES == ring + geo::WARP_BYTES ? ring : take + geo::SLOT_BYTES;
@@ -342,7 +354,7 @@ __global__ void __launch_bounds__(CA_THREADS, (ca_geom<FMT, D, NT>::BLOCKS_PER_S
   int4 desc = make_int4(0, 0, 0, 0);
   int2 key = make_int2(-1, 0);                       // the unit whose piece is left over at the end of the run
   float acc[NT][D / 16][4];
-  float ref[NT][2], sum[NT][2];
+  float from[NT][2], sum[NT][2];                     // reference minus headroom; denominator, this lane's tokens
   while (u.left > 0) {
     const int b = u.b, sub = u.sub, t0 = u.t;
     const ca_span s = u.s;
@@ -412,7 +424,7 @@ __global__ void __launch_bounds__(CA_THREADS, (ca_geom<FMT, D, NT>::BLOCKS_PER_S
     for (int nt = 0; nt < NT; ++nt) {
 #pragma unroll
       for (int m = 0; m < D / 16; ++m) acc[nt][m][0] = acc[nt][m][1] = acc[nt][m][2] = acc[nt][m][3] = 0.f;
-      ref[nt][0] = ref[nt][1] = -INFINITY;
+      from[nt][0] = from[nt][1] = CA_NONE;
       sum[nt][0] = sum[nt][1] = 0.f;
     }
 
@@ -420,7 +432,7 @@ __global__ void __launch_bounds__(CA_THREADS, (ca_geom<FMT, D, NT>::BLOCKS_PER_S
       const int tok0 = (s.tile0 + t0 + i) << 4;
       // ---- scores
       float z[NT][4];
-      int kex0 = 0, kex1 = 0, vex0 = 0, vex1 = 0;
+      float vex0 = 0.f, vex1 = 0.f;                                   // log2 of the value scales of tokens g, g + 8
       ca_wait<NS - 1>();
       __syncwarp();
       {
@@ -429,7 +441,13 @@ __global__ void __launch_bounds__(CA_THREADS, (ca_geom<FMT, D, NT>::BLOCKS_PER_S
         for (int nt = 0; nt < NT; ++nt)
           z[nt][0] = z[nt][1] = z[nt][2] = z[nt][3] = z2[nt][0] = z2[nt][1] = z2[nt][2] = z2[nt][3] = 0.f;
         const uint32_t at = take + k_row;
+        float by0 = 1.f, by1 = 1.f;                                   // key scales of tokens g, g + 8
         if (FP8) {
+          // byte 0 (a row of magnitude below 2^-118) counts as zero here
+          by0 = __uint_as_float((uint32_t)ca_lds_byte(take + geo::EXP_AT + g) << 23);
+          by1 = __uint_as_float((uint32_t)ca_lds_byte(take + geo::EXP_AT + g + 8) << 23);
+          vex0 = (float)(ca_lds_byte(take + geo::EXP_AT + 16 + g) - 127);
+          vex1 = (float)(ca_lds_byte(take + geo::EXP_AT + 16 + g + 8) - 127);
 #pragma unroll
           for (int c = 0; c < D / 32; ++c) {
             uint32_t r[4];                                            // four codes each: rows g, g + 8 of chunk 2c, of chunk 2c + 1
@@ -443,10 +461,6 @@ __global__ void __launch_bounds__(CA_THREADS, (ca_geom<FMT, D, NT>::BLOCKS_PER_S
               for (int nt = 0; nt < NT; ++nt) ca_mma<FMT>(w ? z2[nt] : z[nt], a0, a1, a2, a3, qf[nt][4 * c + 2 * w], qf[nt][4 * c + 2 * w + 1]);
             }
           }
-          kex0 = ca_lds_byte(take + geo::HALF_BYTES + g);
-          kex1 = ca_lds_byte(take + geo::HALF_BYTES + g + 8);
-          vex0 = ca_lds_byte(take + geo::HALF_BYTES + 16 + g) - 127;
-          vex1 = ca_lds_byte(take + geo::HALF_BYTES + 16 + g + 8) - 127;
         } else {
 #pragma unroll
           for (int c = 0; c < D / 16; ++c) {
@@ -459,12 +473,9 @@ __global__ void __launch_bounds__(CA_THREADS, (ca_geom<FMT, D, NT>::BLOCKS_PER_S
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            z[nt][e] = (z[nt][e] + z2[nt][e]) * zs[nt][e & 1];
-            if (FP8) z[nt][e] *= dd_two_to_byte(e < 2 ? kex0 : kex1);
-          }
+          for (int e = 0; e < 4; ++e) z[nt][e] = (z[nt][e] + z2[nt][e]) * (FP8 ? zs[nt][e & 1] * (e < 2 ? by0 : by1) : zs[nt][e & 1]);
       }
-      use_up();
+      if (!geo::WHOLE) use_up();
 
       // ---- masks: z[.][0..1] is token tok0 + g, z[.][2..3] token tok0 + g + 8
       const bool partial = tok0 + 15 > pos_lo || (a.window > 0 && tok0 <= pos_hi - a.window);
@@ -478,50 +489,56 @@ __global__ void __launch_bounds__(CA_THREADS, (ca_geom<FMT, D, NT>::BLOCKS_PER_S
           }
       }
 
-      // ---- weights against the reference
+      // ---- weights against the reference: 2^x with x = z - ref + headroom for the denominator, + log2 of the value's scale
+      // for the product. Weights of values with a scale below 2^-96 do not let the denominator grow out of range: their
+      // reference is taken as if the scale were 2^-96.
       uint32_t pb[NT][2];
 #pragma unroll
       for (int nt = 0; nt < NT; ++nt) {
-        float w[4];
+        float x[4], y[4];
+        bool above = false;
 #pragma unroll
-        for (int e = 0; e < 4; ++e) w[e] = FP8 ? z[nt][e] + (float)max(e < 2 ? vex0 : vex1, -96) : z[nt][e];
-        const bool above = w[0] > ref[nt][0] + CA_LAZY || w[2] > ref[nt][0] + CA_LAZY ||
-                           w[1] > ref[nt][1] + CA_LAZY || w[3] > ref[nt][1] + CA_LAZY;
+        for (int e = 0; e < 4; ++e) {
+          x[e] = z[nt][e] - from[nt][e & 1];
+          y[e] = FP8 ? x[e] + (e < 2 ? vex0 : vex1) : x[e];
+          above |= y[e] > CA_LAZY + CA_HEADROOM;
+          if (FP8) above |= x[e] > CA_LAZY + CA_HEADROOM + 96.f;
+        }
         if (__any_sync(0xffffffffu, above)) {
 #pragma unroll
           for (int c = 0; c < 2; ++c) {
-            float top = fmaxf(w[c], w[2 + c]);
+            float top = FP8 ? fmaxf(z[nt][c] + fmaxf(vex0, -96.f), z[nt][2 + c] + fmaxf(vex1, -96.f)) : fmaxf(z[nt][c], z[nt][2 + c]);
             top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 4));
             top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 8));
             top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 16));
-            top = fmaxf(top, ref[nt][c]);
-            const float fix = top == -INFINITY ? 1.f : ca_exp2(ref[nt][c] - top);
-            ref[nt][c] = top;
+            top = fmaxf(top - CA_HEADROOM, from[nt][c]);
+            const float fix = ca_exp2(from[nt][c] - top);
+            from[nt][c] = top;
             sum[nt][c] *= fix;
 #pragma unroll
             for (int m = 0; m < D / 16; ++m) { acc[nt][m][c] *= fix; acc[nt][m][2 + c] *= fix; }
+          }
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            x[e] = z[nt][e] - from[nt][e & 1];
+            y[e] = FP8 ? x[e] + (e < 2 ? vex0 : vex1) : x[e];
           }
         }
         float p[4];
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-          const float from = (ref[nt][e & 1] == -INFINITY ? 0.f : ref[nt][e & 1]) - CA_HEADROOM;
-          if (FP8) {
-            const int ve = e < 2 ? vex0 : vex1;
-            sum[nt][e & 1] += ca_exp2(z[nt][e] - from);
-            p[e] = ca_exp2(z[nt][e] + (float)ve - from);
-          } else {
-            p[e] = ca_exp2(z[nt][e] - from);
-            sum[nt][e & 1] += p[e];
-          }
+          p[e] = ca_exp2(y[e]);
+          sum[nt][e & 1] += FP8 ? ca_exp2(x[e]) : p[e];
         }
         pb[nt][0] = ca_transpose(dd_pack2<TP>(p[0], p[1]));
         pb[nt][1] = ca_transpose(dd_pack2<TP>(p[2], p[3]));
       }
 
       // ---- weighted values
-      ca_wait<NS - 1>();
-      __syncwarp();
+      if (!geo::WHOLE) {
+        ca_wait<NS - 1>();
+        __syncwarp();
+      }
       // Registers of V^T: r[0], r[1] hold tokens 2t | 2t+1 (low | high half), r[2], r[3] tokens 2t+8 | 2t+9, for the channels of
       // rows g and g + 8.
       auto value_frag = [&](uint32_t (&r)[4], const uint32_t (&raw)[4], int half) {
@@ -534,7 +551,7 @@ __global__ void __launch_bounds__(CA_THREADS, (ca_geom<FMT, D, NT>::BLOCKS_PER_S
           for (int e = 0; e < 4; ++e) r[e] = raw[e];
         }
       };
-      const uint32_t at = take + v_row;
+      const uint32_t at = take + v_row + (geo::WHOLE ? geo::HALF_BYTES : 0);
       if (!(partial && a.Tq > 1)) {
 #pragma unroll
         for (int c = 0; c < D / (FP8 ? 32 : 16); ++c) {
@@ -616,7 +633,7 @@ __global__ void __launch_bounds__(CA_THREADS, (ca_geom<FMT, D, NT>::BLOCKS_PER_S
                 *reinterpret_cast<unsigned short*>(o + 2 * (ca_channel(FP8, g, m) + ca_pair(FP8))) = (unsigned short)(w >> 16);
               }
             }
-            if (a.lse && g == 0) a.lse[tn * a.n_q_heads + h] = empty ? -INFINITY : ca_lse(ref[nt][c], sum[nt][c]);
+            if (a.lse && g == 0) a.lse[tn * a.n_q_heads + h] = empty ? -INFINITY : ca_lse(from[nt][c], sum[nt][c]);
           }
         }
     } else if (ends) {
@@ -629,8 +646,8 @@ __global__ void __launch_bounds__(CA_THREADS, (ca_geom<FMT, D, NT>::BLOCKS_PER_S
 #pragma unroll
           for (int e = 0; e < 4; ++e) po[(nt * geo::NACC + m * 4 + e) * 32 + lane] = acc[nt][m][e];
         if (g == 0) {
-          a.part_ml[2LL * me * NT * 8 + nt * 8 + 2 * t] = make_float2(ref[nt][0], sum[nt][0]);
-          a.part_ml[2LL * me * NT * 8 + nt * 8 + 2 * t + 1] = make_float2(ref[nt][1], sum[nt][1]);
+          a.part_ml[2LL * me * NT * 8 + nt * 8 + 2 * t] = make_float2(from[nt][0], sum[nt][0]);
+          a.part_ml[2LL * me * NT * 8 + nt * 8 + 2 * t + 1] = make_float2(from[nt][1], sum[nt][1]);
         }
       }
     } else {
@@ -644,6 +661,17 @@ __global__ void __launch_bounds__(CA_THREADS, (ca_geom<FMT, D, NT>::BLOCKS_PER_S
     if (u.left > 0) ca_next_unit(a, u, subs);
   }
   if (lane == 0) a.desc[me] = desc;
+  // units without a token: zeros and -inf, shared out over the blocks
+  for (int b = blockIdx.x; b < B; b += gridDim.x) {
+    if (ca_span_of(a, b, false).tiles == 0) {
+      for (int i = threadIdx.x; i < a.Tq * a.n_q_heads * (D / 8); i += CA_THREADS) {
+        const int row = i / (D / 8), tok = row / a.n_q_heads, h = row - tok * a.n_q_heads;
+        char* o = a.out + ((long long)b * a.Tq + tok) * a.out_token_stride + h * a.out_head_stride;
+        *reinterpret_cast<uint4*>(o + (i % (D / 8)) * 16) = make_uint4(0u, 0u, 0u, 0u);
+        if (a.lse && i % (D / 8) == 0) a.lse[((long long)b * a.Tq + tok) * a.n_q_heads + h] = -INFINITY;
+      }
+    }
+  }
   ca_wait<0>();
   __syncwarp();
 
@@ -659,8 +687,8 @@ __global__ void __launch_bounds__(CA_THREADS, (ca_geom<FMT, D, NT>::BLOCKS_PER_S
 #pragma unroll
         for (int e = 0; e < 4; ++e) own[(nt * geo::NACC + m * 4 + e) * 32 + lane] = acc[nt][m][e];
       if (g == 0) {
-        sh_ml[warp][nt * 8 + 2 * t] = make_float2(ref[nt][0], sum[nt][0]);
-        sh_ml[warp][nt * 8 + 2 * t + 1] = make_float2(ref[nt][1], sum[nt][1]);
+        sh_ml[warp][nt * 8 + 2 * t] = make_float2(from[nt][0], sum[nt][0]);
+        sh_ml[warp][nt * 8 + 2 * t + 1] = make_float2(from[nt][1], sum[nt][1]);
       }
     }
   }
@@ -675,11 +703,11 @@ __global__ void __launch_bounds__(CA_THREADS, (ca_geom<FMT, D, NT>::BLOCKS_PER_S
     for (int k = 0; k < NT * geo::NACC * 32 / CA_THREADS; ++k) {
       const int e = k * CA_THREADS + threadIdx.x;
       const int row = e / (geo::NACC * 32) * 8 + 2 * (e & 3) + ((e >> 5) & 1);
-      float M = -INFINITY, L = 0.f, x = 0.f;
+      float M = CA_NONE, L = 0.f, x = 0.f;
       for (int w = w0; w < w1; ++w) M = fmaxf(M, sh_ml[w][row].x);
       for (int w = w0; w < w1; ++w) {
         const float2 ml = sh_ml[w][row];
-        const float sc = ml.x == -INFINITY ? 1.f : ca_exp2(ml.x - M);  // without a finite weight: zeros, or a NaN to pass on
+        const float sc = ca_exp2(ml.x - M);
         L = fmaf(ml.y, sc, L);
         x = fmaf(reinterpret_cast<const float*>(ca_smem + w * geo::WARP_BYTES)[e], sc, x);
       }
@@ -699,14 +727,17 @@ __global__ void __launch_bounds__(256) dd_cache_attn_join_kernel(const ca_args a
   constexpr int NACC = D / 4;
   extern __shared__ float ja_scale[];                                 // [parts][8] of the column tile
   __shared__ float2 sh_ml[8];
+  __shared__ int4 sh_desc[CA_WARPS];
   dd_grid_dependency_wait();
   const int e = blockIdx.y * 256 + threadIdx.x;                       // element: [nt][register][lane]
   const int nt = (blockIdx.y * 256) / (NACC * 32);
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int reg = (e / 32) % NACC, m = reg >> 2, g = lane >> 2, t = lane & 3;
   const int col = 2 * t + (reg & 1);
+  if (threadIdx.x < CA_WARPS) sh_desc[threadIdx.x] = a.desc[blockIdx.x * CA_WARPS + threadIdx.x];
+  __syncthreads();
   for (int w0 = blockIdx.x * CA_WARPS; w0 < (blockIdx.x + 1) * CA_WARPS; ++w0) {
-    const int4 d = a.desc[w0];
+    const int4 d = sh_desc[w0 % CA_WARPS];
     if (d.z == 0) continue;
     const int w1 = d.z - 1, first_block = w0 / CA_WARPS;
     const int n = (w1 - 1) / CA_WARPS - first_block + 2;              // partials
@@ -715,14 +746,14 @@ __global__ void __launch_bounds__(256) dd_cache_attn_join_kernel(const ca_args a
     {
       // warp w: the scales of row w of the column tile
       const int row = nt * 8 + warp;
-      float M = -INFINITY;
+      float M = CA_NONE;
       for (int i = lane; i < n; i += 32) M = fmaxf(M, a.part_ml[slot(i) * NT * 8 + row].x);
 #pragma unroll
       for (int o = 16; o; o >>= 1) M = fmaxf(M, __shfl_xor_sync(0xffffffffu, M, o));
       float L = 0.f;
       for (int i = lane; i < n; i += 32) {
         const float2 ml = a.part_ml[slot(i) * NT * 8 + row];
-        const float sc = ml.x == -INFINITY ? 1.f : ca_exp2(ml.x - M);
+        const float sc = ca_exp2(ml.x - M);
         ja_scale[i * 8 + warp] = sc;
         L += ml.y * sc;
       }
