@@ -109,16 +109,15 @@ __device__ __forceinline__ int ca_lds_byte(uint32_t a) {
   asm volatile("ld.shared.u8 %0, [%1];" : "=r"(v) : "r"(a) : "memory");
   return (int)v;
 }
-__device__ __forceinline__ void ca_mma_half(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
-  asm volatile(
-      "mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
-      : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
-      : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
-}
+// D(16x8, fp32) += A(16x16, row) * B(16x8, col). Not volatile: the compiler may place it where its operands are ready.
 template <int FMT>
 __device__ __forceinline__ void ca_mma(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
-  if (FMT == 0) dd_mma_bf16(c, a0, a1, a2, a3, b0, b1);
-  else ca_mma_half(c, a0, a1, a2, a3, b0, b1);
+  if (FMT == 0)
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+        : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+  else
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+        : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
 __device__ __forceinline__ uint32_t ca_transpose(uint32_t a) {       // 8x8 matrix of 16-bit values across the warp
   uint32_t d;
@@ -204,6 +203,7 @@ __global__ void __launch_bounds__(CA_THREADS, (ca_geom<FMT, D, NT>::BLOCKS_PER_S
   constexpr int NS = geo::STAGES;
   extern __shared__ __align__(128) unsigned char ca_smem[];
   __shared__ float2 sh_ml[CA_WARPS][NT * 8];
+  __shared__ float sh_scale[CA_WARPS][NT * 8];
   __shared__ int2 sh_key[CA_WARPS];
 
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -213,6 +213,8 @@ __global__ void __launch_bounds__(CA_THREADS, (ca_geom<FMT, D, NT>::BLOCKS_PER_S
   const int me = blockIdx.x * CA_WARPS + warp;
 
   dd_grid_dependency_wait();
+  // the joining kernel's blocks may take the places that this grid's blocks leave (it waits for all of them)
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
 
   // ---- this warp's run of the flat list: every warp adds up the list by itself, 32 requests at a time
   ca_cursor is;
@@ -448,26 +450,31 @@ __global__ void __launch_bounds__(CA_THREADS, (ca_geom<FMT, D, NT>::BLOCKS_PER_S
           by1 = __uint_as_float((uint32_t)ca_lds_byte(take + geo::EXP_AT + g + 8) << 23);
           vex0 = (float)(ca_lds_byte(take + geo::EXP_AT + 16 + g) - 127);
           vex1 = (float)(ca_lds_byte(take + geo::EXP_AT + 16 + g + 8) - 127);
+          uint32_t r[D / 32][4];                                      // four codes each: rows g, g + 8 of chunk 2c, of chunk 2c + 1
+#pragma unroll
+          for (int c = 0; c < D / 32; ++c) ca_ldsm(r[c], at + (k_x ^ (c << 5)));
 #pragma unroll
           for (int c = 0; c < D / 32; ++c) {
-            uint32_t r[4];                                            // four codes each: rows g, g + 8 of chunk 2c, of chunk 2c + 1
-            ca_ldsm(r, at + (k_x ^ (c << 5)));
 #pragma unroll
             for (int w = 0; w < 2; ++w) {
               uint32_t a0, a1, a2, a3;
-              dd_e4m3x4_to_half(r[2 * w], a0, a2);
-              dd_e4m3x4_to_half(r[2 * w + 1], a1, a3);
+              dd_e4m3x4_to_half(r[c][2 * w], a0, a2);
+              dd_e4m3x4_to_half(r[c][2 * w + 1], a1, a3);
 #pragma unroll
               for (int nt = 0; nt < NT; ++nt) ca_mma<FMT>(w ? z2[nt] : z[nt], a0, a1, a2, a3, qf[nt][4 * c + 2 * w], qf[nt][4 * c + 2 * w + 1]);
             }
           }
         } else {
 #pragma unroll
-          for (int c = 0; c < D / 16; ++c) {
-            uint32_t r[4];
-            ca_ldsm(r, at + (k_x ^ (c << 5)));
+          for (int c4 = 0; c4 < D / 16; c4 += 4) {
+            uint32_t r[4][4];
 #pragma unroll
-            for (int nt = 0; nt < NT; ++nt) ca_mma<FMT>((c & 1) ? z2[nt] : z[nt], r[0], r[1], r[2], r[3], qf[nt][2 * c], qf[nt][2 * c + 1]);
+            for (int c = 0; c < 4; ++c) ca_ldsm(r[c], at + (k_x ^ ((c4 + c) << 5)));
+#pragma unroll
+            for (int c = 0; c < 4; ++c)
+#pragma unroll
+              for (int nt = 0; nt < NT; ++nt)
+                ca_mma<FMT>((c & 1) ? z2[nt] : z[nt], r[c][0], r[c][1], r[c][2], r[c][3], qf[nt][2 * (c4 + c)], qf[nt][2 * (c4 + c) + 1]);
           }
         }
 #pragma unroll
@@ -476,6 +483,15 @@ __global__ void __launch_bounds__(CA_THREADS, (ca_geom<FMT, D, NT>::BLOCKS_PER_S
           for (int e = 0; e < 4; ++e) z[nt][e] = (z[nt][e] + z2[nt][e]) * (FP8 ? zs[nt][e & 1] * (e < 2 ? by0 : by1) : zs[nt][e & 1]);
       }
       if (!geo::WHOLE) use_up();
+      // whole tiles: V is there already, its first registers come in behind the soft-max
+      constexpr int V_LOADS = D / (FP8 ? 32 : 16), V_BATCH = V_LOADS < 4 ? V_LOADS : 4;
+      uint32_t raw[V_BATCH][4];
+      auto load_values = [&](int c0) {
+        const uint32_t at = take + v_row + (geo::WHOLE ? geo::HALF_BYTES : 0);
+#pragma unroll
+        for (int c = 0; c < V_BATCH; ++c) ca_ldsm_trans(raw[c], at + (v_x ^ ((c0 + c) << 5)));
+      };
+      if (geo::WHOLE) load_values(0);
 
       // ---- masks: z[.][0..1] is token tok0 + g, z[.][2..3] token tok0 + g + 8
       const bool partial = tok0 + 15 > pos_lo || (a.window > 0 && tok0 <= pos_hi - a.window);
@@ -541,29 +557,29 @@ __global__ void __launch_bounds__(CA_THREADS, (ca_geom<FMT, D, NT>::BLOCKS_PER_S
       }
       // Registers of V^T: r[0], r[1] hold tokens 2t | 2t+1 (low | high half), r[2], r[3] tokens 2t+8 | 2t+9, for the channels of
       // rows g and g + 8.
-      auto value_frag = [&](uint32_t (&r)[4], const uint32_t (&raw)[4], int half) {
+      auto value_frag = [&](uint32_t (&r)[4], const uint32_t (&v)[4], int half) {
         if (FP8) {
           // bytes of a register: two channels of token 2t, the same two of 2t+1; token pairs side by side, then as halves
-          dd_e4m3x4_to_half(__byte_perm(raw[2 * half], 0u, 0x3120u), r[0], r[1]);
-          dd_e4m3x4_to_half(__byte_perm(raw[2 * half + 1], 0u, 0x3120u), r[2], r[3]);
+          dd_e4m3x4_to_half(__byte_perm(v[2 * half], 0u, 0x3120u), r[0], r[1]);
+          dd_e4m3x4_to_half(__byte_perm(v[2 * half + 1], 0u, 0x3120u), r[2], r[3]);
         } else {
 #pragma unroll
-          for (int e = 0; e < 4; ++e) r[e] = raw[e];
+          for (int e = 0; e < 4; ++e) r[e] = v[e];
         }
       };
-      const uint32_t at = take + v_row + (geo::WHOLE ? geo::HALF_BYTES : 0);
       if (!(partial && a.Tq > 1)) {
 #pragma unroll
-        for (int c = 0; c < D / (FP8 ? 32 : 16); ++c) {
-          uint32_t raw[4];
-          ca_ldsm_trans(raw, at + (v_x ^ (c << 5)));
+        for (int c0 = 0; c0 < V_LOADS; c0 += V_BATCH) {
+          if (!geo::WHOLE || c0 > 0) load_values(c0);
 #pragma unroll
-          for (int half = 0; half < (FP8 ? 2 : 1); ++half) {
-            uint32_t r[4];
-            value_frag(r, raw, half);
+          for (int c = 0; c < V_BATCH; ++c)
 #pragma unroll
-            for (int nt = 0; nt < NT; ++nt) ca_mma<FMT>(acc[nt][FP8 ? 2 * c + half : c], r[0], r[1], r[2], r[3], pb[nt][0], pb[nt][1]);
-          }
+            for (int half = 0; half < (FP8 ? 2 : 1); ++half) {
+              uint32_t r[4];
+              value_frag(r, raw[c], half);
+#pragma unroll
+              for (int nt = 0; nt < NT; ++nt) ca_mma<FMT>(acc[nt][FP8 ? 2 * (c0 + c) + half : c0 + c], r[0], r[1], r[2], r[3], pb[nt][0], pb[nt][1]);
+            }
         }
       } else {
         // Some tokens are seen by some rows of the tile and not by others: a weight of zero does not keep an infinity or NaN
@@ -573,26 +589,28 @@ __global__ void __launch_bounds__(CA_THREADS, (ca_geom<FMT, D, NT>::BLOCKS_PER_S
           uint32_t keep[2];                                           // tokens 2t | 2t+1 and 2t+8 | 2t+9
 #pragma unroll
           for (int k = 0; k < 2; ++k) {
-            const int tok = tok0 + 2 * t + 8 * k, from = a.window > 0 ? p - a.window : -1;
-            keep[k] = ((tok <= p && tok > from) ? 0xffffu : 0u) | ((tok + 1 <= p && tok + 1 > from) ? 0xffff0000u : 0u);
+            const int tok = tok0 + 2 * t + 8 * k, first = a.window > 0 ? p - a.window : -1;
+            keep[k] = ((tok <= p && tok > first) ? 0xffffu : 0u) | ((tok + 1 <= p && tok + 1 > first) ? 0xffff0000u : 0u);
           }
 #pragma unroll
-          for (int c = 0; c < D / (FP8 ? 32 : 16); ++c) {
-            uint32_t raw[4];
-            ca_ldsm_trans(raw, at + (v_x ^ (c << 5)));
+          for (int c0 = 0; c0 < V_LOADS; c0 += V_BATCH) {
+            load_values(c0);
 #pragma unroll
-            for (int e = 0; e < 4; ++e) raw[e] &= keep[FP8 ? (e & 1) : (e >> 1)];
+            for (int c = 0; c < V_BATCH; ++c) {
 #pragma unroll
-            for (int half = 0; half < (FP8 ? 2 : 1); ++half) {
-              uint32_t r[4];
-              value_frag(r, raw, half);
+              for (int e = 0; e < 4; ++e) raw[c][e] &= keep[FP8 ? (e & 1) : (e >> 1)];
 #pragma unroll
-              for (int nt = 0; nt < NT; ++nt) {
-                float one[4] = {0.f, 0.f, 0.f, 0.f};
-                ca_mma<FMT>(one, r[0], r[1], r[2], r[3], pb[nt][0], pb[nt][1]);
+              for (int half = 0; half < (FP8 ? 2 : 1); ++half) {
+                uint32_t r[4];
+                value_frag(r, raw[c], half);
 #pragma unroll
-                for (int e = 0; e < 4; ++e)
-                  if (pos[nt][e & 1] == p) acc[nt][FP8 ? 2 * c + half : c][e] += one[e];
+                for (int nt = 0; nt < NT; ++nt) {
+                  float one[4] = {0.f, 0.f, 0.f, 0.f};
+                  ca_mma<FMT>(one, r[0], r[1], r[2], r[3], pb[nt][0], pb[nt][1]);
+#pragma unroll
+                  for (int e = 0; e < 4; ++e)
+                    if (pos[nt][e & 1] == p) acc[nt][FP8 ? 2 * (c0 + c) + half : c0 + c][e] += one[e];
+                }
               }
             }
           }
@@ -693,69 +711,92 @@ __global__ void __launch_bounds__(CA_THREADS, (ca_geom<FMT, D, NT>::BLOCKS_PER_S
     }
   }
   __syncthreads();
-  for (int w0 = 0; w0 < CA_WARPS;) {
+  auto chain_end = [&](int w0) {                     // warps w0 .. w1 - 1 hold pieces of one unit
     const int2 k0 = sh_key[w0];
     int w1 = w0 + 1;
-    if (k0.x < 0) { w0 = w1; continue; }
     while (w1 < CA_WARPS && sh_key[w1].x == k0.x && sh_key[w1].y == k0.y) ++w1;
-    const long long slot = 2LL * (blockIdx.x * CA_WARPS + w0) + 1;
+    return w1;
+  };
+  for (int i = threadIdx.x; i < CA_WARPS * NT * 8; i += CA_THREADS) {
+    const int w = i / (NT * 8), row = i % (NT * 8);
+    const int2 k0 = sh_key[w];
+    if (k0.x < 0) continue;
+    int w0 = w;
+    while (w0 > 0 && sh_key[w0 - 1].x == k0.x && sh_key[w0 - 1].y == k0.y) --w0;
+    const int w1 = chain_end(w0);
+    float M = CA_NONE, L = 0.f;
+    for (int v = w0; v < w1; ++v) M = fmaxf(M, sh_ml[v][row].x);
+    for (int v = w0; v < w1; ++v) L = fmaf(sh_ml[v][row].y, ca_exp2(sh_ml[v][row].x - M), L);
+    sh_scale[w][row] = ca_exp2(sh_ml[w][row].x - M);
+    if (w == w0) a.part_ml[(2LL * (blockIdx.x * CA_WARPS + w0) + 1) * NT * 8 + row] = make_float2(M, L);
+  }
+  __syncthreads();
+  for (int w0 = 0, w1; w0 < CA_WARPS; w0 = w1) {
+    w1 = w0 + 1;
+    if (sh_key[w0].x < 0) continue;
+    w1 = chain_end(w0);
+    float* po = a.part_o + (2LL * (blockIdx.x * CA_WARPS + w0) + 1) * NT * geo::NACC * 32;
 #pragma unroll
     for (int k = 0; k < NT * geo::NACC * 32 / CA_THREADS; ++k) {
       const int e = k * CA_THREADS + threadIdx.x;
       const int row = e / (geo::NACC * 32) * 8 + 2 * (e & 3) + ((e >> 5) & 1);
-      float M = CA_NONE, L = 0.f, x = 0.f;
-      for (int w = w0; w < w1; ++w) M = fmaxf(M, sh_ml[w][row].x);
-      for (int w = w0; w < w1; ++w) {
-        const float2 ml = sh_ml[w][row];
-        const float sc = ca_exp2(ml.x - M);
-        L = fmaf(ml.y, sc, L);
-        x = fmaf(reinterpret_cast<const float*>(ca_smem + w * geo::WARP_BYTES)[e], sc, x);
-      }
-      a.part_o[slot * NT * geo::NACC * 32 + e] = x;
-      if (((e >> 2) & 7) == 0 && ((e >> 5) % geo::NACC) < 2) a.part_ml[slot * NT * 8 + row] = make_float2(M, L);
+      float x = 0.f;
+#pragma unroll
+      for (int w = 0; w < CA_WARPS; ++w)
+        if (w >= w0 && w < w1) x = fmaf(reinterpret_cast<const float*>(ca_smem + w * geo::WARP_BYTES)[e], sh_scale[w][row], x);
+      po[e] = x;
     }
-    w0 = w1;
   }
 }
 
 // Adds the partials of the cut units that begin in block x of the attention kernel. Grid (blocks of the attention kernel,
 // NT * D / 32): every thread owns one accumulator element. The partials of a unit from run w0 (where it begins) to run w1
 // (where it ends) are: one per block among the runs w0 .. w1 - 1, in the slot of the first of them, and the last piece.
+// What bounds it is latency: (descriptors) -> (references, sums, the first partials, the length) -> result.
 template <int FMT, int D, int NT>
 __global__ void __launch_bounds__(256) dd_cache_attn_join_kernel(const ca_args a) {
   using TQ = typename ca_types<FMT>::Q;
   constexpr int NACC = D / 4;
+  constexpr int AHEAD = 8;                                            // partials fetched before the scales are known
   extern __shared__ float ja_scale[];                                 // [parts][8] of the column tile
   __shared__ float2 sh_ml[8];
-  __shared__ int4 sh_desc[CA_WARPS];
-  dd_grid_dependency_wait();
   const int e = blockIdx.y * 256 + threadIdx.x;                       // element: [nt][register][lane]
   const int nt = (blockIdx.y * 256) / (NACC * 32);
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int reg = (e / 32) % NACC, m = reg >> 2, g = lane >> 2, t = lane & 3;
   const int col = 2 * t + (reg & 1);
-  if (threadIdx.x < CA_WARPS) sh_desc[threadIdx.x] = a.desc[blockIdx.x * CA_WARPS + threadIdx.x];
-  __syncthreads();
-  for (int w0 = blockIdx.x * CA_WARPS; w0 < (blockIdx.x + 1) * CA_WARPS; ++w0) {
-    const int4 d = sh_desc[w0 % CA_WARPS];
-    if (d.z == 0) continue;
-    const int w1 = d.z - 1, first_block = w0 / CA_WARPS;
+  dd_grid_dependency_wait();
+  // the descriptors of the block's warps, one per lane, handed round by shuffles
+  int4 mine = make_int4(0, 0, 0, 0);
+  if (lane < CA_WARPS) mine = a.desc[blockIdx.x * CA_WARPS + lane];
+  unsigned todo = __ballot_sync(0xffffffffu, mine.z != 0);            // the same in every warp
+  while (todo) {
+    const int l = __ffs(todo) - 1;
+    todo &= todo - 1;
+    const int b = __shfl_sync(0xffffffffu, mine.x, l), sub = __shfl_sync(0xffffffffu, mine.y, l);
+    const int w0 = blockIdx.x * CA_WARPS + l, w1 = __shfl_sync(0xffffffffu, mine.z, l) - 1, first_block = blockIdx.x;
     const int n = (w1 - 1) / CA_WARPS - first_block + 2;              // partials
     auto slot = [&](int i) -> long long { return i == 0 ? 2LL * w0 + 1 : (i == n - 1 ? 2LL * w1 : 2LL * (first_block + i) * CA_WARPS + 1); };
-    __syncthreads();
+    const ca_span s = ca_span_of(a, b, false);
+    float ahead[AHEAD];
+#pragma unroll
+    for (int i = 0; i < AHEAD; ++i) ahead[i] = i < n ? a.part_o[slot(i) * (NT * NACC * 32) + e] : 0.f;
     {
       // warp w: the scales of row w of the column tile
       const int row = nt * 8 + warp;
-      float M = CA_NONE;
-      for (int i = lane; i < n; i += 32) M = fmaxf(M, a.part_ml[slot(i) * NT * 8 + row].x);
+      const float2 own = lane < n ? a.part_ml[slot(lane) * NT * 8 + row] : make_float2(CA_NONE, 0.f);
+      float M = own.x;
+      for (int i = lane + 32; i < n; i += 32) M = fmaxf(M, a.part_ml[slot(i) * NT * 8 + row].x);
 #pragma unroll
       for (int o = 16; o; o >>= 1) M = fmaxf(M, __shfl_xor_sync(0xffffffffu, M, o));
-      float L = 0.f;
-      for (int i = lane; i < n; i += 32) {
+      const float sc0 = ca_exp2(own.x - M);
+      float L = own.y * sc0;
+      if (lane < n) ja_scale[lane * 8 + warp] = sc0;
+      for (int i = lane + 32; i < n; i += 32) {
         const float2 ml = a.part_ml[slot(i) * NT * 8 + row];
         const float sc = ca_exp2(ml.x - M);
         ja_scale[i * 8 + warp] = sc;
-        L += ml.y * sc;
+        L = fmaf(ml.y, sc, L);
       }
 #pragma unroll
       for (int o = 16; o; o >>= 1) L += __shfl_xor_sync(0xffffffffu, L, o);
@@ -763,14 +804,16 @@ __global__ void __launch_bounds__(256) dd_cache_attn_join_kernel(const ca_args a
     }
     __syncthreads();
     float x = 0.f;
+#pragma unroll
+    for (int i = 0; i < AHEAD; ++i)
+      if (i < n) x = fmaf(ahead[i], ja_scale[i * 8 + col], x);
 #pragma unroll 8
-    for (int i = 0; i < n; ++i) x = fmaf(a.part_o[slot(i) * (NT * NACC * 32) + e], ja_scale[i * 8 + col], x);
-    const int rt = d.y / a.c.n_kv_heads, head = d.y - rt * a.c.n_kv_heads;
+    for (int i = AHEAD; i < n; ++i) x = fmaf(a.part_o[slot(i) * (NT * NACC * 32) + e], ja_scale[i * 8 + col], x);
+    const int rt = sub / a.c.n_kv_heads, head = sub - rt * a.c.n_kv_heads;
     const int r = rt * NT * 8 + nt * 8 + col;
     if (r < a.n_rows) {
-      const ca_span s = ca_span_of(a, d.x, false);
       const int tok = r / a.G, h = head * a.G + r - tok * a.G;
-      const long long tn = (long long)d.x * a.Tq + tok;
+      const long long tn = (long long)b * a.Tq + tok;
       const bool empty = s.end - a.Tq + tok < 0;
       const float2 ml = sh_ml[col];
       const int ch = ca_channel(FMT >= 2, g, m) + (reg & 2 ? ca_pair(FMT >= 2) : 0);
@@ -778,6 +821,7 @@ __global__ void __launch_bounds__(256) dd_cache_attn_join_kernel(const ca_args a
       *reinterpret_cast<unsigned short*>(a.out + tn * a.out_token_stride + h * a.out_head_stride + 2 * ch) = (unsigned short)w;
       if (a.lse && ch == 0) a.lse[tn * a.n_q_heads + h] = empty ? -INFINITY : ca_lse(ml.x, ml.y);
     }
+    __syncthreads();                                                  // before the scales are written again
   }
 }
 
