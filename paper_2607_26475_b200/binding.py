@@ -10,6 +10,7 @@ from __future__ import annotations
 
 import ctypes as C
 import os
+import struct
 
 import torch
 
@@ -194,8 +195,14 @@ def _view(ptr: int, shape, kind: str) -> torch.Tensor:
     return torch.as_tensor(_DevMem(ptr, shape, "<" + kind), device="cuda")
 
 
+# The current stream as a number, without building a Stream object (3 us less per call); torch offers it to generated code.
+_raw_stream, _raw_device = getattr(torch._C, "_cuda_getCurrentRawStream", None), getattr(torch._C, "_cuda_getDevice", None)
+
+
 def _stream(s) -> int:
     if s is None:
+        if _raw_stream is not None and torch.cuda.is_initialized():
+            return _raw_stream(_raw_device())
         return torch.cuda.current_stream().cuda_stream
     if isinstance(s, int):
         return s
@@ -216,38 +223,67 @@ def sparse_decode_attn_static(q, slot, idx, ctx_len, out, out_lse=None, *, n_spl
 
 
 _ROW_TYPES = {torch.bfloat16: DD_BF16, torch.float16: DD_FP16}
+_PACK_ROWS = struct.Struct("<Qiiqq").pack          # a `dd_rows`, byte for byte
+assert C.sizeof(DDRows) == 32
 
 
 def _invalid(message: str) -> DDError:
     return DDError(DD_ERR_INVALID_ARG, message)
 
 
-def _rows(t, name: str, head_dim: int, tokens: int | None = None):
+def _handle(name: str, *argtypes):
+    """The entry point again, with structures passed by address (ints, packed bytes or None): cheaper to call."""
+    f = lib[name]
+    f.argtypes, f.restype = argtypes, C.c_int
+    return f
+
+
+_P, _I = C.c_void_p, C.c_int
+_rope_apply = _handle("dd_rope_apply", _P, _I, _I, _P, _P, _P, _P, _P, _I, _P)
+_cache_append = _handle("dd_cache_append", _P, _I, _P, _P, _P, _P, _P, _P, _P, _P)
+_cache_read = _handle("dd_cache_read", _P, _P, _I, _P, _I, _P)
+_cache_decode_attn = _handle("dd_cache_decode_attn", _P, _I, _P, _P, _P, _P, _I, C.c_float, _P, C.c_size_t, _P)
+
+
+def _rows(t, name: str, head_dim: int, tokens: int):
     """`dd_rows` of a tensor [tokens, heads, head_dim] whose rows are dense (slices of a larger tensor are fine)."""
-    if t is None:
-        return None
-    kind = _ROW_TYPES.get(t.dtype)
+    kind, shape = _ROW_TYPES.get(t.dtype), t.shape
     if kind is None:
         raise _invalid(f"{name} must be bfloat16 or float16, not {t.dtype}")
-    if t.dim() != 3 or t.shape[2] != head_dim or (tokens is not None and t.shape[0] != tokens):
-        raise _invalid(f"{name} must be [{'tokens' if tokens is None else tokens}, heads, {head_dim}], not {tuple(t.shape)}")
+    if len(shape) != 3 or shape[2] != head_dim or shape[0] != tokens:
+        raise _invalid(f"{name} must be [{tokens}, heads, {head_dim}], not {tuple(shape)}")
     token, head, one = t.stride()
     if one != 1:
         raise _invalid(f"the elements of a row of {name} must be adjacent")
+    h = shape[1]
     # a stride that is never stepped over may be anything: hand on one that passes
-    return DDRows(t.data_ptr(), kind, t.shape[1], token if t.shape[0] > 1 else head_dim * t.shape[1], head if t.shape[1] > 1 else head_dim)
+    return _PACK_ROWS(t.data_ptr(), kind, h, token if tokens > 1 else head_dim * h, head if h > 1 else head_dim)
 
 
-def _ints(t, name: str, shape=None):
-    if t.dtype != torch.int32 or not t.is_contiguous() or (shape is not None and tuple(t.shape) != tuple(shape)):
-        raise _invalid(f"{name} must be a dense int32 tensor{'' if shape is None else ' of shape ' + str(tuple(shape))}, "
-                       f"not {t.dtype} {tuple(t.shape)}")
+def _rows4(t, name: str, head_dim: int):
+    """`dd_rows` of [batch, tokens, heads, head_dim] as batch * tokens rows with one stride."""
+    kind = _ROW_TYPES.get(t.dtype)
+    if kind is None:
+        raise _invalid(f"{name} must be bfloat16 or float16, not {t.dtype}")
+    b, n, h, d = t.shape
+    request, token, head, one = t.stride()
+    if d != head_dim or one != 1:
+        raise _invalid(f"{name} must be [batch, tokens, heads, {head_dim}] with dense rows, not {tuple(t.shape)}")
+    if n == 1:
+        token = request
+    elif b > 1 and request != n * token:
+        raise _invalid(f"the tokens of {name} must lie at one stride: [batch, tokens] has to fold into one dimension")
+    return _PACK_ROWS(t.data_ptr(), kind, h, token if b * n > 1 else head_dim * h, head if h > 1 else head_dim)
+
+
+def _ints(t, name: str, shape):
+    if t.dtype is not torch.int32 or t.shape != shape or not t.is_contiguous():
+        raise _invalid(f"{name} must be a dense int32 tensor of shape {tuple(shape)}, not {t.dtype} {tuple(t.shape)}")
     return t.data_ptr()
 
 
 def _raise_last(rc: int):
-    if rc != DD_OK:
-        raise DDError(rc, lib.dd_last_error_message(None).decode())
+    raise DDError(rc, lib.dd_last_error_message(None).decode())
 
 
 class Rope:
@@ -259,21 +295,25 @@ class Rope:
         self.head_dim, self.rot_dim = head_dim, head_dim if rot_dim is None else rot_dim
         n = max(1, self.rot_dim // 2)
         host = (C.c_double * n)()
-        _raise_last(lib.dd_rope_turns(self.rot_dim, base, scaling, factor, original_len, low_turns, high_turns, host))
+        rc = lib.dd_rope_turns(self.rot_dim, base, scaling, factor, original_len, low_turns, high_turns, host)
+        if rc != DD_OK:
+            _raise_last(rc)
         self.turns_host = torch.tensor(list(host), dtype=torch.float64)
         self.turns = self.turns_host.to(device)
         self.c = DDRope(self.turns.data_ptr(), self.rot_dim, layout, amplitude)
+        self._addr = C.addressof(self.c)
 
     def apply(self, positions, q, k, q_out=None, k_out=None, *, backward=False, stream=None):
         """Turns q [N, Hq, d] and k [N, Hkv, d] (either may be None) by their positions [N] into q_out and k_out; without
         an output, in place. backward: the transpose, i.e. the gradient with respect to the inputs."""
-        n = positions.shape[0]
-        rq, rk = _rows(q, "q", self.head_dim, n), _rows(k, "k", self.head_dim, n)
-        oq = _rows(q_out, "q_out", self.head_dim, n) if q_out is not None else rq
-        ok = _rows(k_out, "k_out", self.head_dim, n) if k_out is not None else rk
-        rc = lib.dd_rope_apply(self.c, self.head_dim, n, _ints(positions, "positions", (n,)), rq, rk, oq, ok,
-                               1 if backward else 0, _stream(stream))
-        _raise_last(rc)
+        n, d = positions.shape[0], self.head_dim
+        rq = None if q is None else _rows(q, "q", d, n)
+        rk = None if k is None else _rows(k, "k", d, n)
+        rc = _rope_apply(self._addr, d, n, _ints(positions, "positions", (n,)), rq, rk,
+                         rq if q_out is None else _rows(q_out, "q_out", d, n), rk if k_out is None else _rows(k_out, "k_out", d, n),
+                         1 if backward else 0, _stream(stream))
+        if rc != DD_OK:
+            _raise_last(rc)
 
 
 class PagedCache:
@@ -307,6 +347,8 @@ class PagedCache:
         self.c = DDCache(data.data_ptr(), cache_format, n_kv_heads, head_dim, page_tokens, n_blocks, block_stride, head_stride,
                          block_table.data_ptr(), batch, max_pages, block_table.stride(0) if batch > 1 else max_pages,
                          self.status.data_ptr())
+        self._addr = C.addressof(self.c)
+        self._batch, self._heads, self._device = batch, n_kv_heads, block_table.device
         self._workspace_bytes = {}
 
     @classmethod
@@ -325,49 +367,58 @@ class PagedCache:
     def append(self, k, v, positions, requests=None, *, rope=None, q=None, q_out=None, stream=None):
         """Writes k and v [N, Hkv, d] of N new tokens to position positions[n] of request requests[n] (None: N / batch tokens
         of each request in turn); with `rope`, k is turned on the way and q [N, Hq, d] into q_out (None: in place)."""
-        n = positions.shape[0]
-        if rope is not None and rope.head_dim != self.head_dim:
+        n, d = positions.shape[0], self.head_dim
+        if rope is not None and rope.head_dim != d:
             raise _invalid("rope and cache differ in head_dim")
-        rq = _rows(q, "q", self.head_dim, n)
-        oq = _rows(q_out, "q_out", self.head_dim, n) if q_out is not None else rq
-        rc = lib.dd_cache_append(self.c, n, _ints(positions, "positions", (n,)),
-                                 None if requests is None else _ints(requests, "requests", (n,)),
-                                 _rows(k, "k", self.head_dim, n), _rows(v, "v", self.head_dim, n),
-                                 rope.c if rope is not None else None, rq, oq, _stream(stream))
-        _raise_last(rc)
+        rq = None if q is None else _rows(q, "q", d, n)
+        rc = _cache_append(self._addr, n, _ints(positions, "positions", (n,)),
+                           None if requests is None else _ints(requests, "requests", (n,)),
+                           _rows(k, "k", d, n), _rows(v, "v", d, n), None if rope is None else rope._addr, rq,
+                           rq if q_out is None else _rows(q_out, "q_out", d, n), _stream(stream))
+        if rc != DD_OK:
+            _raise_last(rc)
 
     def read(self, idx, out, stream=None):
         """Pages idx [batch, Hkv, k] (numbers within each request) in attention layout into out
         [batch, Hkv, 2, k * page_tokens, d], dense bfloat16 or float16."""
-        kind = _ROW_TYPES.get(out.dtype)
-        c = self.c
-        if idx.dim() != 3 or idx.shape[0] != c.batch or idx.shape[1] != c.n_kv_heads:
-            raise _invalid(f"idx must be [{c.batch}, {c.n_kv_heads}, k], not {tuple(idx.shape)}")
+        kind, b, h = _ROW_TYPES.get(out.dtype), self._batch, self._heads
+        if idx.dim() != 3:
+            raise _invalid(f"idx must be [{b}, {h}, k], not {tuple(idx.shape)}")
         k = idx.shape[2]
-        if kind is None or not out.is_contiguous() or tuple(out.shape) != (c.batch, c.n_kv_heads, 2, k * self.page_tokens, self.head_dim):
-            raise _invalid(f"out must be a dense 16-bit tensor {(c.batch, c.n_kv_heads, 2, k * self.page_tokens, self.head_dim)}")
-        _raise_last(lib.dd_cache_read(c, _ints(idx, "idx"), k, out.data_ptr(), kind, _stream(stream)))
+        if kind is None or not out.is_contiguous() or out.shape != (b, h, 2, k * self.page_tokens, self.head_dim):
+            raise _invalid(f"out must be a dense 16-bit tensor {(b, h, 2, k * self.page_tokens, self.head_dim)}")
+        rc = _cache_read(self._addr, _ints(idx, "idx", (b, h, k)), k, out.data_ptr(), kind, _stream(stream))
+        if rc != DD_OK:
+            _raise_last(rc)
 
     def decode_attn(self, q, ctx_len, out, out_lse=None, *, window=0, scale=0.0, workspace=None, stream=None):
         """Attention of the last Tq tokens of every request over its cached tokens. q, out [batch, Tq, Hq, d]; ctx_len
         [batch] int32; out_lse [batch, Tq, Hq] float32. Without a workspace the call takes one from torch's allocator on
         the stream it runs on (safe for several streams and for graph capture)."""
-        c = self.c
-        if q.dim() != 4 or q.shape[0] != c.batch or out.shape != q.shape:
-            raise _invalid(f"q and out must be [{c.batch}, tokens, heads, {self.head_dim}], not {tuple(q.shape)} and {tuple(out.shape)}")
-        B, Tq, Hq, _ = q.shape
+        b, shape = self._batch, q.shape
+        if len(shape) != 4 or shape[0] != b or out.shape != shape:
+            raise _invalid(f"q and out must be [{b}, tokens, heads, {self.head_dim}], not {tuple(shape)} and {tuple(out.shape)}")
+        Tq, Hq = shape[1], shape[2]
         rq, ro = _rows4(q, "q", self.head_dim), _rows4(out, "out", self.head_dim)
-        if out_lse is not None and (out_lse.dtype != torch.float32 or not out_lse.is_contiguous() or tuple(out_lse.shape) != (B, Tq, Hq)):
-            raise _invalid(f"out_lse must be a dense float32 tensor {(B, Tq, Hq)}")
-        need = self._workspace_bytes.get((Hq, Tq))
-        if need is None:
-            need = lib.dd_cache_decode_attn_workspace(Hq, c.n_kv_heads, self.head_dim, Tq)
-            self._workspace_bytes[(Hq, Tq)] = need
+        if out_lse is not None and (out_lse.dtype is not torch.float32 or out_lse.shape != (b, Tq, Hq) or not out_lse.is_contiguous()):
+            raise _invalid(f"out_lse must be a dense float32 tensor {(b, Tq, Hq)}")
         if workspace is None:
-            workspace = _scratch(max(need, 16), stream)
-        rc = lib.dd_cache_decode_attn(c, Tq, rq, _ints(ctx_len, "ctx_len", (B,)), ro, _ptr(out_lse), window, scale,
-                                      workspace.data_ptr(), workspace.numel() * workspace.element_size(), _stream(stream))
-        _raise_last(rc)
+            need = self._workspace_bytes.get((Hq, Tq))
+            if need is None:
+                need = max(16, lib.dd_cache_decode_attn_workspace(Hq, self._heads, self.head_dim, Tq))
+                self._workspace_bytes[(Hq, Tq)] = need
+            if stream is None:
+                workspace = torch.empty(need, dtype=torch.uint8, device=self._device)
+            else:
+                with torch.cuda.stream(torch.cuda.ExternalStream(stream) if isinstance(stream, int) else stream):
+                    workspace = torch.empty(need, dtype=torch.uint8, device=self._device)
+        else:
+            need = workspace.numel() * workspace.element_size()
+        rc = _cache_decode_attn(self._addr, Tq, rq, _ints(ctx_len, "ctx_len", (b,)), ro,
+                                None if out_lse is None else out_lse.data_ptr(), window, scale, workspace.data_ptr(), need,
+                                _stream(stream))
+        if rc != DD_OK:
+            _raise_last(rc)
 
     def workspace(self, n_q_heads: int, n_q_tokens: int = 1) -> torch.Tensor:
         """A workspace for decode_attn calls of this shape."""
@@ -379,22 +430,6 @@ class PagedCache:
         code, detail = self.status.tolist()
         self.status.zero_()
         return code, detail
-
-
-def _rows4(t, name: str, head_dim: int):
-    """`dd_rows` of [batch, tokens, heads, head_dim] as batch * tokens rows with one stride."""
-    B, Tq = t.shape[0], t.shape[1]
-    if B > 1 and Tq > 1 and t.stride(0) != Tq * t.stride(1):
-        raise _invalid(f"the tokens of {name} must lie at one stride: [batch, tokens] has to fold into one dimension")
-    step = t.stride(1) if Tq > 1 else t.stride(0)
-    return _rows(t.as_strided((B * Tq, t.shape[2], t.shape[3]), (step, t.stride(2), t.stride(3))), name, head_dim)
-
-
-def _scratch(n_bytes: int, stream) -> torch.Tensor:
-    if stream is None:
-        return torch.empty(n_bytes, dtype=torch.uint8, device="cuda")
-    with torch.cuda.stream(torch.cuda.ExternalStream(stream) if isinstance(stream, int) else stream):
-        return torch.empty(n_bytes, dtype=torch.uint8, device="cuda")
 
 
 class Context:
