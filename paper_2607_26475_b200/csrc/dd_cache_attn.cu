@@ -31,14 +31,17 @@
 // Joining. A unit inside one warp's run is finished there. The pieces of a cut unit that the warps of one block hold when
 // their runs end are added in shared memory; what is left (one fp32 partial per block, and the unit's last piece) goes to
 // the workspace, and a second small kernel adds those, always in the order of the list: the result does not depend on
-// timing. The warp in whose run a cut unit begins writes down where it ends.
+// timing. Its blocks are launched early and wait for the first kernel's end. (Letting the last block of a unit to arrive do
+// it, by a counter or by flags, took 4 to 7 us more: fences and contended words cost more round trips than a launch that
+// is already there.)
 #include "dd_cache.cuh"
 
 namespace {
 
 constexpr int CA_WARPS = 8;
 constexpr int CA_THREADS = CA_WARPS * 32;
-constexpr int CA_UNIT_COST = 1;              // empty places behind a unit in the flat list
+constexpr int CA_UNIT_COST = 3;              // empty places behind a unit in the flat list
+constexpr int CA_MIN_RUN = 2;                // places of a run at least
 constexpr float CA_HEADROOM = 6.f;           // log2 of the factor on P
 constexpr float CA_LAZY = 8.f;               // how far (log2) a weight may exceed the reference
 constexpr float CA_NONE = -3.0e38f;          // reference before any token: every finite score exceeds it
@@ -83,9 +86,9 @@ struct ca_args {
   long long q_token_stride, q_head_stride, out_token_stride, out_head_stride;   // bytes
   const int* ctx_len;
   float* lse;
-  float* part_o;       // [2 * warps][NT][D / 4][32]
+  float4* part_o;      // [2 * warps][NT][D / 16][32]
   float2* part_ml;     // [2 * warps][NT * 8]
-  int4* desc;          // [warps]: (request, row tile * heads + head, last warp of the unit + 1) of the cut unit that begins in a warp's run, or 0
+  int4* desc;          // [warps]: (request, sub, last run + 1) of the cut unit that begins in a warp's run, or 0
   int n_q_heads, G, Tq, n_rows, row_tiles, window;
   float scale_log2;
 };
@@ -192,6 +195,23 @@ __device__ __forceinline__ void ca_step(const ca_args& a, ca_cursor& k, int subs
 __device__ __forceinline__ int ca_channel(bool fp8, int g, int m) { return 16 * m + (fp8 ? 2 * g : g); }
 __device__ __forceinline__ constexpr int ca_pair(bool fp8) { return fp8 ? 1 : 8; }
 
+// Two neighbouring results of a query row (accumulator m, rows g and g + 8 of the product) to the row's output.
+template <bool FP8> __device__ __forceinline__ void ca_store(char* row, int g, int m, uint32_t w) {
+  if (FP8) {
+    *reinterpret_cast<uint32_t*>(row + 2 * ca_channel(FP8, g, m)) = w;
+  } else {
+    *reinterpret_cast<unsigned short*>(row + 2 * ca_channel(FP8, g, m)) = (unsigned short)w;
+    *reinterpret_cast<unsigned short*>(row + 2 * (ca_channel(FP8, g, m) + ca_pair(FP8))) = (unsigned short)(w >> 16);
+  }
+}
+// x += v * (scale of the column): elements 0 and 2 belong to the lane's first column, 1 and 3 to its second
+__device__ __forceinline__ void ca_add(float4& x, const float4& v, float s0, float s1) {
+  x.x = fmaf(v.x, s0, x.x);
+  x.y = fmaf(v.y, s1, x.y);
+  x.z = fmaf(v.z, s0, x.z);
+  x.w = fmaf(v.w, s1, x.w);
+}
+
 __device__ __forceinline__ float ca_lse(float from, float den) { return (from + log2f(den)) * 0.6931471805599453f; }
 
 template <int FMT, int D, int NT>
@@ -204,7 +224,7 @@ __global__ void __launch_bounds__(CA_THREADS, (ca_geom<FMT, D, NT>::BLOCKS_PER_S
   extern __shared__ __align__(128) unsigned char ca_smem[];
   __shared__ float2 sh_ml[CA_WARPS][NT * 8];
   __shared__ float sh_scale[CA_WARPS][NT * 8];
-  __shared__ int2 sh_key[CA_WARPS];
+  __shared__ int2 sh_piece[CA_WARPS];                // (request, sub) of the unit a run ends inside, or -1
 
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int g = lane >> 2, t = lane & 3;
@@ -213,7 +233,7 @@ __global__ void __launch_bounds__(CA_THREADS, (ca_geom<FMT, D, NT>::BLOCKS_PER_S
   const int me = blockIdx.x * CA_WARPS + warp;
 
   dd_grid_dependency_wait();
-  // the joining kernel's blocks may take the places that this grid's blocks leave (it waits for all of them)
+  // the joining kernel's blocks may take the places that this grid's blocks leave (each waits for all of them)
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
 
   // ---- this warp's run of the flat list: every warp adds up the list by itself, 32 requests at a time
@@ -226,7 +246,7 @@ __global__ void __launch_bounds__(CA_THREADS, (ca_geom<FMT, D, NT>::BLOCKS_PER_S
   for (int b = lane + 32; b < B; b += 32) total += places(ca_span_of(a, b, blockIdx.x == 0 && warp == 0));
 #pragma unroll
   for (int o = 16; o; o >>= 1) total += __shfl_xor_sync(0xffffffffu, total, o);
-  const long long share = max(1LL, ca_div(total + (long long)gridDim.x * CA_WARPS - 1, (int)gridDim.x * CA_WARPS));
+  const long long share = max((long long)CA_MIN_RUN, ca_div(total + (long long)gridDim.x * CA_WARPS - 1, (int)gridDim.x * CA_WARPS));
   const long long f0 = share * me;
   if (f0 < total) {
     long long at = 0;                                                 // first place of the 32 requests looked at
@@ -354,7 +374,7 @@ __global__ void __launch_bounds__(CA_THREADS, (ca_geom<FMT, D, NT>::BLOCKS_PER_S
 
   // ---- the using side, unit by unit
   int4 desc = make_int4(0, 0, 0, 0);
-  int2 key = make_int2(-1, 0);                       // the unit whose piece is left over at the end of the run
+  int2 inside = make_int2(-1, 0);
   float acc[NT][D / 16][4];
   float from[NT][2], sum[NT][2];                     // reference minus headroom; denominator, this lane's tokens
   while (u.left > 0) {
@@ -642,43 +662,49 @@ __global__ void __launch_bounds__(CA_THREADS, (ca_geom<FMT, D, NT>::BLOCKS_PER_S
             const float inv = empty ? 0.f : 1.f / sum[nt][c];
             char* o = a.out + tn * a.out_token_stride + h * a.out_head_stride;
 #pragma unroll
-            for (int m = 0; m < D / 16; ++m) {
-              const uint32_t w = empty ? 0u : dd_pack2<TQ>(acc[nt][m][c] * inv, acc[nt][m][2 + c] * inv);
-              if (FP8) {
-                *reinterpret_cast<uint32_t*>(o + 2 * ca_channel(FP8, g, m)) = w;
-              } else {
-                *reinterpret_cast<unsigned short*>(o + 2 * ca_channel(FP8, g, m)) = (unsigned short)w;
-                *reinterpret_cast<unsigned short*>(o + 2 * (ca_channel(FP8, g, m) + ca_pair(FP8))) = (unsigned short)(w >> 16);
-              }
-            }
+            for (int m = 0; m < D / 16; ++m) ca_store<FP8>(o, g, m, empty ? 0u : dd_pack2<TQ>(acc[nt][m][c] * inv, acc[nt][m][2 + c] * inv));
             if (a.lse && g == 0) a.lse[tn * a.n_q_heads + h] = empty ? -INFINITY : ca_lse(from[nt][c], sum[nt][c]);
           }
         }
-    } else if (ends) {
-      // the last piece of a unit that began in an earlier run: slot 2 me
-      float* po = a.part_o + 2LL * me * NT * geo::NACC * 32;
+    } else if (ends) {                                                // the last piece of a unit that began earlier: slot 2 me
+      float4* po = a.part_o + 2LL * me * NT * (D / 16) * 32;
 #pragma unroll
       for (int nt = 0; nt < NT; ++nt) {
 #pragma unroll
-        for (int m = 0; m < D / 16; ++m)
-#pragma unroll
-          for (int e = 0; e < 4; ++e) po[(nt * geo::NACC + m * 4 + e) * 32 + lane] = acc[nt][m][e];
+        for (int m = 0; m < D / 16; ++m) po[(nt * (D / 16) + m) * 32 + lane] = make_float4(acc[nt][m][0], acc[nt][m][1], acc[nt][m][2], acc[nt][m][3]);
         if (g == 0) {
           a.part_ml[2LL * me * NT * 8 + nt * 8 + 2 * t] = make_float2(from[nt][0], sum[nt][0]);
           a.part_ml[2LL * me * NT * 8 + nt * 8 + 2 * t + 1] = make_float2(from[nt][1], sum[nt][1]);
         }
       }
     } else {
-      key = make_int2(b, sub);                                        // the run ends inside the unit
+      inside = make_int2(b, sub);                                     // the run ends here
+      if (t0 == 0) desc = make_int4(b, sub, (int)ca_div(share * me + (share - u.left) + s.tiles - 1, (int)share) + 1, 0);
     }
-    if (t0 == 0 && !ends)                                             // it begins here: its last tile lies in run ...
-      desc = make_int4(b, sub, (int)((share * me + (share - u.left) + s.tiles - 1) / share) + 1, 0);
 
     // ---- the next unit
     u.left -= n_here + CA_UNIT_COST;
     if (u.left > 0) ca_next_unit(a, u, subs);
   }
   if (lane == 0) a.desc[me] = desc;
+  ca_wait<0>();
+  __syncwarp();
+
+  // ---- pieces left over at the ends of the runs: neighbouring warps inside the same unit become one partial, in slot
+  // 2 w + 1 of the first of them
+  if (lane == 0) sh_piece[warp] = inside;
+  if (inside.x >= 0) {
+    float4* own = reinterpret_cast<float4*>(ca_smem + warp * geo::WARP_BYTES);
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt) {
+#pragma unroll
+      for (int m = 0; m < D / 16; ++m) own[(nt * (D / 16) + m) * 32 + lane] = make_float4(acc[nt][m][0], acc[nt][m][1], acc[nt][m][2], acc[nt][m][3]);
+      if (g == 0) {
+        sh_ml[warp][nt * 8 + 2 * t] = make_float2(from[nt][0], sum[nt][0]);
+        sh_ml[warp][nt * 8 + 2 * t + 1] = make_float2(from[nt][1], sum[nt][1]);
+      }
+    }
+  }
   // units without a token: zeros and -inf, shared out over the blocks
   for (int b = blockIdx.x; b < B; b += gridDim.x) {
     if (ca_span_of(a, b, false).tiles == 0) {
@@ -690,39 +716,18 @@ __global__ void __launch_bounds__(CA_THREADS, (ca_geom<FMT, D, NT>::BLOCKS_PER_S
       }
     }
   }
-  ca_wait<0>();
-  __syncwarp();
-
-  // ---- pieces left over at the ends of the runs: neighbouring warps inside the same unit become one partial, in slot
-  // 2 w + 1 of the first of them
-  if (lane == 0) sh_key[warp] = key;
-  if (key.x >= 0) {
-    float* own = reinterpret_cast<float*>(ca_smem + warp * geo::WARP_BYTES);
-#pragma unroll
-    for (int nt = 0; nt < NT; ++nt) {
-#pragma unroll
-      for (int m = 0; m < D / 16; ++m)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) own[(nt * geo::NACC + m * 4 + e) * 32 + lane] = acc[nt][m][e];
-      if (g == 0) {
-        sh_ml[warp][nt * 8 + 2 * t] = make_float2(from[nt][0], sum[nt][0]);
-        sh_ml[warp][nt * 8 + 2 * t + 1] = make_float2(from[nt][1], sum[nt][1]);
-      }
-    }
-  }
   __syncthreads();
+  auto same = [&](int v, int w) { return sh_piece[v].x == sh_piece[w].x && sh_piece[v].y == sh_piece[w].y; };
   auto chain_end = [&](int w0) {                     // warps w0 .. w1 - 1 hold pieces of one unit
-    const int2 k0 = sh_key[w0];
     int w1 = w0 + 1;
-    while (w1 < CA_WARPS && sh_key[w1].x == k0.x && sh_key[w1].y == k0.y) ++w1;
+    while (w1 < CA_WARPS && same(w1, w0)) ++w1;
     return w1;
   };
   for (int i = threadIdx.x; i < CA_WARPS * NT * 8; i += CA_THREADS) {
     const int w = i / (NT * 8), row = i % (NT * 8);
-    const int2 k0 = sh_key[w];
-    if (k0.x < 0) continue;
+    if (sh_piece[w].x < 0) continue;
     int w0 = w;
-    while (w0 > 0 && sh_key[w0 - 1].x == k0.x && sh_key[w0 - 1].y == k0.y) --w0;
+    while (w0 > 0 && same(w0 - 1, w)) --w0;
     const int w1 = chain_end(w0);
     float M = CA_NONE, L = 0.f;
     for (int v = w0; v < w1; ++v) M = fmaxf(M, sh_ml[v][row].x);
@@ -731,40 +736,43 @@ __global__ void __launch_bounds__(CA_THREADS, (ca_geom<FMT, D, NT>::BLOCKS_PER_S
     if (w == w0) a.part_ml[(2LL * (blockIdx.x * CA_WARPS + w0) + 1) * NT * 8 + row] = make_float2(M, L);
   }
   __syncthreads();
+  constexpr int QUADS = NT * (D / 16) * 32;          // groups of four accumulators: [column tile][product][lane]
   for (int w0 = 0, w1; w0 < CA_WARPS; w0 = w1) {
     w1 = w0 + 1;
-    if (sh_key[w0].x < 0) continue;
+    if (sh_piece[w0].x < 0) continue;
     w1 = chain_end(w0);
-    float* po = a.part_o + (2LL * (blockIdx.x * CA_WARPS + w0) + 1) * NT * geo::NACC * 32;
-#pragma unroll
-    for (int k = 0; k < NT * geo::NACC * 32 / CA_THREADS; ++k) {
-      const int e = k * CA_THREADS + threadIdx.x;
-      const int row = e / (geo::NACC * 32) * 8 + 2 * (e & 3) + ((e >> 5) & 1);
-      float x = 0.f;
+    float4* po = a.part_o + (2LL * (blockIdx.x * CA_WARPS + w0) + 1) * QUADS;
+    for (int e = threadIdx.x; e < QUADS; e += CA_THREADS) {
+      const int row = e / (D / 16 * 32) * 8 + 2 * (e & 3);
+      float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
       for (int w = 0; w < CA_WARPS; ++w)
-        if (w >= w0 && w < w1) x = fmaf(reinterpret_cast<const float*>(ca_smem + w * geo::WARP_BYTES)[e], sh_scale[w][row], x);
+        if (w >= w0 && w < w1) ca_add(x, reinterpret_cast<const float4*>(ca_smem + w * geo::WARP_BYTES)[e], sh_scale[w][row], sh_scale[w][row + 1]);
       po[e] = x;
     }
   }
+
 }
 
-// Adds the partials of the cut units that begin in block x of the attention kernel. Grid (blocks of the attention kernel,
-// NT * D / 32): every thread owns one accumulator element. The partials of a unit from run w0 (where it begins) to run w1
-// (where it ends) are: one per block among the runs w0 .. w1 - 1, in the slot of the first of them, and the last piece.
-// What bounds it is latency: (descriptors) -> (references, sums, the first partials, the length) -> result.
+// Adds the partials of the cut units that begin in block x of the attention kernel. The partials of a unit from run w0
+// (where it begins) to run w1 (where it ends) are one per block among the runs w0 .. w1 - 1, in the slot of the first of
+// them, and the last piece. Grid (blocks of the attention kernel, groups of 64 quads of accumulators); four groups of
+// threads take every fourth partial of the same 64 quads. What bounds it is latency: (descriptors) -> (references, sums,
+// the first 32 partials, the length) -> result.
+constexpr int CJ_GROUPS = 4;
 template <int FMT, int D, int NT>
-__global__ void __launch_bounds__(256) dd_cache_attn_join_kernel(const ca_args a) {
+__global__ void __launch_bounds__(64 * CJ_GROUPS) dd_cache_attn_join_kernel(const ca_args a) {
   using TQ = typename ca_types<FMT>::Q;
-  constexpr int NACC = D / 4;
-  constexpr int AHEAD = 8;                                            // partials fetched before the scales are known
-  extern __shared__ float ja_scale[];                                 // [parts][8] of the column tile
+  constexpr bool FP8 = FMT >= 2;
+  constexpr int QUADS = NT * (D / 16) * 32;
+  constexpr int AHEAD = 8;                                            // partials of a group fetched before the scales are known
+  extern __shared__ float cj_scale[];                                 // [parts][8] of the column tile
   __shared__ float2 sh_ml[8];
-  const int e = blockIdx.y * 256 + threadIdx.x;                       // element: [nt][register][lane]
-  const int nt = (blockIdx.y * 256) / (NACC * 32);
+  __shared__ float4 sh_x[CJ_GROUPS][64];
+  const int q = threadIdx.x & 63, grp = threadIdx.x >> 6;
+  const int e = blockIdx.y * 64 + q;                                  // quad: [column tile][product][lane]
+  const int nt = blockIdx.y * 64 / (D / 16 * 32), m = (e / 32) % (D / 16), ge = (e & 31) >> 2, col = 2 * (e & 3);
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const int reg = (e / 32) % NACC, m = reg >> 2, g = lane >> 2, t = lane & 3;
-  const int col = 2 * t + (reg & 1);
   dd_grid_dependency_wait();
   // the descriptors of the block's warps, one per lane, handed round by shuffles
   int4 mine = make_int4(0, 0, 0, 0);
@@ -774,13 +782,14 @@ __global__ void __launch_bounds__(256) dd_cache_attn_join_kernel(const ca_args a
     const int l = __ffs(todo) - 1;
     todo &= todo - 1;
     const int b = __shfl_sync(0xffffffffu, mine.x, l), sub = __shfl_sync(0xffffffffu, mine.y, l);
-    const int w0 = blockIdx.x * CA_WARPS + l, w1 = __shfl_sync(0xffffffffu, mine.z, l) - 1, first_block = blockIdx.x;
-    const int n = (w1 - 1) / CA_WARPS - first_block + 2;              // partials
-    auto slot = [&](int i) -> long long { return i == 0 ? 2LL * w0 + 1 : (i == n - 1 ? 2LL * w1 : 2LL * (first_block + i) * CA_WARPS + 1); };
-    const ca_span s = ca_span_of(a, b, false);
-    float ahead[AHEAD];
+    const int w0 = blockIdx.x * CA_WARPS + l, w1 = __shfl_sync(0xffffffffu, mine.z, l) - 1;
+    const int n = (w1 - 1) / CA_WARPS - (int)blockIdx.x + 2;          // partials
+    auto slot = [&](int i) -> long long { return i == 0 ? 2LL * w0 + 1 : (i == n - 1 ? 2LL * w1 : 2LL * ((int)blockIdx.x + i) * CA_WARPS + 1); };
+    const int end = ca_span_of(a, b, false).end;
+    float4 ahead[AHEAD];
 #pragma unroll
-    for (int i = 0; i < AHEAD; ++i) ahead[i] = i < n ? a.part_o[slot(i) * (NT * NACC * 32) + e] : 0.f;
+    for (int i = 0; i < AHEAD; ++i)
+      if (grp + CJ_GROUPS * i < n) ahead[i] = a.part_o[slot(grp + CJ_GROUPS * i) * QUADS + e];
     {
       // warp w: the scales of row w of the column tile
       const int row = nt * 8 + warp;
@@ -791,11 +800,11 @@ __global__ void __launch_bounds__(256) dd_cache_attn_join_kernel(const ca_args a
       for (int o = 16; o; o >>= 1) M = fmaxf(M, __shfl_xor_sync(0xffffffffu, M, o));
       const float sc0 = ca_exp2(own.x - M);
       float L = own.y * sc0;
-      if (lane < n) ja_scale[lane * 8 + warp] = sc0;
+      if (lane < n) cj_scale[lane * 8 + warp] = sc0;
       for (int i = lane + 32; i < n; i += 32) {
         const float2 ml = a.part_ml[slot(i) * NT * 8 + row];
         const float sc = ca_exp2(ml.x - M);
-        ja_scale[i * 8 + warp] = sc;
+        cj_scale[i * 8 + warp] = sc;
         L = fmaf(ml.y, sc, L);
       }
 #pragma unroll
@@ -803,23 +812,36 @@ __global__ void __launch_bounds__(256) dd_cache_attn_join_kernel(const ca_args a
       if (lane == 0) sh_ml[warp] = make_float2(M, L);
     }
     __syncthreads();
-    float x = 0.f;
+    float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
-    for (int i = 0; i < AHEAD; ++i)
-      if (i < n) x = fmaf(ahead[i], ja_scale[i * 8 + col], x);
+    for (int i = 0; i < AHEAD; ++i) {
+      const int k = grp + CJ_GROUPS * i;
+      if (k < n) ca_add(x, ahead[i], cj_scale[k * 8 + col], cj_scale[k * 8 + col + 1]);
+    }
 #pragma unroll 8
-    for (int i = AHEAD; i < n; ++i) x = fmaf(a.part_o[slot(i) * (NT * NACC * 32) + e], ja_scale[i * 8 + col], x);
-    const int rt = sub / a.c.n_kv_heads, head = sub - rt * a.c.n_kv_heads;
-    const int r = rt * NT * 8 + nt * 8 + col;
-    if (r < a.n_rows) {
-      const int tok = r / a.G, h = head * a.G + r - tok * a.G;
-      const long long tn = (long long)b * a.Tq + tok;
-      const bool empty = s.end - a.Tq + tok < 0;
-      const float2 ml = sh_ml[col];
-      const int ch = ca_channel(FMT >= 2, g, m) + (reg & 2 ? ca_pair(FMT >= 2) : 0);
-      const uint32_t w = dd_pack2<TQ>(empty ? 0.f : x / ml.y, 0.f);
-      *reinterpret_cast<unsigned short*>(a.out + tn * a.out_token_stride + h * a.out_head_stride + 2 * ch) = (unsigned short)w;
-      if (a.lse && ch == 0) a.lse[tn * a.n_q_heads + h] = empty ? -INFINITY : ca_lse(ml.x, ml.y);
+    for (int k = grp + CJ_GROUPS * AHEAD; k < n; k += CJ_GROUPS)
+      ca_add(x, a.part_o[slot(k) * QUADS + e], cj_scale[k * 8 + col], cj_scale[k * 8 + col + 1]);
+    sh_x[grp][q] = x;
+    __syncthreads();
+    if (grp < 2) {                                                    // group c finishes the quads' column c
+      const int c = grp;
+      float lo = 0.f, hi = 0.f;
+#pragma unroll
+      for (int k = 0; k < CJ_GROUPS; ++k) {
+        const float4 v = sh_x[k][q];
+        lo += c ? v.y : v.x;
+        hi += c ? v.w : v.z;
+      }
+      const int rt = sub / a.c.n_kv_heads, head = sub - rt * a.c.n_kv_heads;
+      const int r = rt * NT * 8 + nt * 8 + col + c;
+      if (r < a.n_rows) {
+        const int tok = r / a.G, h = head * a.G + r - tok * a.G;
+        const long long tn = (long long)b * a.Tq + tok;
+        const bool empty = end - a.Tq + tok < 0;
+        const float2 ml = sh_ml[col + c];
+        ca_store<FP8>(a.out + tn * a.out_token_stride + h * a.out_head_stride, ge, m, empty ? 0u : dd_pack2<TQ>(lo / ml.y, hi / ml.y));
+        if (a.lse && m == 0 && ge == 0) a.lse[tn * a.n_q_heads + h] = empty ? -INFINITY : ca_lse(ml.x, ml.y);
+      }
     }
     __syncthreads();                                                  // before the scales are written again
   }
@@ -828,13 +850,13 @@ __global__ void __launch_bounds__(256) dd_cache_attn_join_kernel(const ca_args a
 struct ca_plan {
   const void* main_kernel;
   const void* join_kernel;
-  int smem, blocks_per_sm, nt;
+  int smem, blocks_per_sm;
 };
 template <int FMT, int D, int NT> ca_plan ca_plan_of() {
   using geo = ca_geom<FMT, D, NT>;
   static_assert(geo::SMEM <= 227 * 1024, "shared memory of a block");
   static_assert(geo::BLOCKS_PER_SM == 1 || geo::SMEM + 1024 + 2048 <= 114 * 1024, "shared memory of two blocks");
-  return {(const void*)dd_cache_attn_kernel<FMT, D, NT>, (const void*)dd_cache_attn_join_kernel<FMT, D, NT>, geo::SMEM, geo::BLOCKS_PER_SM, NT};
+  return {(const void*)dd_cache_attn_kernel<FMT, D, NT>, (const void*)dd_cache_attn_join_kernel<FMT, D, NT>, geo::SMEM, geo::BLOCKS_PER_SM};
 }
 template <int FMT> ca_plan ca_pick(int d, int nt) {
   if (d == 128) return nt == 1 ? ca_plan_of<FMT, 128, 1>() : ca_plan_of<FMT, 128, 2>();
@@ -917,7 +939,7 @@ extern "C" int dd_cache_decode_attn(const dd_cache* cache, int n_q_tokens, const
   a.out_token_stride = out->token_stride * 2; a.out_head_stride = out->head_stride * 2;
   a.ctx_len = ctx_len;
   a.lse = out_lse;
-  a.part_o = (float*)workspace;
+  a.part_o = (float4*)workspace;
   a.part_ml = (float2*)((char*)workspace + z.part_o);
   a.desc = (int4*)((char*)workspace + z.part_o + z.part_ml);
   a.n_q_heads = q->n_heads;
@@ -947,8 +969,8 @@ extern "C" int dd_cache_decode_attn(const dd_cache* cache, int n_q_tokens, const
   cfg.dynamicSmemBytes = p.smem;
   void* args[] = {&a};
   DD_CUDA_TRY(nullptr, cudaLaunchKernelExC(&cfg, p.main_kernel, args));
-  cfg.gridDim = dim3((unsigned)blocks, (unsigned)(nt * cache->head_dim / 32));
-  cfg.blockDim = dim3(256);
+  cfg.gridDim = dim3((unsigned)blocks, (unsigned)(nt * (cache->head_dim / 16) * 32 / 64));
+  cfg.blockDim = dim3(64 * CJ_GROUPS);
   cfg.dynamicSmemBytes = (size_t)(blocks + 1) * 8 * sizeof(float);     // at most one partial per block and the last piece
   DD_CUDA_TRY(nullptr, cudaLaunchKernelExC(&cfg, p.join_kernel, args));
   return DD_OK;
