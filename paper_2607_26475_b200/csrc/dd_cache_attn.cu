@@ -7,8 +7,8 @@
 // Work split. The context of every (request, row tile, KV head) "unit" is cut into tiles of 16 tokens, and all tiles of
 // the launch form one flat list, request by request, with a few empty places behind each unit that stand for what a unit
 // costs besides its tiles. Every warp of a grid that fills the device once takes an equal run of the list; lengths are
-// read on the device, so the launch does not depend on them (a captured graph may be replayed with other lengths). A
-// warp works alone: it keeps a ring of half tiles (K or V) in flight with 16-byte cp.async, and the ring runs on across the
+// read on the device, so the launch does not depend on them (a captured graph may be replayed with other lengths). Units
+// of at most 8 tiles are not cut. A warp works alone: it keeps a ring of half tiles (K or V) in flight with 16-byte cp.async, and the ring runs on across the
 // borders of units. A copy instruction takes 512 contiguous bytes (whole 128-byte lines; fragments fetched straight from
 // global memory touch half lines and ran at half the rate), and the chunks of a row are placed by row ^ chunk, so that
 // ldmatrix reads them without bank conflicts: K as it lies, V transposed.
@@ -41,7 +41,7 @@ namespace {
 constexpr int CA_WARPS = 8;
 constexpr int CA_THREADS = CA_WARPS * 32;
 constexpr int CA_UNIT_COST = 3;              // empty places behind a unit in the flat list
-constexpr int CA_MIN_RUN = 2;                // places of a run at least
+constexpr int CA_WHOLE = 8;                  // a unit of at most so many tiles is not cut: it belongs to the run it begins in
 constexpr float CA_HEADROOM = 6.f;           // log2 of the factor on P
 constexpr float CA_LAZY = 8.f;               // how far (log2) a weight may exceed the reference
 constexpr float CA_NONE = -3.0e38f;          // reference before any token: every finite score exceeds it
@@ -172,6 +172,10 @@ struct ca_cursor {
   int b, sub, t, left;   // sub = row tile * heads + head
   ca_span s;
 };
+// At the first tile of a unit: the run takes all of it where it is short.
+__device__ __forceinline__ void ca_keep_whole(ca_cursor& k) {
+  if (k.s.tiles <= CA_WHOLE && k.left < k.s.tiles) k.left = k.s.tiles;
+}
 // To the first tile of the next unit.
 __device__ __forceinline__ void ca_next_unit(const ca_args& a, ca_cursor& k, int subs) {
   k.t = 0;
@@ -182,6 +186,7 @@ __device__ __forceinline__ void ca_next_unit(const ca_args& a, ca_cursor& k, int
       k.s = ca_span_of(a, ++k.b, false);
     } while (k.s.tiles == 0);
   }
+  ca_keep_whole(k);
 }
 __device__ __forceinline__ void ca_step(const ca_args& a, ca_cursor& k, int subs) {
   --k.left;
@@ -246,7 +251,7 @@ __global__ void __launch_bounds__(CA_THREADS, (ca_geom<FMT, D, NT>::BLOCKS_PER_S
   for (int b = lane + 32; b < B; b += 32) total += places(ca_span_of(a, b, blockIdx.x == 0 && warp == 0));
 #pragma unroll
   for (int o = 16; o; o >>= 1) total += __shfl_xor_sync(0xffffffffu, total, o);
-  const long long share = max((long long)CA_MIN_RUN, ca_div(total + (long long)gridDim.x * CA_WARPS - 1, (int)gridDim.x * CA_WARPS));
+  const long long share = max(1LL, ca_div(total + (long long)gridDim.x * CA_WARPS - 1, (int)gridDim.x * CA_WARPS));
   const long long f0 = share * me;
   if (f0 < total) {
     long long at = 0;                                                 // first place of the 32 requests looked at
@@ -280,7 +285,10 @@ __global__ void __launch_bounds__(CA_THREADS, (ca_geom<FMT, D, NT>::BLOCKS_PER_S
       at += __shfl_sync(0xffffffffu, incl, 31);
       if (b0 + 32 >= B) break;                                        // lengths changed under the call
     }
-    if (is.left > 0 && is.t >= is.s.tiles) {                          // the run begins in the empty places behind a unit
+    if (is.left > 0 && is.t == 0) {
+      ca_keep_whole(is);
+    } else if (is.left > 0 && (is.t >= is.s.tiles || is.s.tiles <= CA_WHOLE)) {
+      // the run begins in the empty places behind a unit, or inside a short one, which is the run before's
       is.left -= is.s.tiles + CA_UNIT_COST - is.t;
       if (is.left > 0) ca_next_unit(a, is, subs);
     }
@@ -969,6 +977,7 @@ extern "C" int dd_cache_decode_attn(const dd_cache* cache, int n_q_tokens, const
   cfg.dynamicSmemBytes = p.smem;
   void* args[] = {&a};
   DD_CUDA_TRY(nullptr, cudaLaunchKernelExC(&cfg, p.main_kernel, args));
+  if ((long long)cache->max_pages * cache->page_tokens <= 16 * CA_WHOLE) return DD_OK;   // no unit can have been cut
   cfg.gridDim = dim3((unsigned)blocks, (unsigned)(nt * (cache->head_dim / 16) * 32 / 64));
   cfg.blockDim = dim3(64 * CJ_GROUPS);
   cfg.dynamicSmemBytes = (size_t)(blocks + 1) * 8 * sizeof(float);     // at most one partial per block and the last piece
