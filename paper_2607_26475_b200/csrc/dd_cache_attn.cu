@@ -57,9 +57,11 @@ struct ca_geom {
   static constexpr int ES = FP8 ? 1 : 2;
   static constexpr int ROW = D * ES;                                  // bytes of a row: 64, 128 or 256
   static constexpr int HALF_BYTES = 16 * ROW;                         // K (or V) of a tile
-  // What one copy group of a warp brings: a whole tile where that is at most 4 KiB, else K or V of a tile in turn.
-  static constexpr bool WHOLE = 2 * HALF_BYTES <= 4096;
-  static constexpr int EXP_AT = 2 * HALF_BYTES;                       // e4m3: exponents of the tile, 16 of K and 16 of V
+  // What one copy group of a warp brings: K or V of a tile in turn, or a whole tile where that is small. Halves of 2 KiB keep
+  // more in flight (e4m3 at head_dim 128, 8 x 32K tokens: 102 us against 108 with whole tiles), halves of 1 KiB cost more than they
+  // bring (head_dim 64: 74 against 63 us), and with the deep ring of two column tiles whole tiles win (126 against 136 us).
+  static constexpr bool WHOLE = 2 * HALF_BYTES <= (NT == 1 ? 2048 : 4096);
+  static constexpr int EXP_AT = (WHOLE ? 2 : 1) * HALF_BYTES;         // e4m3: exponents of the tile, 16 of K and 16 of V, behind K or all
   static constexpr int SLOT_BYTES = (WHOLE ? 2 : 1) * HALF_BYTES + (FP8 ? 32 : 0);
   static constexpr int COPIES = HALF_BYTES / 512;
   static constexpr int BLOCKS_PER_SM = NT == 1 ? 2 : 1;               // two column tiles need the registers of a whole SM
@@ -70,7 +72,6 @@ struct ca_geom {
   static constexpr int SMEM = CA_WARPS * WARP_BYTES;
   static constexpr int NACC = D / 4;                                  // accumulator registers per column tile
   static_assert(WARP_BYTES >= NT * NACC * 128, "a warp's ring holds its accumulators at the end");
-  static_assert(!FP8 || WHOLE, "exponents travel with a whole tile");
 };
 
 // Byte offset of 16-byte chunk c of row r in a half tile: a column of 8 rows covers all 32 banks.
