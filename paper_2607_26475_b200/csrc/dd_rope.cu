@@ -14,11 +14,14 @@
 // magnitude is one reduction over the group.
 #include <math.h>
 
+#include <type_traits>
+
 #include "dd_cache.cuh"
 
 namespace {
 
 constexpr int RP_THREADS = 256;
+constexpr int RP_BLOCKS = 3;         // per SM, by registers
 constexpr int RP_BATCH = 4;          // heads whose loads are in flight together
 
 struct rp_rows {
@@ -53,7 +56,7 @@ __device__ __forceinline__ void rp_angle(double turns, int pos, float amplitude,
 
 // FMT: -1 rotation only; DD_CACHE_* append. T: type of the rows.
 template <typename T, int D, int FMT>
-__global__ void __launch_bounds__(RP_THREADS) dd_rope_kernel(rp_args a) {
+__global__ void __launch_bounds__(RP_THREADS, RP_BLOCKS) dd_rope_kernel(rp_args a) {
   constexpr int LANES = D / 16;
   constexpr int PER_WARP = 32 / LANES;
   const int lane = threadIdx.x & 31, j = lane % LANES;
@@ -111,101 +114,116 @@ __global__ void __launch_bounds__(RP_THREADS) dd_rope_kernel(rp_args a) {
   else if (turned) { c0 = 8 * j; c1 = c0 + 8 * a.rot16; }
   else { c0 = 16 * a.rot16 + 16 * (j - a.rot16); c1 = c0 + 8; }
 
-  for (int hb = h0; hb < h1; hb += RP_BATCH) {
-    uint4 r0[RP_BATCH], r1[RP_BATCH];
-#pragma unroll
-    for (int u = 0; u < RP_BATCH; ++u) {
-      const int h = hb + u;
-      r0[u] = r1[u] = make_uint4(0u, 0u, 0u, 0u);
-      if (h < h1 && live) {
-        const rp_rows& src = h < a.n_q ? a.q : (h < a.n_q + a.n_k ? a.k : a.v);
-        const int hh = h < a.n_q ? h : (h < a.n_q + a.n_k ? h - a.n_q : h - a.n_q - a.n_k);
-        const char* row = src.data + n * src.token_stride + hh * src.head_stride;
-        r0[u] = *reinterpret_cast<const uint4*>(row + 2 * c0);
-        r1[u] = *reinterpret_cast<const uint4*>(row + 2 * c1);
-      }
+  // One kind of rows at a time (0 queries, 1 keys, 2 values), heads [lo, hi) of it.
+  auto rows = [&](auto kind_, int lo, int hi, const rp_rows& from, const rp_rows& to) {
+    constexpr int kind = decltype(kind_)::value;
+    constexpr bool paged = FMT >= 0 && kind > 0;               // goes to the cache
+    if (lo >= hi) return;
+    const char* in = from.data + n * from.token_stride + lo * from.head_stride;
+    char* out = nullptr;
+    long long out_stride;
+    if (paged) {
+      out_stride = a.cache.head_stride;
+      if (live) out = page_at + lo * out_stride;
+    } else {
+      out_stride = to.head_stride;
+      out = to.data + n * to.token_stride + lo * out_stride;
     }
+    const int row_off = paged ? ((kind == 2 ? page_tokens : 0) + off) * (FMT == DD_CACHE_E4M3 ? D : 2 * D) : 0;
+    for (int h = lo; h < hi; h += RP_BATCH) {
+      uint4 r0[RP_BATCH], r1[RP_BATCH];
 #pragma unroll
-    for (int u = 0; u < RP_BATCH; ++u) {
-      const int h = hb + u;
-      if (h >= h1) break;
-      const bool is_q = h < a.n_q, is_v = h >= a.n_q + a.n_k;
-      float x[16];
-      const uint32_t w[8] = {r0[u].x, r0[u].y, r0[u].z, r0[u].w, r1[u].x, r1[u].y, r1[u].z, r1[u].w};
-#pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        const float2 f = dd_unpack2<T>(w[i]);
-        x[2 * i] = f.x;
-        x[2 * i + 1] = f.y;
-      }
-      if (turned && !is_v) {
-        if (a.interleaved) {
-#pragma unroll
-          for (int i = 0; i < 8; ++i) {
-            const float p = x[2 * i], q = x[2 * i + 1];
-            x[2 * i] = fmaf(p, cs[i], -q * sn[i]);
-            x[2 * i + 1] = fmaf(q, cs[i], p * sn[i]);
-          }
-        } else {
-#pragma unroll
-          for (int i = 0; i < 8; ++i) {
-            const float p = x[i], q = x[8 + i];
-            x[i] = fmaf(p, cs[i], -q * sn[i]);
-            x[8 + i] = fmaf(q, cs[i], p * sn[i]);
-          }
+      for (int u = 0; u < RP_BATCH; ++u) {
+        r0[u] = r1[u] = make_uint4(0u, 0u, 0u, 0u);
+        if (h + u < hi && live) {
+          r0[u] = *reinterpret_cast<const uint4*>(in + 2 * c0);
+          r1[u] = *reinterpret_cast<const uint4*>(in + 2 * c1);
         }
+        in += from.head_stride;
       }
-      if (FMT == DD_CACHE_E4M3 && !is_q) {
-        float amax = 0.f;
 #pragma unroll
-        for (int i = 0; i < 16; ++i) {
-          const float m = fabsf(x[i]);
-          if (m <= 3.4028234e38f) amax = fmaxf(amax, m);       // finite values only
-          else x[i] = __uint_as_float(0x7fc00000u);
+      for (int u = 0; u < RP_BATCH; ++u) {
+        if (h + u >= hi) break;
+        if (!(paged && FMT == DD_CACHE_E4M3) && !(turned && kind < 2)) {       // copied bit for bit
+          if (live) {
+            *reinterpret_cast<uint4*>(out + row_off + 2 * c0) = r0[u];
+            *reinterpret_cast<uint4*>(out + row_off + 2 * c1) = r1[u];
+          }
+          out += out_stride;
+          continue;
         }
+        float x[16];
+        const uint32_t w[8] = {r0[u].x, r0[u].y, r0[u].z, r0[u].w, r1[u].x, r1[u].y, r1[u].z, r1[u].w};
 #pragma unroll
-        for (int m = 1; m < LANES; m <<= 1) amax = fmaxf(amax, __shfl_xor_sync(0xffffffffu, amax, m));
-        const int byte = dd_e4m3_exponent_byte(amax);
-        const float inv = dd_two_to_byte(254 - byte);          // 2^(127 - byte): exact, so the code is rounded once
+        for (int i = 0; i < 8; ++i) {
+          const float2 f = dd_unpack2<T>(w[i]);
+          x[2 * i] = f.x;
+          x[2 * i + 1] = f.y;
+        }
+        if (kind < 2 && turned) {
+          if (a.interleaved) {
 #pragma unroll
-        for (int i = 0; i < 16; ++i) x[i] *= inv;
-        if (live) {
-          const int hh = is_v ? h - a.n_q - a.n_k : h - a.n_q;
-          char* pg = page_at + hh * a.cache.head_stride;
-          char* row = pg + ((is_v ? page_tokens : 0) + off) * D;
-          const uint2 lo = make_uint2(dd_float_to_e4m3x4(x[0], x[1], x[2], x[3]), dd_float_to_e4m3x4(x[4], x[5], x[6], x[7]));
-          const uint2 hi = make_uint2(dd_float_to_e4m3x4(x[8], x[9], x[10], x[11]), dd_float_to_e4m3x4(x[12], x[13], x[14], x[15]));
-          if (c1 == c0 + 8) {
-            *reinterpret_cast<uint4*>(row + c0) = make_uint4(lo.x, lo.y, hi.x, hi.y);
+            for (int i = 0; i < 8; ++i) {
+              const float p = x[2 * i], q = x[2 * i + 1];
+              x[2 * i] = fmaf(p, cs[i], -q * sn[i]);
+              x[2 * i + 1] = fmaf(q, cs[i], p * sn[i]);
+            }
           } else {
-            *reinterpret_cast<uint2*>(row + c0) = lo;
-            *reinterpret_cast<uint2*>(row + c1) = hi;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+              const float p = x[i], q = x[8 + i];
+              x[i] = fmaf(p, cs[i], -q * sn[i]);
+              x[8 + i] = fmaf(q, cs[i], p * sn[i]);
+            }
           }
-          if (j == 0) pg[2 * page_tokens * D + (is_v ? page_tokens : 0) + off] = (char)byte;
         }
-      } else if (live) {
-        char* row;
-        if (is_q) {
-          row = a.q_out.data + n * a.q_out.token_stride + h * a.q_out.head_stride;
-        } else if (FMT < 0) {
-          row = a.k_out.data + n * a.k_out.token_stride + (h - a.n_q) * a.k_out.head_stride;
-        } else {
-          const int hh = is_v ? h - a.n_q - a.n_k : h - a.n_q;
-          row = page_at + hh * a.cache.head_stride + ((is_v ? page_tokens : 0) + off) * (2 * D);
+        if (paged && FMT == DD_CACHE_E4M3) {
+          float amax = 0.f;
+#pragma unroll
+          for (int i = 0; i < 16; ++i) amax = fmaxf(amax, fabsf(x[i]));
+#pragma unroll
+          for (int m = 1; m < LANES; m <<= 1) amax = fmaxf(amax, __shfl_xor_sync(0xffffffffu, amax, m));
+          if (amax > 3.4028234e38f) {                          // an infinity (fmaxf passes over NaN): finite values only
+            amax = 0.f;
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+              const float v = fabsf(x[i]);
+              if (v <= 3.4028234e38f) amax = fmaxf(amax, v);
+              else x[i] = __uint_as_float(0x7fc00000u);
+            }
+            const unsigned peers = LANES == 8 ? 0xffu << (lane & 24) : 0xfu << (lane & 28);
+#pragma unroll
+            for (int m = 1; m < LANES; m <<= 1) amax = fmaxf(amax, __shfl_xor_sync(peers, amax, m));
+          }
+          const int byte = dd_e4m3_exponent_byte(amax);
+          const float inv = dd_two_to_byte(254 - byte);        // 2^(127 - byte): exact, so the code is rounded once
+#pragma unroll
+          for (int i = 0; i < 16; ++i) x[i] *= inv;
+          if (live) {
+            char* row = out + row_off;
+            const uint2 lo8 = make_uint2(dd_float_to_e4m3x4(x[0], x[1], x[2], x[3]), dd_float_to_e4m3x4(x[4], x[5], x[6], x[7]));
+            const uint2 hi8 = make_uint2(dd_float_to_e4m3x4(x[8], x[9], x[10], x[11]), dd_float_to_e4m3x4(x[12], x[13], x[14], x[15]));
+            if (c1 == c0 + 8) {
+              *reinterpret_cast<uint4*>(row + c0) = make_uint4(lo8.x, lo8.y, hi8.x, hi8.y);
+            } else {
+              *reinterpret_cast<uint2*>(row + c0) = lo8;
+              *reinterpret_cast<uint2*>(row + c1) = hi8;
+            }
+            if (j == 0) out[2 * page_tokens * D + (kind == 2 ? page_tokens : 0) + off] = (char)byte;
+          }
+        } else if (live) {
+          *reinterpret_cast<uint4*>(out + row_off + 2 * c0) =
+              make_uint4(dd_pack2<T>(x[0], x[1]), dd_pack2<T>(x[2], x[3]), dd_pack2<T>(x[4], x[5]), dd_pack2<T>(x[6], x[7]));
+          *reinterpret_cast<uint4*>(out + row_off + 2 * c1) =
+              make_uint4(dd_pack2<T>(x[8], x[9]), dd_pack2<T>(x[10], x[11]), dd_pack2<T>(x[12], x[13]), dd_pack2<T>(x[14], x[15]));
         }
-        uint4 o0, o1;
-        if (turned && !is_v) {
-          o0 = make_uint4(dd_pack2<T>(x[0], x[1]), dd_pack2<T>(x[2], x[3]), dd_pack2<T>(x[4], x[5]), dd_pack2<T>(x[6], x[7]));
-          o1 = make_uint4(dd_pack2<T>(x[8], x[9]), dd_pack2<T>(x[10], x[11]), dd_pack2<T>(x[12], x[13]), dd_pack2<T>(x[14], x[15]));
-        } else {                                               // copied bit for bit
-          o0 = r0[u];
-          o1 = r1[u];
-        }
-        *reinterpret_cast<uint4*>(row + 2 * c0) = o0;
-        *reinterpret_cast<uint4*>(row + 2 * c1) = o1;
+        out += out_stride;
       }
     }
-  }
+  };
+  rows(std::integral_constant<int, 0>(), h0, min(h1, a.n_q), a.q, a.q_out);
+  rows(std::integral_constant<int, 1>(), max(h0 - a.n_q, 0), min(h1 - a.n_q, a.n_k), a.k, a.k_out);
+  if (FMT >= 0) rows(std::integral_constant<int, 2>(), max(h0 - a.n_q - a.n_k, 0), h1 - a.n_q - a.n_k, a.v, a.v);
 }
 
 template <typename T, int D>
@@ -223,7 +241,7 @@ int rp_launch(rp_args& a, int head_dim, int dtype, int fmt, cudaStream_t st, con
   int sms = 0;
   cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, device);
   if (sms <= 0) sms = 148;
-  const long long target = (long long)sms * 2048 / lanes;       // groups that fill every thread slot
+  const long long target = (long long)sms * RP_BLOCKS * RP_THREADS / lanes;   // groups that fill the device once
   long long slices = (target + a.n_tokens - 1) / a.n_tokens;
   if (slices > n_heads) slices = n_heads;
   if (slices < 1) slices = 1;
