@@ -58,6 +58,10 @@ extern "C" {
 #define DD_ATTN_STREAM  2           /* streaming kernel: equal runs of pages per block, TMA-fed shared-memory ring */
 #define DD_ATTN_TC      3           /* the streaming split on tcgen05: tiles of 8 pages, accumulators in tensor memory */
 
+#define DD_CACHE_BF16 0             /* formats of a KV page, described at dd_cache */
+#define DD_CACHE_FP16 1
+#define DD_CACHE_E4M3 2             /* 8-bit floating point, one power-of-two scale per token and head */
+
 #define DD_SELECT_AUTO         0    /* fused cluster kernel when the request fits, else the two-kernel path */
 #define DD_SELECT_TWO_KERNELS  1    /* scoring kernel + top-k kernel with logits in global scratch */
 
@@ -93,6 +97,9 @@ typedef struct dd_config {
   int stage_block_pages;     /* DD_GATHER_STAGED: 0 = copy exactly the selected runs; 2, 4, 8, 16 or 32 = copy every
                                 aligned block of that many pages that holds a selected page (over-fetch, no stragglers) */
   int attn_mode;             /* DD_ATTN_AUTO, DD_ATTN_SPLIT, DD_ATTN_STREAM or DD_ATTN_TC (attn_splits applies to the split kernel) */
+  int store_format;          /* format of the KV store: DD_CACHE_BF16 (0) or DD_CACHE_E4M3 (pages of 4128 bytes as written by
+                                dd_cache_append; halves the bytes on the host link; DD_GATHER_LOADS only). Landmarks, slots
+                                and everything behind them stay bf16 */
 } dd_config;
 
 /* ---- context ------------------------------------------------------------------------------- */
@@ -129,7 +136,9 @@ int dd_sync(dd_ctx* ctx, double timeout_s);
  * compressed landmarks; Sec. 4.1: built before decoding and fixed afterwards). Here a
  * landmark is the mean of the valid keys of a page: fp32 sum in token order, fp32 divide,
  * round-to-nearest-even to bf16; a page with no valid token gets zeros.
- *   kv_layer   pinned or dev, bf16 [B][Hkv][P][2][T][d] ([..][0] = K, [..][1] = V)
+ *   kv_layer   pinned or dev, bf16 [B][Hkv][P][2][T][d] ([..][0] = K, [..][1] = V); with store_format = DD_CACHE_E4M3 here and
+ *              in every call below that takes a layer of the store: [B][Hkv][P] pages of dd_cache_page_bytes(), and what is
+ *              said of its bits is said of the values that its codes stand for
  *   ctx_len    dev int32 [B], tokens per request
  *   landmarks  dev bf16 [B][Hkv][P][d], written
  * With landmark_chunk_tokens = c < 16 a page has R = 16/c landmarks, one per c consecutive tokens, and the
@@ -311,10 +320,6 @@ int dd_sparse_decode_attn_static(int batch, int n_q_heads, int n_kv_heads, int h
 
 #define DD_BF16 0
 #define DD_FP16 1
-
-#define DD_CACHE_BF16 0
-#define DD_CACHE_FP16 1
-#define DD_CACHE_E4M3 2   /* 8-bit floating point, one power-of-two scale per token and head */
 
 #define DD_ROPE_HALF        0   /* element i turns with element i + rot_dim/2 */
 #define DD_ROPE_INTERLEAVED 1   /* element 2i turns with element 2i + 1 */

@@ -73,6 +73,9 @@ static const char* dd_check_config(const dd_config* c) {
   if (c->attn_mode != DD_ATTN_AUTO && c->attn_mode != DD_ATTN_SPLIT && c->attn_mode != DD_ATTN_STREAM &&
       c->attn_mode != DD_ATTN_TC)
     return "unknown attn_mode";
+  if (c->store_format != DD_CACHE_BF16 && c->store_format != DD_CACHE_E4M3) return "store_format must be DD_CACHE_BF16 or DD_CACHE_E4M3";
+  if (c->store_format == DD_CACHE_E4M3 && c->gather_mode != DD_GATHER_LOADS)
+    return "a quantised store is gathered with DD_GATHER_LOADS only (the other engines copy pages as they are)";
   if (c->attn_splits > 512) return "attn_splits must be <= 512";
   if (c->attn_splits > 64 && c->attn_splits % 8) return "attn_splits above 64 must be a multiple of 8";
   if ((long long)c->batch * c->n_kv_heads * c->k_pages > 0x7fffffffLL) return "too many selected pages";

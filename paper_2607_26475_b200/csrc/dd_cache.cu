@@ -127,9 +127,7 @@ dd_cache_view dd_make_view(const dd_cache* c, const char* data_dev) {
 constexpr int CR_THREADS = 256;
 
 //
-// LINES: for e4m3 pages in host memory. Their 4128 bytes start anywhere in a 128-byte line, and a load instruction that
-// straddles lines asks the host link for each part of a line by itself; loads are then aligned to the lines of each run
-// (372 -> 340 us for 4096 pages of 4 KiB; the stores, two half-used ones per load, do not matter at that rate).
+// LINES: e4m3 pages in host memory, read by aligned lines (dd_e4m3_tile_by_lines).
 template <int FMT, typename T, int D, bool LINES>
 __global__ void __launch_bounds__(CR_THREADS) dd_cache_read_kernel(dd_cache_view c, const int* __restrict__ idx,
                                                                   char* __restrict__ out, int k_pages, long long n_tiles) {
@@ -161,44 +159,10 @@ __global__ void __launch_bounds__(CR_THREADS) dd_cache_read_kernel(dd_cache_view
     char* dst = out + (((bg * 2 * k_pages + j) << tile_shift) + tile) * (16LL * 2 * D);
     const long long v_off = ((long long)k_pages << tile_shift) * (16LL * 2 * D);
     if (LINES) {
-      constexpr int NW = 16 * D / 512 + 1;             // aligned windows of 512 bytes that cover a run
-      uint4 w[2][NW];
-      int q[2] = {0, 0}, ex = 0;                       // this lane's first chunk of 16 codes of each run (may be negative)
-#pragma unroll
-      for (int kv = 0; kv < 2; ++kv) {
-        const char* run = c.data + (blk < 0 ? 0 : blk * c.block_stride + g * c.head_stride) + (kv * page_tokens + tile * 16) * D;
-        q[kv] = lane - (int)(((uintptr_t)run & 127) >> 4);
-#pragma unroll
-        for (int i = 0; i < NW; ++i) {
-          w[kv][i] = make_uint4(0u, 0u, 0u, 0u);
-          if (blk >= 0 && q[kv] + i * 32 >= 0 && q[kv] + i * 32 < D) w[kv][i] = dd_ld_stream(run + (q[kv] + i * 32) * 16);
-        }
-      }
-      if (blk >= 0)
-        ex = *reinterpret_cast<const unsigned char*>(c.data + blk * c.block_stride + g * c.head_stride + 2 * page_tokens * D +
-                                                     (lane >> 4) * page_tokens + tile * 16 + (lane & 15));
-#pragma unroll
-      for (int kv = 0; kv < 2; ++kv)
-#pragma unroll
-        for (int i = 0; i < NW; ++i) {
-          const int at = q[kv] + i * 32;
-          const float s = dd_two_to_byte(__shfl_sync(0xffffffffu, ex, kv * 16 + ((at < 0 ? 0 : at) * 16 / D & 15)));
-          if (at >= 0 && at < D) {
-            const uint32_t v4[4] = {w[kv][i].x, w[kv][i].y, w[kv][i].z, w[kv][i].w};
-            uint32_t o[8];
-#pragma unroll
-            for (int k = 0; k < 4; ++k) {
-              uint32_t lo, hi;
-              dd_e4m3x4_to_half(v4[k], lo, hi);
-              const float2 u = dd_unpack2<__half>(lo), v = dd_unpack2<__half>(hi);
-              o[2 * k] = dd_pack2<T>(u.x * s, u.y * s);
-              o[2 * k + 1] = dd_pack2<T>(v.x * s, v.y * s);
-            }
-            char* to = dst + (kv ? v_off : 0) + at * 32;
-            dd_st_v4(to, make_uint4(o[0], o[1], o[2], o[3]));
-            dd_st_v4(to + 16, make_uint4(o[4], o[5], o[6], o[7]));
-          }
-        }
+      const char* page = c.data + (blk < 0 ? 0 : blk * c.block_stride + g * c.head_stride);
+      const char* run = page + tile * 16 * D;
+      dd_e4m3_tile_by_lines<T, D>(run, run + page_tokens * D, page + 2 * page_tokens * D + (lane >> 4) * page_tokens + tile * 16 + (lane & 15),
+                                  blk >= 0, dst, dst + v_off);
       continue;
     }
     uint4 r[2][NL];                                    // e4m3: the first two words

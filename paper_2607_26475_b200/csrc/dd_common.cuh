@@ -14,6 +14,7 @@ constexpr int DD_T = 16;           // tokens per page
 constexpr int DD_ROW_BYTES = DD_D * 2;
 constexpr int DD_HALF_PAGE_BYTES = DD_T * DD_ROW_BYTES;   // K (or V) part of a page: 4 KiB
 constexpr int DD_PAGE_BYTES = 2 * DD_HALF_PAGE_BYTES;     // 8 KiB
+constexpr int DD_PAGE_BYTES_E4M3 = 2 * DD_T * DD_D + 2 * DD_T;   // quantised store: codes and one exponent byte per row, 4128 B
 constexpr int DD_MAX_RING = 8;
 constexpr int DD_SCORE_TILE = 128; // pages scored by one thread block
 constexpr int DD_STAGE_LISTS = 8;  // page-locked descriptor buffers of the staged gather (host may run this far ahead)

@@ -5,7 +5,7 @@
 // pairs the m-th missing page with the m-th victim position, writes the repaired page list of the slot and
 // appends (unit, position, page) to a compact fix list. dd_gather_fix_kernel copies the listed pages from
 // the pinned store, one warp per page, exactly like the prefetch gather.
-#include "dd_common.cuh"
+#include "dd_cache.cuh"
 
 __device__ __forceinline__ bool dd_sorted_contains(const int* __restrict__ a, int n, int v) {
   int lo = 0, hi = n;
@@ -74,6 +74,7 @@ __global__ void __launch_bounds__(128) dd_diff_kernel(const int* __restrict__ pr
   }
 }
 
+template <bool E4M3>
 __global__ void __launch_bounds__(256) dd_gather_fix_kernel(const char* __restrict__ kv, const int4* __restrict__ fix_list,
                                                             const unsigned int* __restrict__ fix_count,
                                                             char* __restrict__ slot, int P, int k, int* err_word) {
@@ -86,6 +87,13 @@ __global__ void __launch_bounds__(256) dd_gather_fix_kernel(const char* __restri
     if (page < 0 || page >= P) {
       dd_report(err_word, DD_ERR_INDEX_RANGE, page);
       page = page < 0 ? 0 : P - 1;
+    }
+    if (E4M3) {                                       // a quantised store, as in the prefetch gather
+      const char* src = kv + ((size_t)f.x * P + page) * DD_PAGE_BYTES_E4M3;
+      char* dst_k = slot + ((size_t)f.x * 2 * k + f.y) * DD_HALF_PAGE_BYTES;
+      dd_e4m3_tile_by_lines<__nv_bfloat16, DD_D>(src, src + DD_T * DD_D, src + 2 * DD_T * DD_D + lane, true, dst_k,
+                                                 dst_k + (size_t)k * DD_HALF_PAGE_BYTES);
+      continue;
     }
     const char* src = kv + ((size_t)f.x * P + page) * DD_PAGE_BYTES + lane * 16;
     char* dst_k = slot + ((size_t)f.x * 2 * k + f.y) * DD_HALF_PAGE_BYTES + lane * 16;
@@ -116,9 +124,9 @@ int dd_launch_gather_fix(dd_ctx* ctx, const void* kv_dev, int slot, cudaStream_t
   const dd_config& c = ctx->cfg;
   const size_t per_slot = (size_t)c.batch * c.n_kv_heads * c.k_pages;
   const int ctas = c.gather_ctas > 0 ? c.gather_ctas : 16;
-  dd_gather_fix_kernel<<<ctas, 256, 0, st>>>((const char*)kv_dev, ctx->fix_list + slot * per_slot, ctx->fix_count + slot,
-                                             ctx->ring + (size_t)slot * ctx->slot_bytes, c.max_pages, c.k_pages,
-                                             ctx->err_word);
+  auto* kernel = c.store_format == DD_CACHE_E4M3 ? dd_gather_fix_kernel<true> : dd_gather_fix_kernel<false>;
+  kernel<<<ctas, 256, 0, st>>>((const char*)kv_dev, ctx->fix_list + slot * per_slot, ctx->fix_count + slot,
+                               ctx->ring + (size_t)slot * ctx->slot_bytes, c.max_pages, c.k_pages, ctx->err_word);
   DD_CUDA_TRY(ctx, cudaGetLastError());
   return DD_OK;
 }

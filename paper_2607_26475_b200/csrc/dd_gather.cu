@@ -14,7 +14,7 @@
 #include <chrono>
 #include <vector>
 
-#include "dd_common.cuh"
+#include "dd_cache.cuh"
 
 __device__ __forceinline__ int dd_checked_page(const int* idx, const int* n_pages, int item, int b, int P,
                                                int* err_word) {
@@ -54,6 +54,24 @@ __global__ void __launch_bounds__(256) dd_gather_loads_kernel(const char* __rest
     for (int i = 0; i < 8; ++i) dd_st_v4(dst_k + i * 512, r[i]);
 #pragma unroll
     for (int i = 0; i < 8; ++i) dd_st_v4(dst_v + i * 512, r[8 + i]);
+  }
+}
+
+// The same over a quantised store (dd_config.store_format = DD_CACHE_E4M3): 4128 bytes of a page cross the link instead of
+// 8192, and the slot gets the values they stand for in bf16 (exact). Bound: the host link.
+__global__ void __launch_bounds__(256) dd_gather_e4m3_kernel(const char* __restrict__ kv, const int* __restrict__ idx,
+                                                             const int* __restrict__ n_pages, char* __restrict__ slot,
+                                                             int Hkv, int P, int k, int total, int* err_word) {
+  const int lane = threadIdx.x & 31;
+  const int n_warps = gridDim.x * (blockDim.x >> 5);
+  for (int item = (threadIdx.x >> 5) * gridDim.x + blockIdx.x; item < total; item += n_warps) {
+    const int j = item % k;
+    const int bg = item / k;
+    const int p = dd_checked_page(idx, n_pages, item, bg / Hkv, P, err_word);
+    const char* page = kv + ((size_t)bg * P + p) * DD_PAGE_BYTES_E4M3;
+    char* dst_k = slot + ((size_t)bg * 2 * k + j) * DD_HALF_PAGE_BYTES;
+    dd_e4m3_tile_by_lines<__nv_bfloat16, DD_D>(page, page + DD_T * DD_D, page + 2 * DD_T * DD_D + lane, true, dst_k,
+                                               dst_k + (size_t)k * DD_HALF_PAGE_BYTES);
   }
 }
 
@@ -166,8 +184,12 @@ int dd_launch_gather(dd_ctx* ctx, const void* kv_dev, const int* idx, const int*
     int ctas = c.gather_ctas > 0 ? c.gather_ctas : 16;
     const int max_ctas = (total + 7) / 8;
     if (ctas > max_ctas) ctas = max_ctas;
-    dd_gather_loads_kernel<<<ctas, 256, 0, st>>>((const char*)kv_dev, idx, n_pages, slot, c.n_kv_heads, c.max_pages,
-                                                 c.k_pages, total, ctx->err_word);
+    if (c.store_format == DD_CACHE_E4M3)
+      dd_gather_e4m3_kernel<<<ctas, 256, 0, st>>>((const char*)kv_dev, idx, n_pages, slot, c.n_kv_heads, c.max_pages,
+                                                  c.k_pages, total, ctx->err_word);
+    else
+      dd_gather_loads_kernel<<<ctas, 256, 0, st>>>((const char*)kv_dev, idx, n_pages, slot, c.n_kv_heads, c.max_pages,
+                                                   c.k_pages, total, ctx->err_word);
   }
   DD_CUDA_TRY(ctx, cudaGetLastError());
   return DD_OK;

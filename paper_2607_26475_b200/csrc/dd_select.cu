@@ -7,12 +7,13 @@
 // followed by an ordered compaction that emits ascending page numbers.
 #include <cooperative_groups.h>
 
-#include "dd_common.cuh"
+#include "dd_cache.cuh"
 
 // ------------------------------------------------------------------------------------------------
 // Landmarks: mean of the valid keys of a chunk (a page, or 1/R of a page), fp32 sum in token order, fp32
 // divide, RNE to bf16. One warp per chunk; a lane owns 4 consecutive channels.
 // ------------------------------------------------------------------------------------------------
+template <bool E4M3>
 __global__ void __launch_bounds__(256) dd_landmark_kernel(const __nv_bfloat16* __restrict__ kv,
                                                           const int* __restrict__ ctx_len,
                                                           __nv_bfloat16* __restrict__ lm, int Hkv, int P, int R,
@@ -30,7 +31,21 @@ __global__ void __launch_bounds__(256) dd_landmark_kernel(const __nv_bfloat16* _
     cnt = cnt > c ? c : cnt;
     const __nv_bfloat16* src = kv + page * (2 * DD_T * DD_D) + (size_t)r * c * DD_D + lane * 4;   // K half comes first
     float a0 = 0.f, a1 = 0.f, a2 = 0.f, a3 = 0.f;
-    for (int i = 0; i < cnt; ++i) {
+    if (E4M3) {                                    // a quantised store: the same sum over the values the codes stand for
+      const char* pg = reinterpret_cast<const char*>(kv) + page * DD_PAGE_BYTES_E4M3;
+      for (int i = 0; i < cnt; ++i) {
+        const int tok = r * c + i;
+        uint32_t lo, hi;
+        dd_e4m3x4_to_half(*reinterpret_cast<const uint32_t*>(pg + tok * DD_D + lane * 4), lo, hi);
+        const float s = dd_two_to_byte(*reinterpret_cast<const unsigned char*>(pg + 2 * DD_T * DD_D + tok));
+        const float2 u = dd_unpack2<__half>(lo), v = dd_unpack2<__half>(hi);
+        a0 = __fadd_rn(a0, u.x * s);
+        a1 = __fadd_rn(a1, u.y * s);
+        a2 = __fadd_rn(a2, v.x * s);
+        a3 = __fadd_rn(a3, v.y * s);
+      }
+    }
+    for (int i = 0; !E4M3 && i < cnt; ++i) {
       uint2 w = *reinterpret_cast<const uint2*>(src + i * DD_D);
       __nv_bfloat162 lo = *reinterpret_cast<__nv_bfloat162*>(&w.x);
       __nv_bfloat162 hi = *reinterpret_cast<__nv_bfloat162*>(&w.y);
@@ -58,7 +73,8 @@ int dd_launch_build_landmarks(dd_ctx* ctx, const void* kv_dev, const int* ctx_le
   long long blocks = (total + warps_per_block - 1) / warps_per_block;
   const long long cap = (long long)ctx->sm_count * 16;
   if (blocks > cap) blocks = cap;
-  dd_landmark_kernel<<<(unsigned)blocks, warps_per_block * 32, 0, st>>>(
+  auto* kernel = c.store_format == DD_CACHE_E4M3 ? dd_landmark_kernel<true> : dd_landmark_kernel<false>;
+  kernel<<<(unsigned)blocks, warps_per_block * 32, 0, st>>>(
       (const __nv_bfloat16*)kv_dev, ctx_len, (__nv_bfloat16*)landmarks, c.n_kv_heads, c.max_pages, ctx->R, total);
   DD_CUDA_TRY(ctx, cudaGetLastError());
   return DD_OK;

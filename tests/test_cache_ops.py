@@ -177,3 +177,20 @@ def test_reference_quantiser_against_torch():
     assert torch.equal(y.float().to(torch.float8_e4m3fn).double(), back)
     top = y.abs().amax(-1)
     assert bool((top <= 448).all()) and bool((top > 224).all())
+
+
+def test_store_format_of_a_context(dd):
+    """A quantised store is taken with the zero-copy gather only; other formats and engines are refused before a device is
+    asked for."""
+    cfg = dd.DDConfig(n_layers=2, batch=2, n_q_heads=32, n_kv_heads=8, head_dim=128, page_tokens=16, max_pages=64, k_pages=8,
+                      n_q_tokens=2, ring_depth=2, store_format=dd.DD_CACHE_E4M3)
+    assert dd.lib.dd_slot_bytes(cfg) == 2 * 8 * 8 * 8192                      # slots stay bf16
+    for kw in (dict(gather_mode=dd.DD_GATHER_BULK), dict(gather_mode=dd.DD_GATHER_STAGED), dict(store_format=dd.DD_CACHE_FP16),
+               dict(store_format=-1)):
+        bad = dd.DDConfig.from_buffer_copy(cfg)
+        for k, v in kw.items():
+            setattr(bad, k, v)
+        assert dd.lib.dd_slot_bytes(bad) == 0
+        h = ctypes.c_void_p()
+        assert dd.lib.dd_create(bad, ctypes.byref(h)) == dd.DD_ERR_INVALID_ARG
+        assert b"store" in dd.lib.dd_last_error_message(None)
