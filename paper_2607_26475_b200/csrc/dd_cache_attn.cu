@@ -34,6 +34,8 @@
 // timing. Its blocks are launched early and wait for the first kernel's end. (Letting the last block of a unit to arrive do
 // it, by a counter or by flags, took 4 to 7 us more: fences and contended words cost more round trips than a launch that
 // is already there.)
+#include <type_traits>
+
 #include "dd_cache.cuh"
 
 namespace {
@@ -68,6 +70,9 @@ struct ca_geom {
   static constexpr int RING_BUDGET = (BLOCKS_PER_SM == 2 ? 110 : 220) * 1024;
   static constexpr int STAGES_ = RING_BUDGET / (CA_WARPS * SLOT_BYTES);
   static constexpr int STAGES = STAGES_ > 8 ? 8 : STAGES_;
+  // A second copy of the tile's code without masks and questions. Where registers are scarce (one column tile, head_dim 128) its
+  // spills cost what it saves (8 x 32K tokens e4m3 104 -> 106 us); elsewhere 131 -> 111 us (128 query heads), 63 -> 59 (head_dim 64).
+  static constexpr bool PLAIN_LOOP = NT == 2 || D == 64;
   static constexpr int WARP_BYTES = STAGES * SLOT_BYTES;
   static constexpr int SMEM = CA_WARPS * WARP_BYTES;
   static constexpr int NACC = D / 4;                                  // accumulator registers per column tile
@@ -91,6 +96,7 @@ struct ca_args {
   float2* part_ml;     // [2 * warps][NT * 8]
   int4* desc;          // [warps]: (request, sub, last run + 1) of the cut unit that begins in a warp's run, or 0
   int n_q_heads, G, Tq, n_rows, row_tiles, window;
+  uint32_t by_G;       // ceil(2^31 / G): row / G by a multiplication
   float scale_log2;
 };
 
@@ -101,6 +107,9 @@ __device__ __forceinline__ void ca_cp4(uint32_t dst, const void* src, uint32_t b
   asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(dst), "l"(src), "r"(bytes) : "memory");
 }
 __device__ __forceinline__ void ca_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+__device__ __forceinline__ void ca_cp4_all(uint32_t dst, const void* src) {
+  asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(dst), "l"(src) : "memory");
+}
 template <int N> __device__ __forceinline__ void ca_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
 __device__ __forceinline__ void ca_ldsm(uint32_t (&r)[4], uint32_t at) {
   asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0,%1,%2,%3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(at) : "memory");
@@ -122,6 +131,16 @@ __device__ __forceinline__ void ca_mma(float (&c)[4], uint32_t a0, uint32_t a1, 
   else
     asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
         : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+// The first product of a chain: nothing to add to.
+template <int FMT>
+__device__ __forceinline__ void ca_mma_first(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+  if (FMT == 0)
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%10,%10,%10,%10};"
+        : "=f"(c[0]), "=f"(c[1]), "=f"(c[2]), "=f"(c[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1), "f"(0.f));
+  else
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%10,%10,%10,%10};"
+        : "=f"(c[0]), "=f"(c[1]), "=f"(c[2]), "=f"(c[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1), "f"(0.f));
 }
 __device__ __forceinline__ uint32_t ca_transpose(uint32_t a) {       // 8x8 matrix of 16-bit values across the warp
   uint32_t d;
@@ -167,6 +186,10 @@ __device__ __forceinline__ ca_span ca_span_of(const ca_args& a, int b, bool repo
   s.tiles = len > 0 ? ((len + 15) >> 4) - s.tile0 : 0;
   return s;
 }
+
+// Query token of row r < 2^16 of a unit (r / G, exact for G <= 1024), and a unit's row tile.
+__device__ __forceinline__ int ca_token(const ca_args& a, int r) { return (int)__umulhi((uint32_t)r << 1, a.by_G); }
+__device__ __forceinline__ int ca_row_tile(const ca_args& a, int sub) { return a.row_tiles == 1 ? 0 : sub / a.c.n_kv_heads; }
 
 // A place in the flat list: tile t of unit (b, sub), `left` places before the end of the run.
 struct ca_cursor {
@@ -300,16 +323,31 @@ __global__ void __launch_bounds__(CA_THREADS, (ca_geom<FMT, D, NT>::BLOCKS_PER_S
   ca_cursor u = is;                                  // the using side starts at the same place
   const int page_mask = (1 << a.c.page_shift) - 1;
   // Table entries of the next 32 tiles of the unit, one per lane.
-  int blocks = 0, blocks_from = 0;
+  int blocks = 0, blocks_from = 0, blocks_of = -1;   // entries at hand, the first one's tile, their request
   const char* head_at = nullptr;                     // page 0 of the unit's head
   auto look_up = [&]() {
     blocks_from = is.t;
+    blocks_of = is.b;
     const int i = min(is.t + lane, is.s.tiles - 1);
     blocks = __ldg(a.c.table + is.b * a.c.table_stride + (((is.s.tile0 + i) << 4) >> a.c.page_shift));
   };
+  auto all_good = [&]() { return __all_sync(0xffffffffu, (unsigned)blocks < (unsigned)a.c.n_blocks); };
   auto enter_unit = [&]() {
-    head_at = a.c.data + (is.sub % a.c.n_kv_heads) * a.c.head_stride;
-    look_up();
+    const int rt = ca_row_tile(a, is.sub), head = is.sub - rt * a.c.n_kv_heads;
+    head_at = a.c.data + head * a.c.head_stride;
+    // the next head of the same request has the same table: short units would wait for it anew at every head
+    if (blocks_of != is.b || blocks_from != 0 || is.t != 0) look_up();
+    // The unit's query rows are called into L1 a few tiles ahead of their use, every 32-byte sector of them.
+    constexpr int SECTORS = D / 16;
+#pragma unroll
+    for (int i = 0; i < NT * 8 * SECTORS; i += 32) {
+      const int row = rt * NT * 8 + (i + lane) / SECTORS;
+      if (row < a.n_rows) {
+        const int tok = ca_token(a, row);
+        const char* at = a.q + ((long long)is.b * a.Tq + tok) * a.q_token_stride + (head * a.G + row - tok * a.G) * a.q_head_stride;
+        asm volatile("prefetch.global.L1 [%0];" ::"l"(at + (i + lane) % SECTORS * 32));
+      }
+    }
   };
   if (is.left > 0) enter_unit();
   const char* src = nullptr;                         // K of the tile being issued; V lies page_tokens rows behind
@@ -319,11 +357,14 @@ __global__ void __launch_bounds__(CA_THREADS, (ca_geom<FMT, D, NT>::BLOCKS_PER_S
   const uint32_t place0 = ca_place<geo::ROW>(lane / (geo::ROW / 16), lane % (geo::ROW / 16));
 
   // Copy i of a half takes bytes [512 i, 512 i + 512): 8, 4 or 2 rows; its row numbers change the swizzle by a constant.
+  auto copy_full = [&](uint32_t to, const char* from) {
+#pragma unroll
+    for (int i = 0; i < geo::COPIES; ++i)
+      ca_cp16_all(to + (place0 ^ ca_twist<geo::ROW>(i)) + i * 512, from + i * 512 + lane * 16);
+  };
   auto copy_half = [&](uint32_t to, const char* from) {
     if (n_first <= 0 && n_valid >= 16) {
-#pragma unroll
-      for (int i = 0; i < geo::COPIES; ++i)
-        ca_cp16_all(to + (place0 ^ ca_twist<geo::ROW>(i)) + i * 512, from + i * 512 + lane * 16);
+      copy_full(to, from);
     } else {
 #pragma unroll
       for (int i = 0; i < geo::COPIES; ++i) {
@@ -369,11 +410,40 @@ __global__ void __launch_bounds__(CA_THREADS, (ca_geom<FMT, D, NT>::BLOCKS_PER_S
   };
 #pragma unroll 1
   for (int i = 0; i < NS; ++i) issue();
+  // The same inside a unit, where nothing has to be asked: a complete tile of a good block, not the last of the run, the unit
+  // or the entries at hand. First half of a pair: V of the tile at hand if the ring's depth is odd, else K (or everything) of it.
+  constexpr bool V_FIRST = !geo::WHOLE && (NS & 1);
+  auto plain_k = [&]() {
+    const int in_page = ((is.s.tile0 + is.t) << 4) & page_mask;
+    const char* page = head_at + __shfl_sync(0xffffffffu, blocks, is.t - blocks_from) * a.c.block_stride;
+    src = page + in_page * geo::ROW;
+    copy_full(put, src);
+    if (FP8 && lane < 8) ca_cp4_all(put + geo::EXP_AT + lane * 4, page + (2 * D + (lane >> 2)) * (page_mask + 1) + in_page + (lane & 3) * 4);
+    if (geo::WHOLE) copy_full(put + geo::HALF_BYTES, src + (page_mask + 1) * geo::ROW);
+  };
+  auto plain_v = [&]() { copy_full(put, src + (page_mask + 1) * geo::ROW); };
+  auto next_put = [&]() {
+    ca_commit();
+    put = put + geo::SLOT_BYTES == ring + geo::WARP_BYTES ? ring : put + geo::SLOT_BYTES;
+  };
+  auto issue_plain = [&](bool first) {
+    if (first != V_FIRST) {
+      plain_k();
+    } else {
+      plain_v();
+    }
+    if (geo::WHOLE || first == V_FIRST) {            // the tile is complete: on to the next
+      ++is.t;
+      --is.left;
+    }
+    next_put();
+  };
   uint32_t take = ring;                              // slot of the next copy group to use
-  auto use_up = [&]() {                              // everything of the slot is in registers: refill it
+  auto use_up = [&](bool plain, bool first) {        // everything of the slot is in registers: refill it
     __syncwarp();
     take = take + geo::SLOT_BYTES == ring + geo::WARP_BYTES ? ring : take + geo::SLOT_BYTES;
-    issue();
+    if (plain) issue_plain(first);
+    else issue();
   };
   // ldmatrix addresses: K matrices (rows 0-7 | 8-15) x (chunk 2i | 2i+1), V matrices the same or with the two swapped
   const int r8 = lane & 7, m1 = (lane >> 3) & 1, m2 = lane >> 4;
@@ -391,7 +461,7 @@ __global__ void __launch_bounds__(CA_THREADS, (ca_geom<FMT, D, NT>::BLOCKS_PER_S
     const ca_span s = u.s;
     const int n_here = min(s.tiles - t0, u.left);                     // tiles of the unit in this run
     if (n_here <= 0) break;                                           // lengths changed under the call: stop
-    const int rt = sub / a.c.n_kv_heads, head = sub - rt * a.c.n_kv_heads;
+    const int rt = ca_row_tile(a, sub), head = sub - rt * a.c.n_kv_heads;
     const int r0 = rt * NT * 8;                                       // first row of the tile
 
     // query fragments: column n = g of column tile nt is row r0 + 8 nt + g
@@ -402,7 +472,7 @@ __global__ void __launch_bounds__(CA_THREADS, (ca_geom<FMT, D, NT>::BLOCKS_PER_S
     for (int nt = 0; nt < NT; ++nt) {
       const int row = r0 + nt * 8 + g;
       if (row < a.n_rows) {
-        const int tok = row / a.G;
+        const int tok = ca_token(a, row);
         const char* qr = a.q + ((long long)b * a.Tq + tok) * a.q_token_stride + (head * a.G + row - tok * a.G) * a.q_head_stride;
 #pragma unroll
         for (int ks = 0; ks < D / 16; ++ks) {
@@ -445,11 +515,11 @@ __global__ void __launch_bounds__(CA_THREADS, (ca_geom<FMT, D, NT>::BLOCKS_PER_S
       for (int c = 0; c < 2; ++c) {
         zs[nt][c] = a.scale_log2 * (FP8 ? __shfl_sync(0xffffffffu, back, (2 * t + c) * 4) : 1.f);
         const int r = r0 + nt * 8 + 2 * t + c;
-        pos[nt][c] = r < a.n_rows ? s.end - a.Tq + r / a.G : -1;
+        pos[nt][c] = r < a.n_rows ? s.end - a.Tq + ca_token(a, r) : -1;
       }
     }
-    const int pos_lo = s.end - a.Tq + r0 / a.G;                       // positions of the first and last row of the tile
-    const int pos_hi = s.end - a.Tq + (min(a.n_rows, r0 + NT * 8) - 1) / a.G;
+    const int pos_lo = s.end - a.Tq + ca_token(a, r0);                       // positions of the first and last row of the tile
+    const int pos_hi = s.end - a.Tq + ca_token(a, min(a.n_rows, r0 + NT * 8) - 1);
 
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt) {
@@ -459,7 +529,8 @@ __global__ void __launch_bounds__(CA_THREADS, (ca_geom<FMT, D, NT>::BLOCKS_PER_S
       sum[nt][0] = sum[nt][1] = 0.f;
     }
 
-    for (int i = 0; i < n_here; ++i) {
+    auto tile = [&](auto plain_, int i) {
+      constexpr bool plain = decltype(plain_)::value;                 // no mask, and the refills need no questions
       const int tok0 = (s.tile0 + t0 + i) << 4;
       // ---- scores
       float z[NT][4];
@@ -468,9 +539,6 @@ __global__ void __launch_bounds__(CA_THREADS, (ca_geom<FMT, D, NT>::BLOCKS_PER_S
       __syncwarp();
       {
         float z2[NT][4];                                              // two chains: the products of one depend on each other
-#pragma unroll
-        for (int nt = 0; nt < NT; ++nt)
-          z[nt][0] = z[nt][1] = z[nt][2] = z[nt][3] = z2[nt][0] = z2[nt][1] = z2[nt][2] = z2[nt][3] = 0.f;
         const uint32_t at = take + k_row;
         float by0 = 1.f, by1 = 1.f;                                   // key scales of tokens g, g + 8
         if (FP8) {
@@ -490,7 +558,10 @@ __global__ void __launch_bounds__(CA_THREADS, (ca_geom<FMT, D, NT>::BLOCKS_PER_S
               dd_e4m3x4_to_half(r[c][2 * w], a0, a2);
               dd_e4m3x4_to_half(r[c][2 * w + 1], a1, a3);
 #pragma unroll
-              for (int nt = 0; nt < NT; ++nt) ca_mma<FMT>(w ? z2[nt] : z[nt], a0, a1, a2, a3, qf[nt][4 * c + 2 * w], qf[nt][4 * c + 2 * w + 1]);
+              for (int nt = 0; nt < NT; ++nt) {
+                if (c == 0) ca_mma_first<FMT>(w ? z2[nt] : z[nt], a0, a1, a2, a3, qf[nt][2 * w], qf[nt][2 * w + 1]);
+                else ca_mma<FMT>(w ? z2[nt] : z[nt], a0, a1, a2, a3, qf[nt][4 * c + 2 * w], qf[nt][4 * c + 2 * w + 1]);
+              }
             }
           }
         } else {
@@ -502,8 +573,10 @@ __global__ void __launch_bounds__(CA_THREADS, (ca_geom<FMT, D, NT>::BLOCKS_PER_S
 #pragma unroll
             for (int c = 0; c < 4; ++c)
 #pragma unroll
-              for (int nt = 0; nt < NT; ++nt)
-                ca_mma<FMT>((c & 1) ? z2[nt] : z[nt], r[c][0], r[c][1], r[c][2], r[c][3], qf[nt][2 * (c4 + c)], qf[nt][2 * (c4 + c) + 1]);
+              for (int nt = 0; nt < NT; ++nt) {
+                if (c4 + c < 2) ca_mma_first<FMT>((c & 1) ? z2[nt] : z[nt], r[c][0], r[c][1], r[c][2], r[c][3], qf[nt][2 * c], qf[nt][2 * c + 1]);
+                else ca_mma<FMT>((c & 1) ? z2[nt] : z[nt], r[c][0], r[c][1], r[c][2], r[c][3], qf[nt][2 * (c4 + c)], qf[nt][2 * (c4 + c) + 1]);
+              }
           }
         }
 #pragma unroll
@@ -511,7 +584,7 @@ __global__ void __launch_bounds__(CA_THREADS, (ca_geom<FMT, D, NT>::BLOCKS_PER_S
 #pragma unroll
           for (int e = 0; e < 4; ++e) z[nt][e] = (z[nt][e] + z2[nt][e]) * (FP8 ? zs[nt][e & 1] * (e < 2 ? by0 : by1) : zs[nt][e & 1]);
       }
-      if (!geo::WHOLE) use_up();
+      if (!geo::WHOLE) use_up(plain, true);
       // whole tiles: V is there already, its first registers come in behind the soft-max
       constexpr int V_LOADS = D / (FP8 ? 32 : 16), V_BATCH = V_LOADS < 4 ? V_LOADS : 4;
       uint32_t raw[V_BATCH][4];
@@ -523,7 +596,7 @@ __global__ void __launch_bounds__(CA_THREADS, (ca_geom<FMT, D, NT>::BLOCKS_PER_S
       if (geo::WHOLE) load_values(0);
 
       // ---- masks: z[.][0..1] is token tok0 + g, z[.][2..3] token tok0 + g + 8
-      const bool partial = tok0 + 15 > pos_lo || (a.window > 0 && tok0 <= pos_hi - a.window);
+      const bool partial = !plain && (tok0 + 15 > pos_lo || (a.window > 0 && tok0 <= pos_hi - a.window));
       if (partial) {
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt)
@@ -645,7 +718,23 @@ __global__ void __launch_bounds__(CA_THREADS, (ca_geom<FMT, D, NT>::BLOCKS_PER_S
           }
         }
       }
-      use_up();
+      use_up(plain, geo::WHOLE);
+    };
+    for (int i = 0; i < n_here;) {
+      // how many tiles from here are plain on both sides: seen by every row of the tile, and refilled from complete tiles of
+      // this lookup, the last of them left to the careful form
+      int n = 0;
+      if (geo::PLAIN_LOOP && is.left > 1) {
+        n = min(min(is.left, blocks_from + 32 - is.t), ((is.s.end - 16) >> 4) - is.s.tile0 - is.t + 1) - 1;
+        n = min(n, min(n_here - i, ((pos_lo - 15) >> 4) - (s.tile0 + t0 + i) + 1));
+        if (a.window > 0 && (((s.tile0 + t0 + i) << 4) <= pos_hi - a.window || ((is.s.tile0 + is.t) << 4) < is.s.first)) n = 0;
+        if (!all_good()) n = 0;
+      }
+      if constexpr (geo::PLAIN_LOOP) {
+#pragma unroll 1
+        for (; n > 0; --n, ++i) tile(std::true_type(), i);
+      }
+      if (i < n_here) tile(std::false_type(), i++);
     }
 
     // ---- the end of the unit, or of the run
@@ -665,10 +754,10 @@ __global__ void __launch_bounds__(CA_THREADS, (ca_geom<FMT, D, NT>::BLOCKS_PER_S
         for (int c = 0; c < 2; ++c) {
           const int r = r0 + nt * 8 + 2 * t + c;
           if (r < a.n_rows) {
-            const int tok = r / a.G, h = head * a.G + r - tok * a.G;
+            const int tok = ca_token(a, r), h = head * a.G + r - tok * a.G;
             const long long tn = (long long)b * a.Tq + tok;
             const bool empty = pos[nt][c] < 0;
-            const float inv = empty ? 0.f : 1.f / sum[nt][c];
+            const float inv = empty ? 0.f : __frcp_rn(sum[nt][c]);
             char* o = a.out + tn * a.out_token_stride + h * a.out_head_stride;
 #pragma unroll
             for (int m = 0; m < D / 16; ++m) ca_store<FP8>(o, g, m, empty ? 0u : dd_pack2<TQ>(acc[nt][m][c] * inv, acc[nt][m][2 + c] * inv));
@@ -844,7 +933,7 @@ __global__ void __launch_bounds__(64 * CJ_GROUPS) dd_cache_attn_join_kernel(cons
       const int rt = sub / a.c.n_kv_heads, head = sub - rt * a.c.n_kv_heads;
       const int r = rt * NT * 8 + nt * 8 + col + c;
       if (r < a.n_rows) {
-        const int tok = r / a.G, h = head * a.G + r - tok * a.G;
+        const int tok = ca_token(a, r), h = head * a.G + r - tok * a.G;
         const long long tn = (long long)b * a.Tq + tok;
         const bool empty = end - a.Tq + tok < 0;
         const float2 ml = sh_ml[col + c];
@@ -937,6 +1026,7 @@ extern "C" int dd_cache_decode_attn(const dd_cache* cache, int n_q_tokens, const
   ca_args a = {};
   a.G = q->n_heads / cache->n_kv_heads;
   a.n_rows = n_q_tokens * a.G;
+  a.by_G = (uint32_t)((0x80000000ull + a.G - 1) / a.G);
   const ca_sizes z = ca_size(cache->head_dim, a.n_rows, sms);
   if (workspace_bytes < z.total())
     return dd_fail(nullptr, DD_ERR_INVALID_ARG, "%s: workspace holds %zu bytes, %zu needed", who, workspace_bytes, z.total());
