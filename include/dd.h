@@ -416,7 +416,7 @@ int dd_cache_read(const dd_cache* cache, const int* idx, int k_pages, void* out,
  * the pages behind ctx_len is never used, whatever its bits. Any number of query heads per KV head, any ctx_len up to
  * max_pages * page_tokens (more is reported in status and cut; a negative one counts as 0); a table entry out of range is
  * reported and its page reads as zeros. Only entries of pages that hold a visible token are read.
- *   q, out     dev [batch * n_q_tokens][n_q_heads][head_dim], one dtype (that of a 16-bit cache)
+ *   q, out     dev [batch * n_q_tokens][n_q_heads][head_dim], one dtype (that of a 16-bit cache); out may be q itself
  *   ctx_len    dev int32 [batch]
  *   out_lse    dev fp32 [batch * n_q_tokens][n_q_heads] or NULL
  *   workspace  dev, dd_cache_decode_attn_workspace() bytes, 16-byte aligned, contents irrelevant. Calls that may run at

@@ -399,6 +399,8 @@ class PagedCache:
         b, shape = self._batch, q.shape
         if len(shape) != 4 or shape[0] != b or out.shape != shape:
             raise _invalid(f"q and out must be [{b}, tokens, heads, {self.head_dim}], not {tuple(shape)} and {tuple(out.shape)}")
+        if not 0 <= window < 1 << 31:
+            raise _invalid(f"window must be in [0, 2^31), not {window}")
         Tq, Hq = shape[1], shape[2]
         rq, ro = _rows4(q, "q", self.head_dim), _rows4(out, "out", self.head_dim)
         if out_lse is not None and (out_lse.dtype is not torch.float32 or out_lse.shape != (b, Tq, Hq) or not out_lse.is_contiguous()):

@@ -99,6 +99,13 @@ int dd_check_cache_memory(const dd_cache* c, const char* who, int device, bool a
   return DD_OK;
 }
 
+int dd_launch(const char* who, const cudaLaunchConfig_t* cfg, const void* kernel, void** args) {
+  const cudaError_t e = cudaLaunchKernelExC(cfg, kernel, args);
+  if (e == cudaSuccess) return DD_OK;
+  cudaGetLastError();
+  return dd_fail(nullptr, DD_ERR_CUDA, "%s: launch: %s", who, cudaGetErrorString(e));
+}
+
 dd_cache_view dd_make_view(const dd_cache* c, const char* data_dev) {
   dd_cache_view v;
   v.data = const_cast<char*>(data_dev);
@@ -252,7 +259,6 @@ extern "C" int dd_cache_read(const dd_cache* cache, const int* idx, int k_pages,
   cfg.attrs = &at;
   cfg.numAttrs = 1;
   void* args[] = {&v, &idx, &out, &k_pages, &n_tiles};
-  DD_CUDA_TRY(nullptr, cudaLaunchKernelExC(&cfg, cache->head_dim == 128 ? cr_kernel_of<128>(cache->format, out_dtype, on_host)
-                                                                        : cr_kernel_of<64>(cache->format, out_dtype, on_host), args));
-  return DD_OK;
+  return dd_launch(who, &cfg, cache->head_dim == 128 ? cr_kernel_of<128>(cache->format, out_dtype, on_host)
+                                                     : cr_kernel_of<64>(cache->format, out_dtype, on_host), args);
 }

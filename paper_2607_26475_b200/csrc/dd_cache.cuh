@@ -31,6 +31,8 @@ struct dd_cache_view {
   int page_shift;                        // log2 of the tokens per page
 };
 dd_cache_view dd_make_view(const dd_cache* c, const char* data_dev);
+// A launch whose failure is reported here and left behind nowhere (the runtime's last error is cleared).
+int dd_launch(const char* who, const cudaLaunchConfig_t* cfg, const void* kernel, void** args);
 
 static inline int dd_log2i(int x) { int s = 0; while ((1 << s) < x) ++s; return s; }
 

@@ -44,6 +44,7 @@ constexpr int CA_WARPS = 8;
 constexpr int CA_THREADS = CA_WARPS * 32;
 constexpr int CA_UNIT_COST = 3;              // empty places behind a unit in the flat list
 constexpr int CA_WHOLE = 8;                  // a unit of at most so many tiles is not cut: it belongs to the run it begins in
+constexpr int CA_MAX_CLUSTER = 8;
 constexpr float CA_HEADROOM = 6.f;           // log2 of the factor on P
 constexpr float CA_LAZY = 8.f;               // how far (log2) a weight may exceed the reference
 constexpr float CA_NONE = -3.0e38f;          // reference before any token: every finite score exceeds it
@@ -67,13 +68,18 @@ struct ca_geom {
   static constexpr int SLOT_BYTES = (WHOLE ? 2 : 1) * HALF_BYTES + (FP8 ? 32 : 0);
   static constexpr int COPIES = HALF_BYTES / 512;
   static constexpr int BLOCKS_PER_SM = NT == 1 ? 2 : 1;               // two column tiles need the registers of a whole SM
-  static constexpr int RING_BUDGET = (BLOCKS_PER_SM == 2 ? 110 : 220) * 1024;
+  static constexpr int RING_BUDGET = (BLOCKS_PER_SM == 2 ? 106 : 212) * 1024;
   static constexpr int STAGES_ = RING_BUDGET / (CA_WARPS * SLOT_BYTES);
   static constexpr int STAGES = STAGES_ > 8 ? 8 : STAGES_;
   // A second copy of the tile's code without masks and questions. Where registers are scarce (one column tile, head_dim 128) its
   // spills cost what it saves (8 x 32K tokens e4m3 104 -> 106 us); elsewhere 131 -> 111 us (128 query heads), 63 -> 59 (head_dim 64).
   static constexpr bool PLAIN_LOOP = NT == 2 || D == 64;
   static constexpr int WARP_BYTES = STAGES * SLOT_BYTES;
+  static constexpr int QUADS = NT * (D / 16) * 32;                    // groups of four accumulators: [column tile][product][lane]
+  // behind the rings, for clusters: what a block receives of its slice of the quads, and every block's references and sums
+  static constexpr int RECV_AT = CA_WARPS * WARP_BYTES;
+  static constexpr int RECV_ML_AT = RECV_AT + QUADS * 16;
+  static constexpr int SMEM_CLUSTER = RECV_ML_AT + CA_MAX_CLUSTER * NT * 8 * 8;
   static constexpr int SMEM = CA_WARPS * WARP_BYTES;
   static constexpr int NACC = D / 4;                                  // accumulator registers per column tile
   static_assert(WARP_BYTES >= NT * NACC * 128, "a warp's ring holds its accumulators at the end");
@@ -96,6 +102,7 @@ struct ca_args {
   float2* part_ml;     // [2 * warps][NT * 8]
   int4* desc;          // [warps]: (request, sub, last run + 1) of the cut unit that begins in a warp's run, or 0
   int n_q_heads, G, Tq, n_rows, row_tiles, window;
+  int cluster;         // blocks of a cluster that share one unit, 0 = the flat list
   uint32_t by_G;       // ceil(2^31 / G): row / G by a multiplication
   float scale_log2;
 };
@@ -253,6 +260,7 @@ __global__ void __launch_bounds__(CA_THREADS, (ca_geom<FMT, D, NT>::BLOCKS_PER_S
   extern __shared__ __align__(128) unsigned char ca_smem[];
   __shared__ float2 sh_ml[CA_WARPS][NT * 8];
   __shared__ float sh_scale[CA_WARPS][NT * 8];
+  __shared__ float2 sh_blk[NT * 8];                  // clusters: the block's references and sums
   __shared__ int2 sh_piece[CA_WARPS];                // (request, sub) of the unit a run ends inside, or -1
 
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -265,9 +273,21 @@ __global__ void __launch_bounds__(CA_THREADS, (ca_geom<FMT, D, NT>::BLOCKS_PER_S
   // the joining kernel's blocks may take the places that this grid's blocks leave (each waits for all of them)
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
 
-  // ---- this warp's run of the flat list: every warp adds up the list by itself, 32 requests at a time
   ca_cursor is;
   is.b = is.sub = is.t = is.left = 0;
+  long long share = 1;
+  if (a.cluster) {
+    // ---- one unit per cluster, cut evenly among its warps
+    asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");   // waited for before the first write into a peer
+    const int unit = blockIdx.x / a.cluster, w = blockIdx.x % a.cluster * CA_WARPS + warp;
+    is.b = unit / subs;
+    is.sub = unit - is.b * subs;
+    is.s = ca_span_of(a, is.b, is.sub == 0 && w == 0);
+    const int each = (is.s.tiles + a.cluster * CA_WARPS - 1) / (a.cluster * CA_WARPS);
+    is.t = each * w;
+    is.left = max(0, min(each, is.s.tiles - is.t));
+  } else {
+  // ---- this warp's run of the flat list: every warp adds up the list by itself, 32 requests at a time
   is.s = ca_span_of(a, min(lane, B - 1), blockIdx.x == 0 && warp == 0 && lane < B);
   auto places = [&](const ca_span& sp) -> long long { return sp.tiles > 0 ? (long long)(sp.tiles + CA_UNIT_COST) * subs : 0; };
   const long long cost0 = lane < B ? places(is.s) : 0;               // of the first 32 requests
@@ -275,7 +295,7 @@ __global__ void __launch_bounds__(CA_THREADS, (ca_geom<FMT, D, NT>::BLOCKS_PER_S
   for (int b = lane + 32; b < B; b += 32) total += places(ca_span_of(a, b, blockIdx.x == 0 && warp == 0));
 #pragma unroll
   for (int o = 16; o; o >>= 1) total += __shfl_xor_sync(0xffffffffu, total, o);
-  const long long share = max(1LL, ca_div(total + (long long)gridDim.x * CA_WARPS - 1, (int)gridDim.x * CA_WARPS));
+  share = max(1LL, ca_div(total + (long long)gridDim.x * CA_WARPS - 1, (int)gridDim.x * CA_WARPS));
   const long long f0 = share * me;
   if (f0 < total) {
     long long at = 0;                                                 // first place of the 32 requests looked at
@@ -316,6 +336,7 @@ __global__ void __launch_bounds__(CA_THREADS, (ca_geom<FMT, D, NT>::BLOCKS_PER_S
       is.left -= is.s.tiles + CA_UNIT_COST - is.t;
       if (is.left > 0) ca_next_unit(a, is, subs);
     }
+  }
   }
 
   // ---- the issuing side
@@ -747,6 +768,7 @@ __global__ void __launch_bounds__(CA_THREADS, (ca_geom<FMT, D, NT>::BLOCKS_PER_S
         sum[nt][c] += __shfl_xor_sync(0xffffffffu, sum[nt][c], 16);
       }
     const bool ends = t0 + n_here == s.tiles;
+    if (a.cluster) break;                                             // one piece a warp
     if (ends && t0 == 0) {
 #pragma unroll
       for (int nt = 0; nt < NT; ++nt)
@@ -784,12 +806,22 @@ __global__ void __launch_bounds__(CA_THREADS, (ca_geom<FMT, D, NT>::BLOCKS_PER_S
     u.left -= n_here + CA_UNIT_COST;
     if (u.left > 0) ca_next_unit(a, u, subs);
   }
-  if (lane == 0) a.desc[me] = desc;
+  if (lane == 0 && !a.cluster) a.desc[me] = desc;
   ca_wait<0>();
   __syncwarp();
 
   // ---- pieces left over at the ends of the runs: neighbouring warps inside the same unit become one partial, in slot
   // 2 w + 1 of the first of them
+  if (a.cluster && u.left <= 0) {                    // a warp without a tile
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt) {
+#pragma unroll
+      for (int m = 0; m < D / 16; ++m) acc[nt][m][0] = acc[nt][m][1] = acc[nt][m][2] = acc[nt][m][3] = 0.f;
+      from[nt][0] = from[nt][1] = CA_NONE;
+      sum[nt][0] = sum[nt][1] = 0.f;
+    }
+  }
+  if (a.cluster) inside = make_int2(0, 0);           // all of one unit
   if (lane == 0) sh_piece[warp] = inside;
   if (inside.x >= 0) {
     float4* own = reinterpret_cast<float4*>(ca_smem + warp * geo::WARP_BYTES);
@@ -831,10 +863,70 @@ __global__ void __launch_bounds__(CA_THREADS, (ca_geom<FMT, D, NT>::BLOCKS_PER_S
     for (int v = w0; v < w1; ++v) M = fmaxf(M, sh_ml[v][row].x);
     for (int v = w0; v < w1; ++v) L = fmaf(sh_ml[v][row].y, ca_exp2(sh_ml[v][row].x - M), L);
     sh_scale[w][row] = ca_exp2(sh_ml[w][row].x - M);
-    if (w == w0) a.part_ml[(2LL * (blockIdx.x * CA_WARPS + w0) + 1) * NT * 8 + row] = make_float2(M, L);
+    if (w == w0 && a.cluster) sh_blk[row] = make_float2(M, L);
+    else if (w == w0) a.part_ml[(2LL * (blockIdx.x * CA_WARPS + w0) + 1) * NT * 8 + row] = make_float2(M, L);
   }
   __syncthreads();
-  constexpr int QUADS = NT * (D / 16) * 32;          // groups of four accumulators: [column tile][product][lane]
+  constexpr int QUADS = geo::QUADS;
+  if (a.cluster) {
+    // ---- the blocks of a cluster: block r owns a slice of the quads; every block sends it its part of them (remote stores, nobody
+    // waits for an answer), one barrier makes them visible, and every block adds and writes its slice
+    const int C = a.cluster, slice = QUADS / C, rank = blockIdx.x % C;
+    asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+    const uint32_t recv = (uint32_t)__cvta_generic_to_shared(ca_smem) + geo::RECV_AT, recv_ml = (uint32_t)__cvta_generic_to_shared(ca_smem) + geo::RECV_ML_AT;
+    for (int e = threadIdx.x; e < QUADS; e += CA_THREADS) {
+      const int row = e / (D / 16 * 32) * 8 + 2 * (e & 3);
+      float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+      for (int w = 0; w < CA_WARPS; ++w)
+        ca_add(x, reinterpret_cast<const float4*>(ca_smem + w * geo::WARP_BYTES)[e], sh_scale[w][row], sh_scale[w][row + 1]);
+      uint32_t to;
+      asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(to) : "r"(recv + (rank * slice + e % slice) * 16), "r"(e / slice));
+      asm volatile("st.shared::cluster.v4.f32 [%0], {%1, %2, %3, %4};" ::"r"(to), "f"(x.x), "f"(x.y), "f"(x.z), "f"(x.w) : "memory");
+    }
+    for (int i = threadIdx.x; i < C * NT * 8; i += CA_THREADS) {
+      const float2 ml = sh_blk[i % (NT * 8)];
+      uint32_t to;
+      asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(to) : "r"(recv_ml + (rank * NT * 8 + i % (NT * 8)) * 8), "r"(i / (NT * 8)));
+      asm volatile("st.shared::cluster.v2.f32 [%0], {%1, %2};" ::"r"(to), "f"(ml.x), "f"(ml.y) : "memory");
+    }
+    asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
+    asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+    const float4* in = reinterpret_cast<const float4*>(ca_smem + geo::RECV_AT);
+    const float2* in_ml = reinterpret_cast<const float2*>(ca_smem + geo::RECV_ML_AT);
+    for (int i = threadIdx.x; i < slice; i += CA_THREADS) {
+      const int e = rank * slice + i, row = e / (D / 16 * 32) * 8 + 2 * (e & 3);
+      float M[2] = {CA_NONE, CA_NONE}, L[2] = {0.f, 0.f};
+      for (int k = 0; k < C; ++k) {
+        M[0] = fmaxf(M[0], in_ml[k * NT * 8 + row].x);
+        M[1] = fmaxf(M[1], in_ml[k * NT * 8 + row + 1].x);
+      }
+      float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
+      for (int k = 0; k < C; ++k) {
+        const float2 m0 = in_ml[k * NT * 8 + row], m1 = in_ml[k * NT * 8 + row + 1];
+        const float s0 = ca_exp2(m0.x - M[0]), s1 = ca_exp2(m1.x - M[1]);
+        L[0] = fmaf(m0.y, s0, L[0]);
+        L[1] = fmaf(m1.y, s1, L[1]);
+        ca_add(x, in[k * slice + i], s0, s1);
+      }
+      const int unit = blockIdx.x / C, b = unit / subs, sub = unit - b * subs;
+      const int rt = ca_row_tile(a, sub), head = sub - rt * a.c.n_kv_heads, m = (e / 32) % (D / 16), ge = (e & 31) >> 2;
+      const ca_span s = ca_span_of(a, b, false);
+#pragma unroll
+      for (int c = 0; c < 2; ++c) {
+        const int r = rt * NT * 8 + row + c;
+        if (r < a.n_rows && s.tiles > 0) {           // (a request without a token has been written above)
+          const int tok = ca_token(a, r), h = head * a.G + r - tok * a.G;
+          const long long tn = (long long)b * a.Tq + tok;
+          const bool empty = s.end - a.Tq + tok < 0;
+          const float lo = c ? x.y : x.x, hi = c ? x.w : x.z;
+          ca_store<FP8>(a.out + tn * a.out_token_stride + h * a.out_head_stride, ge, m, empty ? 0u : dd_pack2<TQ>(lo / L[c], hi / L[c]));
+          if (a.lse && m == 0 && ge == 0) a.lse[tn * a.n_q_heads + h] = empty ? -INFINITY : ca_lse(M[c], L[c]);
+        }
+      }
+    }
+    return;
+  }
   for (int w0 = 0, w1; w0 < CA_WARPS; w0 = w1) {
     w1 = w0 + 1;
     if (sh_piece[w0].x < 0) continue;
@@ -948,13 +1040,13 @@ __global__ void __launch_bounds__(64 * CJ_GROUPS) dd_cache_attn_join_kernel(cons
 struct ca_plan {
   const void* main_kernel;
   const void* join_kernel;
-  int smem, blocks_per_sm;
+  int smem, smem_cluster, blocks_per_sm;
 };
 template <int FMT, int D, int NT> ca_plan ca_plan_of() {
   using geo = ca_geom<FMT, D, NT>;
-  static_assert(geo::SMEM <= 227 * 1024, "shared memory of a block");
-  static_assert(geo::BLOCKS_PER_SM == 1 || geo::SMEM + 1024 + 2048 <= 114 * 1024, "shared memory of two blocks");
-  return {(const void*)dd_cache_attn_kernel<FMT, D, NT>, (const void*)dd_cache_attn_join_kernel<FMT, D, NT>, geo::SMEM, geo::BLOCKS_PER_SM};
+  static_assert(geo::SMEM_CLUSTER + 2048 <= 227 * 1024, "shared memory of a block");
+  static_assert(geo::BLOCKS_PER_SM == 1 || geo::SMEM_CLUSTER + 1024 + 2048 <= 114 * 1024, "shared memory of two blocks");
+  return {(const void*)dd_cache_attn_kernel<FMT, D, NT>, (const void*)dd_cache_attn_join_kernel<FMT, D, NT>, geo::SMEM, geo::SMEM_CLUSTER, geo::BLOCKS_PER_SM};
 }
 template <int FMT> ca_plan ca_pick(int d, int nt) {
   if (d == 128) return nt == 1 ? ca_plan_of<FMT, 128, 1>() : ca_plan_of<FMT, 128, 2>();
@@ -968,6 +1060,17 @@ int ca_sm_count() {
     return 148;
   }
   return sms;
+}
+
+// Blocks of a cluster per unit, 0 for the flat list. Few and short units (known from the table's width, not from the lengths,
+// which are on the device): a cluster per unit joins its pieces through distributed shared memory and needs no second
+// kernel and no look at the other requests. At most 8 tiles a warp, and all clusters resident at once; units that fit one warp's
+// run uncut are left to the flat list. One request, 8 KV heads: 2048 tokens 11.5 -> 8.5 us, 4096 13.1 -> 10.4, 8192 14.6 -> 13.8.
+int ca_cluster_of(long long units, long long tiles, int blocks) {
+  if (tiles <= CA_WHOLE) return 0;
+  int c = 2;
+  while (c < CA_MAX_CLUSTER && tiles > 2LL * c * CA_WARPS) c *= 2;
+  return tiles <= 8LL * c * CA_WARPS && units * c <= blocks * 7 / 8 ? c : 0;
 }
 
 // Rows of a unit that go through the MMA together: up to 8 in one column tile, up to 16 in two.
@@ -1056,22 +1159,34 @@ extern "C" int dd_cache_decode_attn(const dd_cache* cache, int n_q_tokens, const
     default: p = ca_pick<3>(cache->head_dim, nt); break;
   }
   const int blocks = sms * p.blocks_per_sm;
-  DD_CUDA_TRY(nullptr, cudaFuncSetAttribute(p.main_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, p.smem));
+  const long long units = (long long)cache->batch * a.row_tiles * cache->n_kv_heads;
+  long long tiles = ((long long)cache->max_pages * cache->page_tokens + 15) / 16;
+  if (window > 0 && ((long long)window + n_q_tokens + 29) / 16 < tiles) tiles = ((long long)window + n_q_tokens + 29) / 16;
+  a.cluster = ca_cluster_of(units, tiles, blocks);
+  DD_CUDA_TRY(nullptr, cudaFuncSetAttribute(p.main_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, p.smem_cluster));
   cudaLaunchConfig_t cfg = {};
-  cudaLaunchAttribute at;
-  dd_pdl_attr(&at);
-  cfg.attrs = &at;
+  cudaLaunchAttribute at[2];
+  dd_pdl_attr(&at[0]);
+  cfg.attrs = at;
   cfg.numAttrs = 1;
   cfg.stream = (cudaStream_t)stream;
-  cfg.gridDim = dim3((unsigned)blocks);
   cfg.blockDim = dim3(CA_THREADS);
-  cfg.dynamicSmemBytes = p.smem;
   void* args[] = {&a};
-  DD_CUDA_TRY(nullptr, cudaLaunchKernelExC(&cfg, p.main_kernel, args));
+  if (a.cluster) {
+    at[1].id = cudaLaunchAttributeClusterDimension;
+    at[1].val.clusterDim.x = (unsigned)a.cluster;
+    at[1].val.clusterDim.y = at[1].val.clusterDim.z = 1;
+    cfg.numAttrs = 2;
+    cfg.gridDim = dim3((unsigned)(units * a.cluster));
+    cfg.dynamicSmemBytes = p.smem_cluster;
+    return dd_launch(who, &cfg, p.main_kernel, args);
+  }
+  cfg.gridDim = dim3((unsigned)blocks);
+  cfg.dynamicSmemBytes = p.smem;
+  DD_TRY(dd_launch(who, &cfg, p.main_kernel, args));
   if ((long long)cache->max_pages * cache->page_tokens <= 16 * CA_WHOLE) return DD_OK;   // no unit can have been cut
   cfg.gridDim = dim3((unsigned)blocks, (unsigned)(nt * (cache->head_dim / 16) * 32 / 64));
   cfg.blockDim = dim3(64 * CJ_GROUPS);
   cfg.dynamicSmemBytes = (size_t)(blocks + 1) * 8 * sizeof(float);     // at most one partial per block and the last piece
-  DD_CUDA_TRY(nullptr, cudaLaunchKernelExC(&cfg, p.join_kernel, args));
-  return DD_OK;
+  return dd_launch(who, &cfg, p.join_kernel, args);
 }

@@ -261,8 +261,7 @@ int rp_launch(rp_args& a, int head_dim, int dtype, int fmt, cudaStream_t st, con
   cfg.attrs = &at;
   cfg.numAttrs = 1;
   void* args[] = {&a};
-  DD_CUDA_TRY(nullptr, cudaLaunchKernelExC(&cfg, f, args));
-  return DD_OK;
+  return dd_launch(who, &cfg, f, args);
 }
 
 rp_rows rp_of(const dd_rows* r) {

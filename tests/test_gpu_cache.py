@@ -210,7 +210,7 @@ def test_append_turns_keys_and_queries_on_the_way(dd, fmt, kind, d, rot, layout)
 
 
 @pytest.mark.parametrize("fmt,out,T,d,H,k,pinned", [
-    ("e4m3", "bf16", 16, 128, 8, 7, False), ("e4m3", "fp16", 64, 64, 2, 3, False), ("bf16", "bf16", 16, 128, 2, 5, True), ("e4m3", "bf16", 16, 128, 4, 60, True),
+    ("e4m3", "bf16", 16, 128, 8, 7, False), ("e4m3", "fp16", 64, 64, 2, 3, False), ("bf16", "bf16", 16, 128, 2, 5, True), ("e4m3", "bf16", 16, 128, 4, 60, True), ("e4m3", "fp16", 32, 64, 3, 9, True), ("e4m3", "bf16", 64, 128, 1, 4, True),
     ("fp16", "fp16", 32, 64, 1, 1, False), ("bf16", "bf16", 256, 128, 1, 2, False), ("e4m3", "fp16", 128, 128, 1, 9, False)])
 def test_read_brings_back_what_the_pages_stand_for(dd, fmt, out, T, d, H, k, pinned):
     gen = torch.Generator().manual_seed(T * d + k)
@@ -625,3 +625,63 @@ def test_a_layer_of_the_store_seen_as_a_cache(dd):
     table = cache.block_table.cpu()
     flat = np.stack([raw[:, 0][h * P + np.arange((B - 1) * H * P + P)] for h in range(H)], 1)     # [block, head, bytes]
     check_attn(full, None, q, flat, table, lens.tolist(), "bf16", "bf16", T)
+
+
+def test_offsets_beyond_32_bits(dd):
+    """Pages at the far end of a pool of 4.8 GB: written, attended to and read back."""
+    gen = torch.Generator().manual_seed(15)
+    n, T, d, H, G = 580000, 16, 128, 2, 4
+    pool = torch.empty(n, H, 4128, dtype=torch.uint8, device="cuda")
+    assert pool.numel() > 1 << 32
+    far = torch.tensor([[n - 1, n - 5, n - 3, n - 2], [0, n - 4, 1, 2]], dtype=torch.int32)
+    wide = torch.full((2, 9), -1, dtype=torch.int32)               # a table with rows longer than the cache's
+    wide[:, :4] = far
+    cache = dd.PagedCache(pool, wide.cuda()[:, :4], cache_format=dd.DD_CACHE_E4M3)
+    k, v = (torch.randn(2 * 64, H, d, generator=gen).to(torch.bfloat16).cuda() for _ in range(2))
+    cache.append(k, v, torch.arange(64, dtype=torch.int32).repeat(2).cuda())
+    q = torch.randn(2, 1, H * G, d, generator=gen).to(torch.bfloat16).cuda()
+    out, lse = run_attn(cache, q, [64, 49])
+    used = far.flatten().long()
+    raw = pool[used.cuda()].cpu().numpy()
+    table = torch.arange(8).view(2, 4)
+    for i in range(8):
+        want = torch.stack([k.view(2, 4, T, H, d)[i // 4, i % 4], v.view(2, 4, T, H, d)[i // 4, i % 4]], 0)     # [2, T, H, d]
+        for h in range(H):
+            assert np.array_equal(raw[i, h], ref.encode_pages(f64(want[:, :, h]), "e4m3"))
+    check_attn(out, lse, q, raw, table, [64, 49], "e4m3", "bf16", T)
+    idx = torch.arange(4, dtype=torch.int32).expand(2, H, 4).contiguous().cuda()
+    back = torch.empty(2, H, 2, 64, d, dtype=torch.bfloat16, device="cuda")
+    cache.read(idx, back)
+    want = ref.decode_pages(raw.reshape(2, 4, H, 4128), "e4m3", T, d).transpose(0, 2, 3, 1, 4, 5).reshape(2, H, 2, 64, d)
+    assert np.array_equal(f64(back), want)
+    assert cache.device_error() == (0, 0)
+
+
+def test_output_in_place_of_the_queries(dd):
+    """Every row of the queries is read before its place is written, whichever way the work is split."""
+    gen = torch.Generator().manual_seed(16)
+    for lens, H, G in (([4000, 17, 0], 2, 4), ([100, 90], 1, 8), ([3000] * 12, 8, 4)):
+        cache, raw, table, q = make_attn(dd, gen, lens, H, G, 128, 16, "bf16", "bf16", 1)
+        l = torch.tensor(lens, dtype=torch.int32).cuda()
+        out = torch.empty_like(q)
+        cache.decode_attn(q, l, out)
+        same = q.clone()
+        cache.decode_attn(same, l, same)
+        assert torch.equal(out, same)
+
+
+def test_every_way_to_split_the_work_gives_the_definition(dd):
+    """Table widths on both sides of each rule: one warp a unit, clusters of 2, 4 and 8 blocks, the flat list; few units and many;
+    lengths below what the table could hold."""
+    gen = torch.Generator().manual_seed(17)
+    for lens, H, G, Tq, fmt in (([128], 1, 4, 1, "bf16"), ([129, 3], 1, 4, 2, "bf16"), ([512], 2, 3, 1, "e4m3"), ([513, 5], 1, 16, 1, "bf16"), ([1025], 4, 8, 1, "e4m3"),
+                                ([4096, 0, 33], 1, 2, 3, "bf16"), ([8192], 1, 4, 1, "e4m3"), ([8193], 1, 4, 1, "e4m3"), ([700] * 40, 2, 4, 1, "bf16"),
+                                ([2000] * 9, 2, 24, 1, "e4m3")):
+        cache, raw, table, q = make_attn(dd, gen, lens, H, G, 128, 16, fmt, "bf16", Tq)
+        out, lse = run_attn(cache, q, lens)
+        check_attn(out, lse, q, raw, table, lens, fmt, "bf16", 16)
+        short = [max(0, n - 300) for n in lens]
+        out, lse = run_attn(cache, q, short)
+        keep = raw.copy()
+        check_attn(out, lse, q, keep, table, short, fmt, "bf16", 16)
+        assert cache.device_error() == (0, 0)
