@@ -22,8 +22,9 @@
  *     be stream-ordered with respect to each other (the pipelined path does this itself).
  *   - tensors are dense, row-major in the index order written; bf16 tensors 16-byte aligned,
  *     int32 and fp32 arrays 4-byte aligned.
- *   - geometry supported by the kernels: head_dim 128, page_tokens 16,
+ *   - geometry supported by the kernels of the method: head_dim 128, page_tokens 16,
  *     n_q_tokens * (n_q_heads / n_kv_heads) <= 8. Anything else is DD_ERR_INVALID_ARG.
+ *     (The calls on a paged cache at the end of this file need no context and have limits of their own.)
  *
  * Notation: B requests, L layers, Hq query heads, Hkv KV heads, G = Hq/Hkv, d = head_dim,
  * T = page_tokens, P = max_pages, k = k_pages, Tq = n_q_tokens (token 0 = current output

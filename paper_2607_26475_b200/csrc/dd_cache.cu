@@ -130,7 +130,8 @@ dd_cache_view dd_make_view(const dd_cache* c, const char* data_dev) {
 // 16-bit rows. A lane takes as many elements per load as it writes in one 16-byte store, so that every load and store of a
 // warp covers one contiguous piece: 8-byte loads for e4m3 (16-byte loads left two half-used stores: 44 against 33 us for
 // 32768 pages). Bound: HBM, or the host link for a page-locked pool. The exponents of a tile are 16 bytes for K and 16 for V:
-// one byte per lane in one load, handed out by shuffles.
+// one byte per lane in one load, handed out by shuffles. Measured on a B200: 8192 e4m3 pages of 16 x 128 15.3 us (6.6 TB/s of
+// reads and writes, inputs partly in L2); 4096 pages from page-locked memory 339 us (51 GB/s, what kernel reads get there).
 constexpr int CR_THREADS = 256;
 
 //

@@ -34,6 +34,10 @@
 // timing. Its blocks are launched early and wait for the first kernel's end. (Letting the last block of a unit to arrive do
 // it, by a counter or by flags, took 4 to 7 us more: fences and contended words cost more round trips than a launch that
 // is already there.)
+//
+// Measured on a B200 (device time of a call, 32 query and 8 KV heads of 128): 8 requests of 32768 tokens bf16 166 us (6.45 TB/s, a
+// copy's rate), e4m3 104 us (5.2 TB/s; twice the instructions per byte, and four warps a scheduler do not cover their latencies),
+// one request of 1M tokens e4m3 372 us (5.8 TB/s), 48 requests of 0 to 32768 tokens e4m3 79 us, one request of 4096 tokens 10.4 us.
 #include <type_traits>
 
 #include "dd_cache.cuh"
@@ -287,56 +291,56 @@ __global__ void __launch_bounds__(CA_THREADS, (ca_geom<FMT, D, NT>::BLOCKS_PER_S
     is.t = each * w;
     is.left = max(0, min(each, is.s.tiles - is.t));
   } else {
-  // ---- this warp's run of the flat list: every warp adds up the list by itself, 32 requests at a time
-  is.s = ca_span_of(a, min(lane, B - 1), blockIdx.x == 0 && warp == 0 && lane < B);
-  auto places = [&](const ca_span& sp) -> long long { return sp.tiles > 0 ? (long long)(sp.tiles + CA_UNIT_COST) * subs : 0; };
-  const long long cost0 = lane < B ? places(is.s) : 0;               // of the first 32 requests
-  long long total = cost0;
-  for (int b = lane + 32; b < B; b += 32) total += places(ca_span_of(a, b, blockIdx.x == 0 && warp == 0));
+    // ---- this warp's run of the flat list: every warp adds up the list by itself, 32 requests at a time
+    is.s = ca_span_of(a, min(lane, B - 1), blockIdx.x == 0 && warp == 0 && lane < B);
+    auto places = [&](const ca_span& sp) -> long long { return sp.tiles > 0 ? (long long)(sp.tiles + CA_UNIT_COST) * subs : 0; };
+    const long long cost0 = lane < B ? places(is.s) : 0;               // of the first 32 requests
+    long long total = cost0;
+    for (int b = lane + 32; b < B; b += 32) total += places(ca_span_of(a, b, blockIdx.x == 0 && warp == 0));
 #pragma unroll
-  for (int o = 16; o; o >>= 1) total += __shfl_xor_sync(0xffffffffu, total, o);
-  share = max(1LL, ca_div(total + (long long)gridDim.x * CA_WARPS - 1, (int)gridDim.x * CA_WARPS));
-  const long long f0 = share * me;
-  if (f0 < total) {
-    long long at = 0;                                                 // first place of the 32 requests looked at
-    for (int b0 = 0;; b0 += 32) {
-      ca_span sp = is.s;
-      long long cost = cost0;
-      if (b0 > 0) {
-        sp = ca_span_of(a, min(b0 + lane, B - 1), false);
-        cost = b0 + lane < B ? places(sp) : 0;
-      }
-      long long incl = cost;
+    for (int o = 16; o; o >>= 1) total += __shfl_xor_sync(0xffffffffu, total, o);
+    share = max(1LL, ca_div(total + (long long)gridDim.x * CA_WARPS - 1, (int)gridDim.x * CA_WARPS));
+    const long long f0 = share * me;
+    if (f0 < total) {
+      long long at = 0;                                                 // first place of the 32 requests looked at
+      for (int b0 = 0;; b0 += 32) {
+        ca_span sp = is.s;
+        long long cost = cost0;
+        if (b0 > 0) {
+          sp = ca_span_of(a, min(b0 + lane, B - 1), false);
+          cost = b0 + lane < B ? places(sp) : 0;
+        }
+        long long incl = cost;
 #pragma unroll
-      for (int o = 1; o < 32; o <<= 1) {
-        const long long v = __shfl_up_sync(0xffffffffu, incl, o);
-        if (lane >= o) incl += v;
+        for (int o = 1; o < 32; o <<= 1) {
+          const long long v = __shfl_up_sync(0xffffffffu, incl, o);
+          if (lane >= o) incl += v;
+        }
+        const unsigned in = __ballot_sync(0xffffffffu, f0 >= at + incl - cost && f0 < at + incl);
+        if (in) {
+          const int l = __ffs(in) - 1;
+          is.b = b0 + l;
+          is.s.end = __shfl_sync(0xffffffffu, sp.end, l);
+          is.s.first = __shfl_sync(0xffffffffu, sp.first, l);
+          is.s.tile0 = __shfl_sync(0xffffffffu, sp.tile0, l);
+          is.s.tiles = __shfl_sync(0xffffffffu, sp.tiles, l);
+          const long long off = f0 - (at + __shfl_sync(0xffffffffu, incl - cost, l));
+          is.sub = (int)ca_div(off, is.s.tiles + CA_UNIT_COST);
+          is.t = (int)(off - (long long)is.sub * (is.s.tiles + CA_UNIT_COST));
+          is.left = (int)min(share, 0x7fffffffLL);
+          break;
+        }
+        at += __shfl_sync(0xffffffffu, incl, 31);
+        if (b0 + 32 >= B) break;                                        // lengths changed under the call
       }
-      const unsigned in = __ballot_sync(0xffffffffu, f0 >= at + incl - cost && f0 < at + incl);
-      if (in) {
-        const int l = __ffs(in) - 1;
-        is.b = b0 + l;
-        is.s.end = __shfl_sync(0xffffffffu, sp.end, l);
-        is.s.first = __shfl_sync(0xffffffffu, sp.first, l);
-        is.s.tile0 = __shfl_sync(0xffffffffu, sp.tile0, l);
-        is.s.tiles = __shfl_sync(0xffffffffu, sp.tiles, l);
-        const long long off = f0 - (at + __shfl_sync(0xffffffffu, incl - cost, l));
-        is.sub = (int)ca_div(off, is.s.tiles + CA_UNIT_COST);
-        is.t = (int)(off - (long long)is.sub * (is.s.tiles + CA_UNIT_COST));
-        is.left = (int)min(share, 0x7fffffffLL);
-        break;
+      if (is.left > 0 && is.t == 0) {
+        ca_keep_whole(is);
+      } else if (is.left > 0 && (is.t >= is.s.tiles || is.s.tiles <= CA_WHOLE)) {
+        // the run begins in the empty places behind a unit, or inside a short one, which is the run before's
+        is.left -= is.s.tiles + CA_UNIT_COST - is.t;
+        if (is.left > 0) ca_next_unit(a, is, subs);
       }
-      at += __shfl_sync(0xffffffffu, incl, 31);
-      if (b0 + 32 >= B) break;                                        // lengths changed under the call
     }
-    if (is.left > 0 && is.t == 0) {
-      ca_keep_whole(is);
-    } else if (is.left > 0 && (is.t >= is.s.tiles || is.s.tiles <= CA_WHOLE)) {
-      // the run begins in the empty places behind a unit, or inside a short one, which is the run before's
-      is.left -= is.s.tiles + CA_UNIT_COST - is.t;
-      if (is.left > 0) ca_next_unit(a, is, subs);
-    }
-  }
   }
 
   // ---- the issuing side
