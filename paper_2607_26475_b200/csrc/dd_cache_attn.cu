@@ -948,7 +948,7 @@ __global__ void __launch_bounds__(CA_THREADS, (ca_geom<FMT, D, NT>::BLOCKS_PER_S
 
 }
 
-// Adds the partials of the cut units that begin in block x of the attention kernel. The partials of a unit from run w0
+// Adds the partials of the cut units that begin in the attention kernel's runs x, x + gridDim.x, ... The partials of a unit from run w0
 // (where it begins) to run w1 (where it ends) are one per block among the runs w0 .. w1 - 1, in the slot of the first of
 // them, and the last piece. Grid (blocks of the attention kernel, groups of 64 quads of accumulators); four groups of
 // threads take every fourth partial of the same 64 quads. What bounds it is latency: (descriptors) -> (references, sums,
@@ -968,17 +968,18 @@ __global__ void __launch_bounds__(64 * CJ_GROUPS) dd_cache_attn_join_kernel(cons
   const int nt = blockIdx.y * 64 / (D / 16 * 32), m = (e / 32) % (D / 16), ge = (e & 31) >> 2, col = 2 * (e & 3);
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   dd_grid_dependency_wait();
-  // the descriptors of the block's warps, one per lane, handed round by shuffles
+  // every gridDim.x-th descriptor, one per lane, handed round by shuffles (neighbouring ones in different blocks: where units are
+  // short, neighbouring runs all have one)
   int4 mine = make_int4(0, 0, 0, 0);
-  if (lane < CA_WARPS) mine = a.desc[blockIdx.x * CA_WARPS + lane];
+  if (lane < CA_WARPS) mine = a.desc[lane * gridDim.x + blockIdx.x];
   unsigned todo = __ballot_sync(0xffffffffu, mine.z != 0);            // the same in every warp
   while (todo) {
     const int l = __ffs(todo) - 1;
     todo &= todo - 1;
     const int b = __shfl_sync(0xffffffffu, mine.x, l), sub = __shfl_sync(0xffffffffu, mine.y, l);
-    const int w0 = blockIdx.x * CA_WARPS + l, w1 = __shfl_sync(0xffffffffu, mine.z, l) - 1;
-    const int n = (w1 - 1) / CA_WARPS - (int)blockIdx.x + 2;          // partials
-    auto slot = [&](int i) -> long long { return i == 0 ? 2LL * w0 + 1 : (i == n - 1 ? 2LL * w1 : 2LL * ((int)blockIdx.x + i) * CA_WARPS + 1); };
+    const int w0 = l * gridDim.x + blockIdx.x, w1 = __shfl_sync(0xffffffffu, mine.z, l) - 1, first = w0 / CA_WARPS;
+    const int n = (w1 - 1) / CA_WARPS - first + 2;                    // partials
+    auto slot = [&](int i) -> long long { return i == 0 ? 2LL * w0 + 1 : (i == n - 1 ? 2LL * w1 : 2LL * (first + i) * CA_WARPS + 1); };
     const int end = ca_span_of(a, b, false).end;
     float4 ahead[AHEAD];
 #pragma unroll
