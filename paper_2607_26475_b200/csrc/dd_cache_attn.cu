@@ -75,8 +75,9 @@ struct ca_geom {
   static constexpr int RING_BUDGET = (BLOCKS_PER_SM == 2 ? 106 : 212) * 1024;
   static constexpr int STAGES_ = RING_BUDGET / (CA_WARPS * SLOT_BYTES);
   static constexpr int STAGES = STAGES_ > 8 ? 8 : STAGES_;
-  // A second copy of the tile's code without masks and questions. Where registers are scarce (one column tile, head_dim 128) its
-  // spills cost what it saves (8 x 32K tokens e4m3 104 -> 106 us); elsewhere 131 -> 111 us (128 query heads), 63 -> 59 (head_dim 64).
+  // A second copy of the tile's code without masks and questions: 131 -> 111 us (128 query heads, 8 x 32K tokens e4m3), 63 -> 59
+  // (head_dim 64). Where registers are scarce (one column tile, head_dim 128) its spills cost what it saves (104 -> 106 us) and more
+  // where units are short (ragged 79 -> 89 us); e4m3 pages have it there as a kernel of its own for long units (LONG, ca_long).
   static constexpr bool PLAIN_LOOP = NT == 2 || D == 64;
   static constexpr int WARP_BYTES = STAGES * SLOT_BYTES;
   static constexpr int QUADS = NT * (D / 16) * 32;                    // groups of four accumulators: [column tile][product][lane]
@@ -254,9 +255,10 @@ __device__ __forceinline__ void ca_add(float4& x, const float4& v, float s0, flo
 
 __device__ __forceinline__ float ca_lse(float from, float den) { return (from + log2f(den)) * 0.6931471805599453f; }
 
-template <int FMT, int D, int NT>
+template <int FMT, int D, int NT, bool LONG>
 __global__ void __launch_bounds__(CA_THREADS, (ca_geom<FMT, D, NT>::BLOCKS_PER_SM)) dd_cache_attn_kernel(const ca_args a) {
   using geo = ca_geom<FMT, D, NT>;
+  constexpr bool PLAIN_LOOP = geo::PLAIN_LOOP || LONG;
   using TQ = typename ca_types<FMT>::Q;
   using TP = typename ca_types<FMT == 0 ? 0 : 1>::Q;
   constexpr bool FP8 = geo::FP8;
@@ -749,13 +751,13 @@ __global__ void __launch_bounds__(CA_THREADS, (ca_geom<FMT, D, NT>::BLOCKS_PER_S
       // how many tiles from here are plain on both sides: seen by every row of the tile, and refilled from complete tiles of
       // this lookup, the last of them left to the careful form
       int n = 0;
-      if (geo::PLAIN_LOOP && is.left > 1) {
+      if (PLAIN_LOOP && is.left > 1) {
         n = min(min(is.left, blocks_from + 32 - is.t), ((is.s.end - 16) >> 4) - is.s.tile0 - is.t + 1) - 1;
         n = min(n, min(n_here - i, ((pos_lo - 15) >> 4) - (s.tile0 + t0 + i) + 1));
         if (a.window > 0 && (((s.tile0 + t0 + i) << 4) <= pos_hi - a.window || ((is.s.tile0 + is.t) << 4) < is.s.first)) n = 0;
         if (!all_good()) n = 0;
       }
-      if constexpr (geo::PLAIN_LOOP) {
+      if constexpr (PLAIN_LOOP) {
 #pragma unroll 1
         for (; n > 0; --n, ++i) tile(std::true_type(), i);
       }
@@ -1044,6 +1046,7 @@ __global__ void __launch_bounds__(64 * CJ_GROUPS) dd_cache_attn_join_kernel(cons
 
 struct ca_plan {
   const void* main_kernel;
+  const void* long_kernel;
   const void* join_kernel;
   int smem, smem_cluster, blocks_per_sm;
 };
@@ -1051,7 +1054,10 @@ template <int FMT, int D, int NT> ca_plan ca_plan_of() {
   using geo = ca_geom<FMT, D, NT>;
   static_assert(geo::SMEM_CLUSTER + 2048 <= 227 * 1024, "shared memory of a block");
   static_assert(geo::BLOCKS_PER_SM == 1 || geo::SMEM_CLUSTER + 1024 + 2048 <= 114 * 1024, "shared memory of two blocks");
-  return {(const void*)dd_cache_attn_kernel<FMT, D, NT>, (const void*)dd_cache_attn_join_kernel<FMT, D, NT>, geo::SMEM, geo::SMEM_CLUSTER, geo::BLOCKS_PER_SM};
+  const void* main = (const void*)dd_cache_attn_kernel<FMT, D, NT, false>;
+  const void* by_long = main;
+  if constexpr (geo::FP8 && !geo::PLAIN_LOOP) by_long = (const void*)dd_cache_attn_kernel<FMT, D, NT, true>;
+  return {main, by_long, (const void*)dd_cache_attn_join_kernel<FMT, D, NT>, geo::SMEM, geo::SMEM_CLUSTER, geo::BLOCKS_PER_SM};
 }
 template <int FMT> ca_plan ca_pick(int d, int nt) {
   if (d == 128) return nt == 1 ? ca_plan_of<FMT, 128, 1>() : ca_plan_of<FMT, 128, 2>();
@@ -1076,6 +1082,13 @@ int ca_cluster_of(long long units, long long tiles, int blocks) {
   int c = 2;
   while (c < CA_MAX_CLUSTER && tiles > 2LL * c * CA_WARPS) c *= 2;
   return tiles <= 8LL * c * CA_WARPS && units * c <= blocks * 7 / 8 ? c : 0;
+}
+
+// Long units: so few that each is cut into 64 runs or more, of 32 tiles or more if the table is used to its width. One request of 1M
+// tokens e4m3 takes 372 us with either kernel at 1965 MHz, and 397 against 409 where the power cap holds the SMs at 1.6 GHz.
+bool ca_long(long long units, long long tiles, int blocks) {
+  const long long runs = (long long)blocks * CA_WARPS;
+  return units * 64 <= runs && units * tiles >= 32 * runs;
 }
 
 // Rows of a unit that go through the MMA together: up to 8 in one column tile, up to 16 in two.
@@ -1168,6 +1181,7 @@ extern "C" int dd_cache_decode_attn(const dd_cache* cache, int n_q_tokens, const
   long long tiles = ((long long)cache->max_pages * cache->page_tokens + 15) / 16;
   if (window > 0 && ((long long)window + n_q_tokens + 29) / 16 < tiles) tiles = ((long long)window + n_q_tokens + 29) / 16;
   a.cluster = ca_cluster_of(units, tiles, blocks);
+  if (!a.cluster && ca_long(units, tiles, blocks)) p.main_kernel = p.long_kernel;
   DD_CUDA_TRY(nullptr, cudaFuncSetAttribute(p.main_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, p.smem_cluster));
   cudaLaunchConfig_t cfg = {};
   cudaLaunchAttribute at[2];

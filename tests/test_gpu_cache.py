@@ -685,3 +685,41 @@ def test_every_way_to_split_the_work_gives_the_definition(dd):
         keep = raw.copy()
         check_attn(out, lse, q, keep, table, short, fmt, "bf16", 16)
         assert cache.device_error() == (0, 0)
+
+
+@pytest.mark.parametrize("fmt,kind,Tq", [("e4m3", "bf16", 1), ("e4m3", "fp16", 2), ("bf16", "bf16", 1)])
+def test_long_requests_over_few_pages(dd, fmt, kind, Tq):
+    """A request of 1.25 million tokens whose table names 61 pages over and over: the definition is attention over the 61
+    pages' tokens, each weighted by how often it is seen."""
+    gen = torch.Generator().manual_seed(18)
+    T, d, H, G, n_pages, M = 16, 128, 1, 4, 61, 78200
+    lens = M * T - 5
+    raw = random_pages(gen, n_pages, H, fmt, T, d, gain=1.5)
+    _, pool = pool_of(raw)
+    table = (torch.arange(M, dtype=torch.int32) * 7 % n_pages).view(1, M)
+    cache = dd.PagedCache(pool, table.cuda(), cache_format=fmt_code(dd, fmt), head_dim=d, page_tokens=T)
+    q = torch.randn(1, Tq, G, d, generator=gen).to(TYPES[kind]).cuda()
+    out, lse = run_attn(cache, q, [lens])
+    again, _ = run_attn(cache, q, [lens])
+    assert torch.equal(out, again) and cache.device_error() == (0, 0)
+    kv = ref.decode_pages(raw[:, 0], fmt, T, d)                     # [pages, 2, T, d]
+    K, V = kv[:, 0].reshape(-1, d), kv[:, 1].reshape(-1, d)
+    for t in range(Tq):
+        seen = np.zeros((n_pages, T))
+        end = lens - Tq + t + 1
+        np.add.at(seen, table[0, :end // T].numpy(), 1.0)
+        seen[int(table[0, end // T]), :end % T] += 1.0
+        for h in range(G):
+            row = f64(q[0, t, h])
+            z = K @ row / math.sqrt(d)
+            p = np.exp(z - z.max()) * seen.reshape(-1)
+            want_lse = z.max() + math.log(p.sum())
+            p /= p.sum()
+            want, absum = p @ V, p @ np.abs(V)
+            unit = (np.abs(K) @ np.abs(row)).max() / math.sqrt(d)
+            # as for shorter requests; a warp adds up to 40 tiles before its sums are merged, 2048 merges of fp32 partials follow
+            dz = (d + 8) * 2.0 ** -24 * unit + 2.0 ** -21 * (1 + abs(want_lse))
+            rel = (STEP["bf16"] if fmt == "bf16" else STEP["fp16"]) + 2 * dz + lens * 2.0 ** -31 * 4 + 2.0 ** -12
+            tol = STEP[kind] * np.abs(want) + rel * np.maximum(absum, absum.max() * 2.0 ** -10)
+            assert np.all(np.abs(f64(out[0, t, h]) - want) <= tol)
+            assert abs(float(lse[0, t, h]) - want_lse) <= dz + 2.0 ** -12
