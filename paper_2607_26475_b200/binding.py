@@ -337,6 +337,9 @@ class PagedCache:
             n_blocks, n_kv_heads = data.shape[0], data.shape[1]
             block_stride = data.stride(0) * size if n_blocks > 1 else page * n_kv_heads
             head_stride = data.stride(1) * size if n_kv_heads > 1 else page
+        extent = (n_blocks - 1) * block_stride + (n_kv_heads - 1) * head_stride + page
+        if extent > data.untyped_storage().nbytes() - data.storage_offset() * size:
+            raise _invalid(f"the pages reach over {extent} bytes, behind the end of data")
         if block_table.dtype != torch.int32 or block_table.dim() != 2 or (block_table.shape[1] > 1 and block_table.stride(1) != 1):
             raise _invalid("block_table must be int32 [batch, max_pages] with dense rows")
         batch, max_pages = block_table.shape

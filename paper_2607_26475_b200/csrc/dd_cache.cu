@@ -31,14 +31,19 @@ int dd_check_ptr(const void* p, const char* who, const char* what, int align, in
   return DD_OK;
 }
 
-int dd_check_rows(const dd_rows* r, const char* who, const char* what, int head_dim, bool is_output) {
+int dd_check_rows(const dd_rows* r, const char* who, const char* what, int head_dim, long long n_tokens, bool is_output) {
   if (!r) return dd_fail(nullptr, DD_ERR_INVALID_ARG, "%s: %s is NULL", who, what);
   if (r->dtype != DD_BF16 && r->dtype != DD_FP16) return dd_fail(nullptr, DD_ERR_INVALID_ARG, "%s: %s has an unknown dtype", who, what);
   if (r->n_heads < 1) return dd_fail(nullptr, DD_ERR_INVALID_ARG, "%s: %s has no heads", who, what);
   if (r->token_stride < 0 || r->head_stride < 0 || r->token_stride % 8 || r->head_stride % 8)
     return dd_fail(nullptr, DD_ERR_INVALID_ARG, "%s: strides of %s must be non-negative multiples of 8 elements", who, what);
-  if (is_output && (r->token_stride < head_dim || (r->n_heads > 1 && r->head_stride < head_dim)))
-    return dd_fail(nullptr, DD_ERR_INVALID_ARG, "%s: rows of %s overlap", who, what);
+  if (is_output) {
+    // rows of an output must not meet: tokens behind all heads of the one before, or heads behind all tokens of the one before
+    const bool tokens_apart = n_tokens < 2 || r->token_stride >= (long long)(r->n_heads - 1) * r->head_stride + head_dim;
+    const bool heads_apart = r->n_heads < 2 || r->head_stride >= (n_tokens - 1) * r->token_stride + head_dim;
+    if ((n_tokens > 1 && r->token_stride < head_dim) || (r->n_heads > 1 && r->head_stride < head_dim) || (!tokens_apart && !heads_apart))
+      return dd_fail(nullptr, DD_ERR_INVALID_ARG, "%s: rows of %s overlap", who, what);
+  }
   if (!r->data) return dd_fail(nullptr, DD_ERR_INVALID_ARG, "%s: %s is NULL", who, what);
   return DD_OK;
 }

@@ -9,7 +9,7 @@
 // be said without a device is checked first (dd_check_cache, dd_check_rows, dd_check_rope), the pointers after that.
 int dd_current_device();
 int dd_check_cache(const dd_cache* c, const char* who);
-int dd_check_rows(const dd_rows* r, const char* who, const char* what, int head_dim, bool is_output);
+int dd_check_rows(const dd_rows* r, const char* who, const char* what, int head_dim, long long n_tokens, bool is_output);
 int dd_check_rope(const dd_rope* r, const char* who, int head_dim);
 int dd_check_cache_memory(const dd_cache* c, const char* who, int device, bool allow_host, const char** data_dev, bool* on_host);
 int dd_check_ptr(const void* p, const char* who, const char* what, int align, int device);

@@ -1125,8 +1125,9 @@ extern "C" int dd_cache_decode_attn(const dd_cache* cache, int n_q_tokens, const
                                     size_t workspace_bytes, void* stream) {
   const char* who = "dd_cache_decode_attn";
   DD_TRY(dd_check_cache(cache, who));
-  DD_TRY(dd_check_rows(q, who, "q", cache->head_dim, false));
-  DD_TRY(dd_check_rows(out, who, "out", cache->head_dim, true));
+  const long long n_tokens = (long long)cache->batch * n_q_tokens;
+  DD_TRY(dd_check_rows(q, who, "q", cache->head_dim, n_tokens, false));
+  DD_TRY(dd_check_rows(out, who, "out", cache->head_dim, n_tokens, true));
   if (const char* why = ca_check_heads(q->n_heads, cache->n_kv_heads, cache->head_dim, n_q_tokens))
     return dd_fail(nullptr, DD_ERR_INVALID_ARG, "%s: %s", who, why);
   if (out->n_heads != q->n_heads || out->dtype != q->dtype)

@@ -310,11 +310,11 @@ int dd_check_rope(const dd_rope* r, const char* who, int head_dim) {
   return DD_OK;
 }
 
-static int rp_check_pair(const dd_rows* in, const dd_rows* out, const char* who, const char* name, const char* name_out, int head_dim) {
+static int rp_check_pair(const dd_rows* in, const dd_rows* out, const char* who, const char* name, const char* name_out, int head_dim, int n_tokens) {
   if (!in != !out) return dd_fail(nullptr, DD_ERR_INVALID_ARG, "%s: %s and %s go together", who, name, name_out);
   if (!in) return DD_OK;
-  DD_TRY(dd_check_rows(in, who, name, head_dim, false));
-  DD_TRY(dd_check_rows(out, who, name_out, head_dim, true));
+  DD_TRY(dd_check_rows(in, who, name, head_dim, n_tokens, false));
+  DD_TRY(dd_check_rows(out, who, name_out, head_dim, n_tokens, true));
   if (in->n_heads != out->n_heads || in->dtype != out->dtype)
     return dd_fail(nullptr, DD_ERR_INVALID_ARG, "%s: %s and %s differ in heads or type", who, name, name_out);
   return DD_OK;
@@ -330,8 +330,8 @@ extern "C" int dd_rope_apply(const dd_rope* rope, int head_dim, int n_tokens, co
   if (!q && !k) return dd_fail(nullptr, DD_ERR_INVALID_ARG, "%s: neither q nor k is given", who);
   DD_TRY(dd_check_rope(rope, who, head_dim));
   if (n_tokens == 0) return DD_OK;
-  DD_TRY(rp_check_pair(q, q_out, who, "q", "q_out", head_dim));
-  DD_TRY(rp_check_pair(k, k_out, who, "k", "k_out", head_dim));
+  DD_TRY(rp_check_pair(q, q_out, who, "q", "q_out", head_dim, n_tokens));
+  DD_TRY(rp_check_pair(k, k_out, who, "k", "k_out", head_dim, n_tokens));
   if (q && k && q->dtype != k->dtype) return dd_fail(nullptr, DD_ERR_INVALID_ARG, "%s: q and k differ in type", who);
   const int device = dd_current_device();
   DD_TRY(dd_check_ptr(rope->turns, who, "rope->turns", 8, device));
@@ -365,14 +365,14 @@ extern "C" int dd_cache_append(const dd_cache* cache, int n_tokens, const int* p
   if ((q || q_out) && !rope) return dd_fail(nullptr, DD_ERR_INVALID_ARG, "%s: q is turned with rope, which is NULL", who);
   if (rope) DD_TRY(dd_check_rope(rope, who, cache->head_dim));
   if (n_tokens == 0) return DD_OK;
-  DD_TRY(dd_check_rows(k, who, "k", cache->head_dim, false));
-  DD_TRY(dd_check_rows(v, who, "v", cache->head_dim, false));
+  DD_TRY(dd_check_rows(k, who, "k", cache->head_dim, n_tokens, false));
+  DD_TRY(dd_check_rows(v, who, "v", cache->head_dim, n_tokens, false));
   if (k->n_heads != cache->n_kv_heads || v->n_heads != cache->n_kv_heads)
     return dd_fail(nullptr, DD_ERR_INVALID_ARG, "%s: k and v must have the cache's %d heads", who, cache->n_kv_heads);
   if (k->dtype != v->dtype) return dd_fail(nullptr, DD_ERR_INVALID_ARG, "%s: k and v differ in type", who);
   if ((cache->format == DD_CACHE_BF16 && k->dtype != DD_BF16) || (cache->format == DD_CACHE_FP16 && k->dtype != DD_FP16))
     return dd_fail(nullptr, DD_ERR_INVALID_ARG, "%s: a 16-bit cache takes rows of its own type", who);
-  DD_TRY(rp_check_pair(q, q_out, who, "q", "q_out", cache->head_dim));
+  DD_TRY(rp_check_pair(q, q_out, who, "q", "q_out", cache->head_dim, n_tokens));
   if (q && q->dtype != k->dtype) return dd_fail(nullptr, DD_ERR_INVALID_ARG, "%s: q and k differ in type", who);
   const int device = dd_current_device();
   const char* data = nullptr;

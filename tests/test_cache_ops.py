@@ -129,8 +129,12 @@ def test_bad_arguments_are_refused(dd):
     refuses(attn(tq=0), "n_q_tokens")
     refuses(attn(tq=65), "n_q_tokens")
     refuses(attn(q=_rows(dd, n_heads=3)), "multiple of n_kv_heads")
-    refuses(attn(out=_rows(dd, n_heads=4)), "differ in heads")
+    refuses(attn(out=_rows(dd, n_heads=4, token_stride=512)), "differ in heads")
     refuses(attn(out=_rows(dd, token_stride=64)), "overlap")
+    refuses(attn(out=_rows(dd, token_stride=128, head_stride=128)), "overlap")          # token 1 of head 0 is token 0 of head 1
+    refuses(attn(out=_rows(dd, token_stride=128, head_stride=128), tq=2), "overlap")
+    assert attn(out=_rows(dd, token_stride=128, head_stride=256)) == bad                # head-major is fine: the next check refuses
+    assert "overlap" not in lib.dd_last_error_message(None).decode()
     refuses(attn(window=-1), "window")
     refuses(attn(scale=-1.0), "scale")
     refuses(attn(scale=float("nan")), "scale")
@@ -145,6 +149,9 @@ def test_python_side_refuses_wrong_shapes_and_types(dd):
                      (data, table, dict(head_dim=96)), (data, table[:0], {}), (data[0], table, {})]:
         with pytest.raises(dd.DDError):
             dd.PagedCache(d, t, cache_format=dd.DD_CACHE_E4M3, **kw)
+    with pytest.raises(dd.DDError) as e:
+        dd.PagedCache(data, table, cache_format=dd.DD_CACHE_E4M3, n_blocks=4, block_stride=2 * 4128, head_stride=4144, n_kv_heads=2)
+    assert "behind the end" in str(e.value)
     c = dd.PagedCache(data, table, cache_format=dd.DD_CACHE_E4M3)
     k, pos = torch.zeros(2, 2, 128, dtype=torch.bfloat16), torch.zeros(2, dtype=torch.int32)
     for args in [(k.float(), k, pos), (k[:, :, :64], k, pos), (k, k[:1], pos), (k.transpose(0, 2).contiguous().transpose(0, 2), k, pos),
