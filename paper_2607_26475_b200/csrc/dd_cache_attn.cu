@@ -37,9 +37,7 @@
 //
 // Measured on a B200 (device time of a call, 32 query and 8 KV heads of 128): 8 requests of 32768 tokens bf16 166 us (6.45 TB/s, a
 // copy's rate), e4m3 104 us (5.2 TB/s; twice the instructions per byte, and four warps a scheduler do not cover their latencies),
-// one request of 1M tokens e4m3 372 us (5.8 TB/s), 48 requests of 0 to 32768 tokens e4m3 79 us, one request of 4096 tokens 10.4 us.
-#include <type_traits>
-
+// one request of 1M tokens e4m3 366 us (5.9 TB/s), 48 requests of 0 to 32768 tokens e4m3 77 us, one request of 4096 tokens 10.0 us.
 #include "dd_cache.cuh"
 
 namespace {
@@ -75,10 +73,10 @@ struct ca_geom {
   static constexpr int RING_BUDGET = (BLOCKS_PER_SM == 2 ? 106 : 212) * 1024;
   static constexpr int STAGES_ = RING_BUDGET / (CA_WARPS * SLOT_BYTES);
   static constexpr int STAGES = STAGES_ > 8 ? 8 : STAGES_;
-  // A second copy of the tile's code without masks and questions: 131 -> 111 us (128 query heads, 8 x 32K tokens e4m3), 63 -> 59
-  // (head_dim 64). Where registers are scarce (one column tile, head_dim 128) its spills cost what it saves (104 -> 106 us) and more
-  // where units are short (ragged 79 -> 89 us); e4m3 pages have it there as a kernel of its own for long units (LONG, ca_long).
-  static constexpr bool PLAIN_LOOP = NT == 2 || D == 64;
+  // A second copy of the tile's code without masks and questions: 131 -> 111 us (128 query heads, 8 x 32K tokens e4m3), 63 -> 58
+  // (head_dim 64), 106 -> 104 (e4m3, head_dim 128). bf16 and half pages with one column tile at head_dim 128 wait for memory with
+  // either and go without.
+  static constexpr bool PLAIN_LOOP = FP8 || NT == 2 || D == 64;
   static constexpr int WARP_BYTES = STAGES * SLOT_BYTES;
   static constexpr int QUADS = NT * (D / 16) * 32;                    // groups of four accumulators: [column tile][product][lane]
   // behind the rings, for clusters: what a block receives of its slice of the quads, and every block's references and sums
@@ -255,10 +253,10 @@ __device__ __forceinline__ void ca_add(float4& x, const float4& v, float s0, flo
 
 __device__ __forceinline__ float ca_lse(float from, float den) { return (from + log2f(den)) * 0.6931471805599453f; }
 
-template <int FMT, int D, int NT, bool LONG>
+template <int FMT, int D, int NT>
 __global__ void __launch_bounds__(CA_THREADS, (ca_geom<FMT, D, NT>::BLOCKS_PER_SM)) dd_cache_attn_kernel(const ca_args a) {
   using geo = ca_geom<FMT, D, NT>;
-  constexpr bool PLAIN_LOOP = geo::PLAIN_LOOP || LONG;
+  constexpr bool PLAIN_LOOP = geo::PLAIN_LOOP;
   using TQ = typename ca_types<FMT>::Q;
   using TP = typename ca_types<FMT == 0 ? 0 : 1>::Q;
   constexpr bool FP8 = geo::FP8;
@@ -267,6 +265,7 @@ __global__ void __launch_bounds__(CA_THREADS, (ca_geom<FMT, D, NT>::BLOCKS_PER_S
   __shared__ float2 sh_ml[CA_WARPS][NT * 8];
   __shared__ float sh_scale[CA_WARPS][NT * 8];
   __shared__ float2 sh_blk[NT * 8];                  // clusters: the block's references and sums
+  __shared__ int4 sh_rest[CA_WARPS][2];              // the using cursor, while the registers are needed for the tiles
   __shared__ int2 sh_piece[CA_WARPS];                // (request, sub) of the unit a run ends inside, or -1
 
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -379,7 +378,6 @@ __global__ void __launch_bounds__(CA_THREADS, (ca_geom<FMT, D, NT>::BLOCKS_PER_S
   if (is.left > 0) enter_unit();
   const char* src = nullptr;                         // K of the tile being issued; V lies page_tokens rows behind
   int n_first = 0, n_valid = 0;                      // tokens [n_first, n_valid) of it exist (and are visible to some row)
-  bool second = false;                               // the next half to issue is V
   uint32_t put = ring;                               // slot it goes to
   const uint32_t place0 = ca_place<geo::ROW>(lane / (geo::ROW / 16), lane % (geo::ROW / 16));
 
@@ -400,9 +398,9 @@ __global__ void __launch_bounds__(CA_THREADS, (ca_geom<FMT, D, NT>::BLOCKS_PER_S
       }
     }
   };
-  auto issue = [&]() {
+  auto issue = [&](bool v_half) {                    // K (or everything) of the tile at hand, or its V, which ends it
     if (is.left > 0) {
-      if (geo::WHOLE || !second) {
+      if (geo::WHOLE || !v_half) {
         const int tok0 = (is.s.tile0 + is.t) << 4;
         int blk = __shfl_sync(0xffffffffu, blocks, is.t - blocks_from);
         n_first = is.s.first - tok0;
@@ -422,7 +420,7 @@ __global__ void __launch_bounds__(CA_THREADS, (ca_geom<FMT, D, NT>::BLOCKS_PER_S
           ca_cp4(put + geo::EXP_AT + lane * 4, ex, n_valid > 0 ? 4u : 0u);
         }
       }
-      if (geo::WHOLE || second) {
+      if (geo::WHOLE || v_half) {
         copy_half(put + (geo::WHOLE ? geo::HALF_BYTES : 0), src + (page_mask + 1) * geo::ROW);
         ca_step(a, is, subs);
         if (is.left > 0) {
@@ -430,13 +428,12 @@ __global__ void __launch_bounds__(CA_THREADS, (ca_geom<FMT, D, NT>::BLOCKS_PER_S
           else if (is.t - blocks_from == 32) look_up();
         }
       }
-      second = !second;
     }
     ca_commit();
     put = put + geo::SLOT_BYTES == ring + geo::WARP_BYTES ? ring : put + geo::SLOT_BYTES;
   };
 #pragma unroll 1
-  for (int i = 0; i < NS; ++i) issue();
+  for (int i = 0; i < NS; ++i) issue(i & 1);
   // The same inside a unit, where nothing has to be asked: a complete tile of a good block, not the last of the run, the unit
   // or the entries at hand. First half of a pair: V of the tile at hand if the ring's depth is odd, else K (or everything) of it.
   constexpr bool V_FIRST = !geo::WHOLE && (NS & 1);
@@ -470,7 +467,7 @@ __global__ void __launch_bounds__(CA_THREADS, (ca_geom<FMT, D, NT>::BLOCKS_PER_S
     __syncwarp();
     take = take + geo::SLOT_BYTES == ring + geo::WARP_BYTES ? ring : take + geo::SLOT_BYTES;
     if (plain) issue_plain(first);
-    else issue();
+    else issue(first == V_FIRST);
   };
   // ldmatrix addresses: K matrices (rows 0-7 | 8-15) x (chunk 2i | 2i+1), V matrices the same or with the two swapped
   const int r8 = lane & 7, m1 = (lane >> 3) & 1, m2 = lane >> 4;
@@ -484,12 +481,12 @@ __global__ void __launch_bounds__(CA_THREADS, (ca_geom<FMT, D, NT>::BLOCKS_PER_S
   float acc[NT][D / 16][4];
   float from[NT][2], sum[NT][2];                     // reference minus headroom; denominator, this lane's tokens
   while (u.left > 0) {
-    const int b = u.b, sub = u.sub, t0 = u.t;
-    const ca_span s = u.s;
-    const int n_here = min(s.tiles - t0, u.left);                     // tiles of the unit in this run
+    int b = u.b, sub = u.sub, t0 = u.t;
+    ca_span s = u.s;
+    int n_here = min(s.tiles - t0, u.left);                           // tiles of the unit in this run
     if (n_here <= 0) break;                                           // lengths changed under the call: stop
-    const int rt = ca_row_tile(a, sub), head = sub - rt * a.c.n_kv_heads;
-    const int r0 = rt * NT * 8;                                       // first row of the tile
+    int rt = ca_row_tile(a, sub), head = sub - rt * a.c.n_kv_heads;
+    int r0 = rt * NT * 8;                                       // first row of the tile
 
     // query fragments: column n = g of column tile nt is row r0 + 8 nt + g
     uint32_t qf[NT][D / 8];
@@ -556,9 +553,15 @@ __global__ void __launch_bounds__(CA_THREADS, (ca_geom<FMT, D, NT>::BLOCKS_PER_S
       sum[nt][0] = sum[nt][1] = 0.f;
     }
 
+    const int first_tile = s.tile0 + t0;
+    if (lane == 0) {
+      sh_rest[warp][0] = make_int4(u.b, u.sub, u.t, u.left);
+      sh_rest[warp][1] = make_int4(s.end, s.first, s.tile0, s.tiles);
+    }
+    __syncwarp();
     auto tile = [&](auto plain_, int i) {
       constexpr bool plain = decltype(plain_)::value;                 // no mask, and the refills need no questions
-      const int tok0 = (s.tile0 + t0 + i) << 4;
+      const int tok0 = (first_tile + i) << 4;
       // ---- scores
       float z[NT][4];
       float vex0 = 0.f, vex1 = 0.f;                                   // log2 of the value scales of tokens g, g + 8
@@ -753,8 +756,8 @@ __global__ void __launch_bounds__(CA_THREADS, (ca_geom<FMT, D, NT>::BLOCKS_PER_S
       int n = 0;
       if (PLAIN_LOOP && is.left > 1) {
         n = min(min(is.left, blocks_from + 32 - is.t), ((is.s.end - 16) >> 4) - is.s.tile0 - is.t + 1) - 1;
-        n = min(n, min(n_here - i, ((pos_lo - 15) >> 4) - (s.tile0 + t0 + i) + 1));
-        if (a.window > 0 && (((s.tile0 + t0 + i) << 4) <= pos_hi - a.window || ((is.s.tile0 + is.t) << 4) < is.s.first)) n = 0;
+        n = min(n, min(n_here - i, ((pos_lo - 15) >> 4) - (first_tile + i) + 1));
+        if (a.window > 0 && (((first_tile + i) << 4) <= pos_hi - a.window || ((is.s.tile0 + is.t) << 4) < is.s.first)) n = 0;
         if (!all_good()) n = 0;
       }
       if constexpr (PLAIN_LOOP) {
@@ -765,6 +768,23 @@ __global__ void __launch_bounds__(CA_THREADS, (ca_geom<FMT, D, NT>::BLOCKS_PER_S
     }
 
     // ---- the end of the unit, or of the run
+    {
+      __syncwarp();
+      const volatile int* rest = reinterpret_cast<const volatile int*>(&sh_rest[warp][0]);
+      u.b = b = rest[0];
+      u.sub = sub = rest[1];
+      u.t = t0 = rest[2];
+      u.left = rest[3];
+      s.end = rest[4];
+      s.first = rest[5];
+      s.tile0 = rest[6];
+      s.tiles = rest[7];
+      u.s = s;
+      n_here = min(s.tiles - t0, u.left);
+      rt = ca_row_tile(a, sub);
+      head = sub - rt * a.c.n_kv_heads;
+      r0 = rt * NT * 8;
+    }
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
@@ -1046,7 +1066,6 @@ __global__ void __launch_bounds__(64 * CJ_GROUPS) dd_cache_attn_join_kernel(cons
 
 struct ca_plan {
   const void* main_kernel;
-  const void* long_kernel;
   const void* join_kernel;
   int smem, smem_cluster, blocks_per_sm;
 };
@@ -1054,10 +1073,7 @@ template <int FMT, int D, int NT> ca_plan ca_plan_of() {
   using geo = ca_geom<FMT, D, NT>;
   static_assert(geo::SMEM_CLUSTER + 2048 <= 227 * 1024, "shared memory of a block");
   static_assert(geo::BLOCKS_PER_SM == 1 || geo::SMEM_CLUSTER + 1024 + 2048 <= 114 * 1024, "shared memory of two blocks");
-  const void* main = (const void*)dd_cache_attn_kernel<FMT, D, NT, false>;
-  const void* by_long = main;
-  if constexpr (geo::FP8 && !geo::PLAIN_LOOP) by_long = (const void*)dd_cache_attn_kernel<FMT, D, NT, true>;
-  return {main, by_long, (const void*)dd_cache_attn_join_kernel<FMT, D, NT>, geo::SMEM, geo::SMEM_CLUSTER, geo::BLOCKS_PER_SM};
+  return {(const void*)dd_cache_attn_kernel<FMT, D, NT>, (const void*)dd_cache_attn_join_kernel<FMT, D, NT>, geo::SMEM, geo::SMEM_CLUSTER, geo::BLOCKS_PER_SM};
 }
 template <int FMT> ca_plan ca_pick(int d, int nt) {
   if (d == 128) return nt == 1 ? ca_plan_of<FMT, 128, 1>() : ca_plan_of<FMT, 128, 2>();
@@ -1076,19 +1092,12 @@ int ca_sm_count() {
 // Blocks of a cluster per unit, 0 for the flat list. Few and short units (known from the table's width, not from the lengths,
 // which are on the device): a cluster per unit joins its pieces through distributed shared memory and needs no second
 // kernel and no look at the other requests. At most 8 tiles a warp, and all clusters resident at once; units that fit one warp's
-// run uncut are left to the flat list. One request, 8 KV heads: 2048 tokens 11.5 -> 8.5 us, 4096 13.1 -> 10.4, 8192 14.6 -> 13.8.
+// run uncut are left to the flat list. One request, 8 KV heads: 2048 tokens 11.5 -> 8.5 us, 4096 13.1 -> 10.0, 8192 14.6 -> 13.6.
 int ca_cluster_of(long long units, long long tiles, int blocks) {
   if (tiles <= CA_WHOLE) return 0;
   int c = 2;
   while (c < CA_MAX_CLUSTER && tiles > 2LL * c * CA_WARPS) c *= 2;
   return tiles <= 8LL * c * CA_WARPS && units * c <= blocks * 7 / 8 ? c : 0;
-}
-
-// Long units: so few that each is cut into 64 runs or more, of 32 tiles or more if the table is used to its width. One request of 1M
-// tokens e4m3 takes 372 us with either kernel at 1965 MHz, and 397 against 409 where the power cap holds the SMs at 1.6 GHz.
-bool ca_long(long long units, long long tiles, int blocks) {
-  const long long runs = (long long)blocks * CA_WARPS;
-  return units * 64 <= runs && units * tiles >= 32 * runs;
 }
 
 // Rows of a unit that go through the MMA together: up to 8 in one column tile, up to 16 in two.
@@ -1182,7 +1191,6 @@ extern "C" int dd_cache_decode_attn(const dd_cache* cache, int n_q_tokens, const
   long long tiles = ((long long)cache->max_pages * cache->page_tokens + 15) / 16;
   if (window > 0 && ((long long)window + n_q_tokens + 29) / 16 < tiles) tiles = ((long long)window + n_q_tokens + 29) / 16;
   a.cluster = ca_cluster_of(units, tiles, blocks);
-  if (!a.cluster && ca_long(units, tiles, blocks)) p.main_kernel = p.long_kernel;
   DD_CUDA_TRY(nullptr, cudaFuncSetAttribute(p.main_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, p.smem_cluster));
   cudaLaunchConfig_t cfg = {};
   cudaLaunchAttribute at[2];
