@@ -530,11 +530,12 @@ def test_decode_steps_through_the_cache(dd):
     assert cache.device_error() == (0, 0)
 
 
-def test_captured_steps_replayed_with_other_lengths(dd):
+@pytest.mark.parametrize("M", [5, 40, 600])                       # a warp a unit, clusters, the flat list
+def test_captured_steps_replayed_with_other_lengths(dd, M):
     """Two graphs of the same cache hold an append and an attention each; replayed in turn with other lengths and rows
     than at capture, they give the eager calls' bits. The two graphs take workspaces of their own."""
     gen = torch.Generator().manual_seed(12)
-    B, H, G, d, T, M = 4, 2, 4, 128, 16, 40
+    B, H, G, d, T = 4, 2, 4, 128, 16
     raw = random_pages(gen, B * M, H, "bf16", T, d)
     _, pool = pool_of(raw)
     table = torch.randperm(B * M, generator=gen).view(B, M).to(torch.int32).cuda()
