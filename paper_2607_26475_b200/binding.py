@@ -210,6 +210,11 @@ def _stream(s) -> int:
     return s.cuda_stream
 
 
+def _torch_stream(s, device):
+    """The stream of `device` behind a raw handle, 0 being the default one (torch makes a new stream of an external 0)."""
+    return torch.cuda.ExternalStream(s, device=device) if s else torch.cuda.default_stream(device)
+
+
 def sparse_decode_attn_static(q, slot, idx, ctx_len, out, out_lse=None, *, n_splits=1, page_tokens=16, stream=None):
     """Attention over a gathered slot without a context and without any allocation: for callers that are
     not allowed to allocate device memory. The library's built-in scratch array (8 MiB per GPU) is shared
@@ -354,6 +359,20 @@ class PagedCache:
         self._addr = C.addressof(self.c)
         self._batch, self._heads, self._device = batch, n_kv_heads, block_table.device
         self._workspace_bytes = {}
+        # the error word is zeroed on the stream the cache is made on: until that has run, calls on other streams wait for it
+        self._made_on = self._made = None
+        if self.status.is_cuda and not torch.cuda.is_current_stream_capturing():
+            made_on = torch.cuda.current_stream(self._device)
+            self._made_on, self._made = made_on.cuda_stream, made_on.record_event()
+
+    def _stream(self, s) -> int:
+        s = _stream(s)
+        if self._made is not None and s != self._made_on and not torch.cuda.is_current_stream_capturing():
+            if not self._made.query():
+                _torch_stream(s, self._device).wait_event(self._made)
+            else:
+                self._made = None
+        return s
 
     @classmethod
     def of_store(cls, kv_layer, *, cache_format=DD_CACHE_BF16, head_dim=128, page_tokens=16, device="cuda"):
@@ -378,7 +397,7 @@ class PagedCache:
         rc = _cache_append(self._addr, n, _ints(positions, "positions", (n,)),
                            None if requests is None else _ints(requests, "requests", (n,)),
                            _rows(k, "k", d, n), _rows(v, "v", d, n), None if rope is None else rope._addr, rq,
-                           rq if q_out is None else _rows(q_out, "q_out", d, n), _stream(stream))
+                           rq if q_out is None else _rows(q_out, "q_out", d, n), self._stream(stream))
         if rc != DD_OK:
             _raise_last(rc)
 
@@ -391,7 +410,7 @@ class PagedCache:
         k = idx.shape[2]
         if kind is None or not out.is_contiguous() or out.shape != (b, h, 2, k * self.page_tokens, self.head_dim):
             raise _invalid(f"out must be a dense 16-bit tensor {(b, h, 2, k * self.page_tokens, self.head_dim)}")
-        rc = _cache_read(self._addr, _ints(idx, "idx", (b, h, k)), k, out.data_ptr(), kind, _stream(stream))
+        rc = _cache_read(self._addr, _ints(idx, "idx", (b, h, k)), k, out.data_ptr(), kind, self._stream(stream))
         if rc != DD_OK:
             _raise_last(rc)
 
@@ -422,7 +441,7 @@ class PagedCache:
             need = workspace.numel() * workspace.element_size()
         rc = _cache_decode_attn(self._addr, Tq, rq, _ints(ctx_len, "ctx_len", (b,)), ro,
                                 None if out_lse is None else out_lse.data_ptr(), window, scale, workspace.data_ptr(), need,
-                                _stream(stream))
+                                self._stream(stream))
         if rc != DD_OK:
             _raise_last(rc)
 
@@ -432,9 +451,15 @@ class PagedCache:
                            dtype=torch.uint8, device=self.block_table.device)
 
     def device_error(self):
-        """(code, detail) of the first index that a kernel found out of range; synchronises and clears it."""
+        """(code, detail) of the first index that a kernel found out of range, whatever stream its call went to; waits for all
+        work of the device and clears it."""
+        if self.status.is_cuda:
+            torch.cuda.synchronize(self._device)
         code, detail = self.status.tolist()
-        self.status.zero_()
+        if code:
+            self.status.zero_()
+            if self.status.is_cuda:
+                torch.cuda.current_stream(self._device).synchronize()      # before a call on another stream reports again
         return code, detail
 
 
