@@ -435,7 +435,7 @@ class PagedCache:
             if stream is None:
                 workspace = torch.empty(need, dtype=torch.uint8, device=self._device)
             else:
-                with torch.cuda.stream(torch.cuda.ExternalStream(stream) if isinstance(stream, int) else stream):
+                with torch.cuda.stream(_torch_stream(stream, self._device) if isinstance(stream, int) else stream):
                     workspace = torch.empty(need, dtype=torch.uint8, device=self._device)
         else:
             need = workspace.numel() * workspace.element_size()

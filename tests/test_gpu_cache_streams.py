@@ -97,3 +97,27 @@ def test_calls_run_on_the_stream_they_are_given(dd):
     want = steps(x, kv)
     torch.cuda.synchronize()
     assert all(torch.equal(a, b) for a, b in zip(got, want)) and cache.device_error() == (0, 0)
+
+
+def test_own_workspace_belongs_to_the_stream_of_the_call(dd, monkeypatch):
+    """A workspace of the call's own comes from the allocator's pool of the very stream it is used on, the default one (0) among
+    them: memory of another stream's pool could be handed out there while the call still runs."""
+    gen = torch.Generator().manual_seed(24)
+    cache, raw, table, q = make_attn(dd, gen, [40], 1, 4, 128, 16, "bf16", "bf16", 1)
+    lens, out = torch.tensor([40], dtype=torch.int32).cuda(), torch.empty_like(q)
+    taken_on, empty = [], torch.empty
+
+    def watch(*args, **kw):
+        taken_on.append(torch.cuda.current_stream().cuda_stream)
+        return empty(*args, **kw)
+
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    monkeypatch.setattr(dd.torch, "empty", watch)
+    for current in (torch.cuda.default_stream(), side):
+        for stream in (0, side.cuda_stream, side, torch.cuda.default_stream()):
+            with torch.cuda.stream(current):
+                cache.decode_attn(q, lens, out, stream=stream)
+            torch.cuda.synchronize()
+            assert taken_on.pop() == (stream if isinstance(stream, int) else stream.cuda_stream)
+    assert not taken_on
