@@ -438,6 +438,8 @@ class PagedCache:
                 with torch.cuda.stream(_torch_stream(stream, self._device) if isinstance(stream, int) else stream):
                     workspace = torch.empty(need, dtype=torch.uint8, device=self._device)
         else:
+            if not workspace.is_contiguous():
+                raise _invalid("workspace must be dense")
             need = workspace.numel() * workspace.element_size()
         rc = _cache_decode_attn(self._addr, Tq, rq, _ints(ctx_len, "ctx_len", (b,)), ro,
                                 None if out_lse is None else out_lse.data_ptr(), window, scale, workspace.data_ptr(), need,
