@@ -336,6 +336,10 @@ class PagedCache:
         if page == 0:
             raise _invalid(f"format {cache_format} with {page_tokens} tokens of {head_dim} elements a page is not supported")
         size = data.element_size()
+        if data.numel() == 0 or n_blocks == 0 or n_kv_heads == 0:
+            raise _invalid("data is empty")
+        if n_blocks is not None and (block_stride is None or head_stride is None or n_kv_heads is None):
+            raise _invalid("n_blocks, block_stride, head_stride and n_kv_heads go together")
         if n_blocks is None:
             if data.dim() < 3 or data[0, 0].numel() * size != page or not data[0, 0].is_contiguous():
                 raise _invalid(f"data must be [n_blocks, n_kv_heads, ...] with dense pages of {page} bytes, not {tuple(data.shape)}")
@@ -379,6 +383,8 @@ class PagedCache:
         """A layer of the method's store, [B, Hkv, P, ...] dense, seen as a cache: page p of request b is its page p."""
         if kv_layer.dim() < 4 or not kv_layer.is_contiguous():
             raise _invalid("kv_layer must be a dense [batch, n_kv_heads, max_pages, ...] tensor")
+        if kv_layer.numel() == 0:
+            raise _invalid("kv_layer is empty")
         B, H, P = kv_layer.shape[:3]
         page = lib.dd_cache_page_bytes(cache_format, page_tokens, head_dim)
         if kv_layer[0, 0, 0].numel() * kv_layer.element_size() != page:
