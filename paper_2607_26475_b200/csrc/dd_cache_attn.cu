@@ -25,8 +25,14 @@
 // normal). Queries are multiplied by a power of two per row to fill the half's range: exact for every element above
 // 2^-28 of the row's largest.
 //
-// Rounding: P to bf16 (bf16 pages; off by 2^-8 relative at most: the MMA takes both operands in one type) or half (2^-11), q
-// as said, the output once. Scores, reference, denominators, accumulators and partial results are fp32.
+// Rounding. A weight enters the second product as two 16-bit parts, its rounded value and the rounded rest (an MMA takes both
+// operands in one type): off by 2^-16 relative at most for bf16 pages, by 2^-22 for half pages and half queries, so that the
+// output's own rounding is the one that shows. One part (2^-8, 2^-11) left an error of 0.0023 relative on 4096 bf16 tokens where
+// the output's rounding alone is 0.00165 (half: 0.00028 for 0.00021). The second part costs 168.1 -> 169.4 us on 8 x 32K tokens
+// of bf16, 9.8 -> 10.1 us on 4096, and the same for half. e4m3 pages with bf16 queries go without: half weights (2^-11) are an
+// eighth of the output's half step (0.00162 against 0.00161), and the part would cost 369 -> 375 us on 1M tokens. Halves end at
+// 2^-24: a weight more than 2^31 below the reference is dropped, one above is off by 2^-31 of the reference at most. Queries as
+// said, the output once. Scores, reference, denominators, accumulators and partial results are fp32.
 //
 // Joining. A unit inside one warp's run is finished there. The pieces of a cut unit that the warps of one block hold when
 // their runs end are added in shared memory; what is left (one fp32 partial per block, and the unit's last piece) goes to
@@ -73,6 +79,8 @@ struct ca_geom {
   static constexpr int RING_BUDGET = (BLOCKS_PER_SM == 2 ? 106 : 212) * 1024;
   static constexpr int STAGES_ = RING_BUDGET / (CA_WARPS * SLOT_BYTES);
   static constexpr int STAGES = STAGES_ > 8 ? 8 : STAGES_;
+  // Weights as two 16-bit parts (see "Rounding").
+  static constexpr bool PAIR = FMT != 2;
   // A second copy of the tile's code without masks and questions: 131 -> 111 us (128 query heads, 8 x 32K tokens e4m3), 63 -> 58
   // (head_dim 64), 106 -> 104 (e4m3, head_dim 128). bf16 and half pages with one column tile at head_dim 128 wait for memory with
   // either and go without.
@@ -640,7 +648,7 @@ __global__ void __launch_bounds__(CA_THREADS, (ca_geom<FMT, D, NT>::BLOCKS_PER_S
       // ---- weights against the reference: 2^x with x = z - ref + headroom for the denominator, + log2 of the value's scale
       // for the product. Weights of values with a scale below 2^-96 do not let the denominator grow out of range: their
       // reference is taken as if the scale were 2^-96.
-      uint32_t pb[NT][2];
+      uint32_t pb[NT][2], pr[NT][2];                                  // weights, their rests
 #pragma unroll
       for (int nt = 0; nt < NT; ++nt) {
         float x[4], y[4];
@@ -678,8 +686,15 @@ __global__ void __launch_bounds__(CA_THREADS, (ca_geom<FMT, D, NT>::BLOCKS_PER_S
           p[e] = ca_exp2(y[e]);
           sum[nt][e & 1] += FP8 ? ca_exp2(x[e]) : p[e];
         }
-        pb[nt][0] = ca_transpose(dd_pack2<TP>(p[0], p[1]));
-        pb[nt][1] = ca_transpose(dd_pack2<TP>(p[2], p[3]));
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+          const uint32_t w = dd_pack2<TP>(p[2 * k], p[2 * k + 1]);
+          pb[nt][k] = ca_transpose(w);
+          if (geo::PAIR) {
+            const float2 had = dd_unpack2<TP>(w);
+            pr[nt][k] = ca_transpose(dd_pack2<TP>(p[2 * k] - had.x, p[2 * k + 1] - had.y));
+          }
+        }
       }
 
       // ---- weighted values
@@ -710,7 +725,10 @@ __global__ void __launch_bounds__(CA_THREADS, (ca_geom<FMT, D, NT>::BLOCKS_PER_S
               uint32_t r[4];
               value_frag(r, raw[c], half);
 #pragma unroll
-              for (int nt = 0; nt < NT; ++nt) ca_mma<FMT>(acc[nt][FP8 ? 2 * (c0 + c) + half : c0 + c], r[0], r[1], r[2], r[3], pb[nt][0], pb[nt][1]);
+              for (int nt = 0; nt < NT; ++nt) {
+                ca_mma<FMT>(acc[nt][FP8 ? 2 * (c0 + c) + half : c0 + c], r[0], r[1], r[2], r[3], pb[nt][0], pb[nt][1]);
+                if (geo::PAIR) ca_mma<FMT>(acc[nt][FP8 ? 2 * (c0 + c) + half : c0 + c], r[0], r[1], r[2], r[3], pr[nt][0], pr[nt][1]);
+              }
             }
         }
       } else {
@@ -739,6 +757,7 @@ __global__ void __launch_bounds__(CA_THREADS, (ca_geom<FMT, D, NT>::BLOCKS_PER_S
                 for (int nt = 0; nt < NT; ++nt) {
                   float one[4] = {0.f, 0.f, 0.f, 0.f};
                   ca_mma<FMT>(one, r[0], r[1], r[2], r[3], pb[nt][0], pb[nt][1]);
+                  if (geo::PAIR) ca_mma<FMT>(one, r[0], r[1], r[2], r[3], pr[nt][0], pr[nt][1]);
 #pragma unroll
                   for (int e = 0; e < 4; ++e)
                     if (pos[nt][e & 1] == p) acc[nt][FP8 ? 2 * (c0 + c) + half : c0 + c][e] += one[e];

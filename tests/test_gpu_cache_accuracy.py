@@ -1,0 +1,52 @@
+"""Attention over the cache to within the rounding of its own output: nothing before that may cost a visible part of it.
+
+A result is the correctly rounded value of something that lies within `slack` of the definition; slack counts the fp32
+arithmetic and the weights. Weights are held as two 16-bit parts (off by (2^-8)^2 = 2^-16 of a weight for bf16 pages, by
+2^-22 for half queries), for e4m3 pages with bf16 queries as one half (2^-11, an eighth of the output's half step)."""
+import numpy as np
+import pytest
+import torch
+
+from tests import _cache_ref as ref
+from tests._cache_ref import f64
+from tests.test_gpu_cache import TINY, dd, make_attn, run_attn  # noqa: F401  (dd is the fixture)
+
+pytestmark = pytest.mark.gpu
+
+BITS = {"bf16": 8, "fp16": 11}
+
+
+def half_step(x, kind):
+    """Half of the distance between neighbours of the type at magnitude |x|."""
+    return np.maximum(np.exp2(np.frexp(np.abs(x))[1] - BITS[kind] - 1.0), TINY[kind])
+
+
+CASES = [  # lens, H, G, d, T, fmt, query type, Tq, window, scale
+    ([2, 3, 7, 40, 1], 2, 4, 128, 16, "bf16", "bf16", 1, 0, 0.0),
+    ([300, 17, 2], 1, 4, 128, 16, "bf16", "bf16", 2, 0, 0.0),
+    ([300, 17, 2], 1, 16, 128, 16, "bf16", "bf16", 1, 20, 0.0),
+    ([77, 5], 2, 5, 64, 32, "bf16", "bf16", 3, 0, 0.0),
+    ([4000], 2, 4, 128, 16, "bf16", "bf16", 1, 0, 0.3),
+    ([2, 3, 7, 40, 1], 2, 4, 128, 16, "fp16", "fp16", 1, 0, 0.02),
+    ([300, 17, 2], 1, 12, 64, 16, "fp16", "fp16", 2, 0, 0.02),
+    ([2, 3, 7, 40, 1], 2, 4, 128, 16, "e4m3", "fp16", 1, 0, 0.02),
+    ([300, 17, 2], 1, 12, 64, 16, "e4m3", "fp16", 2, 0, 0.02),
+    ([2, 3, 7, 40, 1], 2, 4, 128, 16, "e4m3", "bf16", 1, 0, 0.0),
+    ([300, 17, 2], 1, 12, 64, 16, "e4m3", "bf16", 2, 0, 0.0),
+]
+
+
+@pytest.mark.parametrize("lens,H,G,d,T,fmt,kind,Tq,window,scale", CASES)
+def test_only_the_output_is_rounded_visibly(dd, lens, H, G, d, T, fmt, kind, Tq, window, scale):
+    gen = torch.Generator().manual_seed(sum(lens) + G + d)
+    cache, raw, table, q = make_attn(dd, gen, lens, H, G, d, T, fmt, kind, Tq)
+    out, lse = run_attn(cache, q, lens, window, scale)
+    want, want_lse, absum, unit = ref.attention(f64(q), raw, table.numpy(), lens, fmt, T, window, scale or None)
+    # a score: d products added in fp32 (each addition off by 2^-24 of a partial sum, at most sum |q||k|), two multiplications;
+    # weight and denominator both carry it
+    dz = (d + 8) * 2.0 ** -24 * unit + 2.0 ** -21 * (1 + np.where(np.isfinite(want_lse), np.abs(want_lse), 0.0))
+    weight = 2.0 ** -11 if (fmt, kind) == ("e4m3", "bf16") else 2.0 ** -16 if fmt == "bf16" else 2.0 ** -22
+    rel = weight + 2 * dz + max(lens) * 2.0 ** -29 + 2.0 ** -16
+    slack = rel[..., None] * np.maximum(absum, absum.max(-1, keepdims=True) * 2.0 ** -10)
+    off = np.abs(f64(out) - want) - half_step(np.abs(want) + slack, kind)
+    assert np.all(off <= slack), f"{(off / slack).max()} times the slack"
