@@ -580,9 +580,9 @@ __global__ void __launch_bounds__(CA_THREADS, (ca_geom<FMT, D, NT>::BLOCKS_PER_S
         const uint32_t at = take + k_row;
         float by0 = 1.f, by1 = 1.f;                                   // key scales of tokens g, g + 8
         if (FP8) {
-          // byte 0 (a row of magnitude below 2^-118) counts as zero here
-          by0 = __uint_as_float((uint32_t)ca_lds_byte(take + geo::EXP_AT + g) << 23);
-          by1 = __uint_as_float((uint32_t)ca_lds_byte(take + geo::EXP_AT + g + 8) << 23);
+          // byte 0 stands for 2^-127, whose bits lie below those of all the others
+          by0 = __uint_as_float(max((uint32_t)ca_lds_byte(take + geo::EXP_AT + g) << 23, 0x00400000u));
+          by1 = __uint_as_float(max((uint32_t)ca_lds_byte(take + geo::EXP_AT + g + 8) << 23, 0x00400000u));
           vex0 = (float)(ca_lds_byte(take + geo::EXP_AT + 16 + g) - 127);
           vex1 = (float)(ca_lds_byte(take + geo::EXP_AT + 16 + g + 8) - 127);
           uint32_t r[D / 32][4];                                      // four codes each: rows g, g + 8 of chunk 2c, of chunk 2c + 1

@@ -9,7 +9,7 @@ import torch
 
 from tests import _cache_ref as ref
 from tests._cache_ref import f64
-from tests.test_gpu_cache import TINY, dd, make_attn, run_attn  # noqa: F401  (dd is the fixture)
+from tests.test_gpu_cache import TINY, check_attn, dd, make_attn, run_attn  # noqa: F401  (dd is the fixture)
 
 pytestmark = pytest.mark.gpu
 
@@ -50,3 +50,18 @@ def test_only_the_output_is_rounded_visibly(dd, lens, H, G, d, T, fmt, kind, Tq,
     slack = rel[..., None] * np.maximum(absum, absum.max(-1, keepdims=True) * 2.0 ** -10)
     off = np.abs(f64(out) - want) - half_step(np.abs(want) + slack, kind)
     assert np.all(off <= slack), f"{(off / slack).max()} times the slack"
+
+
+@pytest.mark.parametrize("d,G", [(128, 4), (64, 16)])
+def test_keys_of_the_smallest_exponent_count(dd, d, G):
+    """A key row whose exponent byte is 0 holds code * 2^-127; large queries make scores of ordinary size of it."""
+    gen = torch.Generator().manual_seed(d)
+    lens, T = [70, 3], 16
+    cache, raw, table, q = make_attn(dd, gen, lens, 1, G, d, T, "e4m3", "bf16", 1, poison=False)
+    raw[:, :, 2 * T * d:2 * T * d + T] = np.random.RandomState(d).randint(0, 2, (raw.shape[0], 1, T))      # 2^-127 and 2^-126
+    cache.data.copy_(torch.from_numpy(raw).cuda())
+    q = (q.float() * 2.0 ** 120).to(torch.bfloat16)
+    out, lse = run_attn(cache, q, lens)
+    want_lse = ref.attention(f64(q), raw, table.numpy(), lens, "e4m3", T)[1]
+    assert np.ptp(want_lse - np.log(np.array(lens))[:, None, None]) > 0.05              # scores that are not all zero
+    check_attn(out, lse, q, raw, table, lens, "e4m3", "bf16", T)
