@@ -114,6 +114,7 @@ struct ca_args {
   int4* desc;          // [warps]: (request, sub, last run + 1) of the cut unit that begins in a warp's run, or 0
   int n_q_heads, G, Tq, n_rows, row_tiles, window;
   int cluster;         // blocks of a cluster that share one unit, 0 = the flat list
+  int joins;           // the joining kernel follows
   uint32_t by_G;       // ceil(2^31 / G): row / G by a multiplication
   float scale_log2;
 };
@@ -283,8 +284,9 @@ __global__ void __launch_bounds__(CA_THREADS, (ca_geom<FMT, D, NT>::BLOCKS_PER_S
   const int me = blockIdx.x * CA_WARPS + warp;
 
   dd_grid_dependency_wait();
-  // the joining kernel's blocks may take the places that this grid's blocks leave (each waits for all of them)
-  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+  // the joining kernel's blocks may take the places that this grid's blocks leave (each waits for all of them). No signal for
+  // any other kernel: append and attention in turn, 8 requests of 100 tokens, 14.0 us a layer with one, 12.9 without
+  if (a.joins) asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
 
   ca_cursor is;
   is.b = is.sub = is.t = is.left = 0;
@@ -1210,6 +1212,7 @@ extern "C" int dd_cache_decode_attn(const dd_cache* cache, int n_q_tokens, const
   long long tiles = ((long long)cache->max_pages * cache->page_tokens + 15) / 16;
   if (window > 0 && ((long long)window + n_q_tokens + 29) / 16 < tiles) tiles = ((long long)window + n_q_tokens + 29) / 16;
   a.cluster = ca_cluster_of(units, tiles, blocks);
+  a.joins = !a.cluster && (long long)cache->max_pages * cache->page_tokens > 16 * CA_WHOLE;   // else no unit can have been cut
   DD_CUDA_TRY(nullptr, cudaFuncSetAttribute(p.main_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, p.smem_cluster));
   cudaLaunchConfig_t cfg = {};
   cudaLaunchAttribute at[2];
@@ -1231,7 +1234,7 @@ extern "C" int dd_cache_decode_attn(const dd_cache* cache, int n_q_tokens, const
   cfg.gridDim = dim3((unsigned)blocks);
   cfg.dynamicSmemBytes = p.smem;
   DD_TRY(dd_launch(who, &cfg, p.main_kernel, args));
-  if ((long long)cache->max_pages * cache->page_tokens <= 16 * CA_WHOLE) return DD_OK;   // no unit can have been cut
+  if (!a.joins) return DD_OK;
   cfg.gridDim = dim3((unsigned)blocks, (unsigned)(nt * (cache->head_dim / 16) * 32 / 64));
   cfg.blockDim = dim3(64 * CJ_GROUPS);
   cfg.dynamicSmemBytes = (size_t)(blocks + 1) * 8 * sizeof(float);     // at most one partial per block and the last piece

@@ -117,8 +117,10 @@ int dd_fail(dd_ctx* ctx, int code, const char* fmt, ...);
 // kernel of its stream is still draining (its blocks become resident as that kernel's blocks leave). Such a kernel
 // calls dd_grid_dependency_wait() before its first access to global memory: the wait returns once every earlier
 // kernel of the stream has completed and its writes are visible, so the ordering a stream gives is unchanged. Our
-// kernels never signal their dependents early: measured, an early signal packs the next launch's blocks onto the SMs
-// that free up first and slows it. Saves 1.5-2 us per launch behind another kernel (B200, events around 40 launches).
+// kernels do not signal their dependents early: measured, an early signal packs the next launch's blocks onto the SMs
+// that free up first and slows it. The one exception is the attention over the paged cache where its own joining kernel
+// follows: that one waits for data rather than for SMs, and finds its blocks in place. Saves 1.5-2 us per launch behind
+// another kernel (B200, events around 40 launches).
 #ifdef __CUDACC__
 __device__ __forceinline__ void dd_grid_dependency_wait() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
 #endif
