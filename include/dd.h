@@ -414,9 +414,10 @@ int dd_cache_read(const dd_cache* cache, const int* idx, int k_pages, void* out,
  *   z[n]   = <q[b*n_q_tokens + t, h, :], K[n, h / G, :]> * scale        scale 0 = 1 / sqrt(head_dim)
  *   out    = sum softmax(z) * V;  out_lse = ln sum exp(z)
  * A query token before the request's beginning (ctx_len < n_q_tokens; empty requests) gives zeros and -inf. What lies in
- * the pages behind ctx_len is never used, whatever its bits. Any number of query heads per KV head, any ctx_len up to
- * max_pages * page_tokens (more is reported in status and cut; a negative one counts as 0); a table entry out of range is
- * reported and its page reads as zeros. Only entries of pages that hold a visible token are read.
+ * the pages behind ctx_len is never used, whatever its bits. Up to 64 query tokens, up to 1024 query heads per KV head; the
+ * query rows of a KV head go through together up to 16 at a time, and the cache is read once for each 16 of them. Any
+ * ctx_len up to max_pages * page_tokens (more is reported in status and cut; a negative one is reported and counts as 0); a
+ * table entry out of range is reported and its page reads as zeros. Only entries of pages that hold a visible token are read.
  *   q, out     dev [batch * n_q_tokens][n_q_heads][head_dim], one dtype (that of a 16-bit cache); out may be q itself
  *   ctx_len    dev int32 [batch]
  *   out_lse    dev fp32 [batch * n_q_tokens][n_q_heads] or NULL
