@@ -10,7 +10,8 @@ later layer on the side stream (dd_decode_layer_step). `value` counts output tok
 The headline line is the batch-8 / 32K-context workload with its own 64 decode steps. The same line carries,
 measured in the same run: the gather engines side by side (`gather_modes`, with the run-length histogram of the
 selected sets), one pass with miss correction (`miss_correction`), and compact results of the other
-workloads (`other_configs`). `--sweeps` adds a ring-depth sweep, a gather-grid sweep and miss correction against the miss rate.
+workloads (`other_configs`). `--sweeps` adds a ring-depth sweep, a gather-grid sweep, miss correction against the miss rate
+and the same workload over a quantised store.
 
 N > 1 runs N independent replicas, one per GPU (the path has no exchange step): under torchrun as launched,
 otherwise this script starts the N ranks itself. `--impl reference` times the CPU oracle on the host cores
@@ -315,7 +316,8 @@ class Bench:
                   copy_stream=self.copy, landmark_chunk_tokens=a.landmark_chunk, select_stream=self.select,
                   stage_min_run_pages=a.stage_min_run, stage_block_pages=a.stage_block,
                   attn_mode={"auto": dd.DD_ATTN_AUTO, "split": dd.DD_ATTN_SPLIT, "stream": dd.DD_ATTN_STREAM,
-                             "tc": dd.DD_ATTN_TC}[a.attn_mode])
+                             "tc": dd.DD_ATTN_TC}[a.attn_mode],
+                  store_format=getattr(a, "store_format", dd.DD_CACHE_BF16))
         if over.pop("correct", a.correct_misses):
             fifo = over.pop("urgent_fifo", a.urgent_fifo)
             kw.update(miss_correction=True, urgent_stream=self.copy if fifo else self.torch.cuda.Stream(priority=-1))
@@ -564,6 +566,26 @@ def miss_rate_sweep(b, link_peak, fidelities=(0.995, 0.97, 0.9, 0.8, 0.6, 0.3), 
     return out
 
 
+def quantised_store_pass(mods, w, args, rank, world, link_peak, phys=8, steps=16, warm=3):
+    """The same workload over a store of e4m3 pages (4128 bytes instead of 8192 cross the host link): a short pipelined run.
+    Not the headline's precision, and no part of it."""
+    import copy as _copy
+    dd = mods[1]
+    a = _copy.copy(args)
+    a.store_format, a.gather_mode, a.correct_misses = dd.DD_CACHE_E4M3, "loads", False
+    b = Bench(mods, w, a, rank, world, steps, warm, phys_layers=min(phys, w.n_layers), quiet=True)
+    ms, copy_ms = b.timed(b.ctx)
+    n = steps * w.n_layers
+    link_bytes = w.batch * w.n_kv_heads * w.k_pages * dd.lib.dd_cache_page_bytes(dd.DD_CACHE_E4M3, w.page_tokens, w.head_dim)
+    out = {"store": "e4m3 pages", "steps": steps, "warmup": warm, "phys_layers": b.store.n_phys,
+           "host_store_gib": b.store.host_bytes / 2**30, "tok_s": w.batch * steps / (ms * 1e-3), "ms_per_step": ms / steps,
+           "us_per_layer": ms / n * 1e3, "link_bytes_per_layer": link_bytes,
+           "gather_gb_s_live": link_bytes / (copy_ms / n * 1e-3) / 1e9,
+           "frac_of_link_roofline": link_bytes / (link_peak * 1e9) / (ms / n * 1e-3)}
+    b.close()
+    return out
+
+
 def measure_other_config(mods, n, args, rank, world, hbm_peak, link_peak):
     """A compact measurement of another workload: pipelined tok/s, e2e, per-kernel times and roofline fractions.
     The host store keeps two physical layers (logical layer l uses l mod 2; per-layer bytes, page scatter and the
@@ -757,8 +779,11 @@ def run_gpu(args):
         log("miss correction against the miss rate ...")
         line["miss_rate_sweep"] = miss_rate_sweep(b, link_peak)
     b.close()
+    del b, ctx, store
+    if rank == 0 and world == 1 and args.sweeps:
+        log("the same workload over a quantised store ...")
+        line["quantised_store"] = quantised_store_pass(mods, w, args, rank, world, link_peak)
     if extras and args.config == 2 and not (args.layers or args.batch):
-        del b, ctx, store
         line["other_configs"] = {}
         for n in (1, 3, 4, 5):
             log(f"workload {n} ...")
