@@ -133,13 +133,13 @@ dd_cache_view dd_make_view(const dd_cache* c, const char* data_dev) {
 // One warp per 16 tokens of a page: K and V of a tile are two contiguous runs, read with loads that are all in flight before
 // the first store (4 KiB a warp for e4m3 at head_dim 128, 8 KiB for 16-bit pages), and written as two contiguous runs of
 // 16-bit rows. A lane takes as many elements per load as it writes in one 16-byte store, so that every load and store of a
-// warp covers one contiguous piece: 8-byte loads for e4m3 (16-byte loads left two half-used stores: 44 against 33 us for
-// 32768 pages). Bound: HBM, or the host link for a page-locked pool. The exponents of a tile are 16 bytes for K and 16 for V:
-// one byte per lane in one load, handed out by shuffles. Measured on a B200: 8192 e4m3 pages of 16 x 128 15.3 us (6.6 TB/s of
-// reads and writes, inputs partly in L2); 4096 pages from page-locked memory 339 us (51 GB/s, what kernel reads get there).
+// warp covers one contiguous piece: 8-byte loads for e4m3 (16-byte loads left two half-used stores: 44 against 34 us for
+// 16384 pages). Bound: HBM, or the host link for a page-locked pool. The exponents of a tile are 16 bytes for K and 16 for V:
+// one byte per lane in one load, handed out by shuffles. Measured on a B200: 8192 e4m3 pages of 16 x 128 14.9 us (6.8 TB/s of
+// reads and writes, inputs partly in L2), 32768 pages 65 us (6.2 TB/s); 4096 pages from page-locked memory 339 us (49.9 GB/s of
+// the 51 that kernel reads get there), 4096 bf16 pages 656 us (51.1 GB/s).
 constexpr int CR_THREADS = 256;
 
-//
 // LINES: e4m3 pages in host memory, read by aligned lines (dd_e4m3_tile_by_lines).
 template <int FMT, typename T, int D, bool LINES>
 __global__ void __launch_bounds__(CR_THREADS) dd_cache_read_kernel(dd_cache_view c, const int* __restrict__ idx,

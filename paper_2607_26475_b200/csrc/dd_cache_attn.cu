@@ -1,15 +1,16 @@
 // Attention of the newest tokens of every request over all of its cached tokens (paged, 16-bit or e4m3 pages).
 //
-// Bound: HBM. Every K and V byte of the context is read once; 4 * G flops per element and query token are far below the
-// tensor peak. What has to be right is the load side: enough bytes in flight on every SM, no idle SM whatever the lengths
+// Bound: HBM. Every K and V byte of the context is read once for every 16 query rows of its KV head (one row tile; beyond
+// that once per row tile, 8 x 32K tokens bf16 with 24 rows 317 us against 178 with 16); 4 flops per element and row are far
+// below the tensor peak. What has to be right is the load side: enough bytes in flight on every SM, no idle SM whatever the lengths
 // are, and no pause at the border between two requests.
 //
 // Work split. The context of every (request, row tile, KV head) "unit" is cut into tiles of 16 tokens, and all tiles of
 // the launch form one flat list, request by request, with a few empty places behind each unit that stand for what a unit
 // costs besides its tiles. Every warp of a grid that fills the device once takes an equal run of the list; lengths are
 // read on the device, so the launch does not depend on them (a captured graph may be replayed with other lengths). Units
-// of at most 8 tiles are not cut. A warp works alone: it keeps a ring of half tiles (K or V) in flight with 16-byte cp.async, and the ring runs on across the
-// borders of units. A copy instruction takes 512 contiguous bytes (whole 128-byte lines; fragments fetched straight from
+// of at most 8 tiles are not cut. A warp works alone: it keeps a ring of half tiles (K or V) in flight with 16-byte
+// cp.async, and the ring runs on across the borders of units. A copy instruction takes 512 contiguous bytes (whole 128-byte lines; fragments fetched straight from
 // global memory touch half lines and ran at half the rate), and the chunks of a row are placed by row ^ chunk, so that
 // ldmatrix reads them without bank conflicts: K as it lies, V transposed.
 //
@@ -41,9 +42,10 @@
 // it, by a counter or by flags, took 4 to 7 us more: fences and contended words cost more round trips than a launch that
 // is already there.)
 //
-// Measured on a B200 (device time of a call, 32 query and 8 KV heads of 128): 8 requests of 32768 tokens bf16 166 us (6.45 TB/s, a
-// copy's rate), e4m3 104 us (5.2 TB/s; twice the instructions per byte, and four warps a scheduler do not cover their latencies),
-// one request of 1M tokens e4m3 366 us (5.9 TB/s), 48 requests of 0 to 32768 tokens e4m3 77 us, one request of 4096 tokens 10.0 us.
+// Measured on a B200 (device time of a call, 32 query and 8 KV heads of 128): 8 requests of 32768 tokens bf16 166-169 us
+// (6.4 TB/s, a copy's rate), e4m3 105 us (5.2 TB/s; twice the instructions per byte, and four warps a scheduler do not cover
+// their latencies), one request of 1M tokens e4m3 370-378 us (5.8 TB/s; 393 in passes that follow one another), 48 requests of 0
+// to 32768 tokens e4m3 78-79 us, one request of 4096 tokens 10.0 us (13.2 where the table is 8192 pages wide).
 #include "dd_cache.cuh"
 
 namespace {
@@ -1113,7 +1115,8 @@ int ca_sm_count() {
 // Blocks of a cluster per unit, 0 for the flat list. Few and short units (known from the table's width, not from the lengths,
 // which are on the device): a cluster per unit joins its pieces through distributed shared memory and needs no second
 // kernel and no look at the other requests. At most 8 tiles a warp, and all clusters resident at once; units that fit one warp's
-// run uncut are left to the flat list. One request, 8 KV heads: 2048 tokens 11.5 -> 8.5 us, 4096 13.1 -> 10.0, 8192 14.6 -> 13.6.
+// run uncut are left to the flat list. One request, 8 KV heads, a table of just its pages: 2048 tokens 11.8 -> 8.3 us, 4096
+// 13.2 -> 10.0, 8192 14.7 -> 13.6; a table wider than 8192 tokens takes the flat list whatever the length.
 int ca_cluster_of(long long units, long long tiles, int blocks) {
   if (tiles <= CA_WHOLE) return 0;
   int c = 2;
