@@ -26,7 +26,7 @@
 // normal). Queries are multiplied by a power of two per row to fill the half's range: exact for every element above
 // 2^-28 of the row's largest.
 //
-// Rounding. A weight enters the second product as two 16-bit parts, its rounded value and the rounded rest (an MMA takes both
+// Rounding. A weight enters the second product as two 16-bit parts, its value cut off and the rounded rest (an MMA takes both
 // operands in one type): off by 2^-16 relative at most for bf16 pages, by 2^-22 for half pages and half queries, so that the
 // output's own rounding is the one that shows. One part (2^-8, 2^-11) left an error of 0.0023 relative on 4096 bf16 tokens where
 // the output's rounding alone is 0.00165 (half: 0.00028 for 0.00021). The second part costs 168.1 -> 169.4 us on 8 x 32K tokens
@@ -172,6 +172,19 @@ __device__ __forceinline__ float ca_exp2(float x) {
   float y;
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
   return y;
+}
+// First parts of two weights, a little below them, so that the rests p - first are positive too and an infinite value times
+// either part is that infinity (a rest of zero would make it NaN). Zero gives zero. The differences are exact in fp32.
+template <typename T> __device__ __forceinline__ uint32_t ca_first_part(float p0, float p1);
+template <> __device__ __forceinline__ uint32_t ca_first_part<__nv_bfloat16>(float p0, float p1) {
+  constexpr float below = 1.f - 0x1p-16f;                              // then cut off
+  return __byte_perm(__float_as_uint(p0 * below), __float_as_uint(p1 * below), 0x7632u);
+}
+template <> __device__ __forceinline__ uint32_t ca_first_part<__half>(float p0, float p1) {
+  constexpr float below = 1.f - 0x1p-22f, least = 0x1p-24f - 0x1p-32f; // just under the smallest half; then cut off
+  uint32_t r;
+  asm("cvt.rz.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(fmaf(p1, below, -least)), "f"(fmaf(p0, below, -least)));
+  return r;
 }
 __device__ __forceinline__ void ca_cp16_all(uint32_t dst, const void* src) {
   asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
@@ -692,11 +705,13 @@ __global__ void __launch_bounds__(CA_THREADS, (ca_geom<FMT, D, NT>::BLOCKS_PER_S
         }
 #pragma unroll
         for (int k = 0; k < 2; ++k) {
-          const uint32_t w = dd_pack2<TP>(p[2 * k], p[2 * k + 1]);
-          pb[nt][k] = ca_transpose(w);
           if (geo::PAIR) {
+            const uint32_t w = ca_first_part<TP>(p[2 * k], p[2 * k + 1]);
             const float2 had = dd_unpack2<TP>(w);
+            pb[nt][k] = ca_transpose(w);
             pr[nt][k] = ca_transpose(dd_pack2<TP>(p[2 * k] - had.x, p[2 * k + 1] - had.y));
+          } else {
+            pb[nt][k] = ca_transpose(dd_pack2<TP>(p[2 * k], p[2 * k + 1]));
           }
         }
       }

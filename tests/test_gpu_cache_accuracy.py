@@ -65,3 +65,33 @@ def test_keys_of_the_smallest_exponent_count(dd, d, G):
     want_lse = ref.attention(f64(q), raw, table.numpy(), lens, "e4m3", T)[1]
     assert np.ptp(want_lse - np.log(np.array(lens))[:, None, None]) > 0.05              # scores that are not all zero
     check_attn(out, lse, q, raw, table, lens, "e4m3", "bf16", T)
+
+
+@pytest.mark.parametrize("lens,M,G,Tq,fmt", [([50, 7], 0, 4, 1, "bf16"), ([50, 7], 0, 4, 2, "fp16"), ([600], 0, 16, 1, "bf16"), ([600], 0, 4, 1, "fp16"),
+                                             ([3000, 40], 1200, 4, 1, "bf16"), ([3000, 40], 1200, 12, 2, "fp16")])
+def test_infinite_values_that_are_seen_stay_infinite(dd, lens, M, G, Tq, fmt):
+    """A value of +inf or -inf under any positive weight makes that channel +inf or -inf, both make it NaN, and the other
+    channels do not notice. Weights down to 2^-12 of the largest."""
+    gen = torch.Generator().manual_seed(sum(lens) + G)
+    d, T = 128, 16
+    cache, raw, table, q = make_attn(dd, gen, lens, 1, G, d, T, fmt, fmt, Tq, poison=False)
+    if M:                                                           # a wide table: the flat list and its joining kernel
+        table = torch.cat([table, torch.zeros(len(lens), M - table.shape[1], dtype=torch.int32)], 1)
+        cache = dd.PagedCache(cache.data, table.cuda(), cache_format=cache.cache_format, head_dim=d, page_tokens=T)
+    kv = ref.decode_pages(raw, fmt, T, d)
+    for b, n in enumerate(lens):
+        for at, channel, v in ((0, 3, np.inf), (n // 2, 3, np.inf), (1, 9, -np.inf), (n - Tq - 1, 70, np.inf), (0, 70, -np.inf), (2, 100, np.nan)):
+            kv[table[b, at // T], 0, 1, at % T, channel] = v
+    raw = ref.encode_pages(kv, fmt)
+    cache.data.copy_(torch.from_numpy(raw).cuda())
+    scale = 0.1 / np.sqrt(d)                                        # scores within about +-2
+    out, lse = run_attn(cache, q, lens, 0, scale)
+    with np.errstate(invalid="ignore"):
+        want = ref.attention(f64(q), raw, table.numpy(), lens, fmt, T, 0, scale)[0]
+    g = f64(out)
+    assert np.all(np.isposinf(want[..., 3])) and np.all(np.isneginf(want[..., 9])) and np.all(np.isnan(want[..., (70, 100)]))
+    assert np.array_equal(np.isposinf(g), np.isposinf(want)) and np.array_equal(np.isneginf(g), np.isneginf(want))
+    assert np.array_equal(np.isnan(g), np.isnan(want))
+    fine = np.isfinite(want)
+    assert np.abs(g[fine] - want[fine]).max() < 0.02
+    assert cache.device_error() == (0, 0)
