@@ -21,10 +21,11 @@
 // e4m3 pages: codes are exact as halves, so both products run as half MMAs on the codes. The power-of-two scale of a key
 // multiplies its scores; the scale of a value is added to the exponent of its weight: with w = z + log2(scale of v) the
 // running reference is the maximum of w, P = 2^(w - ref) multiplies codes, and the denominator sums 2^(z - ref).
-// The reference moves only when a weight exceeds it by 2^8 (one vote per tile instead of a reduction), so P is at most
-// 2^14 after a factor 2^6 that keeps small weights out of the half's subnormals (a weight 2^-20 of the reference is still
-// normal). Queries are multiplied by a power of two per row to fill the half's range: exact for every element above
-// 2^-28 of the row's largest.
+// The reference moves only when a weight exceeds it by 2^8 (one vote per tile instead of a reduction). Halves take a factor
+// 2^6 that keeps small weights out of their subnormals (P at most 2^14; a weight 2^-20 of the reference is still normal),
+// bf16 one of 2^-8 (P at most 1, as in a plain soft-max). Scales of e4m3 values from 2^-96 to 2^100 keep the denominator in
+// range. Queries over e4m3 pages are multiplied by a power of two per row to fill the half's range: exact for every element
+// above 2^-28 of the row's largest.
 //
 // Rounding. A weight enters the second product as two 16-bit parts, its value cut off and the rounded rest (an MMA takes both
 // operands in one type): off by 2^-16 relative at most for bf16 pages, by 2^-22 for half pages and half queries, so that the
@@ -55,7 +56,6 @@ constexpr int CA_THREADS = CA_WARPS * 32;
 constexpr int CA_UNIT_COST = 3;              // empty places behind a unit in the flat list
 constexpr int CA_WHOLE = 8;                  // a unit of at most so many tiles is not cut: it belongs to the run it begins in
 constexpr int CA_MAX_CLUSTER = 8;
-constexpr float CA_HEADROOM = 6.f;           // log2 of the factor on P
 constexpr float CA_LAZY = 8.f;               // how far (log2) a weight may exceed the reference
 constexpr float CA_NONE = -3.0e38f;          // reference before any token: every finite score exceeds it
 
@@ -81,6 +81,9 @@ struct ca_geom {
   static constexpr int RING_BUDGET = (BLOCKS_PER_SM == 2 ? 106 : 212) * 1024;
   static constexpr int STAGES_ = RING_BUDGET / (CA_WARPS * SLOT_BYTES);
   static constexpr int STAGES = STAGES_ > 8 ? 8 : STAGES_;
+  // log2 of the factor on P: halves are lifted out of their subnormals; bf16 weights end at 1, so that large values do not
+  // leave the range of the fp32 sums.
+  static constexpr float HEADROOM = FMT == 0 ? -CA_LAZY : 6.f;
   // Weights as two 16-bit parts (see "Rounding").
   static constexpr bool PAIR = FMT != 2;
   // A second copy of the tile's code without masks and questions: 131 -> 111 us (128 query heads, 8 x 32K tokens e4m3), 63 -> 58
@@ -674,8 +677,8 @@ __global__ void __launch_bounds__(CA_THREADS, (ca_geom<FMT, D, NT>::BLOCKS_PER_S
         for (int e = 0; e < 4; ++e) {
           x[e] = z[nt][e] - from[nt][e & 1];
           y[e] = FP8 ? x[e] + (e < 2 ? vex0 : vex1) : x[e];
-          above |= y[e] > CA_LAZY + CA_HEADROOM;
-          if (FP8) above |= x[e] > CA_LAZY + CA_HEADROOM + 96.f;
+          above |= y[e] > CA_LAZY + geo::HEADROOM;
+          if (FP8) above |= x[e] > CA_LAZY + geo::HEADROOM + 96.f;
         }
         if (__any_sync(0xffffffffu, above)) {
 #pragma unroll
@@ -684,7 +687,7 @@ __global__ void __launch_bounds__(CA_THREADS, (ca_geom<FMT, D, NT>::BLOCKS_PER_S
             top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 4));
             top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 8));
             top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 16));
-            top = fmaxf(top - CA_HEADROOM, from[nt][c]);
+            top = fmaxf(top - geo::HEADROOM, from[nt][c]);
             const float fix = ca_exp2(from[nt][c] - top);
             from[nt][c] = top;
             sum[nt][c] *= fix;

@@ -95,3 +95,16 @@ def test_infinite_values_that_are_seen_stay_infinite(dd, lens, M, G, Tq, fmt):
     fine = np.isfinite(want)
     assert np.abs(g[fine] - want[fine]).max() < 0.02
     assert cache.device_error() == (0, 0)
+
+
+@pytest.mark.parametrize("lens,G,Tq,power", [([300, 5], 4, 1, 117), ([300, 5], 16, 2, 117), ([9000, 40], 4, 1, 113), ([300, 5], 4, 1, -100)])
+def test_values_near_the_ends_of_bf16(dd, lens, G, Tq, power):
+    """The weighted sum stays within fp32 as long as the number of tokens times the largest value does."""
+    gen = torch.Generator().manual_seed(sum(lens) + G)
+    cache, raw, table, q = make_attn(dd, gen, lens, 1, G, 128, 16, "bf16", "bf16", Tq, poison=False)
+    kv = ref.decode_pages(raw, "bf16", 16, 128)
+    kv[:, :, 1] *= 2.0 ** power                                     # 2^117: sums of 300 values reach 2^127.6 at most
+    raw = ref.encode_pages(kv, "bf16")
+    cache.data.copy_(torch.from_numpy(raw).cuda())
+    out, lse = run_attn(cache, q, lens)
+    check_attn(out, lse, q, raw, table, lens, "bf16", "bf16", 16)
