@@ -370,12 +370,12 @@ class PagedCache:
             self._made_on, self._made = made_on.cuda_stream, made_on.record_event()
 
     def _stream(self, s) -> int:
-        s = _stream(s)
-        if self._made is not None and s != self._made_on and not torch.cuda.is_current_stream_capturing():
-            if not self._made.query():
-                _torch_stream(s, self._device).wait_event(self._made)
-            else:
+        s, made = _stream(s), self._made
+        if made is not None and s != self._made_on and not torch.cuda.is_current_stream_capturing():
+            if made.query():
                 self._made = None
+            else:
+                _torch_stream(s, self._device).wait_event(made)
         return s
 
     @classmethod

@@ -10,9 +10,9 @@
 // costs besides its tiles. Every warp of a grid that fills the device once takes an equal run of the list; lengths are
 // read on the device, so the launch does not depend on them (a captured graph may be replayed with other lengths). Units
 // of at most 8 tiles are not cut. A warp works alone: it keeps a ring of half tiles (K or V) in flight with 16-byte
-// cp.async, and the ring runs on across the borders of units. A copy instruction takes 512 contiguous bytes (whole 128-byte lines; fragments fetched straight from
-// global memory touch half lines and ran at half the rate), and the chunks of a row are placed by row ^ chunk, so that
-// ldmatrix reads them without bank conflicts: K as it lies, V transposed.
+// cp.async, and the ring runs on across the borders of units. A copy instruction takes 512 contiguous bytes (whole 128-byte
+// lines; fragments fetched straight from global memory touch half lines and ran at half the rate), and the chunks of a row are
+// placed by row ^ chunk, so that ldmatrix reads them without bank conflicts: K as it lies, V transposed.
 //
 // Arithmetic, with the up-to-8 query rows of a KV head as the N = 8 columns of the MMA (two column tiles for up to 16
 // rows, several row tiles beyond):
