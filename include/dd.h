@@ -62,6 +62,7 @@ extern "C" {
 #define DD_CACHE_BF16 0             /* formats of a KV page, described at dd_cache */
 #define DD_CACHE_FP16 1
 #define DD_CACHE_E4M3 2             /* 8-bit floating point, one power-of-two scale per token and head */
+#define DD_CACHE_INT4 4             /* 4-bit whole numbers, an e4m3 scale per 16 elements, a power of two per token and head */
 
 #define DD_SELECT_AUTO         0    /* fused cluster kernel when the request fits, else the two-kernel path */
 #define DD_SELECT_TWO_KERNELS  1    /* scoring kernel + top-k kernel with logits in global scratch */
@@ -352,6 +353,11 @@ typedef struct dd_rope {
  *   DD_CACHE_BF16 / FP16   K [page_tokens][head_dim], then V [page_tokens][head_dim]
  *   DD_CACHE_E4M3          the codes of K, the codes of V (same order, one byte each), the exponent bytes of K
  *                          [page_tokens], the exponent bytes of V; a value is code * 2^(byte - 127)
+ *   DD_CACHE_INT4          page_tokens / 16 tiles of 16 tokens (token t of a tile), d = head_dim, two codes to a byte with the lower
+ *                          half first: codes of K [t][d]; codes of V [t / 8][d / 8 parts][t % 8 / 2][t % 2][d / 8 elements]; scales
+ *                          of K [t][d / 16], of V [d / 16][t], each an e4m3 code; the exponent bytes of K [t], of V [t]. A value is
+ *                          (code - 8) * scale * 2^(byte - 127), 7 significant bits. Scales are written as 2^-4 or more, or
+ *                          as the NaN code (of smaller ones attention would round the values to multiples of 2^(byte - 134))
  * Page (block, head) starts at data + block * block_stride + head * head_stride (bytes, multiples of 16). A layer of the
  * method's store [B][Hkv][P][page] is such a pool: block = b * Hkv * P + p with block_stride = page bytes, head_stride =
  * P * page bytes, n_blocks = (B - 1) * Hkv * P + P. */
@@ -392,7 +398,9 @@ int dd_rope_apply(const dd_rope* rope, int head_dim, int n_tokens, const int* po
 /* Writes the K and V rows of n_tokens new tokens into their pages: token n belongs to request requests[n] and lands at
  * position positions[n] of it. DD_CACHE_E4M3: the exponent of a row is the smallest e >= -127 with which its largest
  * finite magnitude is at most 448 * 2^e, a code is the value times 2^-e (exact) rounded to nearest even; infinities and
- * NaN become the NaN code. With `rope` the keys are turned on the way (32 bits, rounded once, into the page), and with q /
+ * NaN become the NaN code. DD_CACHE_INT4: the same with 3136 * 2^e (7 * 448); the scale of 16 elements is their largest finite magnitude
+ * times 2^-e / 7 rounded to e4m3, at least 2^-4, and the NaN code where one of them is not finite; a code is 8 + the value times 2^-e /
+ * scale, rounded to nearest even, within [1, 15]. Codes, scales and exponents of turned keys are those of the 64-bit rotation. With `rope` the keys are turned on the way (32 bits, rounded once, into the page), and with q /
  * q_out the queries of the same tokens are turned in the same launch. A negative position is padding: nothing of that
  * token is written. A request, page or block out of range is reported in status and the token skipped. Two tokens of one
  * call must not name the same place: which of them the page then holds (in parts) is not defined.
@@ -426,6 +434,52 @@ int dd_cache_read(const dd_cache* cache, const int* idx, int k_pages, void* out,
 size_t dd_cache_decode_attn_workspace(int n_q_heads, int n_kv_heads, int head_dim, int n_q_tokens);
 int dd_cache_decode_attn(const dd_cache* cache, int n_q_tokens, const dd_rows* q, const int* ctx_len, const dd_rows* out,
                          float* out_lse, int window, float scale, void* workspace, size_t workspace_bytes, void* stream);
+
+/* ---- pages chosen for each query token ----------------------------------------------------------------------------- */
+
+/* The path above selects once per request and step and gathers before it attends (Sec. 4.1, Sec. 5.4). Where the pages are on the
+ * device already, these calls select for every query token and KV head by itself and attend straight from the pool: a step's
+ * one or two tokens, or the tokens of a prompt chunk. Query token n belongs to request requests[n] (NULL: n_tokens / batch tokens of each in
+ * turn) and stands at positions[n]; it sees the positions up to its own. A negative position is padding.
+ *
+ * Landmarks live in an array of their own, [n_blocks][n_kv_heads] rows of dd_cache_landmark_bytes(): head_dim codes (signed bytes),
+ * one byte e + 64, 15 bytes of zeros. A landmark is the mean of the valid keys of the page (added in 64 bits), each channel times 2^-e rounded to
+ * nearest even, with e the smallest of [-64, 63] that keeps all of them within 127 (beyond 63 they are cut at 127; a channel that is not finite
+ * counts as 0). dd_cache_landmarks writes those of the pages that hold any of the last n_last tokens of a request (0: of all its pages).
+ * Call it after dd_cache_append; a page's landmark is that of the tokens it held then. */
+size_t dd_cache_landmark_bytes(int head_dim);
+int dd_cache_landmarks(const dd_cache* cache, const int* ctx_len, int n_last, void* landmarks, void* stream);
+
+/* The k_pages pages of each query token and KV head, ascending, -1 behind them where fewer are visible: the first first_pages and
+ * the last recent_pages visible ones (at least the token's own, whose landmark a chunk's later tokens have a part in), and the highest scores of the
+ * others; equal scores go to the lower page.
+ *   c        = the sum of the group's query rows (in 64 bits), as whole numbers within 127 like a landmark's (e not below -120)
+ *   score[p] = <c, codes of the landmark of p> * 2^e: exact in fp32
+ * Padding, and a token whose request or position is out of range (reported in status), gets -1 throughout; a table entry out of range is reported and
+ * its page scores 0.
+ *   q          dev [n_tokens][n_q_heads][head_dim], bf16 or half whatever the format of the pages (which are not read)
+ *   out_idx    dev int32 [n_tokens][n_kv_heads][k_pages], written
+ *   workspace  dev, dd_cache_select_workspace() bytes (up to 64 MiB; more for contexts above 512K pages), 16-byte aligned; one per call that may run at the same time */
+size_t dd_cache_select_workspace(int n_tokens, int n_kv_heads, int max_pages);
+int dd_cache_select(const dd_cache* cache, int n_tokens, const int* positions, const int* requests, const dd_rows* q,
+                    const void* landmarks, int k_pages, int first_pages, int recent_pages, int* out_idx, void* workspace,
+                    size_t workspace_bytes, void* stream);
+
+/* Attention of every query token over the tokens up to its own position in the pages listed for it:
+ *   z[i] = <q[n, h, :], K[i, h / G, :]> * scale, i over the tokens of pages idx[n][h / G][0 .. k_pages)   scale 0 = 1 / sqrt(head_dim)
+ *   out[n, h, :] = sum softmax(z) * V;  out_lse = ln sum exp(z)
+ * Entries in any order; -1 is no page, one behind the token's own page has nothing to see, one out of range is reported in status and passed over; a
+ * page listed twice counts twice. At most as many entries are looked at as there are pages up to the token's own: those in front. A token
+ * that sees nothing gives zeros and -inf. The rows of padding, and of a token whose request or position is out of range (reported), stay as they are.
+ * A table entry out of range is reported and its page reads as zeros.
+ *   q, out     dev [n_tokens][n_q_heads][head_dim], one dtype (that of a 16-bit cache); out may be q itself
+ *   idx        dev int32 [n_tokens][n_kv_heads][k_pages]
+ *   out_lse    dev fp32 [n_tokens][n_q_heads] or NULL
+ *   workspace  dev, dd_cache_sparse_attn_workspace() bytes, 16-byte aligned; one per call that may run at the same time */
+size_t dd_cache_sparse_attn_workspace(int n_q_heads, int n_kv_heads, int head_dim);
+int dd_cache_sparse_attn(const dd_cache* cache, int n_tokens, const int* positions, const int* requests, const dd_rows* q,
+                         const int* idx, int k_pages, const dd_rows* out, float* out_lse, float scale, void* workspace,
+                         size_t workspace_bytes, void* stream);
 
 #ifdef __cplusplus
 }

@@ -41,6 +41,7 @@ DD_FP16 = 1
 DD_CACHE_BF16 = 0
 DD_CACHE_FP16 = 1
 DD_CACHE_E4M3 = 2
+DD_CACHE_INT4 = 4
 DD_ROPE_HALF = 0
 DD_ROPE_INTERLEAVED = 1
 DD_ROPE_NONE = 0
@@ -57,6 +58,8 @@ EXPORTS = [
     "dd_fetch_missing_from_host", "dd_get_merged_indices", "dd_miss_stats", "dd_probe_attn_loads", "dd_probe_select_loads",
     "dd_trace_begin", "dd_trace_end", "dd_trace_read", "dd_decode_step_host", "dd_last_device_error",
     "dd_gather_stats", "dd_set_bulk_wait", "dd_test_pick_cluster", "dd_test_stage_plan", "dd_test_attn_split",
+    "dd_cache_landmark_bytes", "dd_cache_landmarks", "dd_cache_select_workspace", "dd_cache_select",
+    "dd_cache_sparse_attn_workspace", "dd_cache_sparse_attn",
     "dd_cache_page_bytes", "dd_rope_turns", "dd_rope_apply", "dd_cache_append", "dd_cache_read",
     "dd_cache_decode_attn_workspace", "dd_cache_decode_attn",
 ]
@@ -167,6 +170,12 @@ def _load() -> C.CDLL:
     lib.dd_cache_decode_attn_workspace.argtypes = [ip, ip, ip, ip]
     lib.dd_cache_decode_attn_workspace.restype = C.c_size_t
     lib.dd_cache_decode_attn.argtypes = [cache, ip, rows, vp, rows, vp, ip, C.c_float, vp, C.c_size_t, vp]
+    for name, n in (("dd_cache_landmark_bytes", 1), ("dd_cache_select_workspace", 3), ("dd_cache_sparse_attn_workspace", 3)):
+        getattr(lib, name).argtypes = [ip] * n
+        getattr(lib, name).restype = C.c_size_t
+    lib.dd_cache_landmarks.argtypes = [cache, vp, ip, vp, vp]
+    lib.dd_cache_select.argtypes = [cache, ip, vp, vp, rows, vp, ip, ip, ip, vp, vp, C.c_size_t, vp]
+    lib.dd_cache_sparse_attn.argtypes = [cache, ip, vp, vp, rows, vp, ip, rows, vp, C.c_float, vp, C.c_size_t, vp]
     return lib
 
 
@@ -249,6 +258,9 @@ _rope_apply = _handle("dd_rope_apply", _P, _I, _I, _P, _P, _P, _P, _P, _I, _P)
 _cache_append = _handle("dd_cache_append", _P, _I, _P, _P, _P, _P, _P, _P, _P, _P)
 _cache_read = _handle("dd_cache_read", _P, _P, _I, _P, _I, _P)
 _cache_decode_attn = _handle("dd_cache_decode_attn", _P, _I, _P, _P, _P, _P, _I, C.c_float, _P, C.c_size_t, _P)
+_cache_landmarks = _handle("dd_cache_landmarks", _P, _P, _I, _P, _P)
+_cache_select = _handle("dd_cache_select", _P, _I, _P, _P, _P, _P, _I, _I, _I, _P, _P, C.c_size_t, _P)
+_cache_sparse_attn = _handle("dd_cache_sparse_attn", _P, _I, _P, _P, _P, _P, _I, _P, _P, C.c_float, _P, C.c_size_t, _P)
 
 
 def _rows(t, name: str, head_dim: int, tokens: int):
@@ -438,18 +450,91 @@ class PagedCache:
             if need is None:
                 need = max(16, lib.dd_cache_decode_attn_workspace(Hq, self._heads, self.head_dim, Tq))
                 self._workspace_bytes[(Hq, Tq)] = need
-            if stream is None:
-                workspace = torch.empty(need, dtype=torch.uint8, device=self._device)
-            else:
-                with torch.cuda.stream(_torch_stream(stream, self._device) if isinstance(stream, int) else stream):
-                    workspace = torch.empty(need, dtype=torch.uint8, device=self._device)
+            workspace = self._take(need, stream)
         else:
-            if not workspace.is_contiguous():
-                raise _invalid("workspace must be dense")
-            need = workspace.numel() * workspace.element_size()
+            need = self._given(workspace)
         rc = _cache_decode_attn(self._addr, Tq, rq, _ints(ctx_len, "ctx_len", (b,)), ro,
                                 None if out_lse is None else out_lse.data_ptr(), window, scale, workspace.data_ptr(), need,
                                 self._stream(stream))
+        if rc != DD_OK:
+            _raise_last(rc)
+
+    def _take(self, need: int, stream) -> torch.Tensor:
+        """A workspace from torch's allocator on the stream of the call."""
+        if stream is None:
+            return torch.empty(need, dtype=torch.uint8, device=self._device)
+        with torch.cuda.stream(_torch_stream(stream, self._device) if isinstance(stream, int) else stream):
+            return torch.empty(need, dtype=torch.uint8, device=self._device)
+
+    @staticmethod
+    def _given(workspace) -> int:
+        if not workspace.is_contiguous():
+            raise _invalid("workspace must be dense")
+        return workspace.numel() * workspace.element_size()
+
+    def new_landmarks(self) -> torch.Tensor:
+        """Zeroed landmarks for every (block, KV head) of the pool: uint8 [n_blocks, Hkv, dd_cache_landmark_bytes()]."""
+        return torch.zeros(self.c.n_blocks, self._heads, lib.dd_cache_landmark_bytes(self.head_dim), dtype=torch.uint8, device=self._device)
+
+    def _check_landmarks(self, landmarks) -> int:
+        shape = (self.c.n_blocks, self._heads, self.head_dim + 16)
+        if landmarks.dtype is not torch.uint8 or landmarks.shape != shape or not landmarks.is_contiguous():
+            raise _invalid(f"landmarks must be a dense uint8 tensor {shape}, not {landmarks.dtype} {tuple(landmarks.shape)}")
+        return landmarks.data_ptr()
+
+    def update_landmarks(self, landmarks, ctx_len, *, n_last=0, stream=None):
+        """Landmarks of the pages that hold any of the last n_last tokens of every request (0: of all its pages); ctx_len [batch]
+        int32, the appended tokens counted in."""
+        if not 0 <= n_last < 1 << 31:
+            raise _invalid(f"n_last must be in [0, 2^31), not {n_last}")
+        rc = _cache_landmarks(self._addr, _ints(ctx_len, "ctx_len", (self._batch,)), n_last, self._check_landmarks(landmarks), self._stream(stream))
+        if rc != DD_OK:
+            _raise_last(rc)
+
+    def _listed(self, positions, idx, requests):
+        """(tokens, pages a token, address of positions, of requests, of idx) of a call on listed pages."""
+        n = positions.shape[0] if positions.dim() == 1 else -1
+        if idx.dim() != 3 or idx.shape[2] < 1:
+            raise _invalid(f"idx must be [tokens, {self._heads}, k], not {tuple(idx.shape)}")
+        return (n, idx.shape[2], _ints(positions, "positions", (n,)), None if requests is None else _ints(requests, "requests", (n,)),
+                _ints(idx, "idx", (n, self._heads, idx.shape[2])))
+
+    def select(self, q, landmarks, positions, idx, requests=None, *, first_pages=0, recent_pages=1, workspace=None, stream=None):
+        """The pages of every query token and KV head into idx [N, Hkv, k] int32 (ascending, -1 behind them): the first first_pages,
+        the last recent_pages, and those with the highest scores. q [N, Hq, d]; positions, requests [N] int32 as for append."""
+        n, k, p, r, i = self._listed(positions, idx, requests)
+        rq = _rows(q, "q", self.head_dim, n)
+        if workspace is None:
+            need = max(16, lib.dd_cache_select_workspace(n, self._heads, self.c.max_pages))
+            workspace = self._take(need, stream)
+        else:
+            need = self._given(workspace)
+        rc = _cache_select(self._addr, n, p, r, rq, self._check_landmarks(landmarks), k, first_pages, recent_pages, i,
+                           workspace.data_ptr(), need, self._stream(stream))
+        if rc != DD_OK:
+            _raise_last(rc)
+
+    def sparse_attn(self, q, idx, positions, out, out_lse=None, requests=None, *, scale=0.0, workspace=None, stream=None):
+        """Attention of every query token over the pages idx [N, Hkv, k] listed for it, up to its own position. q, out [N, Hq, d];
+        positions, requests [N] int32 as for append; out_lse [N, Hq] float32. Without a workspace the call takes one from torch's
+        allocator on the stream it runs on."""
+        n, k, p, r, i = self._listed(positions, idx, requests)
+        if q.shape != out.shape:
+            raise _invalid(f"q and out must have one shape, not {tuple(q.shape)} and {tuple(out.shape)}")
+        rq, ro = _rows(q, "q", self.head_dim, n), _rows(out, "out", self.head_dim, n)
+        heads = q.shape[1]
+        if out_lse is not None and (out_lse.dtype is not torch.float32 or out_lse.shape != (n, heads) or not out_lse.is_contiguous()):
+            raise _invalid(f"out_lse must be a dense float32 tensor {(n, heads)}")
+        if workspace is None:
+            need = self._workspace_bytes.get(heads)
+            if need is None:
+                need = max(16, lib.dd_cache_sparse_attn_workspace(heads, self._heads, self.head_dim))
+                self._workspace_bytes[heads] = need
+            workspace = self._take(need, stream)
+        else:
+            need = self._given(workspace)
+        rc = _cache_sparse_attn(self._addr, n, p, r, rq, i, k, ro, None if out_lse is None else out_lse.data_ptr(), scale,
+                                workspace.data_ptr(), need, self._stream(stream))
         if rc != DD_OK:
             _raise_last(rc)
 

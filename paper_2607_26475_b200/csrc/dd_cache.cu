@@ -53,6 +53,7 @@ extern "C" size_t dd_cache_page_bytes(int format, int page_tokens, int head_dim)
   if (page_tokens < 16 || page_tokens > 256 || (page_tokens & (page_tokens - 1))) return 0;
   if (format == DD_CACHE_BF16 || format == DD_CACHE_FP16) return (size_t)4 * page_tokens * head_dim;
   if (format == DD_CACHE_E4M3) return (size_t)2 * page_tokens * head_dim + 2 * page_tokens;
+  if (format == DD_CACHE_INT4) return (size_t)page_tokens / 16 * dd_int4_tile_bytes(head_dim);
   return 0;
 }
 
@@ -227,8 +228,71 @@ __global__ void __launch_bounds__(CR_THREADS) dd_cache_read_kernel(dd_cache_view
   }
 }
 
+// The same for 4-bit pages. A tile is one run of 18 d + 32 bytes; it goes through shared memory, where a lane finds the codes,
+// scales and exponents of the 8 elements it writes in one 16-byte store.
+template <typename T, int D>
+__global__ void __launch_bounds__(CR_THREADS) dd_cache_read_int4_kernel(dd_cache_view c, const int* __restrict__ idx,
+                                                                       char* __restrict__ out, int k_pages, long long n_tiles) {
+  constexpr int TILE = dd_int4_tile_bytes(D), CHUNKS = TILE / 16;
+  __shared__ __align__(16) unsigned char cr_tile[CR_THREADS / 32][TILE];
+  const int lane = threadIdx.x & 31, tile_shift = c.page_shift - 4;
+  unsigned char* own = cr_tile[threadIdx.x >> 5];
+  const long long n_warps = (long long)gridDim.x * (CR_THREADS / 32);
+  dd_grid_dependency_wait();
+  for (long long item = (long long)(threadIdx.x >> 5) * gridDim.x + blockIdx.x; item < n_tiles; item += n_warps) {
+    const long long entry = item >> tile_shift;
+    const int tile = (int)(item - (entry << tile_shift));
+    const long long bg = (entry >> 31) == 0 ? (long long)((unsigned)entry / (unsigned)k_pages) : entry / k_pages;
+    const int j = (int)(entry - bg * k_pages);
+    const int b = (int)((unsigned)bg / (unsigned)c.n_kv_heads), g = (int)bg - b * c.n_kv_heads;
+    const int p = idx[entry];
+    int blk = -1;
+    if (p < 0 || p >= c.max_pages) {
+      if (lane == 0) dd_status(c.status, p);
+    } else {
+      blk = c.table[b * c.table_stride + p];
+      if (blk < 0 || blk >= c.n_blocks) {
+        if (lane == 0) dd_status(c.status, blk);
+        blk = -1;
+      }
+    }
+    const char* src = c.data + (blk < 0 ? 0 : blk * c.block_stride + g * c.head_stride) + tile * TILE;
+    uint4 r[(CHUNKS + 31) / 32];
+#pragma unroll
+    for (int i = 0; i < (CHUNKS + 31) / 32; ++i) {
+      r[i] = make_uint4(0u, 0u, 0u, 0u);             // scales of zero: all zeros
+      if (blk >= 0 && i * 32 + lane < CHUNKS) r[i] = dd_ld_stream(src + (i * 32 + lane) * 16);
+    }
+    __syncwarp();
+#pragma unroll
+    for (int i = 0; i < (CHUNKS + 31) / 32; ++i)
+      if (i * 32 + lane < CHUNKS) *reinterpret_cast<uint4*>(own + (i * 32 + lane) * 16) = r[i];
+    __syncwarp();
+    char* dst = out + (((bg * 2 * k_pages + j) << tile_shift) + tile) * (16LL * 2 * D);
+    const long long v_off = ((long long)k_pages << tile_shift) * (16LL * 2 * D);
+#pragma unroll
+    for (int kv = 0; kv < 2; ++kv)
+#pragma unroll
+      for (int i = 0; i < 16 * D / 256; ++i) {
+        const int t = (i * 32 + lane) / (D / 8), chunk = (i * 32 + lane) % (D / 8);
+        const uint32_t w = *reinterpret_cast<const uint32_t*>(own + (kv ? dd_int4_v_at<D>(t, chunk) : dd_int4_k_at<D>(t, chunk)));
+        uint32_t s2, unused;
+        dd_e4m3x4_to_half(own[kv ? dd_int4_vs_at<D>(t, chunk >> 1) : dd_int4_ks_at<D>(t, chunk >> 1)], s2, unused);
+        // scale * 2^(byte - 127) in two factors: the second is a power of two
+        const float s = dd_unpack2<__half>(s2).x, by = dd_two_to_byte(own[18 * D + 16 * kv + t]);
+        uint32_t o[4];
+#pragma unroll
+        for (int q = 0; q < 4; ++q)
+          o[q] = dd_pack2<T>((float)((int)(w >> (8 * q) & 15u) - 8) * s * by, (float)((int)(w >> (8 * q + 4) & 15u) - 8) * s * by);
+        dd_st_v4(dst + (kv ? v_off : 0) + i * 512 + lane * 16, make_uint4(o[0], o[1], o[2], o[3]));
+      }
+  }
+}
+
 template <int D>
 static const void* cr_kernel_of(int format, int dtype, bool on_host) {
+  if (format == DD_CACHE_INT4)
+    return dtype == DD_BF16 ? (const void*)dd_cache_read_int4_kernel<__nv_bfloat16, D> : (const void*)dd_cache_read_int4_kernel<__half, D>;
   if (format != DD_CACHE_E4M3) return (const void*)dd_cache_read_kernel<DD_CACHE_BF16, __nv_bfloat16, D, false>;   // a copy of 16-bit words
   if (dtype == DD_BF16)
     return on_host ? (const void*)dd_cache_read_kernel<DD_CACHE_E4M3, __nv_bfloat16, D, true>

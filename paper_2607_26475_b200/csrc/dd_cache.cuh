@@ -34,6 +34,22 @@ dd_cache_view dd_make_view(const dd_cache* c, const char* data_dev);
 // A launch whose failure is reported here and left behind nowhere (the runtime's last error is cleared).
 int dd_launch(const char* who, const cudaLaunchConfig_t* cfg, const void* kernel, void** args);
 
+// A tile of a 4-bit page: 16 tokens of one KV head. Offsets within it: codes of K 0, of V 8 d, scales of K 16 d, of V 17 d, exponent
+// bytes of K 18 d, of V 18 d + 16. A chunk is 8 elements, 4 bytes of codes. V is placed so that the 32 lanes of a warp that read it as
+// an MMA operand take neighbouring 16 (head_dim 128) or 8 bytes: lane 4 i + j the part i of the tokens 2j, 2j + 1 (then + 8).
+#ifdef __CUDACC__
+#define DD_HD __host__ __device__
+#else
+#define DD_HD
+#endif
+DD_HD constexpr int dd_int4_tile_bytes(int d) { return 18 * d + 32; }
+template <int D> DD_HD constexpr int dd_int4_k_at(int t, int chunk) { return t * (D / 2) + chunk * 4; }
+template <int D> DD_HD constexpr int dd_int4_v_at(int t, int chunk) {
+  return 8 * D + (((t >> 3) * 8 + chunk * 64 / D) * 4 + (t & 7) / 2) * (D / 8) + (t & 1) * (D / 16) + (chunk * 64 % D) / 16;
+}
+template <int D> DD_HD constexpr int dd_int4_ks_at(int t, int group) { return 16 * D + t * (D / 16) + group; }
+template <int D> DD_HD constexpr int dd_int4_vs_at(int t, int group) { return 17 * D + group * 16 + t; }
+
 static inline int dd_log2i(int x) { int s = 0; while ((1 << s) < x) ++s; return s; }
 
 #ifdef __CUDACC__
@@ -85,6 +101,13 @@ __device__ __forceinline__ int dd_e4m3_exponent_byte(float amax) {
 }
 __device__ __forceinline__ float dd_two_to_byte(int byte) {      // 2^(byte - 127), byte 0 included (a subnormal)
   return __uint_as_float(byte ? (uint32_t)byte << 23 : 0x00400000u);
+}
+
+// Exponent byte of a 4-bit row: the smallest e >= -127 with amax <= 3136 * 2^e, plus 127. 3136 = 7 * 448 = 1.53125 * 2^11.
+__device__ __forceinline__ int dd_int4_exponent_byte(float amax) {
+  const uint32_t bits = __float_as_uint(amax);
+  const int e = (int)(bits >> 23) - 127 - 11 + ((bits & 0x7fffffu) > 0x440000u ? 1 : 0);
+  return (e < -127 ? -127 : e) + 127;
 }
 
 // One warp brings 16 tokens of an e4m3 page in host memory to two runs of 16-bit rows: K codes at k_run, V codes at v_run

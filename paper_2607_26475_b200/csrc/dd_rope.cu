@@ -24,7 +24,7 @@
 namespace {
 
 constexpr int RP_THREADS = 256;
-constexpr int RP_BLOCKS = 3;         // per SM, by registers
+constexpr int rp_blocks(int fmt) { return fmt == DD_CACHE_INT4 ? 2 : 3; }      // per SM, by registers
 constexpr int RP_BATCH = 4;          // heads whose loads are in flight together
 
 struct rp_rows {
@@ -57,12 +57,141 @@ __device__ __forceinline__ void rp_angle(double turns, int pos, float amplitude,
   s = fmaf(c0, lo, s0) * amplitude;
 }
 
+// ---- 4-bit rows
+// A row is 2^e times groups of 16 whole numbers times their group's scale; what a lane holds of it is two chunks of 8 elements, and
+// the other half of a chunk's group may lie with another lane (rp_mate). The scale comes from one division, a code from a
+// product with the scale's inverse and one correction, which makes quotients that can be represented exact: ties fall as in the definition.
+// A turned element is known in 32 bits to 2^-21.2 of its pair's magnitude (sine and cosine 2^-22 each, product and sum), that is to
+// RP_KNOWN of the row's largest element. Where that leaves a border within reach of the row's exponent, of a scale or of a code (a few
+// rows in a thousand), the row is turned again in 64 bits, so that the bytes written are those of the 64-bit rotation.
+constexpr float RP_KNOWN = 0x1.8p-21f;
+
+// Lane of the group and slot (0 or 1) that hold chunk `chunk` of a row.
+__device__ __forceinline__ void rp_mate(int chunk, int rot16, bool interleaved, int& lane, int& slot) {
+  if (interleaved || chunk >= 2 * rot16) {
+    lane = chunk >> 1;
+    slot = chunk & 1;
+  } else {
+    slot = chunk >= rot16;
+    lane = chunk - slot * rot16;
+  }
+}
+
+// Magnitude for a row's scale: zero where it is not finite.
+__device__ __forceinline__ float rp_finite(float v) { const float m = fabsf(v); return m <= 3.4028234e38f ? m : 0.f; }
+
+// Is s, known to eps, within reach of a point where its rounding to 4 significant bits changes?
+__device__ __forceinline__ bool rp_near_scale(float s, float eps) {
+  const int rest = (int)(__float_as_uint(s) & 0xfffffu) - 0x80000;
+  return fabsf((float)rest) * (__uint_as_float(__float_as_uint(s) & 0x7f800000u) * 0x1p-23f) <= eps;
+}
+__device__ __forceinline__ float rp_round_e4m3(float v, unsigned& code) {
+  code = dd_float_to_e4m3x4(v, v, 0.f, 0.f) & 0xffu;
+  uint32_t h, unused;
+  dd_e4m3x4_to_half(code, h, unused);
+  return dd_unpack2<__half>(h).x;
+}
+
+// The two chunks (16 elements) of a turned row again, in 64 bits.
+template <typename T, int D>
+__device__ __noinline__ void rp_turn_exact(const uint32_t* raw, const double* turns, int pos, float amplitude, int j, bool interleaved, double* x) {
+  for (int i = 0; i < 8; ++i) {
+    double a = turns[8 * j + i] * (double)pos, sn, cs;
+    a -= rint(a);
+    sincospi(2. * a, &sn, &cs);
+    sn *= (double)amplitude;
+    cs *= (double)amplitude;
+    const int iu = interleaved ? 2 * i : i, iw = interleaved ? 2 * i + 1 : 8 + i;
+    const float2 u2 = dd_unpack2<T>(raw[iu >> 1]), w2 = dd_unpack2<T>(raw[iw >> 1]);
+    const double u = (iu & 1) ? u2.y : u2.x, w = (iw & 1) ? w2.y : w2.x;
+    x[iu] = u * cs - w * sn;
+    x[iw] = w * cs + u * sn;
+  }
+}
+
+// Scales (as e4m3 codes) and codes (chunk by chunk, 8 to a word) of a row x whose exponent byte is `byte`: y = x * 2^(127 - byte).
+// Returns whether errors of up to eps in y may have decided anything otherwise.
+__device__ __forceinline__ bool rp_int4_codes(float (&y)[16], float eps, const int (&mate)[2], int slots, unsigned peers, unsigned (&scale)[2], uint32_t (&code)[2]) {
+  bool near = false;
+  float top[2];
+#pragma unroll
+  for (int c = 0; c < 2; ++c) {
+    top[c] = 0.f;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) top[c] = fmaxf(top[c], rp_finite(y[8 * c + i]));
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+      if (!(fabsf(y[8 * c + i]) <= 3.4028234e38f)) top[c] = __uint_as_float(top[c] > 0.f ? __float_as_uint(top[c]) | 0x80000000u : 0x80000000u);
+  }
+  // the sign carries "not finite" to the other half of the group
+  float other[2];
+#pragma unroll
+  for (int c = 0; c < 2; ++c) {
+    const float a = __shfl_sync(peers, top[0], mate[c]), b = __shfl_sync(peers, top[1], mate[c]);
+    other[c] = (slots >> c) & 1 ? b : a;
+  }
+#pragma unroll
+  for (int c = 0; c < 2; ++c) {
+    const bool bad = ((__float_as_uint(top[c]) | __float_as_uint(other[c])) >> 31) != 0;
+    const float r = __fdiv_rn(fmaxf(fabsf(top[c]), fabsf(other[c])), 7.f);
+    near |= r > 0x1p-4f && rp_near_scale(r, eps);
+    const float s = rp_round_e4m3(fmaxf(r, 0x1p-4f), scale[c]);
+    if (bad) scale[c] = 0x7fu;
+    const float inv = __frcp_rn(s);
+    uint32_t w = 0;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const float v = bad ? 0.f : y[8 * c + i];
+      float q = v * inv;
+      q = fmaf(fmaf(-q, s, v), inv, q);
+      const float n = rintf(q);
+      near |= fabsf(fabsf(q - n) - 0.5f) < eps * inv;
+      w |= (uint32_t)((int)fminf(fmaxf(n, -7.f), 7.f) + 8) << (4 * i);
+    }
+    code[c] = w;
+  }
+  return near;
+}
+
+// The same decisions for a row in 64 bits (finite: a row that is not has no use for them).
+template <int LANES>
+__device__ __noinline__ int rp_int4_exact(const double* x, int mate0, int mate1, int slots, unsigned peers, unsigned* scale, uint32_t* code) {
+  const int mate[2] = {mate0, mate1};
+  double top[2] = {0., 0.};
+  for (int i = 0; i < 16; ++i) top[i >> 3] = fmax(top[i >> 3], fabs(x[i]));
+  double amax = fmax(top[0], top[1]);
+  for (int m = 1; m < LANES; m <<= 1) amax = fmax(amax, __shfl_xor_sync(peers, amax, m));
+  int e = -127;
+  if (amax > 0.) {
+    e = ilogb(amax) - 11;
+    if (amax > ldexp(3136., e)) ++e;
+    e = max(e, -127);
+  }
+  for (int c = 0; c < 2; ++c) {
+    const double a = __shfl_sync(peers, top[0], mate[c]), b = __shfl_sync(peers, top[1], mate[c]);
+    const double other = (slots >> c) & 1 ? b : a;
+    const double r = fmax(ldexp(fmax(top[c], other), -e) / 7., 0x1p-4);
+    const double unit = ldexp(1., ilogb(r) - 3);
+    const double s = rint(r / unit) * unit;                    // at most 448: four significant bits, an e4m3 value
+    float unused = rp_round_e4m3((float)s, scale[c]);
+    (void)unused;
+    uint32_t w = 0;
+    for (int i = 0; i < 8; ++i) {
+      const double n = fmin(fmax(rint(ldexp(x[8 * c + i], -e) / s), -7.), 7.);
+      w |= (uint32_t)((int)n + 8) << (4 * i);
+    }
+    code[c] = w;
+  }
+  return e + 127;
+}
+
 // FMT: -1 rotation only; DD_CACHE_* append. T: type of the rows.
 template <typename T, int D, int FMT>
-__global__ void __launch_bounds__(RP_THREADS, RP_BLOCKS) dd_rope_kernel(rp_args a) {
+__global__ void __launch_bounds__(RP_THREADS, rp_blocks(FMT)) dd_rope_kernel(rp_args a) {
   constexpr int LANES = D / 16;
   constexpr int PER_WARP = 32 / LANES;
   const int lane = threadIdx.x & 31, j = lane % LANES;
+  const unsigned peers = LANES == 8 ? 0xffu << (lane & 24) : 0xfu << (lane & 28);      // the lanes that share a token
   const long long group = ((long long)blockIdx.x * (RP_THREADS / 32) + (threadIdx.x >> 5)) * PER_WARP + lane / LANES;
   const int n_heads = a.n_q + a.n_k * (FMT >= 0 ? 2 : 1);
   // the groups of a warp hold neighbouring tokens of the same slice: they take the same branches below
@@ -116,6 +245,16 @@ __global__ void __launch_bounds__(RP_THREADS, RP_BLOCKS) dd_rope_kernel(rp_args 
   if (a.interleaved) { c0 = 16 * j; c1 = c0 + 8; }
   else if (turned) { c0 = 8 * j; c1 = c0 + 8 * a.rot16; }
   else { c0 = 16 * a.rot16 + 16 * (j - a.rot16); c1 = c0 + 8; }
+  int mate[2] = {0, 0}, mate_slots = 0;                        // 4-bit rows: where the other chunk of each chunk's group is
+  if (FMT == DD_CACHE_INT4) {
+#pragma unroll
+    for (int c = 0; c < 2; ++c) {
+      int slot;
+      rp_mate(((c ? c1 : c0) >> 3) ^ 1, a.rot16, a.interleaved, mate[c], slot);
+      mate[c] += lane - j;
+      mate_slots |= slot << c;
+    }
+  }
 
   // One kind of rows at a time (0 queries, 1 keys, 2 values), heads [lo, hi) of it.
   auto rows = [&](auto kind_, int lo, int hi, const rp_rows& from, const rp_rows& to) {
@@ -132,6 +271,7 @@ __global__ void __launch_bounds__(RP_THREADS, RP_BLOCKS) dd_rope_kernel(rp_args 
       out_stride = to.head_stride;
       out = to.data + n * to.token_stride + lo * out_stride;
     }
+    constexpr bool quantised = paged && (FMT == DD_CACHE_E4M3 || FMT == DD_CACHE_INT4);
     const int row_off = paged ? ((kind == 2 ? page_tokens : 0) + off) * (FMT == DD_CACHE_E4M3 ? D : 2 * D) : 0;
     for (int h = lo; h < hi; h += RP_BATCH) {
       uint4 r0[RP_BATCH], r1[RP_BATCH];
@@ -147,7 +287,7 @@ __global__ void __launch_bounds__(RP_THREADS, RP_BLOCKS) dd_rope_kernel(rp_args 
 #pragma unroll
       for (int u = 0; u < RP_BATCH; ++u) {
         if (h + u >= hi) break;
-        if (!(paged && FMT == DD_CACHE_E4M3) && !(turned && kind < 2)) {       // copied bit for bit
+        if (!quantised && !(turned && kind < 2)) {             // copied bit for bit
           if (live) {
             *reinterpret_cast<uint4*>(out + row_off + 2 * c0) = r0[u];
             *reinterpret_cast<uint4*>(out + row_off + 2 * c1) = r1[u];
@@ -180,7 +320,7 @@ __global__ void __launch_bounds__(RP_THREADS, RP_BLOCKS) dd_rope_kernel(rp_args 
             }
           }
         }
-        if (paged && FMT == DD_CACHE_E4M3) {
+        if (quantised) {
           float amax = 0.f;
 #pragma unroll
           for (int i = 0; i < 16; ++i) amax = fmaxf(amax, fabsf(x[i]));
@@ -194,9 +334,56 @@ __global__ void __launch_bounds__(RP_THREADS, RP_BLOCKS) dd_rope_kernel(rp_args 
               if (v <= 3.4028234e38f) amax = fmaxf(amax, v);
               else x[i] = __uint_as_float(0x7fc00000u);
             }
-            const unsigned peers = LANES == 8 ? 0xffu << (lane & 24) : 0xfu << (lane & 28);
 #pragma unroll
             for (int m = 1; m < LANES; m <<= 1) amax = fmaxf(amax, __shfl_xor_sync(peers, amax, m));
+          }
+          if constexpr (FMT == DD_CACHE_INT4) {
+            int byte = dd_int4_exponent_byte(amax);
+            const float up = dd_two_to_byte(254 - byte), top = amax * up;
+            const bool known = kind == 2 || a.rot16 == 0;        // the row is what was given
+            const float eps = known ? 0.f : top * RP_KNOWN;
+            bool near = fabsf(top - 3136.f) < eps || fabsf(top - 1568.f) < eps;
+#pragma unroll
+            for (int i = 0; i < 16; ++i) x[i] *= up;
+            unsigned scale[2];
+            uint32_t code[2];
+            near |= rp_int4_codes(x, eps, mate, mate_slots, peers, scale, code);
+            if (!known && __any_sync(peers, near)) {
+              // the whole row again; a lane without a turned pair has its elements exactly
+              double xx[16];
+              bool finite = true;
+#pragma unroll
+              for (int i = 0; i < 16; ++i) finite = finite && fabsf(x[i]) <= 3.4028234e38f;
+              if (__all_sync(peers, finite)) {
+                uint32_t raw[8];
+#pragma unroll
+                for (int i = 0; i < 8; ++i) raw[i] = w[i];
+                if (turned) {
+                  rp_turn_exact<T, D>(raw, a.turns, pos, a.amplitude, j, a.interleaved, xx);
+                } else {
+#pragma unroll
+                  for (int i = 0; i < 8; ++i) {
+                    const float2 f = dd_unpack2<T>(raw[i]);
+                    xx[2 * i] = f.x;
+                    xx[2 * i + 1] = f.y;
+                  }
+                }
+                byte = rp_int4_exact<LANES>(xx, mate[0], mate[1], mate_slots, peers, scale, code);
+              }
+            }
+            if (live) {
+              const int t = off & 15;
+              char* tile = out + (off >> 4) * dd_int4_tile_bytes(D);
+#pragma unroll
+              for (int c = 0; c < 2; ++c) {
+                const int chunk = (c ? c1 : c0) >> 3;
+                *reinterpret_cast<uint32_t*>(tile + (kind == 2 ? dd_int4_v_at<D>(t, chunk) : dd_int4_k_at<D>(t, chunk))) = code[c];
+                if (!(chunk & 1)) tile[kind == 2 ? dd_int4_vs_at<D>(t, chunk >> 1) : dd_int4_ks_at<D>(t, chunk >> 1)] = (char)scale[c];
+              }
+              if (j == 0) tile[18 * D + (kind == 2 ? 16 : 0) + t] = (char)byte;
+            }
+            out += out_stride;
+            continue;
           }
           const int byte = dd_e4m3_exponent_byte(amax);
           const float inv = dd_two_to_byte(254 - byte);        // 2^(127 - byte): exact, so the code is rounded once
@@ -233,6 +420,7 @@ template <typename T, int D>
 const void* rp_kernel_of(int fmt) {
   if (fmt < 0) return (const void*)dd_rope_kernel<T, D, -1>;
   if (fmt == DD_CACHE_E4M3) return (const void*)dd_rope_kernel<T, D, DD_CACHE_E4M3>;
+  if (fmt == DD_CACHE_INT4) return (const void*)dd_rope_kernel<T, D, DD_CACHE_INT4>;
   return (const void*)dd_rope_kernel<T, D, DD_CACHE_BF16>;      // 16-bit pages of the rows' own type
 }
 
@@ -245,7 +433,7 @@ int rp_launch(rp_args& a, int head_dim, int dtype, int fmt, cudaStream_t st, con
   int sms = 0;
   cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, device);
   if (sms <= 0) sms = 148;
-  const long long fill = (long long)sms * RP_BLOCKS * RP_THREADS / lanes;
+  const long long fill = (long long)sms * rp_blocks(fmt) * RP_THREADS / lanes;
   a.slice_heads = 2 * RP_BATCH;
   while (a.slice_heads > 1 && (long long)a.n_tokens * ((n_heads + a.slice_heads - 1) / a.slice_heads) < fill / 2) a.slice_heads /= 2;
   a.slices = (n_heads + a.slice_heads - 1) / a.slice_heads;
@@ -397,6 +585,6 @@ extern "C" int dd_cache_append(const dd_cache* cache, int n_tokens, const int* p
   a.amplitude = rope ? rope->amplitude : 1.f;
   a.tokens_per_request = requests ? 1 : n_tokens / cache->batch;
   a.cache = dd_make_view(cache, data);
-  return rp_launch(a, cache->head_dim, k->dtype, cache->format == DD_CACHE_E4M3 ? DD_CACHE_E4M3 : DD_CACHE_BF16,
+  return rp_launch(a, cache->head_dim, k->dtype, cache->format == DD_CACHE_E4M3 || cache->format == DD_CACHE_INT4 ? cache->format : DD_CACHE_BF16,
                    (cudaStream_t)stream, who, device);
 }
