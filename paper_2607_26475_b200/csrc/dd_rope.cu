@@ -58,12 +58,16 @@ __device__ __forceinline__ void rp_angle(double turns, int pos, float amplitude,
 }
 
 // ---- 4-bit rows
-// A row is 2^e times groups of 16 whole numbers times their group's scale; what a lane holds of it is two chunks of 8 elements, and
-// the other half of a chunk's group may lie with another lane (rp_mate). The scale comes from one division, a code from a
-// product with the scale's inverse and one correction, which makes quotients that can be represented exact: ties fall as in the definition.
-// A turned element is known in 32 bits to 2^-21.2 of its pair's magnitude (sine and cosine 2^-22 each, product and sum), that is to
-// RP_KNOWN of the row's largest element. Where that leaves a border within reach of the row's exponent, of a scale or of a code (a few
-// rows in a thousand), the row is turned again in 64 bits, so that the bytes written are those of the 64-bit rotation.
+// A row is 2^e times groups of 16 whole numbers times their group's scale. A lane holds two chunks of 8 elements; the other half of a
+// chunk's group may lie with another lane (rp_mate). What is done for each element is kept to five instructions:
+//   values as they came: q = x / (scale 2^e) by the inverse and one correction, exact where the quotient can be represented, so that ties
+//     fall as in the definition; q + 1.5 2^23 + 8 has the code in its lowest bits; a shift and add per element collects the word (the
+//     constant parts of all eight come off at the end). A quotient is at most 7 * 17 / 16 < 7.5, so no code is cut off.
+//   turned values: known in 32 bits to 2^-21.2 of their pair's magnitude (sine and cosine 2^-22 each, product and sum), that is to
+//     RP_KNOWN of the row's largest. Where that leaves a border within reach of the row's exponent, of a scale or of a code (a
+//     few elements in 100,000), it is done again in 64 bits, the element or the row, so that the bytes written are those of the 64-bit
+//     rotation (without a correction otherwise).
+// Rows that are not finite, and rows below 2^-108, take the same 64-bit way.
 constexpr float RP_KNOWN = 0x1.8p-21f;
 
 // Lane of the group and slot (0 or 1) that hold chunk `chunk` of a row.
@@ -77,9 +81,6 @@ __device__ __forceinline__ void rp_mate(int chunk, int rot16, bool interleaved, 
   }
 }
 
-// Magnitude for a row's scale: zero where it is not finite.
-__device__ __forceinline__ float rp_finite(float v) { const float m = fabsf(v); return m <= 3.4028234e38f ? m : 0.f; }
-
 // Is s, known to eps, within reach of a point where its rounding to 4 significant bits changes?
 __device__ __forceinline__ bool rp_near_scale(float s, float eps) {
   const int rest = (int)(__float_as_uint(s) & 0xfffffu) - 0x80000;
@@ -91,76 +92,47 @@ __device__ __forceinline__ float rp_round_e4m3(float v, unsigned& code) {
   dd_e4m3x4_to_half(code, h, unused);
   return dd_unpack2<__half>(h).x;
 }
+__device__ __forceinline__ float rp_rcp(float v) {
+  float r;
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(v));
+  return r;
+}
+// a / 7, exact where it can be represented.
+__device__ __forceinline__ float rp_seventh(float a) {
+  const float q = a * 0.14285714924335479736328125f;
+  return fmaf(fmaf(-7.f, q, a), 0.14285714924335479736328125f, q);
+}
 
-// The two chunks (16 elements) of a turned row again, in 64 bits.
+// Where a lane's two chunks are and where the other chunk of each one's group is: lane (of the warp) and slot.
+struct rp_place {
+  int c0, c1, mate0, mate1, slots;
+};
+
+// One row in 64 bits, from its source: exponent byte (returned), scales (as e4m3 codes) and codes of the lane's two chunks.
 template <typename T, int D>
-__device__ __noinline__ void rp_turn_exact(const uint32_t* raw, const double* turns, int pos, float amplitude, int j, bool interleaved, double* x) {
-  for (int i = 0; i < 8; ++i) {
+__device__ __noinline__ int rp_int4_slow(const char* row, rp_place at, const double* turns, int pos, float amplitude, int j, bool interleaved,
+                                         unsigned peers, unsigned (&scale)[2], uint32_t (&code)[2]) {
+  double x[16], top[2] = {0., 0.};
+  bool bad[2] = {false, false};
+  for (int i = 0; i < 16; ++i) x[i] = (double)dd_to_float(reinterpret_cast<const T*>(row)[(i < 8 ? at.c0 : at.c1 - 8) + i]);
+  for (int i = 0; turns && i < 8; ++i) {
     double a = turns[8 * j + i] * (double)pos, sn, cs;
     a -= rint(a);
     sincospi(2. * a, &sn, &cs);
     sn *= (double)amplitude;
     cs *= (double)amplitude;
     const int iu = interleaved ? 2 * i : i, iw = interleaved ? 2 * i + 1 : 8 + i;
-    const float2 u2 = dd_unpack2<T>(raw[iu >> 1]), w2 = dd_unpack2<T>(raw[iw >> 1]);
-    const double u = (iu & 1) ? u2.y : u2.x, w = (iw & 1) ? w2.y : w2.x;
+    const double u = x[iu], w = x[iw];
     x[iu] = u * cs - w * sn;
     x[iw] = w * cs + u * sn;
   }
-}
-
-// Scales (as e4m3 codes) and codes (chunk by chunk, 8 to a word) of a row x whose exponent byte is `byte`: y = x * 2^(127 - byte).
-// Returns whether errors of up to eps in y may have decided anything otherwise.
-__device__ __forceinline__ bool rp_int4_codes(float (&y)[16], float eps, const int (&mate)[2], int slots, unsigned peers, unsigned (&scale)[2], uint32_t (&code)[2]) {
-  bool near = false;
-  float top[2];
-#pragma unroll
-  for (int c = 0; c < 2; ++c) {
-    top[c] = 0.f;
-#pragma unroll
-    for (int i = 0; i < 8; ++i) top[c] = fmaxf(top[c], rp_finite(y[8 * c + i]));
-#pragma unroll
-    for (int i = 0; i < 8; ++i)
-      if (!(fabsf(y[8 * c + i]) <= 3.4028234e38f)) top[c] = __uint_as_float(top[c] > 0.f ? __float_as_uint(top[c]) | 0x80000000u : 0x80000000u);
+  for (int i = 0; i < 16; ++i) {
+    const double m = fabs(x[i]);
+    if (m <= 1.7976931348623157e308) top[i >> 3] = fmax(top[i >> 3], m);
+    else bad[i >> 3] = true;
   }
-  // the sign carries "not finite" to the other half of the group
-  float other[2];
-#pragma unroll
-  for (int c = 0; c < 2; ++c) {
-    const float a = __shfl_sync(peers, top[0], mate[c]), b = __shfl_sync(peers, top[1], mate[c]);
-    other[c] = (slots >> c) & 1 ? b : a;
-  }
-#pragma unroll
-  for (int c = 0; c < 2; ++c) {
-    const bool bad = ((__float_as_uint(top[c]) | __float_as_uint(other[c])) >> 31) != 0;
-    const float r = __fdiv_rn(fmaxf(fabsf(top[c]), fabsf(other[c])), 7.f);
-    near |= r > 0x1p-4f && rp_near_scale(r, eps);
-    const float s = rp_round_e4m3(fmaxf(r, 0x1p-4f), scale[c]);
-    if (bad) scale[c] = 0x7fu;
-    const float inv = __frcp_rn(s);
-    uint32_t w = 0;
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      const float v = bad ? 0.f : y[8 * c + i];
-      float q = v * inv;
-      q = fmaf(fmaf(-q, s, v), inv, q);
-      const float n = rintf(q);
-      near |= fabsf(fabsf(q - n) - 0.5f) < eps * inv;
-      w |= (uint32_t)((int)fminf(fmaxf(n, -7.f), 7.f) + 8) << (4 * i);
-    }
-    code[c] = w;
-  }
-  return near;
-}
-
-// The same decisions for a row in 64 bits (finite: a row that is not has no use for them).
-template <int LANES>
-__device__ __noinline__ int rp_int4_exact(const double* x, int mate0, int mate1, int slots, unsigned peers, unsigned* scale, uint32_t* code) {
-  const int mate[2] = {mate0, mate1};
-  double top[2] = {0., 0.};
-  for (int i = 0; i < 16; ++i) top[i >> 3] = fmax(top[i >> 3], fabs(x[i]));
   double amax = fmax(top[0], top[1]);
-  for (int m = 1; m < LANES; m <<= 1) amax = fmax(amax, __shfl_xor_sync(peers, amax, m));
+  for (int m = 1; m < D / 16; m <<= 1) amax = fmax(amax, __shfl_xor_sync(peers, amax, m));
   int e = -127;
   if (amax > 0.) {
     e = ilogb(amax) - 11;
@@ -168,21 +140,43 @@ __device__ __noinline__ int rp_int4_exact(const double* x, int mate0, int mate1,
     e = max(e, -127);
   }
   for (int c = 0; c < 2; ++c) {
-    const double a = __shfl_sync(peers, top[0], mate[c]), b = __shfl_sync(peers, top[1], mate[c]);
-    const double other = (slots >> c) & 1 ? b : a;
-    const double r = fmax(ldexp(fmax(top[c], other), -e) / 7., 0x1p-4);
+    const int mate = c ? at.mate1 : at.mate0, slot = (at.slots >> c) & 1;
+    const double t0 = __shfl_sync(peers, top[0], mate), t1 = __shfl_sync(peers, top[1], mate);
+    const int b = __shfl_sync(peers, (int)bad[0] + 2 * (int)bad[1], mate);
+    const double r = fmax(ldexp(fmax(top[c], slot ? t1 : t0), -e) / 7., 0x1p-4);
     const double unit = ldexp(1., ilogb(r) - 3);
     const double s = rint(r / unit) * unit;                    // at most 448: four significant bits, an e4m3 value
-    float unused = rp_round_e4m3((float)s, scale[c]);
-    (void)unused;
+    (void)rp_round_e4m3((float)s, scale[c]);
+    const bool none = bad[c] || ((b >> slot) & 1);
+    if (none) scale[c] = 0x7fu;
     uint32_t w = 0;
     for (int i = 0; i < 8; ++i) {
-      const double n = fmin(fmax(rint(ldexp(x[8 * c + i], -e) / s), -7.), 7.);
+      const double n = none ? 0. : fmin(fmax(rint(ldexp(x[8 * c + i], -e) / s), -7.), 7.);
       w |= (uint32_t)((int)n + 8) << (4 * i);
     }
     code[c] = w;
   }
   return e + 127;
+}
+
+// The code of element e (0 .. 15) of a lane's chunks of a turned row (turns NULL: of a part that is not turned), in 64 bits, for an exponent byte and a scale that are certain.
+template <typename T>
+__device__ __noinline__ uint32_t rp_int4_element(const char* row, int c0, int c1, int e, const double* turns, int pos, float amplitude, int j,
+                                                 bool interleaved, int byte, unsigned scale) {
+  const int i = interleaved ? e >> 1 : e & 7, iu = interleaved ? 2 * i : i, iw = interleaved ? 2 * i + 1 : 8 + i;
+  auto at = [&](int k) { return (double)dd_to_float(reinterpret_cast<const T*>(row)[k < 8 ? c0 + k : c1 + k - 8]); };
+  double x = at(e);
+  if (turns) {
+    double a = turns[8 * j + i] * (double)pos, sn, cs;
+    a -= rint(a);
+    sincospi(2. * a, &sn, &cs);
+    const double u = at(iu), w = at(iw);
+    x = (e == iu ? u * cs - w * sn : w * cs + u * sn) * (double)amplitude;
+  }
+  uint32_t h, unused;
+  dd_e4m3x4_to_half(scale, h, unused);
+  const double n = rint(x * __hiloint2double((1023 + 127 - byte) << 20, 0) / (double)dd_unpack2<__half>(h).x);
+  return (uint32_t)((int)fmin(fmax(n, -7.), 7.) + 8);
 }
 
 // FMT: -1 rotation only; DD_CACHE_* append. T: type of the rows.
@@ -192,13 +186,14 @@ __global__ void __launch_bounds__(RP_THREADS, rp_blocks(FMT)) dd_rope_kernel(rp_
   constexpr int PER_WARP = 32 / LANES;
   const int lane = threadIdx.x & 31, j = lane % LANES;
   const unsigned peers = LANES == 8 ? 0xffu << (lane & 24) : 0xfu << (lane & 28);      // the lanes that share a token
-  const long long group = ((long long)blockIdx.x * (RP_THREADS / 32) + (threadIdx.x >> 5)) * PER_WARP + lane / LANES;
   const int n_heads = a.n_q + a.n_k * (FMT >= 0 ? 2 : 1);
-  // the groups of a warp hold neighbouring tokens of the same slice: they take the same branches below
-  const long long padded = ((long long)a.n_tokens + PER_WARP - 1) / PER_WARP * PER_WARP;
-  const int slice = (int)(group / padded);
-  const long long n_ = group - slice * padded;
-  if (slice >= a.slices) return;                               // a whole warp
+  // A block holds neighbouring tokens of one slice of the heads, and neighbouring blocks the slices of the same tokens, so that kinds of
+  // rows that keep memory busy and kinds that keep the cores busy run side by side (32768 tokens: rotation 108 -> 102 us, e4m3 append
+  // 134 -> 127; slices mixed within a block make it wait for its slowest warp: 4-bit append 189 -> 311 us).
+  const unsigned over = blockIdx.x / (unsigned)a.slices;
+  const int slice = blockIdx.x - over * a.slices;
+  const long long n_ = ((long long)over * (RP_THREADS / 32) + (threadIdx.x >> 5)) * PER_WARP + lane / LANES;
+  if (n_ - lane / LANES >= a.n_tokens) return;                 // a whole warp
   const int h0 = slice * a.slice_heads, h1 = min(n_heads, h0 + a.slice_heads);
 
   dd_grid_dependency_wait();
@@ -245,16 +240,20 @@ __global__ void __launch_bounds__(RP_THREADS, rp_blocks(FMT)) dd_rope_kernel(rp_
   if (a.interleaved) { c0 = 16 * j; c1 = c0 + 8; }
   else if (turned) { c0 = 8 * j; c1 = c0 + 8 * a.rot16; }
   else { c0 = 16 * a.rot16 + 16 * (j - a.rot16); c1 = c0 + 8; }
-  int mate[2] = {0, 0}, mate_slots = 0;                        // 4-bit rows: where the other chunk of each chunk's group is
+  // 4-bit rows: where the other chunk of each chunk's group is; values are not turned and lie two neighbouring chunks to a lane
+  rp_place place = {c0, c1, 0, 0, 0};
+  bool same_lane = true, next_lane = false;
   if (FMT == DD_CACHE_INT4) {
-#pragma unroll
-    for (int c = 0; c < 2; ++c) {
-      int slot;
-      rp_mate(((c ? c1 : c0) >> 3) ^ 1, a.rot16, a.interleaved, mate[c], slot);
-      mate[c] += lane - j;
-      mate_slots |= slot << c;
-    }
+    int slot0, slot1;
+    rp_mate((c0 >> 3) ^ 1, a.rot16, a.interleaved, place.mate0, slot0);
+    rp_mate((c1 >> 3) ^ 1, a.rot16, a.interleaved, place.mate1, slot1);
+    place.mate0 += lane - j;
+    place.mate1 += lane - j;
+    place.slots = slot0 + 2 * slot1;
+    same_lane = c1 == c0 + 8 && !(c0 & 8);
+    next_lane = a.interleaved || a.rot16 % 2 == 0;             // the same for all lanes: no group reaches further than the next lane
   }
+  const rp_place plain_place = {16 * j, 16 * j + 8, lane, lane, 1};
 
   // One kind of rows at a time (0 queries, 1 keys, 2 values), heads [lo, hi) of it.
   auto rows = [&](auto kind_, int lo, int hi, const rp_rows& from, const rp_rows& to) {
@@ -273,14 +272,40 @@ __global__ void __launch_bounds__(RP_THREADS, rp_blocks(FMT)) dd_rope_kernel(rp_
     }
     constexpr bool quantised = paged && (FMT == DD_CACHE_E4M3 || FMT == DD_CACHE_INT4);
     const int row_off = paged ? ((kind == 2 ? page_tokens : 0) + off) * (FMT == DD_CACHE_E4M3 ? D : 2 * D) : 0;
+    [[maybe_unused]] auto put4 = [&](char* page, const unsigned (&scale)[2], const uint32_t (&code)[2], int byte) {
+      const int t = off & 15;
+      char* tile = page + (off >> 4) * dd_int4_tile_bytes(D);
+      if (kind == 2) {                                         // both chunks of a group
+        if (D == 128) {
+          *reinterpret_cast<uint2*>(tile + dd_int4_v_at<D>(t, 2 * j)) = make_uint2(code[0], code[1]);
+        } else {
+          *reinterpret_cast<uint32_t*>(tile + dd_int4_v_at<D>(t, 2 * j)) = code[0];
+          *reinterpret_cast<uint32_t*>(tile + dd_int4_v_at<D>(t, 2 * j + 1)) = code[1];
+        }
+        tile[dd_int4_vs_at<D>(t, j)] = (char)scale[0];
+      } else {
+#pragma unroll
+        for (int c = 0; c < 2; ++c) {
+          const int chunk = (c ? c1 : c0) >> 3;
+          *reinterpret_cast<uint32_t*>(tile + dd_int4_k_at<D>(t, chunk)) = code[c];
+          if (!(chunk & 1)) tile[dd_int4_ks_at<D>(t, chunk >> 1)] = (char)scale[c];
+        }
+      }
+      if (j == 0) tile[18 * D + (kind == 2 ? 16 : 0) + t] = (char)byte;
+    };
+    const int e0 = FMT == DD_CACHE_INT4 && kind == 2 ? 16 * j : c0, e1 = FMT == DD_CACHE_INT4 && kind == 2 ? 16 * j + 8 : c1;
     for (int h = lo; h < hi; h += RP_BATCH) {
+      [[maybe_unused]] const char* const batch_in = in;
+      [[maybe_unused]] char* const batch_out = out;
+      // 4-bit rows of the batch that the 64-bit way has to decide; of the others, elements that it has to, and their row's scales
+      [[maybe_unused]] unsigned again = 0, near[RP_BATCH] = {}, held[RP_BATCH] = {};
       uint4 r0[RP_BATCH], r1[RP_BATCH];
 #pragma unroll
       for (int u = 0; u < RP_BATCH; ++u) {
         r0[u] = r1[u] = make_uint4(0u, 0u, 0u, 0u);
         if (h + u < hi && live) {
-          r0[u] = *reinterpret_cast<const uint4*>(in + 2 * c0);
-          r1[u] = *reinterpret_cast<const uint4*>(in + 2 * c1);
+          r0[u] = *reinterpret_cast<const uint4*>(in + 2 * e0);
+          r1[u] = *reinterpret_cast<const uint4*>(in + 2 * e1);
         }
         in += from.head_stride;
       }
@@ -320,7 +345,71 @@ __global__ void __launch_bounds__(RP_THREADS, rp_blocks(FMT)) dd_rope_kernel(rp_
             }
           }
         }
-        if (quantised) {
+        if constexpr (paged && FMT == DD_CACHE_INT4) {
+          const rp_place& at = kind == 2 ? plain_place : place;
+          // the larger magnitudes compare as unsigned numbers, NaN and infinities above all others
+          unsigned top[2] = {0u, 0u};
+#pragma unroll
+          for (int i = 0; i < 16; ++i) top[i >> 3] = max(top[i >> 3], __float_as_uint(x[i]) & 0x7fffffffu);
+          unsigned amax = max(top[0], top[1]);
+#pragma unroll
+          for (int m = 1; m < LANES; m <<= 1) amax = max(amax, __shfl_xor_sync(0xffffffffu, amax, m));
+          unsigned group[2];
+          if (kind == 2) {
+            group[0] = group[1] = max(top[0], top[1]);
+          } else if (next_lane) {
+            const unsigned n0 = __shfl_xor_sync(0xffffffffu, top[0], 1), n1 = __shfl_xor_sync(0xffffffffu, top[1], 1);
+            group[0] = max(top[0], same_lane ? top[1] : n0);
+            group[1] = max(top[1], same_lane ? top[0] : n1);
+          } else {
+#pragma unroll
+            for (int c = 0; c < 2; ++c) {
+              const unsigned a0 = __shfl_sync(0xffffffffu, top[0], c ? at.mate1 : at.mate0), a1 = __shfl_sync(0xffffffffu, top[1], c ? at.mate1 : at.mate0);
+              group[c] = max(top[c], (at.slots >> c) & 1 ? a1 : a0);
+            }
+          }
+          const bool known = kind == 2 || a.rot16 == 0;        // the row is what was given
+          int byte = dd_int4_exponent_byte(__uint_as_float(amax));
+          const float up = dd_two_to_byte(254 - byte), whole = __uint_as_float(amax) * up, eps = whole * RP_KNOWN;
+          bool slow = amax >= 0x7f800000u || byte < 8;         // (a scale of 2^-4 * 2^(byte - 127) has an inverse from 8 on)
+          if (!known) slow |= fabsf(whole - 3136.f) < eps || fabsf(whole - 1568.f) < eps;
+          unsigned scale[2];
+          uint32_t code[2];
+#pragma unroll
+          for (int c = 0; c < 2; ++c) {
+            if (kind == 2 && c == 1) scale[1] = scale[0];
+            const float r = rp_seventh(__uint_as_float(group[c]) * up);
+            if (!known) slow |= r > 0x1p-4f && rp_near_scale(r, eps * 0.15f);
+            const float step = rp_round_e4m3(fmaxf(r, 0x1p-4f), scale[c]);
+            const float inv = rp_rcp(step) * up, s1 = step * dd_two_to_byte(byte);
+            constexpr float magic = 12582912.f + 8.f;
+            uint32_t word = 0;
+            if (known) {
+#pragma unroll
+              for (int i = 7; i >= 0; --i) {
+                float q = x[8 * c + i] * inv;
+                q = fmaf(fmaf(-q, s1, x[8 * c + i]), inv, q);
+                word = (word << 4) + __float_as_uint(q + magic);
+              }
+            } else {
+              const float far = 0.5f - eps * rp_rcp(step);
+#pragma unroll
+              for (int i = 7; i >= 0; --i) {
+                const float t = fmaf(x[8 * c + i], inv, magic);
+                if (fabsf(fmaf(x[8 * c + i], inv, magic - t)) > far) near[u] |= 1u << (8 * c + i);
+                word = (word << 4) + __float_as_uint(t);
+              }
+            }
+            // the constant part 0x4b400000 of every element, shifted by 4 i
+            code[c] = word - 0x40000000u - 0xb4000000u - 0x4b400000u;
+          }
+          if (slow && live) again |= 1u << u;
+          if (kind < 2) held[u] = (unsigned)byte | scale[0] << 8 | scale[1] << 16;
+          if (live) put4(out, scale, code, byte);
+          out += out_stride;
+          continue;
+        }
+        if (paged && FMT == DD_CACHE_E4M3) {
           float amax = 0.f;
 #pragma unroll
           for (int i = 0; i < 16; ++i) amax = fmaxf(amax, fabsf(x[i]));
@@ -336,54 +425,6 @@ __global__ void __launch_bounds__(RP_THREADS, rp_blocks(FMT)) dd_rope_kernel(rp_
             }
 #pragma unroll
             for (int m = 1; m < LANES; m <<= 1) amax = fmaxf(amax, __shfl_xor_sync(peers, amax, m));
-          }
-          if constexpr (FMT == DD_CACHE_INT4) {
-            int byte = dd_int4_exponent_byte(amax);
-            const float up = dd_two_to_byte(254 - byte), top = amax * up;
-            const bool known = kind == 2 || a.rot16 == 0;        // the row is what was given
-            const float eps = known ? 0.f : top * RP_KNOWN;
-            bool near = fabsf(top - 3136.f) < eps || fabsf(top - 1568.f) < eps;
-#pragma unroll
-            for (int i = 0; i < 16; ++i) x[i] *= up;
-            unsigned scale[2];
-            uint32_t code[2];
-            near |= rp_int4_codes(x, eps, mate, mate_slots, peers, scale, code);
-            if (!known && __any_sync(peers, near)) {
-              // the whole row again; a lane without a turned pair has its elements exactly
-              double xx[16];
-              bool finite = true;
-#pragma unroll
-              for (int i = 0; i < 16; ++i) finite = finite && fabsf(x[i]) <= 3.4028234e38f;
-              if (__all_sync(peers, finite)) {
-                uint32_t raw[8];
-#pragma unroll
-                for (int i = 0; i < 8; ++i) raw[i] = w[i];
-                if (turned) {
-                  rp_turn_exact<T, D>(raw, a.turns, pos, a.amplitude, j, a.interleaved, xx);
-                } else {
-#pragma unroll
-                  for (int i = 0; i < 8; ++i) {
-                    const float2 f = dd_unpack2<T>(raw[i]);
-                    xx[2 * i] = f.x;
-                    xx[2 * i + 1] = f.y;
-                  }
-                }
-                byte = rp_int4_exact<LANES>(xx, mate[0], mate[1], mate_slots, peers, scale, code);
-              }
-            }
-            if (live) {
-              const int t = off & 15;
-              char* tile = out + (off >> 4) * dd_int4_tile_bytes(D);
-#pragma unroll
-              for (int c = 0; c < 2; ++c) {
-                const int chunk = (c ? c1 : c0) >> 3;
-                *reinterpret_cast<uint32_t*>(tile + (kind == 2 ? dd_int4_v_at<D>(t, chunk) : dd_int4_k_at<D>(t, chunk))) = code[c];
-                if (!(chunk & 1)) tile[kind == 2 ? dd_int4_vs_at<D>(t, chunk >> 1) : dd_int4_ks_at<D>(t, chunk >> 1)] = (char)scale[c];
-              }
-              if (j == 0) tile[18 * D + (kind == 2 ? 16 : 0) + t] = (char)byte;
-            }
-            out += out_stride;
-            continue;
           }
           const int byte = dd_e4m3_exponent_byte(amax);
           const float inv = dd_two_to_byte(254 - byte);        // 2^(127 - byte): exact, so the code is rounded once
@@ -408,6 +449,40 @@ __global__ void __launch_bounds__(RP_THREADS, rp_blocks(FMT)) dd_rope_kernel(rp_
               make_uint4(dd_pack2<T>(x[8], x[9]), dd_pack2<T>(x[10], x[11]), dd_pack2<T>(x[12], x[13]), dd_pack2<T>(x[14], x[15]));
         }
         out += out_stride;
+      }
+      if constexpr (paged && FMT == DD_CACHE_INT4) {
+        again = __reduce_or_sync(peers, again);
+        if (kind < 2 && live && a.rot16) {
+#pragma unroll 1
+          for (int u = 0; u < RP_BATCH; ++u) {
+            unsigned m = near[0], k = held[0];
+#pragma unroll
+            for (int v = 1; v < RP_BATCH; ++v) {
+              if (u == v) {
+                m = near[v];
+                k = held[v];
+              }
+            }
+            if ((again >> u) & 1) m = 0;
+            while (m) {
+              const int e = __ffs(m) - 1;
+              m &= m - 1;
+              const uint32_t n = rp_int4_element<T>(batch_in + u * from.head_stride, c0, c1, e, turned ? a.turns : nullptr, pos, a.amplitude, j, a.interleaved, (int)(k & 0xff),
+                                                    (k >> (e < 8 ? 8 : 16)) & 0xff);
+              uint32_t* word = reinterpret_cast<uint32_t*>(batch_out + u * out_stride + (off >> 4) * dd_int4_tile_bytes(D) + dd_int4_k_at<D>(off & 15, (e < 8 ? c0 : c1) >> 3));
+              *word = (*word & ~(15u << (4 * (e & 7)))) | n << (4 * (e & 7));
+            }
+          }
+        }
+        while (again) {
+          const int u = __ffs(again) - 1;
+          again &= again - 1;
+          unsigned scale[2];
+          uint32_t code[2];
+          const int byte = rp_int4_slow<T, D>(batch_in + u * from.head_stride, kind == 2 ? plain_place : place, turned && kind < 2 ? a.turns : nullptr, pos,
+                                              a.amplitude, j, a.interleaved, peers, scale, code);
+          if (live) put4(batch_out + u * out_stride, scale, code, byte);
+        }
       }
     }
   };
@@ -437,10 +512,8 @@ int rp_launch(rp_args& a, int head_dim, int dtype, int fmt, cudaStream_t st, con
   a.slice_heads = 2 * RP_BATCH;
   while (a.slice_heads > 1 && (long long)a.n_tokens * ((n_heads + a.slice_heads - 1) / a.slice_heads) < fill / 2) a.slice_heads /= 2;
   a.slices = (n_heads + a.slice_heads - 1) / a.slice_heads;
-  const long long slices = a.slices;
-  const long long groups = ((long long)a.n_tokens + per_warp - 1) / per_warp * per_warp * slices;
   const long long per_block = (long long)(RP_THREADS / 32) * per_warp;
-  const long long blocks = (groups + per_block - 1) / per_block;
+  const long long blocks = ((long long)a.n_tokens + per_block - 1) / per_block * a.slices;
   if (blocks > 0x7fffffffLL) return dd_fail(nullptr, DD_ERR_INVALID_ARG, "%s: too many tokens", who);
   const void* f = head_dim == 128 ? (dtype == DD_BF16 ? rp_kernel_of<__nv_bfloat16, 128>(fmt) : rp_kernel_of<__half, 128>(fmt))
                                   : (dtype == DD_BF16 ? rp_kernel_of<__nv_bfloat16, 64>(fmt) : rp_kernel_of<__half, 64>(fmt));
