@@ -7,32 +7,37 @@
 // and with them the chosen set, are defined to the last bit. (Adding up the group's rows orders pages as the product of the heads'
 // soft-max probabilities does: what a head's soft-max divides by is the same for all pages.)
 //
-// Scores: whole-number MMAs, 16 pages as rows and 8 query tokens as columns. Few tokens a request: a block per token, which reads each landmark once (HBM
-// bound: 144 bytes a page and head); many: 64 tokens of a head stay in registers while the pages go by. The keys (scores
-// in an order that compares as unsigned numbers) of a bounded number of tokens go through a workspace that L2 holds.
+// Scores: 8-bit whole-number MMAs. Few tokens a request: a block per token, which reads each landmark once (HBM bound: 144 bytes
+// a page and head); many: 64 tokens of a head stay in registers while the pages go by. The keys (scores in an order that
+// compares as unsigned numbers) of a bounded number of tokens go through a workspace that L2 holds.
 //
-// Choice: the k-th largest key by bisection, with the row's keys in registers: a step counts keys at or above the middle. It stops as
-// soon as exactly k are (about a dozen steps for a few thousand keys); all the steps come up only with ties, which go to the lower pages.
+// Choice: bisection for the k-th largest key: a step counts keys at or above the middle. It stops as soon as exactly k are (about a dozen
+// steps); all the steps come up only with ties, which go to the lower pages.
 #include "dd_cache.cuh"
 
 namespace {
 
 // ---- 64-bit rows as whole numbers
 __device__ __forceinline__ double cs_finite(double v) { return fabs(v) <= 1.7976931348623157e308 ? v : 0.0; }
-// The smallest e in [least, 63] with top <= 127 * 2^e (top finite, not negative): 127 = 1.984375 * 2^6.
-__device__ __forceinline__ int cs_exponent(double top, int least) {
-  const int hi = __double2hiint(top), lo = __double2loint(top);
-  const int frac = hi & 0xfffff;
-  const int e = ((hi >> 20) & 0x7ff) - 1023 - 6 + (frac > 0xfc000 || (frac == 0xfc000 && lo != 0) ? 1 : 0);
-  return min(63, max(e, least));
+// The smallest e in [least, 63] with every lane's |v| <= 127 * 2^e (v finite): 127 = 1.984375 * 2^6. The larger magnitudes have the larger
+// upper words; the lower ones matter only where the upper one is 127's.
+template <int N> __device__ __forceinline__ int cs_exponent(const double (&v)[N], int least) {
+  unsigned hi = 0u;
+#pragma unroll
+  for (int i = 0; i < N; ++i) hi = max(hi, (unsigned)__double2hiint(v[i]) & 0x7fffffffu);
+  hi = __reduce_max_sync(0xffffffffu, hi);
+  const unsigned frac = hi & 0xfffffu;
+  bool above = frac > 0xfc000u;
+  if (frac == 0xfc000u) {
+    bool lower = false;
+#pragma unroll
+    for (int i = 0; i < N; ++i) lower |= ((unsigned)__double2hiint(v[i]) & 0x7fffffffu) == hi && __double2loint(v[i]) != 0;
+    above = __any_sync(0xffffffffu, lower);
+  }
+  return min(63, max((int)(hi >> 20) - 1023 - 6 + (above ? 1 : 0), least));
 }
 __device__ __forceinline__ double cs_two_to(int e) { return __hiloint2double((e + 1023) << 20, 0); }
 __device__ __forceinline__ int cs_code(double v, double down) { return (int)fmin(fmax(rint(v * down), -127.0), 127.0); }
-__device__ __forceinline__ double cs_warp_max(double v) {
-#pragma unroll
-  for (int o = 16; o; o >>= 1) v = fmax(v, __shfl_xor_sync(0xffffffffu, v, o));
-  return v;
-}
 constexpr int CS_TAIL = 16;                            // bytes behind the codes of a landmark: the exponent + 64, then nothing
 constexpr int CS_LM_LEAST = -64, CS_Q_LEAST = -120;
 
@@ -100,13 +105,9 @@ __global__ void __launch_bounds__(CL_THREADS) dd_cache_landmark_kernel(dd_cache_
 #pragma unroll
     for (int i = 0; i < N; ++i) sum[i] += (double)v[i];
   }
-  double top = 0.0;
 #pragma unroll
-  for (int i = 0; i < N; ++i) {
-    sum[i] = cs_finite(sum[i] / (double)n);
-    top = fmax(top, fabs(sum[i]));
-  }
-  const int e = cs_exponent(cs_warp_max(top), CS_LM_LEAST);
+  for (int i = 0; i < N; ++i) sum[i] = cs_finite(sum[i] / (double)n);
+  const int e = cs_exponent(sum, CS_LM_LEAST);
   const double down = cs_two_to(-e);
   uint32_t w = 0;
 #pragma unroll
@@ -127,11 +128,12 @@ struct cs_args {
   const int* positions;
   const int* requests;
   uint32_t* keys;                                      // [tokens of the launch][heads][stride]
+  signed char* codes;                                  // [tokens of the launch][heads][D], where they are made ahead
   int* out;
   int first_token, n_tokens, tokens_per_request;       // tokens first_token .. first_token + n_tokens - 1
   int G, k, first, recent;
   int stride;                                          // keys of a row
-  int chunks, chunk_pages;                             // blocks that share a token tile, and how many pages each takes
+  int chunks;                                          // blocks that share a token tile
 };
 
 // Own page of a token, -1 for padding and for one that names no place.
@@ -152,226 +154,735 @@ __device__ __forceinline__ uint32_t cs_key(float z) {
   return b ^ ((int)b < 0 ? 0xffffffffu : 0x80000000u);
 }
 __device__ __forceinline__ float cs_score(uint32_t key) { return __uint_as_float(key ^ ((int)key < 0 ? 0x80000000u : 0xffffffffu)); }
-__device__ __forceinline__ void cs_mma(int (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+// C(16x8, whole numbers) += A(16x32 bytes) * B(32x8 bytes)
+__device__ __forceinline__ void cs_mma(int (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
   asm("mma.sync.aligned.m16n8k32.row.col.s32.s8.s8.s32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
-      : "+r"(c[0]), "+r"(c[1]), "+r"(c[2]), "+r"(c[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+      : "+r"(c[0]), "+r"(c[1]), "+r"(c[2]), "+r"(c[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+// 2^(byte - 64), byte below 128
+__device__ __forceinline__ float cs_power(unsigned byte) { return __uint_as_float(((byte & 127u) + 63u) << 23); }
+
+// A token's queries of one head, added up and as whole numbers: one warp, D / 32 channels a lane.
+template <typename T, int D>
+__device__ __forceinline__ void cs_query(const cs_args& a, int n, int h, signed char* to) {
+  constexpr int N = D / 32;
+  const int lane = threadIdx.x & 31;
+  const char* at = a.q + n * a.q_token_stride + (long long)h * a.G * a.q_head_stride + lane * (2 * N);
+  double sum[N];
+#pragma unroll
+  for (int e = 0; e < N; ++e) sum[e] = 0.0;
+#pragma unroll 4
+  for (int j = 0; j < a.G; ++j) {
+    uint2 w = make_uint2(0u, 0u);
+    if (N == 4) w = *reinterpret_cast<const uint2*>(at + j * a.q_head_stride);
+    else w.x = *reinterpret_cast<const uint32_t*>(at + j * a.q_head_stride);
+    const float2 x = dd_unpack2<T>(w.x), y = dd_unpack2<T>(w.y);
+    sum[0] += (double)x.x;
+    sum[1] += (double)x.y;
+    if (N == 4) { sum[N - 2] += (double)y.x; sum[N - 1] += (double)y.y; }
+  }
+#pragma unroll
+  for (int e = 0; e < N; ++e) sum[e] = cs_finite(sum[e]);
+  const double down = cs_two_to(-cs_exponent(sum, CS_Q_LEAST));
+  uint32_t w = 0;
+#pragma unroll
+  for (int e = 0; e < N; ++e) w |= (uint32_t)(cs_code(sum[e], down) & 0xff) << (8 * e);
+  if (N == 4) *reinterpret_cast<uint32_t*>(to + lane * 4) = w;
+  else *reinterpret_cast<unsigned short*>(to + lane * 2) = (unsigned short)w;
+}
+// The same for all tokens and heads of a launch, into the workspace: [token][head][D] bytes.
+template <typename T, int D>
+__global__ void __launch_bounds__(256) dd_cache_query_kernel(const cs_args a) {
+  const long long item = (long long)blockIdx.x * 8 + (threadIdx.x >> 5);
+  dd_grid_dependency_wait();
+  if (item >= (long long)a.n_tokens * a.c.n_kv_heads) return;
+  const int n = (int)(item / a.c.n_kv_heads), h = (int)(item - (long long)n * a.c.n_kv_heads);
+  cs_query<T, D>(a, a.first_token + n, h, a.codes + item * D);
 }
 
-// TT tokens of one head and a run of pages. Channels are dealt to the MMA's slots as they lie: lane t of a group of four takes the
-// D / 4 channels from D / 4 t on, of landmarks and queries alike.
+__device__ __forceinline__ void cs_copy16(void* to, const void* from) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"((uint32_t)__cvta_generic_to_shared(to)), "l"(from) : "memory");
+}
+__device__ __forceinline__ void cs_copied() { asm volatile("cp.async.commit_group;\n\tcp.async.wait_group 0;" ::: "memory"); }
+
+// TT tokens of one head and up to cs_pages() pages, whose landmarks are brought into shared memory all at once (the chain table entry ->
+// landmark is waited for once a block, not once for every few pages). A warp takes MT tiles of 16 tokens as the rows of its MMAs (their
+// fragments stay in registers) and 8 pages at a time as the columns. Channels are dealt to the MMA's slots as they lie: lane t of a group of
+// four takes the D / 4 channels from D / 4 t on, of landmarks and queries alike; landmarks of D + 16 bytes are read without bank
+// conflicts.
+DD_HD constexpr int cs_pages(int tokens) { return tokens == 1 ? 128 : 256; }
 template <typename T, int D, int TT>
 __global__ void __launch_bounds__(CS_THREADS) dd_cache_score_kernel(const cs_args a) {
-  constexpr int CT = (TT + 7) / 8, N = D / 32;
-  __shared__ __align__(16) unsigned char sh_q[CT * 8][D];
-  __shared__ int sh_own[CT * 8], sh_req[CT * 8];
+  constexpr int ROWS = (TT + 15) / 16 * 16, MT = TT >= 32 ? 2 : 1, LM = D + CS_TAIL;
+  constexpr int SETS = ROWS / (16 * MT), STRIDE = D + 16;               // warps of a set hold the same tokens and share the pages out
+  constexpr int PAGES = cs_pages(TT);
+  extern __shared__ __align__(16) unsigned char cs_smem[];              // landmarks [PAGES][LM]
+  __shared__ __align__(16) signed char sh_q[TT][STRIDE];
+  __shared__ int sh_own[ROWS], sh_req[ROWS];
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
+  const int set = warp % SETS, share = warp / SETS;
+  constexpr int SHARES = CS_THREADS / 32 / SETS;
   const int tile = blockIdx.x / a.chunks, chunk = blockIdx.x - tile * a.chunks, h = blockIdx.y;
   const int n0 = tile * TT;                            // of the launch
   dd_grid_dependency_wait();
-  if (threadIdx.x < CT * 8) {
+  if (threadIdx.x < ROWS) {
     int req = -1, own = -1;
     if (threadIdx.x < TT && n0 + threadIdx.x < a.n_tokens) own = cs_own_page(a, a.first_token + n0 + threadIdx.x, req, chunk == 0 && h == 0);
     sh_own[threadIdx.x] = own;
     sh_req[threadIdx.x] = req;
   }
-  for (int i = warp; i < CT * 8; i += CS_THREADS / 32) {
-    double sum[N];
-#pragma unroll
-    for (int e = 0; e < N; ++e) sum[e] = 0.0;
-    if (i < TT && n0 + i < a.n_tokens) {
-      const char* at = a.q + (a.first_token + n0 + i) * a.q_token_stride + (long long)h * a.G * a.q_head_stride + lane * (2 * N);
-#pragma unroll 4
-      for (int j = 0; j < a.G; ++j) {
-        uint2 w = make_uint2(0u, 0u);
-        if (N == 4) w = *reinterpret_cast<const uint2*>(at + j * a.q_head_stride);
-        else w.x = *reinterpret_cast<const uint32_t*>(at + j * a.q_head_stride);
-        const float2 x = dd_unpack2<T>(w.x), y = dd_unpack2<T>(w.y);
-        sum[0] += (double)x.x;
-        sum[1] += (double)x.y;
-        if (N == 4) { sum[N - 2] += (double)y.x; sum[N - 1] += (double)y.y; }
-      }
-    }
-    double top = 0.0;
-#pragma unroll
-    for (int e = 0; e < N; ++e) {
-      sum[e] = cs_finite(sum[e]);
-      top = fmax(top, fabs(sum[e]));
-    }
-    // (a sum of fp32-sized values stays below 2^64 * 127 only for those; larger ones are held at the largest number)
-    const double down = cs_two_to(-cs_exponent(cs_warp_max(top), CS_Q_LEAST));
-    uint32_t w = 0;
-#pragma unroll
-    for (int e = 0; e < N; ++e) w |= (uint32_t)(cs_code(sum[e], down) & 0xff) << (8 * e);
-    if (N == 4) *reinterpret_cast<uint32_t*>(&sh_q[i][lane * 4]) = w;
-    else *reinterpret_cast<unsigned short*>(&sh_q[i][lane * 2]) = (unsigned short)w;
-  }
   __syncthreads();
-  uint32_t qf[CT][D / 16];                             // of token 8 ct + g: the words of this lane's channels
-#pragma unroll
-  for (int ct = 0; ct < CT; ++ct)
-#pragma unroll
-    for (int i = 0; i < D / 64; ++i) {
-      const uint4 v = *reinterpret_cast<const uint4*>(&sh_q[ct * 8 + g][t * (D / 4) + i * 16]);
-      qf[ct][4 * i] = v.x; qf[ct][4 * i + 1] = v.y; qf[ct][4 * i + 2] = v.z; qf[ct][4 * i + 3] = v.w;
-    }
-  const int p_begin = chunk * a.chunk_pages, p_end = min(p_begin + a.chunk_pages, a.c.max_pages);
+  const int p_begin = chunk * PAGES, p_end = min(p_begin + PAGES, a.c.max_pages);
+  const int row0 = set * 16 * MT;
+  uint32_t qf[MT][D / 32][4];                          // step s: channels D / 4 t + 8 s .. + 7 of tokens g and g + 8
+  bool have_q = false;
   // tokens of one request at a time: tokens s .. e - 1 of the tile
   for (int s = 0, e; s < TT; s = e) {
     const int req = sh_req[s];
-    int most = sh_own[s];
-    for (e = s + 1; e < TT && sh_req[e] == req; ++e) most = max(most, sh_own[e]);
-    if (most < 0) continue;
-    const int* table = a.c.table + req * a.c.table_stride;
+    int most = sh_own[s], least = sh_own[s];
+    for (e = s + 1; e < TT && sh_req[e] == req; ++e) {
+      most = max(most, sh_own[e]);
+      least = min(least, sh_own[e]);
+    }
     const int last = min(p_end, most + 1);
-    for (int p0 = p_begin + warp * 16; p0 < last; p0 += CS_THREADS / 2) {
-      uint32_t r[2][D / 16];
-      float by[2];
+    if (p_begin >= last) continue;                     // the same for the whole block
+    // ---- landmarks of pages p_begin .. last - 1
+    const int* table = a.c.table + req * a.c.table_stride;
+    if (s > 0) __syncthreads();                        // the pages of the tokens before have been used
+    for (int i = threadIdx.x / 2; i < last - p_begin; i += CS_THREADS / 2) {       // two threads a landmark
+      const int blk = __ldg(table + p_begin + i);
+      unsigned char* to = cs_smem + i * LM + (threadIdx.x & 1) * 16;
+      if ((unsigned)blk < (unsigned)a.c.n_blocks) {
+        const char* lm = a.landmarks + ((long long)blk * a.c.n_kv_heads + h) * LM + (threadIdx.x & 1) * 16;
 #pragma unroll
-      for (int k = 0; k < 2; ++k) {
-        const int p = p0 + g + 8 * k;
-        int blk = p < last ? __ldg(table + p) : 0;
-        const bool bad = p >= last || (unsigned)blk >= (unsigned)a.c.n_blocks;
-        if (bad) {
-          if (p < last && t == 0) dd_status(a.c.status, blk);
-          blk = 0;
-        }
-        const char* lm = a.landmarks + ((long long)blk * a.c.n_kv_heads + h) * (D + CS_TAIL);
+        for (int c = 0; c < (LM / 16 + 1) / 2; ++c)
+          if (c < LM / 32 || (threadIdx.x & 1) == 0) cs_copy16(to + c * 32, lm + c * 32);
+      } else {
+        if (threadIdx.x % 2 == 0) dd_status(a.c.status, blk);
 #pragma unroll
-        for (int i = 0; i < D / 64; ++i) {
-          uint4 v = make_uint4(0u, 0u, 0u, 0u);
-          if (!bad) v = *reinterpret_cast<const uint4*>(lm + t * (D / 4) + i * 16);
-          r[k][4 * i] = v.x; r[k][4 * i + 1] = v.y; r[k][4 * i + 2] = v.z; r[k][4 * i + 3] = v.w;
-        }
-        // 2^(byte - 64), byte below 128
-        by[k] = bad ? 0.f : __uint_as_float((uint32_t)((*reinterpret_cast<const unsigned char*>(lm + D) & 127) + 63) << 23);
+        for (int c = 0; c < (LM / 16 + 1) / 2; ++c)
+          if (c < LM / 32 || (threadIdx.x & 1) == 0) *reinterpret_cast<uint4*>(to + c * 32) = make_uint4(0u, 0u, 0u, 0u);
       }
+    }
+    if (!have_q) {
+      if constexpr (TT == 64) {
+        for (int i = threadIdx.x; i < TT * (D / 16); i += CS_THREADS) {
+          const int r = i / (D / 16), c = i % (D / 16);
+          if (n0 + r < a.n_tokens) cs_copy16(&sh_q[r][c * 16], a.codes + ((long long)(n0 + r) * a.c.n_kv_heads + h) * D + c * 16);
+        }
+      } else {
+        for (int i = warp; i < TT; i += CS_THREADS / 32)
+          if (n0 + i < a.n_tokens) cs_query<T, D>(a, a.first_token + n0 + i, h, sh_q[i]);
+      }
+    }
+    cs_copied();
+    __syncthreads();
+    if (!have_q) {
+      have_q = true;
 #pragma unroll
-      for (int ct = 0; ct < CT; ++ct) {
-        if (ct * 8 >= e || ct * 8 + 8 <= s) continue;
+      for (int m = 0; m < MT; ++m)
+#pragma unroll
+        for (int i = 0; i < D / 32; ++i) {
+          const int r0 = row0 + 16 * m + g, r1 = r0 + 8;
+          uint2 lo = make_uint2(0u, 0u), hi = make_uint2(0u, 0u);
+          if (r0 < TT && n0 + r0 < a.n_tokens) lo = *reinterpret_cast<const uint2*>(&sh_q[r0 < TT ? r0 : 0][t * (D / 4) + 8 * i]);
+          if (r1 < TT && n0 + r1 < a.n_tokens) hi = *reinterpret_cast<const uint2*>(&sh_q[r1 < TT ? r1 : 0][t * (D / 4) + 8 * i]);
+          qf[m][i][0] = lo.x; qf[m][i][1] = hi.x; qf[m][i][2] = lo.y; qf[m][i][3] = hi.y;
+        }
+    }
+    if (s >= row0 + 16 * MT || e <= row0) continue;    // none of this warp's tokens
+    const bool all_rows = s <= row0 && e >= row0 + 16 * MT;
+    for (int p0 = p_begin + share * 8; p0 < last; p0 += SHARES * 8) {
+      // lane (g, t): D / 4 bytes of the landmark of page p0 + g (behind the last page: whatever lies there, for nobody)
+      const unsigned char* lm = cs_smem + (p0 - p_begin) * LM;
+      uint32_t r[D / 16];
+#pragma unroll
+      for (int i = 0; i < D / 64; ++i) {
+        const uint4 v = *reinterpret_cast<const uint4*>(lm + g * LM + t * (D / 4) + i * 16);
+        r[4 * i] = v.x; r[4 * i + 1] = v.y; r[4 * i + 2] = v.z; r[4 * i + 3] = v.w;
+      }
+      const float by0 = cs_power(lm[2 * t * LM + D]), by1 = cs_power(lm[(2 * t + 1) * LM + D]);
+      int acc[MT][4];
+#pragma unroll
+      for (int m = 0; m < MT; ++m) acc[m][0] = acc[m][1] = acc[m][2] = acc[m][3] = 0;
+#pragma unroll
+      for (int i = 0; i < D / 32; ++i)
+#pragma unroll
+        for (int m = 0; m < MT; ++m) cs_mma(acc[m], qf[m][i], r[2 * i], r[2 * i + 1]);
+      // pages that all tokens of the run see and none of them keeps anyway
+      const bool plain = all_rows && p0 >= a.first && p0 + 7 <= least - a.recent && p0 + 8 <= last;
+#pragma unroll
+      for (int m = 0; m < MT; ++m)
+#pragma unroll
+        for (int x = 0; x < 2; ++x) {
+          const int i = row0 + 16 * m + g + 8 * x;
+          if (TT < 16 && i >= TT) continue;
+          uint32_t* to = a.keys + ((long long)(n0 + i) * a.c.n_kv_heads + h) * a.stride + p0 + 2 * t;
+          const uint32_t k0 = cs_key((float)acc[m][2 * x] * by0), k1 = cs_key((float)acc[m][2 * x + 1] * by1);
+          if (plain) {
+            *reinterpret_cast<uint2*>(to) = make_uint2(k0, k1);
+          } else if (i >= s && i < e) {
+            const int own = sh_own[i], page = p0 + 2 * t, end = min(own, last - 1);
+            if (page <= end) to[0] = page < a.first || page > own - a.recent ? 0xffffffffu : k0;
+            if (page + 1 <= end) to[1] = page + 1 < a.first || page + 1 > own - a.recent ? 0xffffffffu : k1;
+          }
+        }
+    }
+  }
+}
+
+// ---- the choice
+// The k largest keys of a row that WARPS warps share; `each(f)` calls f(key, page, group) for this lane's run of pages in ascending order,
+// runs in the order of the lanes, key 0 where there is no page. `count(x)` says how many of the lane's keys are x or above, and
+// `list(x, f)` calls f(key, page) for those, in ascending order of their pages. The k-th largest of the maxima of small groups bounds the
+// threshold from below: k keys at least are no smaller. The keys from that bound on, little more than k, are listed in shared
+// memory, and one warp finds the threshold among them by bisection: a step counts keys at or above the middle, and stops as soon as
+// exactly k are. Where the bound lets too many through (more than CAP; ties), the threshold is found among all keys.
+template <int WARPS, int NG, int CAP, typename EACH, typename COUNT, typename LIST, typename SYNC>
+__device__ __forceinline__ void cs_choose(EACH each, COUNT count, LIST list, SYNC sync, int k, int* out, int w, int* sh_a, int* sh_b, uint32_t* sh_key, unsigned* sh_page) {
+  const int lane = threadIdx.x & 31;
+  auto add_up = [&](int v) {                                          // over the row
+    v = __reduce_add_sync(0xffffffffu, v);
+    if (WARPS == 1) return v;
+    sync();
+    if (lane == 0) sh_a[w] = v;
+    sync();
+    return (int)__reduce_add_sync(0xffffffffu, lane < WARPS ? sh_a[lane] : 0);
+  };
+  auto range = [&](uint32_t& lo, uint32_t& hi) {
+    lo = __reduce_min_sync(0xffffffffu, lo);
+    hi = __reduce_max_sync(0xffffffffu, hi);
+    if (WARPS > 1) {
+      sync();
+      if (lane == 0) { sh_a[w] = (int)lo; sh_b[w] = (int)hi; }
+      sync();
+      lo = __reduce_min_sync(0xffffffffu, lane < WARPS ? (uint32_t)sh_a[lane] : 0xffffffffu);
+      hi = __reduce_max_sync(0xffffffffu, lane < WARPS ? (uint32_t)sh_b[lane] : 0u);
+    }
+  };
+  // The middle of two keys' scores at first, which splits their number better than the middle of the keys.
+  auto middle = [&](uint32_t lo, uint32_t hi, int step) {
+    return step < 20 ? min(max(cs_key(0.5f * cs_score(lo) + 0.5f * cs_score(hi)), lo + 1u), hi) : lo + (hi - lo) / 2 + 1;
+  };
+  // ---- the bound
+  uint32_t top[NG];
+#pragma unroll
+  for (int i = 0; i < NG; ++i) top[i] = 0u;
+  each([&](uint32_t v, int, int i) { top[i] = max(top[i], v); });
+  uint32_t bound = 1u;
+  {
+    uint32_t lo = 0xffffffffu, hi = 0u;
+#pragma unroll
+    for (int i = 0; i < NG; ++i)
+      if (top[i] != 0u && top[i] != 0xffffffffu) {
+        lo = min(lo, top[i]);
+        hi = max(hi, top[i]);
+      }
+    range(lo, hi);
+    // at least k maxima at or above `bound` whenever it has moved; a few more than k will do
+    for (int step = 0; step < 24 && lo < hi; ++step) {
+      const uint32_t mid = middle(lo, hi, step);
+      int c = 0;
+#pragma unroll
+      for (int i = 0; i < NG; ++i) c += top[i] >= mid;
+      c = add_up(c);
+      if (c >= k) {
+        bound = lo = mid;
+        if (c <= k + (k >> 3)) break;
+      } else {
+        hi = mid - 1;
+      }
+    }
+  }
+  // ---- the keys that are no smaller
+  const int mine = count(bound);
+  int before = mine;                                                  // of the lanes up to this one
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const int v = __shfl_up_sync(0xffffffffu, before, o);
+    if (lane >= o) before += v;
+  }
+  int listed = __shfl_sync(0xffffffffu, before, 31);
+  before -= mine;
+  if (WARPS > 1) {
+    sync();
+    if (lane == 0) sh_a[w] = listed;
+    sync();
+    const int v = lane < WARPS ? sh_a[lane] : 0;
+    before += __reduce_add_sync(0xffffffffu, lane < w ? v : 0);
+    listed = __reduce_add_sync(0xffffffffu, v);
+  }
+  if (listed <= CAP) {
+    list(bound, [&](uint32_t v, int p) {
+      sh_key[before] = v;
+      sh_page[before] = p;
+      ++before;
+    });
+    sync();
+    if (w > 0) return;
+    // one warp: entry 32 j + lane
+    constexpr int FEW = 4;
+    uint32_t few[FEW];
+#pragma unroll
+    for (int j = 0; j < FEW; ++j) few[j] = 32 * j + lane < listed ? sh_key[32 * j + lane] : 0u;
+    uint32_t lo = 0xffffffffu, hi = 0u;
+    auto all = [&](auto&& f) {
+#pragma unroll
+      for (int j = 0; j < FEW; ++j) f(few[j]);
+      for (int i = 32 * FEW + lane; i < listed; i += 32) f(sh_key[i]);
+    };
+    all([&](uint32_t v) {
+      if (v != 0u && v != 0xffffffffu) {
+        lo = min(lo, v);
+        hi = max(hi, v);
+      }
+    });
+    lo = __reduce_min_sync(0xffffffffu, lo);
+    hi = __reduce_max_sync(0xffffffffu, hi);
+    int take = 0x7fffffff;                                            // how many of the keys equal to the threshold
+    if (listed > k) {
+      bool exact = false;
+      for (int step = 0; lo < hi; ++step) {
+        const uint32_t mid = middle(lo, hi, step);
+        int c = 0;
+        all([&](uint32_t v) { c += v >= mid; });
+        c = __reduce_add_sync(0xffffffffu, c);
+        if (c == k) { lo = mid; exact = true; break; }
+        if (c > k) lo = mid;
+        else hi = mid - 1;
+      }
+      if (!exact) {
+        int c = 0;
+        all([&](uint32_t v) { c += v > lo; });
+        take = k - (int)__reduce_add_sync(0xffffffffu, c);
+      }
+    } else {
+      lo = 1u;
+    }
+    int at = 0, equal = 0;
+    const unsigned below = (1u << lane) - 1u;
+    for (int i = lane; i - lane < listed; i += 32) {
+      const uint32_t v = i < listed ? sh_key[i] : 0u;
+      const unsigned eq = __ballot_sync(0xffffffffu, v == lo);
+      const bool in = v > lo || (v == lo && equal + __popc(eq & below) < take);
+      const unsigned m = __ballot_sync(0xffffffffu, in);
+      if (in) out[at + __popc(m & below)] = (int)sh_page[i];
+      at += __popc(m);
+      equal += __popc(eq);
+    }
+    return;
+  }
+  // ---- among all keys
+  uint32_t lo = 0xffffffffu, hi = 0u;
+  each([&](uint32_t v, int, int) {
+    if (v != 0u && v != 0xffffffffu) {
+      lo = min(lo, v);
+      hi = max(hi, v);
+    }
+  });
+  range(lo, hi);
+  bool exact = false;
+  for (int step = 0; lo < hi; ++step) {
+    const uint32_t mid = middle(lo, hi, step);
+    int c = 0;
+    each([&](uint32_t v, int, int) { c += v >= mid; });
+    c = add_up(c);
+    if (c == k) { lo = mid; exact = true; break; }
+    if (c > k) lo = mid;
+    else hi = mid - 1;
+  }
+  int above = 0, equal = 0;
+  each([&](uint32_t v, int, int) { above += v > lo; equal += v == lo; });
+  int above_to = above, equal_to = equal;
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const int x = __shfl_up_sync(0xffffffffu, above_to, o), y = __shfl_up_sync(0xffffffffu, equal_to, o);
+    if (lane >= o) {
+      above_to += x;
+      equal_to += y;
+    }
+  }
+  int all_above = __shfl_sync(0xffffffffu, above_to, 31);
+  const int warp_equal = __shfl_sync(0xffffffffu, equal_to, 31);
+  above_to -= above;
+  equal_to -= equal;
+  if (WARPS > 1) {
+    sync();
+    if (lane == 0) { sh_a[w] = all_above; sh_b[w] = warp_equal; }
+    sync();
+    const int x = lane < WARPS ? sh_a[lane] : 0, y = lane < WARPS ? sh_b[lane] : 0;
+    all_above = __reduce_add_sync(0xffffffffu, x);
+    above_to += __reduce_add_sync(0xffffffffu, lane < w ? x : 0);
+    equal_to += __reduce_add_sync(0xffffffffu, lane < w ? y : 0);
+  }
+  const int take = exact ? 0x7fffffff : k - all_above;
+  each([&](uint32_t v, int p, int) {
+    const bool eq = v == lo;
+    if (v > lo || (eq && equal_to < take)) out[above_to + min(equal_to, take)] = p;
+    above_to += v > lo;
+    equal_to += eq;
+  });
+}
+
+// Choice from keys in the workspace: WARPS warps a row, a lane's run KPT keys in registers (0: as many as it takes, read again where
+// they are needed).
+template <int WARPS, int KPT>
+__global__ void __launch_bounds__(WARPS * 32) dd_cache_topk_kernel(const cs_args a) {
+  constexpr int NG = 4, CAP = 2048;
+  __shared__ int sh_a[WARPS], sh_b[WARPS];
+  __shared__ uint32_t sh_key[CAP];
+  __shared__ unsigned sh_page[CAP];
+  const int w = threadIdx.x >> 5;
+  const long long row = blockIdx.x;
+  dd_grid_dependency_wait();
+  const int n = (int)(row / a.c.n_kv_heads);
+  int req;
+  const int P = cs_own_page(a, a.first_token + n, req, false) + 1, k = a.k;
+  int* out = a.out + ((long long)a.first_token * a.c.n_kv_heads + row) * k;
+  if (P <= k) {                                                       // everything visible fits
+    for (int i = threadIdx.x; i < k; i += WARPS * 32) out[i] = i < P ? i : -1;
+    return;
+  }
+  const uint32_t* keys = a.keys + row * a.stride;
+  const int run = KPT ? KPT : (P + WARPS * 128 - 1) / (WARPS * 128) * 4, at0 = threadIdx.x * run;
+  auto load4 = [&](uint32_t* to, int at) {                            // no key is 0
+    uint4 v = make_uint4(0u, 0u, 0u, 0u);
+    if (at < P) v = *reinterpret_cast<const uint4*>(keys + at);
+    to[0] = v.x;
+    to[1] = at + 1 < P ? v.y : 0u;
+    to[2] = at + 2 < P ? v.z : 0u;
+    to[3] = at + 3 < P ? v.w : 0u;
+  };
+  auto choose = [&](auto each) {
+    auto count = [&](uint32_t x) {
+      int c = 0;
+      each([&](uint32_t v, int, int) { c += v >= x; });
+      return c;
+    };
+    auto list = [&](uint32_t x, auto&& f) {
+      each([&](uint32_t v, int p, int) {
+        if (v >= x) f(v, p);
+      });
+    };
+    cs_choose<WARPS, NG, CAP>(each, count, list, [] { __syncthreads(); }, k, out, w, sh_a, sh_b, sh_key, sh_page);
+  };
+  if constexpr (KPT > 0) {
+    uint32_t key[KPT];
+#pragma unroll
+    for (int j = 0; j < KPT; j += 4) load4(key + j, at0 + j);
+    auto each = [&](auto&& f) {
+#pragma unroll
+      for (int j = 0; j < KPT; ++j) f(key[j], at0 + j, j * NG / KPT);
+    };
+    choose(each);
+  } else {
+    auto each = [&](auto&& f) {
+#pragma unroll 4
+      for (int j = 0; j < run; j += 4) {
+        uint32_t v[4];
+        load4(v, at0 + j);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) f(v[i], at0 + j + i, i);
+      }
+    };
+    choose(each);
+  }
+}
+
+// Choice for few rows, where the chain of a bisection's steps would be what takes the time: a block of 256 threads a row, a run of up to
+// 16 keys each. The k-th largest of the threads' maxima, found by every thread's rank among all (each compares its own with the 256,
+// read by all at once), bounds the threshold; so does the rank of every listed key among the listed ones decide. k up to 256.
+constexpr int CR_LIST = 1024, CR_RUN = 16, CR_ROW_THREADS = 256;
+// Rank of entry `me` (key v) among n entries padded to a multiple of 4 with zeros: the larger keys, and of its equals those in front. The
+// threads of a warp stand in a row, so that only the 32 entries around them need both questions.
+__device__ __forceinline__ int cr_rank(const uint32_t* all, int n, uint32_t v, int me) {
+  const uint4* all4 = reinterpret_cast<const uint4*>(all);
+  const int n4 = (n + 3) >> 2, here = (me & ~31) >> 2;
+  int r = 0, j = 0;
+#pragma unroll 4
+  for (; j < min(here, n4); ++j) {
+    const uint4 o = all4[j];
+    r += (o.x >= v) + (o.y >= v) + (o.z >= v) + (o.w >= v);
+  }
+#pragma unroll 2
+  for (; j < min(here + 8, n4); ++j) {
+    const uint4 o = all4[j];
+    r += (o.x > v || (o.x == v && 4 * j < me)) + (o.y > v || (o.y == v && 4 * j + 1 < me)) + (o.z > v || (o.z == v && 4 * j + 2 < me)) +
+         (o.w > v || (o.w == v && 4 * j + 3 < me));
+  }
+#pragma unroll 4
+  for (; j < n4; ++j) {
+    const uint4 o = all4[j];
+    r += (o.x > v) + (o.y > v) + (o.z > v) + (o.w > v);
+  }
+  return r;
+}
+__global__ void __launch_bounds__(CR_ROW_THREADS) dd_cache_topk_rank_kernel(const cs_args a) {
+  constexpr int WARPS = CR_ROW_THREADS / 32;
+  __shared__ __align__(16) uint32_t sh_top[CR_ROW_THREADS], sh_key[CR_LIST];
+  __shared__ unsigned sh_page[CR_LIST];
+  __shared__ int sh_a[WARPS], sh_b[WARPS];
+  __shared__ uint32_t sh_bound;
+  const int lane = threadIdx.x & 31, w = threadIdx.x >> 5;
+  const long long row = blockIdx.x;
+  dd_grid_dependency_wait();
+  const int n = (int)(row / a.c.n_kv_heads);
+  int req;
+  const int P = cs_own_page(a, a.first_token + n, req, false) + 1, k = a.k;
+  int* out = a.out + ((long long)a.first_token * a.c.n_kv_heads + row) * k;
+  if (P <= k) {                                                       // everything visible fits
+    for (int i = threadIdx.x; i < k; i += CR_ROW_THREADS) out[i] = i < P ? i : -1;
+    return;
+  }
+  const uint32_t* keys = a.keys + row * a.stride;
+  const int run = (P + CR_ROW_THREADS - 1) / CR_ROW_THREADS, at0 = threadIdx.x * run;
+  uint32_t key[CR_RUN], top = 0u;
+#pragma unroll
+  for (int j = 0; j < CR_RUN; ++j) {
+    key[j] = j < run && at0 + j < P ? keys[at0 + j] : 0u;             // no key is 0
+    top = max(top, key[j]);
+  }
+  sh_top[threadIdx.x] = top;
+  if (threadIdx.x == 0) sh_bound = 1u;
+  __syncthreads();
+  if (top != 0u && cr_rank(sh_top, CR_ROW_THREADS, top, threadIdx.x) == k - 1) sh_bound = top;
+  __syncthreads();
+  const uint32_t bound = sh_bound;
+  auto sums = [&](int v, int& total) {                                // of the threads before this one, and of all
+    int x = v;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const int y = __shfl_up_sync(0xffffffffu, x, o);
+      if (lane >= o) x += y;
+    }
+    __syncthreads();
+    if (lane == 31) sh_a[w] = x;
+    __syncthreads();
+    const int y = lane < WARPS ? sh_a[lane] : 0;
+    total = __reduce_add_sync(0xffffffffu, y);
+    return x - v + (int)__reduce_add_sync(0xffffffffu, lane < w ? y : 0);
+  };
+  int mine = 0, listed;
+#pragma unroll
+  for (int j = 0; j < CR_RUN; ++j) mine += key[j] >= bound;
+  int at = sums(mine, listed);
+  if (listed <= CR_LIST) {
+#pragma unroll
+    for (int j = 0; j < CR_RUN; ++j)
+      if (key[j] >= bound) {
+        sh_key[at] = key[j];
+        sh_page[at++] = at0 + j;
+      }
+    if (threadIdx.x < 3 && listed + threadIdx.x < CR_LIST) sh_key[listed + threadIdx.x] = 0u;
+    __syncthreads();
+    int done = 0;
+    for (int i0 = 0; i0 < listed; i0 += CR_ROW_THREADS) {
+      const int i = i0 + threadIdx.x;
+      const bool in = i < listed && cr_rank(sh_key, listed, sh_key[i < listed ? i : 0], i) < k;
+      int all;
+      const int to = done + sums(in, all);
+      if (in) out[to] = sh_page[i];
+      done += all;
+    }
+    return;
+  }
+  auto each = [&](auto&& f) {
+#pragma unroll
+    for (int j = 0; j < CR_RUN; ++j) f(key[j], at0 + j, j / 4);
+  };
+  auto count = [&](uint32_t x) {
+    int c = 0;
+    each([&](uint32_t v, int, int) { c += v >= x; });
+    return c;
+  };
+  auto list = [&](uint32_t x, auto&& f) {
+    each([&](uint32_t v, int p, int) {
+      if (v >= x) f(v, p);
+    });
+  };
+  cs_choose<WARPS, 4, CR_LIST>(each, count, list, [] { __syncthreads(); }, k, out, w, sh_a, sh_b, sh_key, sh_page);
+}
+
+// ---- scores and choice in one, where the keys of a row fit shared memory: TT tokens of one head (16, or 1) against all of their pages.
+// Landmarks come in groups of CF_PAGES, several on their way while one is used; the 16 warps take 8 pages of a group each. Then a
+// warp a token (TT = 16), or all of them (TT = 1), choose; their lists lie where the landmarks were. One block an SM; what bounds it for 16 tokens is the landmarks' way
+// from L2 to every block (2048 pages: 295 KB for 16 tokens) and the choice's instructions. 2048 tokens x 2048 pages x 8 heads: 143 us (two kernels with keys in the workspace: 165).
+constexpr int CF_PAGES = 128, CF_THREADS = 512;
+template <int TT> struct cf_geom {
+  static constexpr int CAP = TT == 1 ? 2048 : 256;                   // of a row's list
+  static constexpr int STAGES = TT == 1 ? 8 : 4;
+};
+constexpr int CF_MOST = 2048;                                        // pages
+// Keys of a row in shared memory: a lane's run of pages (a multiple of 8), one word, the next lane's: no bank conflicts.
+template <int TT> __host__ __device__ constexpr int cf_lanes() { return TT == 1 ? CF_THREADS : 32; }
+template <int TT> __host__ __device__ constexpr int cf_run(int pages) { return (pages + 8 * cf_lanes<TT>() - 1) / (8 * cf_lanes<TT>()) * 8; }
+template <int TT> __host__ __device__ constexpr int cf_stride(int max_pages) { return cf_lanes<TT>() * (cf_run<TT>(max_pages) + 1); }
+template <int TT> size_t cf_smem(int d, int max_pages) {
+  return (size_t)cf_geom<TT>::STAGES * CF_PAGES * (d + CS_TAIL) + ((size_t)TT * cf_stride<TT>(max_pages) + max_pages) * 4;
+}
+template <typename T, int D, int TT>
+__global__ void __launch_bounds__(CF_THREADS) dd_cache_select_kernel(const cs_args a) {
+  constexpr int LM = D + CS_TAIL, STRIDE = D + 16, CAP = cf_geom<TT>::CAP, WARPS = CF_THREADS / 32;
+  constexpr int STAGES = cf_geom<TT>::STAGES;
+  static_assert(TT * CAP * 8 <= STAGES * CF_PAGES * (64 + CS_TAIL), "the lists lie where the landmarks were");
+  extern __shared__ __align__(16) unsigned char cs_smem[];            // landmarks [STAGES][CF_PAGES][LM], keys [TT][stride], a table row
+  __shared__ __align__(16) signed char sh_q[TT][STRIDE];
+  __shared__ int sh_own[16], sh_req[16], sh_a[WARPS], sh_b[WARPS];
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
+  const int h = blockIdx.y, n0 = blockIdx.x * TT, stride = cf_stride<TT>(a.c.max_pages);
+  uint32_t* const keys = reinterpret_cast<uint32_t*>(cs_smem + STAGES * CF_PAGES * LM);
+  int* const blocks = reinterpret_cast<int*>(keys + TT * stride);
+  uint32_t* const list_key = reinterpret_cast<uint32_t*>(cs_smem);
+  unsigned* const list_page = list_key + TT * CAP;
+  dd_grid_dependency_wait();
+  if (threadIdx.x < 16) {
+    int req = -1, own = -1;
+    if (threadIdx.x < TT && n0 + threadIdx.x < a.n_tokens) own = cs_own_page(a, n0 + threadIdx.x, req, h == 0);
+    sh_own[threadIdx.x] = own;
+    sh_req[threadIdx.x] = req;
+  }
+  __syncthreads();
+  int furthest = 0;                                    // pages of any token of the tile
+  for (int i = 0; i < TT; ++i) furthest = max(furthest, sh_own[i] + 1);
+  const int run = cf_run<TT>(max(furthest, 1));
+  const unsigned by_run = 0xffffffffu / run + 1;       // page / run by a multiplication (below 2^16, exact)
+  uint32_t qf[D / 32][4];                              // step s: channels D / 4 t + 8 s .. + 7 of tokens g and g + 8
+  bool have_q = false;
+  for (int s = 0, e; s < TT; s = e) {                  // tokens of one request at a time
+    const int req = sh_req[s];
+    int most = sh_own[s], least = sh_own[s];
+    for (e = s + 1; e < TT && sh_req[e] == req; ++e) {
+      most = max(most, sh_own[e]);
+      least = min(least, sh_own[e]);
+    }
+    if (most < a.k) continue;                          // everything they see fits (k pages and more: a choice)
+    const int pages = most + 1, groups = (pages + CF_PAGES - 1) / CF_PAGES;
+    const int* table = a.c.table + req * a.c.table_stride;
+    const int mine = threadIdx.x >> 2, part = threadIdx.x & 3;         // four threads a landmark
+    const char* const from = a.landmarks + (long long)h * LM + part * 16;
+    const long long block_bytes = (long long)a.c.n_kv_heads * LM;
+    unsigned char* const into = cs_smem + mine * LM + part * 16;
+    auto fetch = [&](int i) {                          // group i
+      const int p = i * CF_PAGES + mine;
+      unsigned char* to = into + (i & (STAGES - 1)) * (CF_PAGES * LM);
+      if (p < pages) {
+        const int blk = blocks[p];
+        if ((unsigned)blk < (unsigned)a.c.n_blocks) {
+          const char* lm = from + blk * block_bytes;
+#pragma unroll
+          for (int c = 0; c * 64 < LM; ++c)
+            if (c * 64 + 64 <= LM || part == 0) cs_copy16(to + c * 64, lm + c * 64);
+        } else {
+          if (part == 0) dd_status(a.c.status, blk);
+#pragma unroll
+          for (int c = 0; c * 64 < LM; ++c)
+            if (c * 64 + 64 <= LM || part == 0) *reinterpret_cast<uint4*>(to + c * 64) = make_uint4(0u, 0u, 0u, 0u);
+        }
+      }
+      asm volatile("cp.async.commit_group;" ::: "memory");
+    };
+    __syncthreads();                                   // what the tokens before used is free
+    for (int i = threadIdx.x; i < pages; i += CF_THREADS) blocks[i] = __ldg(table + i);
+    __syncthreads();
+#pragma unroll 1
+    for (int i = 0; i < STAGES - 1; ++i) fetch(i);
+    if (!have_q) {
+      if (warp < TT && n0 + warp < a.n_tokens) cs_query<T, D>(a, n0 + warp, h, sh_q[warp]);
+      __syncthreads();
+      have_q = true;
+#pragma unroll
+      for (int i = 0; i < D / 32; ++i) {
+        uint2 lo = make_uint2(0u, 0u), hi = make_uint2(0u, 0u);
+        if (g < TT && n0 + g < a.n_tokens) lo = *reinterpret_cast<const uint2*>(&sh_q[g < TT ? g : 0][t * (D / 4) + 8 * i]);
+        if (g + 8 < TT && n0 + g + 8 < a.n_tokens) hi = *reinterpret_cast<const uint2*>(&sh_q[g + 8 < TT ? g + 8 : 0][t * (D / 4) + 8 * i]);
+        qf[i][0] = lo.x; qf[i][1] = hi.x; qf[i][2] = lo.y; qf[i][3] = hi.y;
+      }
+    }
+    for (int i = 0; i < groups; ++i) {
+      asm volatile("cp.async.wait_group %0;" ::"n"(STAGES - 2) : "memory");
+      __syncwarp();                                    // a warp brings the landmarks that it uses itself
+      fetch(i + STAGES - 1);                           // over the group before this one
+      const int p0 = i * CF_PAGES + warp * 8;
+      if (p0 < pages) {
+        // lane (g, t): D / 4 bytes of the landmark of page p0 + g (behind the last page: whatever lies there, for nobody)
+        const unsigned char* lm = cs_smem + (i & (STAGES - 1)) * (CF_PAGES * LM) + warp * (8 * LM);
+        uint32_t r[D / 16];
+#pragma unroll
+        for (int c = 0; c < D / 64; ++c) {
+          const uint4 v = *reinterpret_cast<const uint4*>(lm + g * LM + t * (D / 4) + c * 16);
+          r[4 * c] = v.x; r[4 * c + 1] = v.y; r[4 * c + 2] = v.z; r[4 * c + 3] = v.w;
+        }
+        const float by0 = cs_power(lm[2 * t * LM + D]), by1 = cs_power(lm[(2 * t + 1) * LM + D]);
         int acc[4] = {0, 0, 0, 0};
 #pragma unroll
-        for (int i = 0; i < D / 32; ++i) cs_mma(acc, r[0][2 * i], r[1][2 * i], r[0][2 * i + 1], r[1][2 * i + 1], qf[ct][2 * i], qf[ct][2 * i + 1]);
+        for (int c = 0; c < D / 32; ++c) cs_mma(acc, qf[c], r[2 * c], r[2 * c + 1]);
+        // pages that all tokens of the run see and none of them keeps anyway
+        const bool plain = TT > 1 && s == 0 && e == TT && p0 >= a.first && p0 + 7 <= least - a.recent;
 #pragma unroll
-        for (int x = 0; x < 4; ++x) {
-          const int i = ct * 8 + 2 * t + (x & 1), p = p0 + g + 8 * (x >> 1);
-          if (i >= s && i < e) {
-            const int own = sh_own[i];
-            if (p <= own && p < last) {
-              const bool kept = p < a.first || p > own - a.recent;
-              a.keys[((long long)(n0 + i) * a.c.n_kv_heads + h) * a.stride + p] = kept ? 0xffffffffu : cs_key((float)acc[x] * by[x >> 1]);
-            }
+        for (int x = 0; x < 2; ++x) {
+          const int row = g + 8 * x;
+          if (row >= TT) continue;
+          uint32_t* to = keys + row * stride + p0 + __umulhi(p0, by_run) + 2 * t;
+          const uint32_t k0 = cs_key((float)acc[2 * x] * by0), k1 = cs_key((float)acc[2 * x + 1] * by1);
+          if (plain) {
+            to[0] = k0;
+            to[1] = k1;
+          } else if (row >= s && row < e) {             // (a tile of 8 pages that any token sees lies in the row whole)
+            const int own = sh_own[row], page = p0 + 2 * t;
+            to[0] = page > own ? 0u : (page < a.first || page > own - a.recent ? 0xffffffffu : k0);
+            to[1] = page + 1 > own ? 0u : (page + 1 < a.first || page + 1 > own - a.recent ? 0xffffffffu : k1);
           }
         }
       }
     }
   }
-}
-
-// ---- the choice: WARPS warps per row, KPT keys a lane (0: more than fit, read again at every step). Warp w holds keys
-// [w * 32 * KPT, ...), every 32nd of them a lane.
-template <int WARPS, int KPT, int ROWS>
-__global__ void __launch_bounds__(WARPS * ROWS * 32) dd_cache_topk_kernel(const cs_args a) {
-  __shared__ int sh_n[ROWS][WARPS], sh_eq[ROWS][WARPS];
-  const int lane = threadIdx.x & 31, w = (threadIdx.x >> 5) % WARPS, sub = (threadIdx.x >> 5) / WARPS;
-  const long long row = (long long)blockIdx.x * ROWS + sub;
-  dd_grid_dependency_wait();
-  if (row >= (long long)a.n_tokens * a.c.n_kv_heads) return;         // a whole row's warps: ROWS is 1 where they share barriers
-  const int n = (int)(row / a.c.n_kv_heads);
-  int req;
-  const int P = cs_own_page(a, a.first_token + n, req, false) + 1;
-  int* out = a.out + ((long long)a.first_token * a.c.n_kv_heads + row) * a.k;
-  const int k = min(a.k, P);
-  for (int i = w * 32 + lane; i < a.k; i += WARPS * 32)
-    if (i >= k || P <= a.k) out[i] = i < k ? i : -1;                  // everything visible fits, and what lies behind the set
-  if (P <= a.k) return;
-  const uint32_t* keys = a.keys + row * a.stride;
-  const int span = KPT ? 32 * KPT : (P + WARPS * 32 - 1) / (WARPS * 32) * 32, at0 = w * span + lane;
-  constexpr int HELD = KPT ? KPT : 1;
-  uint32_t key[HELD];
-  if (KPT) {
-#pragma unroll
-    for (int j = 0; j < HELD; ++j) key[j] = at0 + 32 * j < P ? keys[at0 + 32 * j] : 0u;      // no key is 0
+  asm volatile("cp.async.wait_group 0;" ::: "memory");
+  __syncthreads();
+  // ---- the choice
+  const int row = TT == 1 ? 0 : warp, w = TT == 1 ? warp : 0;
+  if (n0 + row >= a.n_tokens) return;
+  const int P = sh_own[row] + 1, k = a.k;
+  int* out = a.out + ((long long)(n0 + row) * a.c.n_kv_heads + h) * k;
+  if (P <= k) {                                                       // everything visible fits
+    for (int i = w * 32 + lane; i < k; i += (TT == 1 ? CF_THREADS : 32)) out[i] = i < P ? i : -1;
+    return;
   }
+  constexpr int ROW_WARPS = TT == 1 ? WARPS : 1, NG = 8;
+  uint32_t* const mine = keys + row * stride;
+  const int at0 = (w * 32 + lane) * run;
+  // zeros behind the tiles of 8 pages that were scored for this token (those of its request's furthest one here, at least its own)
+  for (int p = (P + 7) / 8 * 8 + lane + 32 * w; p < cf_lanes<TT>() * run; p += cf_lanes<TT>()) mine[p + __umulhi(p, by_run)] = 0u;
+  if (TT == 1) __syncthreads();
+  else __syncwarp();
+  const uint32_t* const keys_of_lane = mine + at0 + (w * 32 + lane);
   auto each = [&](auto&& f) {
-    if (KPT) {
+    for (int j = 0; j < run; j += 8)
 #pragma unroll
-      for (int j = 0; j < HELD; ++j) f(key[j], at0 + 32 * j);
-    } else {
-      for (int j = 0; j < span; j += 32) f(at0 + j < P ? keys[at0 + j] : 0u, at0 + j);
-    }
+      for (int i = 0; i < 8; ++i) f(keys_of_lane[j + i], at0 + j + i, i);
   };
-  auto total = [&](int v) {                                           // over the row
-    v = __reduce_add_sync(0xffffffffu, v);
-    if (WARPS == 1) return v;
-    __syncthreads();
-    if (lane == 0) sh_n[sub][w] = v;
-    __syncthreads();
-    v = lane < WARPS ? sh_n[sub][lane] : 0;
-    return __reduce_add_sync(0xffffffffu, v);
-  };
-  // the largest x with at least k keys >= x lies in [lo, hi] (or all of these are taken along with the pages always kept)
-  uint32_t lo = 0xffffffffu, hi = 0u;
-  each([&](uint32_t v, int p) {
-    if (p < P && v != 0xffffffffu) {
-      lo = min(lo, v);
-      hi = max(hi, v);
-    }
-  });
-  lo = __reduce_min_sync(0xffffffffu, lo);
-  hi = __reduce_max_sync(0xffffffffu, hi);
-  if (WARPS > 1) {
-    if (lane == 0) { sh_n[sub][w] = (int)lo; sh_eq[sub][w] = (int)hi; }
-    __syncthreads();
-    lo = __reduce_min_sync(0xffffffffu, lane < WARPS ? (uint32_t)sh_n[sub][lane] : 0xffffffffu);
-    hi = __reduce_max_sync(0xffffffffu, lane < WARPS ? (uint32_t)sh_eq[sub][lane] : 0u);
-  }
-  bool exact = false;
-  // the middle of the scores at first, which splits their number better than the middle of the keys
-  for (int step = 0; lo < hi; ++step) {
-    uint32_t mid = lo + (hi - lo) / 2 + 1;
-    if (step < 20) mid = min(max(cs_key(0.5f * cs_score(lo) + 0.5f * cs_score(hi)), lo + 1u), hi);
+  auto count = [&](uint32_t x) {
     int c = 0;
-    each([&](uint32_t v, int) { c += v >= mid; });
-    c = total(c);
-    if (c == a.k) { lo = mid; exact = true; break; }
-    if (c > a.k) lo = mid;
-    else hi = mid - 1;
-  }
-  // keys >= lo where there are exactly k, else all keys > lo and the first of those that equal it
-  int above = 0, equal = 0;
-  each([&](uint32_t v, int) { above += v > lo; equal += v == lo; });
-  above = __reduce_add_sync(0xffffffffu, above);
-  equal = __reduce_add_sync(0xffffffffu, equal);
-  int before = 0, before_eq = 0, all_above = above;
-  if (WARPS > 1) {
-    __syncthreads();
-    if (lane == 0) { sh_n[sub][w] = above; sh_eq[sub][w] = equal; }
-    __syncthreads();
-    const int x = lane < WARPS ? sh_n[sub][lane] : 0, y = lane < WARPS ? sh_eq[sub][lane] : 0;
-    all_above = __reduce_add_sync(0xffffffffu, x);
-    before = __reduce_add_sync(0xffffffffu, lane < w ? x : 0);
-    before_eq = __reduce_add_sync(0xffffffffu, lane < w ? y : 0);
-  }
-  const int take = exact ? 0x7fffffff : a.k - all_above;              // how many of the equal ones
-  int at = before + min(before_eq, take), eq_at = before_eq;
-  const unsigned below = (1u << lane) - 1u;
-  each([&](uint32_t v, int p) {
-    const unsigned eq = __ballot_sync(0xffffffffu, v == lo);
-    const bool mine = v > lo || (v == lo && eq_at + __popc(eq & below) < take);
-    const unsigned m = __ballot_sync(0xffffffffu, mine);
-    if (mine) out[at + __popc(m & below)] = p;
-    at += __popc(m);
-    eq_at += __popc(eq);
-  });
-}
-
-int cs_sm_count(int device) {
-  int sms = 0;
-  if (device < 0 || cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, device) != cudaSuccess || sms <= 0) {
-    cudaGetLastError();
-    return 148;
-  }
-  return sms;
+    for (int j = 0; j < run; j += 8)
+#pragma unroll
+      for (int i = 0; i < 8; ++i) c += keys_of_lane[j + i] >= x;
+    return c;
+  };
+  auto list = [&](uint32_t x, auto&& f) {
+    for (int j = 0; j < run; j += 32) {
+      unsigned bits = 0;
+#pragma unroll
+      for (int i8 = 0; i8 < 32; i8 += 8)
+        if (j + i8 < run)
+#pragma unroll
+          for (int i = 0; i < 8; ++i) bits |= (keys_of_lane[j + i8 + i] >= x ? 1u : 0u) << (i8 + i);
+      for (; bits; bits &= bits - 1) {
+        const int i = j + __ffs(bits) - 1;
+        f(keys_of_lane[i], at0 + i);
+      }
+    }
+  };
+  if constexpr (TT == 1) cs_choose<ROW_WARPS, NG, CAP>(each, count, list, [] { __syncthreads(); }, k, out, w, sh_a, sh_b, list_key, list_page);
+  else cs_choose<ROW_WARPS, NG, CAP>(each, count, list, [] { __syncwarp(); }, k, out, w, sh_a, sh_b, list_key + row * CAP, list_page + row * CAP);
 }
 
 template <int D> const void* cs_landmark_kernel(int format) {
@@ -428,7 +939,7 @@ extern "C" int dd_cache_landmarks(const dd_cache* cache, const int* ctx_len, int
 
 extern "C" size_t dd_cache_select_workspace(int n_tokens, int n_kv_heads, int max_pages) {
   if (n_tokens < 1 || n_kv_heads < 1 || max_pages < 1) return 0;
-  return (size_t)cs_tokens_at_once(n_tokens, n_kv_heads, max_pages) * n_kv_heads * cs_stride(max_pages) * 4;
+  return (size_t)cs_tokens_at_once(n_tokens, n_kv_heads, max_pages) * n_kv_heads * (cs_stride(max_pages) * 4 + 128);
 }
 
 extern "C" int dd_cache_select(const dd_cache* cache, int n_tokens, const int* positions, const int* requests, const dd_rows* q,
@@ -473,10 +984,11 @@ extern "C" int dd_cache_select(const dd_cache* cache, int n_tokens, const int* p
   a.first = first_pages;
   a.recent = recent_pages;
   a.stride = cs_stride(cache->max_pages);
-  const int sms = cs_sm_count(device), each = n_tokens / cache->batch;
+  const int each = n_tokens / cache->batch;
   // Tokens of a block: one where requests bring one or two (every token reads its own landmarks), up to 64 where they bring many.
   const int tt = each <= 2 ? 1 : (each < 32 ? 8 : 64);
   const int once = cs_tokens_at_once(n_tokens, cache->n_kv_heads, cache->max_pages);
+  a.codes = (signed char*)((char*)workspace + (size_t)once * cache->n_kv_heads * a.stride * 4);
   cudaLaunchConfig_t cfg = {};
   cudaLaunchAttribute at;
   dd_pdl_attr(&at);
@@ -484,39 +996,60 @@ extern "C" int dd_cache_select(const dd_cache* cache, int n_tokens, const int* p
   cfg.numAttrs = 1;
   cfg.stream = (cudaStream_t)stream;
   void* args[] = {&a};
+  // One kernel where requests bring more than two tokens each and a row's keys fit shared memory. With one token a block it is the slower way (8 requests x 2048 pages: 22
+  // us against 14): few blocks, and every one of them the whole chain.
+  const int ft = each <= 2 ? 1 : 16;
+  if (each > 2 && cache->max_pages <= CF_MOST) {
+    const bool wide = cache->head_dim == 128, bf16 = q->dtype == DD_BF16;
+    const void* f = ft == 1 ? (wide ? (bf16 ? (const void*)dd_cache_select_kernel<__nv_bfloat16, 128, 1> : (const void*)dd_cache_select_kernel<__half, 128, 1>)
+                                    : (bf16 ? (const void*)dd_cache_select_kernel<__nv_bfloat16, 64, 1> : (const void*)dd_cache_select_kernel<__half, 64, 1>))
+                            : (wide ? (bf16 ? (const void*)dd_cache_select_kernel<__nv_bfloat16, 128, 16> : (const void*)dd_cache_select_kernel<__half, 128, 16>)
+                                    : (bf16 ? (const void*)dd_cache_select_kernel<__nv_bfloat16, 64, 16> : (const void*)dd_cache_select_kernel<__half, 64, 16>));
+    a.n_tokens = n_tokens;
+    cfg.dynamicSmemBytes = ft == 1 ? cf_smem<1>(cache->head_dim, cache->max_pages) : cf_smem<16>(cache->head_dim, cache->max_pages);
+    DD_CUDA_TRY(nullptr, cudaFuncSetAttribute(f, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)cfg.dynamicSmemBytes));
+    cfg.gridDim = dim3((unsigned)((n_tokens + ft - 1) / ft), (unsigned)cache->n_kv_heads);
+    cfg.blockDim = dim3(CF_THREADS);
+    return dd_launch(who, &cfg, f, args);
+  }
   for (a.first_token = 0; a.first_token < n_tokens; a.first_token += once) {
     a.n_tokens = n_tokens - a.first_token < once ? n_tokens - a.first_token : once;
-    const long long tiles = (a.n_tokens + tt - 1) / tt, row_blocks = tiles * cache->n_kv_heads;
-    // pages of a block: enough blocks to fill the device a few times, 64 pages at least
-    const long long want = (8LL * sms + row_blocks - 1) / row_blocks;
-    long long pages = ((long long)cache->max_pages + want - 1) / want;
-    pages = (pages + 63) / 64 * 64;
-    a.chunk_pages = (int)pages;
-    a.chunks = (int)((cache->max_pages + pages - 1) / pages);
+    const bool wide = cache->head_dim == 128, bf16 = q->dtype == DD_BF16;
+    const void* f;
+    const long long rows = (long long)a.n_tokens * cache->n_kv_heads, tiles = (a.n_tokens + tt - 1) / tt;
+    const int pages = cs_pages(tt);
+    a.chunks = (cache->max_pages + pages - 1) / pages;
     if (tiles * a.chunks > 0x7fffffffLL) return dd_fail(nullptr, DD_ERR_INVALID_ARG, "%s: too many tokens", who);
+    if (tt == 64) {
+      f = wide ? (bf16 ? (const void*)dd_cache_query_kernel<__nv_bfloat16, 128> : (const void*)dd_cache_query_kernel<__half, 128>)
+               : (bf16 ? (const void*)dd_cache_query_kernel<__nv_bfloat16, 64> : (const void*)dd_cache_query_kernel<__half, 64>);
+      cfg.gridDim = dim3((unsigned)((rows + 7) / 8));
+      cfg.blockDim = dim3(256);
+      cfg.dynamicSmemBytes = 0;
+      DD_TRY(dd_launch(who, &cfg, f, args));
+    }
     cfg.gridDim = dim3((unsigned)(tiles * a.chunks), (unsigned)cache->n_kv_heads);
     cfg.blockDim = dim3(CS_THREADS);
-    const void* f = cache->head_dim == 128 ? (q->dtype == DD_BF16 ? cs_score_kernel<__nv_bfloat16, 128>(tt) : cs_score_kernel<__half, 128>(tt))
-                                           : (q->dtype == DD_BF16 ? cs_score_kernel<__nv_bfloat16, 64>(tt) : cs_score_kernel<__half, 64>(tt));
+    cfg.dynamicSmemBytes = (size_t)pages * (cache->head_dim + CS_TAIL);
+    f = wide ? (bf16 ? cs_score_kernel<__nv_bfloat16, 128>(tt) : cs_score_kernel<__half, 128>(tt))
+             : (bf16 ? cs_score_kernel<__nv_bfloat16, 64>(tt) : cs_score_kernel<__half, 64>(tt));
+    if (tt == 64) DD_CUDA_TRY(nullptr, cudaFuncSetAttribute(f, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)cfg.dynamicSmemBytes));
     DD_TRY(dd_launch(who, &cfg, f, args));
-    const long long rows = (long long)a.n_tokens * cache->n_kv_heads;
-    int threads = 1024, per_block = 1;
-    if (cache->max_pages <= 2048 && rows >= 4LL * sms) {
-      f = (const void*)dd_cache_topk_kernel<1, 64, 4>;
-      threads = 128;
-      per_block = 4;
+    cfg.dynamicSmemBytes = 0;
+    int threads = 1024;
+    if (cache->max_pages <= CR_RUN * CR_ROW_THREADS && k_pages <= CR_ROW_THREADS && rows <= 1024) {
+      f = (const void*)dd_cache_topk_rank_kernel;
+      threads = CR_ROW_THREADS;
     } else if (cache->max_pages <= 4096) {
-      f = (const void*)dd_cache_topk_kernel<8, 16, 1>;
+      f = (const void*)dd_cache_topk_kernel<8, 16>;
       threads = 256;
     } else if (cache->max_pages <= 16384) {
-      f = (const void*)dd_cache_topk_kernel<32, 16, 1>;
-    } else if (cache->max_pages <= 49152) {
-      f = (const void*)dd_cache_topk_kernel<32, 48, 1>;
+      f = (const void*)dd_cache_topk_kernel<32, 16>;
     } else {
-      f = (const void*)dd_cache_topk_kernel<32, 0, 1>;
+      f = (const void*)dd_cache_topk_kernel<32, 0>;
     }
-    if ((rows + per_block - 1) / per_block > 0x7fffffffLL) return dd_fail(nullptr, DD_ERR_INVALID_ARG, "%s: too many tokens", who);
-    cfg.gridDim = dim3((unsigned)((rows + per_block - 1) / per_block));
+    if (rows > 0x7fffffffLL) return dd_fail(nullptr, DD_ERR_INVALID_ARG, "%s: too many tokens", who);
+    cfg.gridDim = dim3((unsigned)rows);
     cfg.blockDim = dim3(threads);
     DD_TRY(dd_launch(who, &cfg, f, args));
   }

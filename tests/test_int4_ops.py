@@ -17,8 +17,8 @@ def test_sizes(dd):
     assert size(dd.DD_CACHE_INT4, 16, 96) == 0 and size(dd.DD_CACHE_INT4, 8, 128) == 0
     assert dd.lib.dd_cache_landmark_bytes(128) == 144 and dd.lib.dd_cache_landmark_bytes(64) == 80 and dd.lib.dd_cache_landmark_bytes(96) == 0
     work = dd.lib.dd_cache_select_workspace
-    assert work(1, 8, 2048) == 8 * 2048 * 4 and work(3, 1, 1) == 3 * 32 * 4
-    assert work(1 << 20, 8, 2048) == 64 << 20 and work(1 << 20, 8, 1 << 20) == 64 * 8 * (1 << 20) * 4
+    assert work(1, 8, 2048) == 8 * (2048 * 4 + 128) and work(3, 1, 1) == 3 * (32 * 4 + 128)
+    assert work(1 << 20, 8, 2048) == (64 << 20) + 1024 * 8 * 128 and work(1 << 20, 8, 1 << 20) == 64 * 8 * ((1 << 22) + 128)
     for bad in [(0, 8, 16), (1, 0, 16), (1, 8, 0), (-1, 8, 16)]:
         assert work(*bad) == 0
     assert dd.lib.dd_cache_sparse_attn_workspace(32, 8, 128) == dd.lib.dd_cache_decode_attn_workspace(32, 8, 128, 1) > 0
