@@ -88,7 +88,7 @@ struct ca_args {
   const int* requests; // NULL: tokens_per_request tokens of each in turn
   const int* idx;      // [batch][n_kv_heads][k_pages]
   int k_pages, tokens_per_request;
-  int unit_tiles;      // places of a unit in the flat list: the tiles of a full list
+  int unit_tiles;      // tiles of a full list
   int cluster;         // blocks of a cluster that share one unit, 0 = the flat list
   int joins;           // the joining kernel follows
   uint32_t by_G;       // ceil(2^31 / G): row / G by a multiplication
@@ -228,24 +228,15 @@ template <bool SP> __device__ __forceinline__ void ca_next_unit(const ca_args& a
     k.sub = 0;
     do {
       if (k.b + 1 >= a.batch) { k.left = 0; return; }
-      k.s = ca_span_of<SP>(a, ++k.b, SP);
-      if (SP && k.s.tiles == 0) {                                     // its places are there all the same
-        const long long gone = (long long)subs * (a.unit_tiles + CA_UNIT_COST);
-        k.left = k.left > gone ? k.left - (int)gone : 0;
-        if (k.left == 0) return;
-      }
+      k.s = ca_span_of<SP>(a, ++k.b, false);
     } while (k.s.tiles == 0);
   }
   ca_keep_whole(k);
 }
-// Empty places behind a unit.
-template <bool SP> __device__ __forceinline__ int ca_behind(const ca_args& a, const ca_span& s) {
-  return CA_UNIT_COST + (SP ? a.unit_tiles - s.tiles : 0);
-}
 template <bool SP> __device__ __forceinline__ void ca_step(const ca_args& a, ca_cursor& k, int subs) {
   --k.left;
   if (++k.t >= k.s.tiles) {
-    k.left -= ca_behind<SP>(a, k.s);
+    k.left -= CA_UNIT_COST;
     if (k.left > 0) ca_next_unit<SP>(a, k, subs);
   }
 }
@@ -360,48 +351,56 @@ __global__ void __launch_bounds__(CA_THREADS, (ca_geom<FMT, D, NT, SP>::BLOCKS_P
     const int each = (is.s.tiles + a.cluster * CA_WARPS - 1) / (a.cluster * CA_WARPS);
     is.t = each * w;
     is.left = max(0, min(each, is.s.tiles - is.t));
-  } else if constexpr (SP) {
-    // ---- this warp's run of the flat list, in which every unit has the same number of places
-    const int unit = a.unit_tiles + CA_UNIT_COST;
-    const long long total = (long long)unit * subs * B;
-    share = max(1LL, ca_div(total + (long long)gridDim.x * CA_WARPS - 1, (int)gridDim.x * CA_WARPS));
-    const long long f0 = share * me;
-    if (f0 < total) {
-      const long long n = ca_div(f0, unit);                           // unit of the launch
-      is.b = (int)ca_div(n, subs);
-      is.sub = (int)(n - (long long)is.b * subs);
-      is.t = (int)(f0 - n * unit);
-      is.left = (int)min(share, 0x7fffffffLL);
-      is.s = ca_span_of<SP>(a, is.b, is.sub == 0);
-      if (is.s.tiles == 0) {                                          // on to the next token
-        const long long gone = (long long)(subs - is.sub) * unit - is.t;
-        is.left = is.left > gone ? is.left - (int)gone : 0;
-        is.sub = subs - 1;
-        if (is.left > 0) ca_next_unit<SP>(a, is, subs);
-      } else if (is.t == 0) {
-        ca_keep_whole(is);
-      } else if (is.t >= is.s.tiles || is.s.tiles <= CA_WHOLE) {
-        is.left -= unit - is.t;
-        if (is.left > 0) ca_next_unit<SP>(a, is, subs);
-      }
-    }
   } else {
-    // ---- this warp's run of the flat list: every warp adds up the list by itself, 32 requests at a time
-    is.s = ca_span_of<SP>(a, min(lane, B - 1), blockIdx.x == 0 && warp == 0 && lane < B);
+    // ---- this warp's run of the flat list
     auto places = [&](const ca_span& sp) -> long long { return sp.tiles > 0 ? (long long)(sp.tiles + CA_UNIT_COST) * subs : 0; };
-    const long long cost0 = lane < B ? places(is.s) : 0;               // of the first 32 requests
-    long long total = cost0;
-    for (int b = lane + 32; b < B; b += 32) total += places(ca_span_of<SP>(a, b, blockIdx.x == 0 && warp == 0));
+    long long cost0 = 0, total = 0;
+    long long at = 0;                                                   // first place of the 32 requests looked at
+    int from_b = 0;
+    if constexpr (SP) {
+      // query tokens may be many: every thread adds up an equal share of them, and the warp looks for its run in the share that has it
+      long long* const sums = reinterpret_cast<long long*>(ca_smem);
+      const int each = (B + CA_THREADS - 1) / CA_THREADS, b1 = min(B, ((int)threadIdx.x + 1) * each);
+      for (int b = threadIdx.x * each; b < b1; ++b) total += places(ca_span_of<SP>(a, b, blockIdx.x == 0));
+      long long incl = total;
 #pragma unroll
-    for (int o = 16; o; o >>= 1) total += __shfl_xor_sync(0xffffffffu, total, o);
+      for (int o = 1; o < 32; o <<= 1) {
+        const long long v = __shfl_up_sync(0xffffffffu, incl, o);
+        if (lane >= o) incl += v;
+      }
+      if (lane == 31) sums[CA_THREADS + warp] = incl;
+      __syncthreads();
+      long long before = 0;
+      total = 0;
+      for (int w = 0; w < CA_WARPS; ++w) {
+        if (w < warp) before += sums[CA_THREADS + w];
+        total += sums[CA_THREADS + w];
+      }
+      sums[threadIdx.x] = before + incl;                                // through this thread's share
+      __syncthreads();
+      share = max(1LL, ca_div(total + (long long)gridDim.x * CA_WARPS - 1, (int)gridDim.x * CA_WARPS));
+      int in = 0;                                                       // the first share that reaches beyond f0
+      for (int i = lane; i < CA_THREADS; i += 32) in += sums[i] <= share * me;
+      in = (int)__reduce_add_sync(0xffffffffu, (unsigned)in);
+      if (in > 0) at = sums[in - 1];
+      from_b = in * each;
+      __syncthreads();                                                  // the rings lie here
+    } else {
+      // every warp adds up the list by itself, 32 requests at a time
+      is.s = ca_span_of<SP>(a, min(lane, B - 1), blockIdx.x == 0 && warp == 0 && lane < B);
+      cost0 = lane < B ? places(is.s) : 0;                              // of the first 32 requests
+      total = cost0;
+      for (int b = lane + 32; b < B; b += 32) total += places(ca_span_of<SP>(a, b, blockIdx.x == 0 && warp == 0));
+#pragma unroll
+      for (int o = 16; o; o >>= 1) total += __shfl_xor_sync(0xffffffffu, total, o);
+    }
     share = max(1LL, ca_div(total + (long long)gridDim.x * CA_WARPS - 1, (int)gridDim.x * CA_WARPS));
     const long long f0 = share * me;
     if (f0 < total) {
-      long long at = 0;                                                 // first place of the 32 requests looked at
-      for (int b0 = 0;; b0 += 32) {
+      for (int b0 = from_b;; b0 += 32) {
         ca_span sp = is.s;
         long long cost = cost0;
-        if (b0 > 0) {
+        if (SP || b0 > 0) {
           sp = ca_span_of<SP>(a, min(b0 + lane, B - 1), false);
           cost = b0 + lane < B ? places(sp) : 0;
         }
@@ -694,6 +693,157 @@ __global__ void __launch_bounds__(CA_THREADS, (ca_geom<FMT, D, NT, SP>::BLOCKS_P
       sh_rest[warp][1] = make_int4(s.end, s.first, s.tile0, s.tiles);
     }
     __syncwarp();
+    // ---- 4-bit tiles: scores (in two chains, without the scales of rows and queries), values' codes and scales, products with weights
+    auto scores4 = [&](uint32_t slot, float (&z)[NT][4], float (&z2)[NT][4], float& by0, float& by1, float& vex0, float& vex1) {
+      by0 = __uint_as_float(max((uint32_t)ca_lds_byte(slot + 18 * D + g) << 23, 0x00400000u));
+      by1 = __uint_as_float(max((uint32_t)ca_lds_byte(slot + 18 * D + g + 8) << 23, 0x00400000u));
+      vex0 = (float)(ca_lds_byte(slot + 18 * D + 16 + g) - 127);
+      vex1 = (float)(ca_lds_byte(slot + 18 * D + 24 + g) - 127);
+      uint32_t r0[D / 32], r1[D / 32];                                // rows g and g + 8: channels D/4 t ...
+      ca_lds(r0, slot + lane * (D / 8));
+      ca_lds(r1, slot + 4 * D + lane * (D / 8));
+      // one scale for every 16 channels: two a lane (head_dim 128) or one
+      constexpr int SC = D / 64;
+      ca_scale4 m0[SC], m1[SC];
+      if constexpr (D == 128) {
+        const uint32_t s0 = ca_e4m3x2_to_half(ca_lds16(slot + 16 * D + g * 8 + t * 2)), s1 = ca_e4m3x2_to_half(ca_lds16(slot + 16 * D + 64 + g * 8 + t * 2));
+        m0[0] = ca_scales4(__byte_perm(s0, 0u, 0x1010u));
+        m0[1] = ca_scales4(__byte_perm(s0, 0u, 0x3232u));
+        m1[0] = ca_scales4(__byte_perm(s1, 0u, 0x1010u));
+        m1[1] = ca_scales4(__byte_perm(s1, 0u, 0x3232u));
+      } else {
+        m0[0] = ca_scales4(ca_e4m3x2_to_half((uint32_t)ca_lds_byte(slot + 16 * D + g * 4 + t) * 0x101u));
+        m1[0] = ca_scales4(ca_e4m3x2_to_half((uint32_t)ca_lds_byte(slot + 16 * D + 32 + g * 4 + t) * 0x101u));
+      }
+#pragma unroll
+      for (int w = 0; w < D / 32; ++w) {
+        uint32_t h0[4], h1[4];
+        ca_int4_pairs(h0, r0[w], m0[w / 2]);
+        ca_int4_pairs(h1, r1[w], m1[w / 2]);
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) {
+          if (w == 0) {
+            ca_mma_first<FMT>(z[nt], h0[0], h1[0], h0[1], h1[1], qf[nt][0], qf[nt][1]);
+            ca_mma_first<FMT>(z2[nt], h0[2], h1[2], h0[3], h1[3], qf[nt][2], qf[nt][3]);
+          } else {
+            ca_mma<FMT>(z[nt], h0[0], h1[0], h0[1], h1[1], qf[nt][4 * w], qf[nt][4 * w + 1]);
+            ca_mma<FMT>(z2[nt], h0[2], h1[2], h0[3], h1[3], qf[nt][4 * w + 2], qf[nt][4 * w + 3]);
+          }
+        }
+      }
+    };
+    // tokens 2t, 2t + 1 | 2t + 8, 2t + 9, part g, and their scales
+    auto values4 = [&](uint32_t slot, uint32_t (&v4)[2][D / 32], uint32_t (&vs4)[2]) {
+#pragma unroll
+      for (int k = 0; k < 2; ++k) {
+        ca_lds(v4[k], slot + 8 * D + (k * 32 + lane) * (D / 8));
+        vs4[k] = ca_e4m3x2_to_half(ca_lds16(slot + 17 * D + (D == 128 ? g : g >> 1) * 16 + 8 * k + 2 * t));
+      }
+    };
+    // one register of each token pair's codes in turn, dealt to the accumulators they feed: add(accumulator, fragment of V^T)
+    auto weigh4 = [&](const uint32_t (&v4)[2][D / 32], const uint32_t (&vs4)[2], auto&& add) {
+      const ca_scale4 m0 = ca_scales4(vs4[0]), m1 = ca_scales4(vs4[1]);
+#pragma unroll
+      for (int q = 0; q < D / 32; ++q) {                              // channels 4 q .. 4 q + 3 of the lane's part
+        const uint32_t pick = (q & 1) ? 0x7632u : 0x5410u;
+        uint32_t h0[4], h1[4];
+        ca_int4_pairs(h0, __byte_perm(v4[0][q >> 1], v4[0][D / 64 + (q >> 1)], pick), m0);
+        ca_int4_pairs(h1, __byte_perm(v4[1][q >> 1], v4[1][D / 64 + (q >> 1)], pick), m1);
+        add(2 * q, h0[0], h0[1], h1[0], h1[1]);
+        add(2 * q + 1, h0[2], h0[3], h1[2], h1[3]);
+      }
+    };
+    // Two complete 4-bit tiles that every row sees at once: one question about the reference for both, and two chains of work that do not
+    // wait for each other.
+    auto pair4 = [&]() {
+      constexpr int U = 2;
+      float z[U][NT][4], vex[U][2];
+      uint32_t slot[U];
+      ca_wait<NS - U>();
+      __syncwarp();
+      slot[0] = take;
+      slot[1] = take + geo::SLOT_BYTES == ring + geo::WARP_BYTES ? ring : take + geo::SLOT_BYTES;
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        float z2[NT][4], by0, by1;
+        scores4(slot[u], z[u], z2, by0, by1, vex[u][0], vex[u][1]);
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) z[u][nt][e] = (z[u][nt][e] + z2[nt][e]) * (zs[nt][e & 1] * (e < 2 ? by0 : by1));
+      }
+      uint32_t pb[U][NT][2], pr[U][NT][2];
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt) {
+        float x[U][4], y[U][4];
+        bool above = false;
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            x[u][e] = z[u][nt][e] - from[nt][e & 1];
+            y[u][e] = x[u][e] + vex[u][e >> 1];
+            above |= y[u][e] > CA_LAZY + geo::HEADROOM || x[u][e] > CA_LAZY + geo::HEADROOM + 96.f;
+          }
+        if (__any_sync(0xffffffffu, above)) {
+#pragma unroll
+          for (int c = 0; c < 2; ++c) {
+            float top = from[nt][c] + geo::HEADROOM;
+#pragma unroll
+            for (int u = 0; u < U; ++u) top = fmaxf(top, fmaxf(z[u][nt][c] + fmaxf(vex[u][0], -96.f), z[u][nt][2 + c] + fmaxf(vex[u][1], -96.f)));
+            top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 4));
+            top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 8));
+            top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 16));
+            top = fmaxf(top - geo::HEADROOM, from[nt][c]);
+            const float fix = ca_exp2(from[nt][c] - top);
+            from[nt][c] = top;
+            sum[nt][c] *= fix;
+#pragma unroll
+            for (int m = 0; m < D / 16; ++m) { acc[nt][m][c] *= fix; acc[nt][m][2 + c] *= fix; }
+          }
+#pragma unroll
+          for (int u = 0; u < U; ++u)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              x[u][e] = z[u][nt][e] - from[nt][e & 1];
+              y[u][e] = x[u][e] + vex[u][e >> 1];
+            }
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+          float p[4];
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            p[e] = ca_exp2(y[u][e]);
+            sum[nt][e & 1] += ca_exp2(x[u][e]);
+          }
+#pragma unroll
+          for (int k = 0; k < 2; ++k) {
+            if (geo::PAIR) {
+              const uint32_t w = ca_first_part<TP>(p[2 * k], p[2 * k + 1]);
+              const float2 had = dd_unpack2<TP>(w);
+              pb[u][nt][k] = ca_transpose(w);
+              pr[u][nt][k] = ca_transpose(dd_pack2<TP>(p[2 * k] - had.x, p[2 * k + 1] - had.y));
+            } else {
+              pb[u][nt][k] = ca_transpose(dd_pack2<TP>(p[2 * k], p[2 * k + 1]));
+            }
+          }
+        }
+      }
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        uint32_t v4[2][D / 32], vs4[2];
+        values4(slot[u], v4, vs4);
+        use_up(true, true);
+        weigh4(v4, vs4, [&](int m, uint32_t r0, uint32_t r1, uint32_t r2, uint32_t r3) {
+#pragma unroll
+          for (int nt = 0; nt < NT; ++nt) {
+            ca_mma<FMT>(acc[nt][m], r0, r1, r2, r3, pb[u][nt][0], pb[u][nt][1]);
+            if (geo::PAIR) ca_mma<FMT>(acc[nt][m], r0, r1, r2, r3, pr[u][nt][0], pr[u][nt][1]);
+          }
+        });
+      }
+    };
     auto tile = [&](auto plain_, int i) {
       constexpr bool plain = decltype(plain_)::value;                 // no mask, and the refills need no questions
       int tok0 = (first_tile + i) << 4;
@@ -708,42 +858,7 @@ __global__ void __launch_bounds__(CA_THREADS, (ca_geom<FMT, D, NT, SP>::BLOCKS_P
         [[maybe_unused]] const uint32_t at = take + k_row;
         float by0 = 1.f, by1 = 1.f;                                   // key scales of tokens g, g + 8
         if constexpr (I4) {
-          by0 = __uint_as_float(max((uint32_t)ca_lds_byte(take + 18 * D + g) << 23, 0x00400000u));
-          by1 = __uint_as_float(max((uint32_t)ca_lds_byte(take + 18 * D + g + 8) << 23, 0x00400000u));
-          vex0 = (float)(ca_lds_byte(take + 18 * D + 16 + g) - 127);
-          vex1 = (float)(ca_lds_byte(take + 18 * D + 24 + g) - 127);
-          uint32_t r0[D / 32], r1[D / 32];                            // rows g and g + 8: channels D/4 t ...
-          ca_lds(r0, take + lane * (D / 8));
-          ca_lds(r1, take + 4 * D + lane * (D / 8));
-          // one scale for every 16 channels: two a lane (head_dim 128) or one
-          uint32_t s0, s1;
-          if (D == 128) {
-            s0 = ca_e4m3x2_to_half(ca_lds16(take + 16 * D + g * 8 + t * 2));
-            s1 = ca_e4m3x2_to_half(ca_lds16(take + 16 * D + 64 + g * 8 + t * 2));
-          } else {
-            s0 = ca_e4m3x2_to_half((uint32_t)ca_lds_byte(take + 16 * D + g * 4 + t) * 0x101u);
-            s1 = ca_e4m3x2_to_half((uint32_t)ca_lds_byte(take + 16 * D + 32 + g * 4 + t) * 0x101u);
-          }
-          const ca_scale4 m0 = ca_scales4(s0), m1 = ca_scales4(s1);
-#pragma unroll
-          for (int w = 0; w < D / 32; ++w) {
-            const uint32_t pick = D == 64 || w < 2 ? 0x1010u : 0x3232u;
-            const ca_scale4 p0 = {__byte_perm(m0.at0, 0u, pick), __byte_perm(m0.at4, 0u, pick), __byte_perm(m0.off, 0u, pick)};
-            const ca_scale4 p1 = {__byte_perm(m1.at0, 0u, pick), __byte_perm(m1.at4, 0u, pick), __byte_perm(m1.off, 0u, pick)};
-            uint32_t h0[4], h1[4];
-            ca_int4_pairs(h0, r0[w], p0);
-            ca_int4_pairs(h1, r1[w], p1);
-#pragma unroll
-            for (int nt = 0; nt < NT; ++nt) {
-              if (w == 0) {
-                ca_mma_first<FMT>(z[nt], h0[0], h1[0], h0[1], h1[1], qf[nt][0], qf[nt][1]);
-                ca_mma_first<FMT>(z2[nt], h0[2], h1[2], h0[3], h1[3], qf[nt][2], qf[nt][3]);
-              } else {
-                ca_mma<FMT>(z[nt], h0[0], h1[0], h0[1], h1[1], qf[nt][4 * w], qf[nt][4 * w + 1]);
-                ca_mma<FMT>(z2[nt], h0[2], h1[2], h0[3], h1[3], qf[nt][4 * w + 2], qf[nt][4 * w + 3]);
-              }
-            }
-          }
+          scores4(take, z, z2, by0, by1, vex0, vex1);
         } else if constexpr (FP8) {
           // byte 0 stands for 2^-127, whose bits lie below those of all the others
           by0 = __uint_as_float(max((uint32_t)ca_lds_byte(take + geo::EXP_AT + g) << 23, 0x00400000u));
@@ -796,13 +911,9 @@ __global__ void __launch_bounds__(CA_THREADS, (ca_geom<FMT, D, NT, SP>::BLOCKS_P
 #pragma unroll
         for (int c = 0; c < V_BATCH; ++c) ca_ldsm_trans(raw[c], at + (v_x ^ ((c0 + c) << 5)));
       };
-      uint32_t v4[2][D / 32], vs4[2] = {0u, 0u};                      // 4-bit: tokens 2t, 2t + 1 | 2t + 8, 2t + 9, part g; their scales
+      [[maybe_unused]] uint32_t v4[2][D / 32], vs4[2] = {0u, 0u};
       if constexpr (I4) {
-#pragma unroll
-        for (int k = 0; k < 2; ++k) {
-          ca_lds(v4[k], take + 8 * D + (k * 32 + lane) * (D / 8));
-          vs4[k] = ca_e4m3x2_to_half(ca_lds16(take + 17 * D + (D == 128 ? g : g >> 1) * 16 + 8 * k + 2 * t));
-        }
+        values4(take, v4, vs4);
       } else if (geo::WHOLE) {
         load_values(0);
       }
@@ -890,22 +1001,9 @@ __global__ void __launch_bounds__(CA_THREADS, (ca_geom<FMT, D, NT, SP>::BLOCKS_P
           for (int e = 0; e < 4; ++e) r[e] = v[e];
         }
       };
-      // 4-bit: one register of each token pair's codes in turn, dealt to the four accumulators they feed
-      auto weigh4 = [&](auto&& add) {
-        const ca_scale4 m0 = ca_scales4(vs4[0]), m1 = ca_scales4(vs4[1]);
-#pragma unroll
-        for (int q = 0; q < D / 32; ++q) {                            // channels 4 q .. 4 q + 3 of the lane's part
-          const uint32_t pick = (q & 1) ? 0x7632u : 0x5410u;
-          uint32_t h0[4], h1[4];
-          ca_int4_pairs(h0, __byte_perm(v4[0][q >> 1], v4[0][D / 64 + (q >> 1)], pick), m0);
-          ca_int4_pairs(h1, __byte_perm(v4[1][q >> 1], v4[1][D / 64 + (q >> 1)], pick), m1);
-          add(2 * q, h0[0], h0[1], h1[0], h1[1]);
-          add(2 * q + 1, h0[2], h0[3], h1[2], h1[3]);
-        }
-      };
       if constexpr (I4) {
         if (!partial) {
-          weigh4([&](int m, uint32_t r0, uint32_t r1, uint32_t r2, uint32_t r3) {
+          weigh4(v4, vs4, [&](int m, uint32_t r0, uint32_t r1, uint32_t r2, uint32_t r3) {
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt) {
               ca_mma<FMT>(acc[nt][m], r0, r1, r2, r3, pb[nt][0], pb[nt][1]);
@@ -925,7 +1023,7 @@ __global__ void __launch_bounds__(CA_THREADS, (ca_geom<FMT, D, NT, SP>::BLOCKS_P
             }
             vs4[0] = had0 & keep[0];
             vs4[1] = had1 & keep[1];
-            weigh4([&](int m, uint32_t r0, uint32_t r1, uint32_t r2, uint32_t r3) {
+            weigh4(v4, vs4, [&](int m, uint32_t r0, uint32_t r1, uint32_t r2, uint32_t r3) {
 #pragma unroll
               for (int nt = 0; nt < NT; ++nt) {
                 float one[4] = {0.f, 0.f, 0.f, 0.f};
@@ -1009,6 +1107,16 @@ __global__ void __launch_bounds__(CA_THREADS, (ca_geom<FMT, D, NT, SP>::BLOCKS_P
         if (a.window > 0 && (((first_tile + i) << 4) <= pos_hi - a.window || ((is.s.tile0 + is.t) << 4) < is.s.first)) n = 0;
         if (!all_good()) n = 0;
       }
+      if constexpr (I4) {
+#pragma unroll 1
+        for (; n > 1; n -= 2, i += 2) {
+          if (SP) {                                                   // nobody has looked where the tiles to be used lie
+            const uint32_t next = take + geo::SLOT_BYTES == ring + geo::WARP_BYTES ? ring : take + geo::SLOT_BYTES;
+            if (max((int)ca_lds32(take + geo::TILE_BYTES), (int)ca_lds32(next + geo::TILE_BYTES)) > pos_lo - 15) break;
+          }
+          pair4();
+        }
+      }
       if constexpr (PLAIN_LOOP) {
 #pragma unroll 1
         for (; n > 0; --n, ++i) tile(std::true_type(), i);
@@ -1086,7 +1194,7 @@ __global__ void __launch_bounds__(CA_THREADS, (ca_geom<FMT, D, NT, SP>::BLOCKS_P
     }
 
     // ---- the next unit
-    u.left -= n_here + ca_behind<SP>(a, s);
+    u.left -= n_here + CA_UNIT_COST;
     if (u.left > 0) ca_next_unit<SP>(a, u, subs);
   }
   if (lane == 0 && !a.cluster) a.desc[me] = desc;

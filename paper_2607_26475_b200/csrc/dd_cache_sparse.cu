@@ -3,8 +3,7 @@
 // Every query token and KV head is a unit with a list of pages; what the kernels of dd_cache_attn.cuh do for the tiles of a request
 // in order, they do here for the tiles of the listed pages. What differs: a table entry is found through the list (two
 // dependent loads for 32 tiles at a time), the first token of a tile travels with the tile, since the list says nothing about
-// where it lies, and all units take equally many places of the flat list, so that the work split needs no look at the other tokens.
-// A token earlier in a prompt than its list is long leaves places empty.
+// where it lies, and the places of the flat list are added up by the threads of a block together, since there may be many tokens.
 #include "dd_cache_attn.cuh"
 
 extern "C" size_t dd_cache_sparse_attn_workspace(int n_q_heads, int n_kv_heads, int head_dim) {
@@ -82,7 +81,10 @@ extern "C" int dd_cache_sparse_attn(const dd_cache* cache, int n_tokens, const i
   }
   const int blocks = sms * p.blocks_per_sm;
   const long long units = (long long)n_tokens * a.row_tiles * cache->n_kv_heads;
-  a.cluster = ca_cluster_of(units, a.unit_tiles, blocks);
+  // A cluster per unit wherever all of them are resident and its warps get at most 8 tiles each: 8 tokens x 8 heads of 128 tiles 19 us with
+  // the flat list and its joining kernel, @CL@ with clusters of 4.
+  for (a.cluster = CA_MAX_CLUSTER; a.cluster > 1 && units * a.cluster > blocks * 7 / 8;) a.cluster /= 2;
+  if (a.cluster < 2 || a.unit_tiles <= CA_WHOLE || a.unit_tiles > 8 * a.cluster * CA_WARPS) a.cluster = 0;
   a.joins = !a.cluster && a.unit_tiles > CA_WHOLE;                    // else no unit can have been cut
   return ca_launch(who, a, p, units, blocks, nt, cache->head_dim, (cudaStream_t)stream);
 }
