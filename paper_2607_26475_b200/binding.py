@@ -374,7 +374,8 @@ class PagedCache:
                          self.status.data_ptr())
         self._addr = C.addressof(self.c)
         self._batch, self._heads, self._device = batch, n_kv_heads, block_table.device
-        self._workspace_bytes = {}
+        self._workspace_bytes, self._select_bytes = {}, {}
+        self._max_pages, self._landmark_shape = max_pages, (n_blocks, n_kv_heads, head_dim + 16)
         # the error word is zeroed on the stream the cache is made on: until that has run, calls on other streams wait for it
         self._made_on = self._made = None
         if self.status.is_cuda and not torch.cuda.is_current_stream_capturing():
@@ -477,7 +478,7 @@ class PagedCache:
         return torch.zeros(self.c.n_blocks, self._heads, lib.dd_cache_landmark_bytes(self.head_dim), dtype=torch.uint8, device=self._device)
 
     def _check_landmarks(self, landmarks) -> int:
-        shape = (self.c.n_blocks, self._heads, self.head_dim + 16)
+        shape = self._landmark_shape
         if landmarks.dtype is not torch.uint8 or landmarks.shape != shape or not landmarks.is_contiguous():
             raise _invalid(f"landmarks must be a dense uint8 tensor {shape}, not {landmarks.dtype} {tuple(landmarks.shape)}")
         return landmarks.data_ptr()
@@ -505,7 +506,9 @@ class PagedCache:
         n, k, p, r, i = self._listed(positions, idx, requests)
         rq = _rows(q, "q", self.head_dim, n)
         if workspace is None:
-            need = max(16, lib.dd_cache_select_workspace(n, self._heads, self.c.max_pages))
+            need = self._select_bytes.get(n)
+            if need is None:
+                need = self._select_bytes[n] = max(16, lib.dd_cache_select_workspace(n, self._heads, self._max_pages))
             workspace = self._take(need, stream)
         else:
             need = self._given(workspace)

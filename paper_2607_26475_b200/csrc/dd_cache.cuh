@@ -32,6 +32,9 @@ struct dd_cache_view {
 };
 dd_cache_view dd_make_view(const dd_cache* c, const char* data_dev);
 // A launch whose failure is reported here and left behind nowhere (the runtime's last error is cleared).
+// Lets a kernel have `bytes` of dynamic shared memory on the current device: asked of the runtime when a kernel first wants more than it
+// has been given there (0.4 us of host time a call otherwise).
+int dd_allow_smem(const char* who, const void* kernel, int bytes);
 int dd_launch(const char* who, const cudaLaunchConfig_t* cfg, const void* kernel, void** args);
 
 // A tile of a 4-bit page: 16 tokens of one KV head. Offsets within it: codes of K 0, of V 8 d, scales of K 16 d, of V 17 d, exponent

@@ -118,7 +118,7 @@ extern "C" int dd_cache_decode_attn(const dd_cache* cache, int n_q_tokens, const
   const long long units = (long long)cache->batch * a.row_tiles * cache->n_kv_heads;
   long long tiles = ((long long)cache->max_pages * cache->page_tokens + 15) / 16;
   if (window > 0 && ((long long)window + n_q_tokens + 29) / 16 < tiles) tiles = ((long long)window + n_q_tokens + 29) / 16;
-  a.cluster = ca_cluster_of(units, tiles, blocks);
+  a.cluster = cache->format == DD_CACHE_INT4 ? ca_cluster_spread(units, tiles, blocks) : ca_cluster_of(units, tiles, blocks);
   a.joins = !a.cluster && (long long)cache->max_pages * cache->page_tokens > 16 * CA_WHOLE;   // else no unit can have been cut
   return ca_launch(who, a, p, units, blocks, nt, cache->head_dim, (cudaStream_t)stream);
 }

@@ -1468,6 +1468,16 @@ inline int ca_cluster_of(long long units, long long tiles, int blocks) {
 // Rows of a unit that go through the MMA together: up to 8 in one column tile, up to 16 in two.
 inline int ca_column_tiles(int rows) { return rows <= 8 ? 1 : 2; }
 
+// The same for 4-bit pages and for listed pages, whose tiles take more instructions than bytes: short units too go to the warps of a block
+// (a cluster of one: 7 tiles one after the other in one warp 11.7 us, 7.9 side by side), and clusters as large as all units leave
+// room for, up to two tiles a warp.
+inline int ca_cluster_spread(long long units, long long tiles, int blocks) {
+  int c = 1;
+  while (c < CA_MAX_CLUSTER && tiles > 2LL * c * CA_WARPS) c *= 2;
+  while (c > 1 && units * c > blocks * 7 / 8) c /= 2;
+  return tiles > 1 && tiles <= 8LL * c * CA_WARPS && units * c <= blocks * 7 / 8 ? c : 0;
+}
+
 // Kernel format of a cache's pages and a type of queries.
 inline int ca_format(int cache_format, int dtype) {
   const int half = dtype == DD_FP16;
@@ -1476,7 +1486,7 @@ inline int ca_format(int cache_format, int dtype) {
 
 // The attention kernel and, where units may be cut, the joining one.
 inline int ca_launch(const char* who, ca_args& a, const ca_plan& p, long long units, int blocks, int nt, int head_dim, cudaStream_t stream) {
-  DD_CUDA_TRY(nullptr, cudaFuncSetAttribute(p.main_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, p.smem_cluster));
+  DD_TRY(dd_allow_smem(who, p.main_kernel, p.smem_cluster));
   cudaLaunchConfig_t cfg = {};
   cudaLaunchAttribute at[2];
   dd_pdl_attr(&at[0]);

@@ -1007,7 +1007,7 @@ extern "C" int dd_cache_select(const dd_cache* cache, int n_tokens, const int* p
                                     : (bf16 ? (const void*)dd_cache_select_kernel<__nv_bfloat16, 64, 16> : (const void*)dd_cache_select_kernel<__half, 64, 16>));
     a.n_tokens = n_tokens;
     cfg.dynamicSmemBytes = ft == 1 ? cf_smem<1>(cache->head_dim, cache->max_pages) : cf_smem<16>(cache->head_dim, cache->max_pages);
-    DD_CUDA_TRY(nullptr, cudaFuncSetAttribute(f, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)cfg.dynamicSmemBytes));
+    DD_TRY(dd_allow_smem(who, f, (int)cfg.dynamicSmemBytes));
     cfg.gridDim = dim3((unsigned)((n_tokens + ft - 1) / ft), (unsigned)cache->n_kv_heads);
     cfg.blockDim = dim3(CF_THREADS);
     return dd_launch(who, &cfg, f, args);
@@ -1033,7 +1033,7 @@ extern "C" int dd_cache_select(const dd_cache* cache, int n_tokens, const int* p
     cfg.dynamicSmemBytes = (size_t)pages * (cache->head_dim + CS_TAIL);
     f = wide ? (bf16 ? cs_score_kernel<__nv_bfloat16, 128>(tt) : cs_score_kernel<__half, 128>(tt))
              : (bf16 ? cs_score_kernel<__nv_bfloat16, 64>(tt) : cs_score_kernel<__half, 64>(tt));
-    if (tt == 64) DD_CUDA_TRY(nullptr, cudaFuncSetAttribute(f, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)cfg.dynamicSmemBytes));
+    if (tt == 64) DD_TRY(dd_allow_smem(who, f, (int)cfg.dynamicSmemBytes));
     DD_TRY(dd_launch(who, &cfg, f, args));
     cfg.dynamicSmemBytes = 0;
     int threads = 1024;

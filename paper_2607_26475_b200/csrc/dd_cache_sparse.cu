@@ -81,10 +81,7 @@ extern "C" int dd_cache_sparse_attn(const dd_cache* cache, int n_tokens, const i
   }
   const int blocks = sms * p.blocks_per_sm;
   const long long units = (long long)n_tokens * a.row_tiles * cache->n_kv_heads;
-  // A cluster per unit wherever all of them are resident and its warps get at most 8 tiles each: 8 tokens x 8 heads of 128 tiles 19 us with
-  // the flat list and its joining kernel, @CL@ with clusters of 4.
-  for (a.cluster = CA_MAX_CLUSTER; a.cluster > 1 && units * a.cluster > blocks * 7 / 8;) a.cluster /= 2;
-  if (a.cluster < 2 || a.unit_tiles <= CA_WHOLE || a.unit_tiles > 8 * a.cluster * CA_WARPS) a.cluster = 0;
+  a.cluster = ca_cluster_spread(units, a.unit_tiles, blocks);
   a.joins = !a.cluster && a.unit_tiles > CA_WHOLE;                    // else no unit can have been cut
   return ca_launch(who, a, p, units, blocks, nt, cache->head_dim, (cudaStream_t)stream);
 }
