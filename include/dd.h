@@ -476,7 +476,7 @@ int dd_cache_select(const dd_cache* cache, int n_tokens, const int* positions, c
  *   idx        dev int32 [n_tokens][n_kv_heads][k_pages]
  *   out_lse    dev fp32 [n_tokens][n_q_heads] or NULL
  *   workspace  dev, dd_cache_sparse_attn_workspace() bytes, 16-byte aligned; one per call that may run at the same time */
-size_t dd_cache_sparse_attn_workspace(int n_q_heads, int n_kv_heads, int head_dim);
+size_t dd_cache_sparse_attn_workspace(int n_tokens, int n_q_heads, int n_kv_heads, int head_dim, int k_pages);
 int dd_cache_sparse_attn(const dd_cache* cache, int n_tokens, const int* positions, const int* requests, const dd_rows* q,
                          const int* idx, int k_pages, const dd_rows* out, float* out_lse, float scale, void* workspace,
                          size_t workspace_bytes, void* stream);

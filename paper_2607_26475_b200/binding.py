@@ -170,7 +170,7 @@ def _load() -> C.CDLL:
     lib.dd_cache_decode_attn_workspace.argtypes = [ip, ip, ip, ip]
     lib.dd_cache_decode_attn_workspace.restype = C.c_size_t
     lib.dd_cache_decode_attn.argtypes = [cache, ip, rows, vp, rows, vp, ip, C.c_float, vp, C.c_size_t, vp]
-    for name, n in (("dd_cache_landmark_bytes", 1), ("dd_cache_select_workspace", 3), ("dd_cache_sparse_attn_workspace", 3)):
+    for name, n in (("dd_cache_landmark_bytes", 1), ("dd_cache_select_workspace", 3), ("dd_cache_sparse_attn_workspace", 5)):
         getattr(lib, name).argtypes = [ip] * n
         getattr(lib, name).restype = C.c_size_t
     lib.dd_cache_landmarks.argtypes = [cache, vp, ip, vp, vp]
@@ -529,10 +529,9 @@ class PagedCache:
         if out_lse is not None and (out_lse.dtype is not torch.float32 or out_lse.shape != (n, heads) or not out_lse.is_contiguous()):
             raise _invalid(f"out_lse must be a dense float32 tensor {(n, heads)}")
         if workspace is None:
-            need = self._workspace_bytes.get(heads)
+            need = self._workspace_bytes.get((n, heads, k))
             if need is None:
-                need = max(16, lib.dd_cache_sparse_attn_workspace(heads, self._heads, self.head_dim))
-                self._workspace_bytes[heads] = need
+                need = self._workspace_bytes[(n, heads, k)] = max(16, lib.dd_cache_sparse_attn_workspace(n, heads, self._heads, self.head_dim, k))
             workspace = self._take(need, stream)
         else:
             need = self._given(workspace)

@@ -100,20 +100,13 @@ extern "C" int dd_cache_decode_attn(const dd_cache* cache, int n_q_tokens, const
   a.n_q_heads = q->n_heads;
   a.Tq = n_q_tokens;
   a.batch = cache->batch;
+  a.unit_cost = ca_unit_cost(cache->format, false);
   a.row_tiles = (a.n_rows + nt * 8 - 1) / (nt * 8);
   a.window = window;
   a.scale_log2 = (float)((scale > 0.f ? (double)scale : 1.0 / sqrt((double)cache->head_dim)) * 1.4426950408889634);
   if ((long long)a.row_tiles * cache->n_kv_heads > 0x7fffffffLL / 64)
     return dd_fail(nullptr, DD_ERR_INVALID_ARG, "%s: too many heads", who);
-  ca_plan p;
-  switch (ca_format(cache->format, q->dtype)) {
-    case 0: p = ca_pick_of<0, false>(cache->head_dim, nt); break;
-    case 1: p = ca_pick_of<1, false>(cache->head_dim, nt); break;
-    case 2: p = ca_pick_of<2, false>(cache->head_dim, nt); break;
-    case 3: p = ca_pick_of<3, false>(cache->head_dim, nt); break;
-    case 4: p = ca_pick_of<4, false>(cache->head_dim, nt); break;
-    default: p = ca_pick_of<5, false>(cache->head_dim, nt); break;
-  }
+  const ca_plan p = ca_pick<0>(ca_format(cache->format, q->dtype), cache->head_dim, nt);
   const int blocks = sms * p.blocks_per_sm;
   const long long units = (long long)cache->batch * a.row_tiles * cache->n_kv_heads;
   long long tiles = ((long long)cache->max_pages * cache->page_tokens + 15) / 16;

@@ -71,39 +71,43 @@ __global__ void __launch_bounds__(CL_THREADS) dd_cache_landmark_kernel(dd_cache_
   double sum[N];
 #pragma unroll
   for (int i = 0; i < N; ++i) sum[i] = 0.0;
-#pragma unroll 8
-  for (int t = 0; t < n; ++t) {
-    float v[N];
-    if (FMT == DD_CACHE_INT4) {
-      const char* tile = page + (t >> 4) * dd_int4_tile_bytes(D);
-      const int r = t & 15;
-      const uint32_t w = N == 4 ? *reinterpret_cast<const unsigned short*>(tile + r * (D / 2) + lane * 2) : *reinterpret_cast<const unsigned char*>(tile + r * (D / 2) + lane);
-      uint32_t s2, unused;
-      dd_e4m3x4_to_half(*reinterpret_cast<const unsigned char*>(tile + dd_int4_ks_at<D>(r, lane * N / 16)), s2, unused);
-      const float s = dd_unpack2<__half>(s2).x, by = dd_two_to_byte(*reinterpret_cast<const unsigned char*>(tile + 18 * D + r));
+  // 16 tokens at a time, all of their loads under way together, however many there are
+  for (int t0 = 0; t0 < n; t0 += 16) {
 #pragma unroll
-      for (int i = 0; i < N; ++i) v[i] = (float)((int)(w >> (4 * i) & 15u) - 8) * s * by;
-    } else if (FMT == DD_CACHE_E4M3) {
-      const uint32_t w = N == 4 ? *reinterpret_cast<const uint32_t*>(page + t * D + lane * 4) : *reinterpret_cast<const unsigned short*>(page + t * D + lane * 2);
-      const float by = dd_two_to_byte(*reinterpret_cast<const unsigned char*>(page + 2 * T * D + t));
-      uint32_t lo, hi;
-      dd_e4m3x4_to_half(w, lo, hi);
-      const float2 x = dd_unpack2<__half>(lo), y = dd_unpack2<__half>(hi);
-      v[0] = x.x * by;
-      v[1] = x.y * by;
-      if (N == 4) { v[N - 2] = y.x * by; v[N - 1] = y.y * by; }
-    } else {
-      uint2 w = make_uint2(0u, 0u);
-      if (N == 4) w = *reinterpret_cast<const uint2*>(page + t * (2 * D) + lane * 8);
-      else w.x = *reinterpret_cast<const uint32_t*>(page + t * (2 * D) + lane * 4);
-      const float2 x = FMT == DD_CACHE_BF16 ? dd_unpack2<__nv_bfloat16>(w.x) : dd_unpack2<__half>(w.x);
-      const float2 y = FMT == DD_CACHE_BF16 ? dd_unpack2<__nv_bfloat16>(w.y) : dd_unpack2<__half>(w.y);
-      v[0] = x.x;
-      v[1] = x.y;
-      if (N == 4) { v[N - 2] = y.x; v[N - 1] = y.y; }
+    for (int j = 0; j < 16; ++j) {
+      const int t = min(t0 + j, n - 1);
+      float v[N];
+      if (FMT == DD_CACHE_INT4) {
+        const char* tile = page + (t >> 4) * dd_int4_tile_bytes(D);
+        const int r = t & 15;
+        const uint32_t w = N == 4 ? *reinterpret_cast<const unsigned short*>(tile + r * (D / 2) + lane * 2) : *reinterpret_cast<const unsigned char*>(tile + r * (D / 2) + lane);
+        uint32_t s2, unused;
+        dd_e4m3x4_to_half(*reinterpret_cast<const unsigned char*>(tile + dd_int4_ks_at<D>(r, lane * N / 16)), s2, unused);
+        const float s = dd_unpack2<__half>(s2).x, by = dd_two_to_byte(*reinterpret_cast<const unsigned char*>(tile + 18 * D + r));
+#pragma unroll
+        for (int i = 0; i < N; ++i) v[i] = (float)((int)(w >> (4 * i) & 15u) - 8) * s * by;
+      } else if (FMT == DD_CACHE_E4M3) {
+        const uint32_t w = N == 4 ? *reinterpret_cast<const uint32_t*>(page + t * D + lane * 4) : *reinterpret_cast<const unsigned short*>(page + t * D + lane * 2);
+        const float by = dd_two_to_byte(*reinterpret_cast<const unsigned char*>(page + 2 * T * D + t));
+        uint32_t lo, hi;
+        dd_e4m3x4_to_half(w, lo, hi);
+        const float2 x = dd_unpack2<__half>(lo), y = dd_unpack2<__half>(hi);
+        v[0] = x.x * by;
+        v[1] = x.y * by;
+        if (N == 4) { v[N - 2] = y.x * by; v[N - 1] = y.y * by; }
+      } else {
+        uint2 w = make_uint2(0u, 0u);
+        if (N == 4) w = *reinterpret_cast<const uint2*>(page + t * (2 * D) + lane * 8);
+        else w.x = *reinterpret_cast<const uint32_t*>(page + t * (2 * D) + lane * 4);
+        const float2 x = FMT == DD_CACHE_BF16 ? dd_unpack2<__nv_bfloat16>(w.x) : dd_unpack2<__half>(w.x);
+        const float2 y = FMT == DD_CACHE_BF16 ? dd_unpack2<__nv_bfloat16>(w.y) : dd_unpack2<__half>(w.y);
+        v[0] = x.x;
+        v[1] = x.y;
+        if (N == 4) { v[N - 2] = y.x; v[N - 1] = y.y; }
+      }
+#pragma unroll
+      for (int i = 0; i < N; ++i) sum[i] += t0 + j < n ? (double)v[i] : 0.0;
     }
-#pragma unroll
-    for (int i = 0; i < N; ++i) sum[i] += (double)v[i];
   }
 #pragma unroll
   for (int i = 0; i < N; ++i) sum[i] = cs_finite(sum[i] / (double)n);

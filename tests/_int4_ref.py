@@ -121,6 +121,7 @@ def listed_attention(q, raw, table, requests, positions, idx, fmt, T, scale=None
     scale = 1 / math.sqrt(d) if scale is None else scale
     out, absum = np.zeros(q.shape), np.zeros(q.shape)
     lse, unit = np.full((N, Hq), -np.inf), np.zeros((N, Hq))
+    pages = decode_pages(raw, fmt, T, d)                             # [blocks, H, 2, T, d]
     for n in range(N):
         pos = int(positions[n])
         for h in range(H if pos >= 0 else 0):
@@ -128,7 +129,7 @@ def listed_attention(q, raw, table, requests, positions, idx, fmt, T, scale=None
             for p in idx[n, h][:pos // T + 1]:
                 if 0 <= p <= pos // T:
                     blk = int(table[int(requests[n]), p])
-                    kv = decode_pages(raw[blk, h], fmt, T, d)[:, :min(T, pos + 1 - p * T)]
+                    kv = pages[blk, h][:, :min(T, pos + 1 - p * T)]
                     ks.append(kv[0])
                     vs.append(kv[1])
             if ks:

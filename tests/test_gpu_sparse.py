@@ -258,6 +258,85 @@ def test_attention_over_lists_of_many_shapes(dd):
         check_listed(out, lse, q, raw, table, np.repeat(np.arange(B), per), positions, idx, fmt, kind, T, 0.02)
 
 
+PAIRS = [  # tokens by request, H, G, d, T, fmt, query type, k
+    ([list(range(200)), list(range(500, 633)), [7]], 8, 4, 128, 16, "int4", "bf16", 9),
+    ([list(range(200)), list(range(500, 633)), [7]], 8, 4, 128, 16, "bf16", "bf16", 9),
+    ([list(range(100, 400))], 8, 2, 64, 16, "e4m3", "fp16", 12),
+    ([list(range(400))], 8, 3, 128, 32, "e4m3", "bf16", 5),
+    ([list(range(150)), list(range(151))], 8, 1, 64, 64, "fp16", "fp16", 3),
+    ([list(range(150)), list(range(151))], 8, 4, 64, 16, "int4", "fp16", 20),
+    ([list(range(5000, 5300))], 8, 4, 64, 16, "int4", "bf16", 270),       # lists too long to be merged
+]
+
+
+@pytest.mark.parametrize("where,H,G,d,T,fmt,kind,k", PAIRS)
+def test_neighbouring_tokens_together(dd, where, H, G, d, T, fmt, kind, k):
+    """Enough tokens of few query heads that two of them share a unit: lists that overlap, tokens of different requests side by
+    side, padding between them, an odd number of tokens, lists that do not ascend."""
+    gen = torch.Generator().manual_seed(k + H + G)
+    lens = [max(w) + 1 for w in where]
+    cache, raw, table = make(dd, gen, lens, H, d, T, fmt)
+    positions = [p for w in where for p in w]
+    requests = [b for b, w in enumerate(where) for _ in w]
+    for at in (0, 7, 50, 51):                                         # padding on either side of a pair, and a pair of it
+        positions.insert(at, -1)
+        requests.insert(at, 0)
+    if len(positions) % 2 == 0:
+        positions.append(-1)
+        requests.append(0)
+    n = len(positions)
+    assert n // 2 * H >= 8 * 148 and n % 2 == 1
+    idx = random_lists(gen, positions, H, k, T)
+    for i in range(0, n - 1, 2):                                      # neighbours share most of their pages
+        if positions[i] >= 0 and positions[i + 1] > positions[i] and requests[i] == requests[i + 1]:
+            idx[i + 1] = idx[i]
+            idx[i + 1, ::2, :1] = 0
+            idx[i + 1] = np.sort(idx[i + 1].astype(np.uint32)).astype(np.int32)          # (-1 behind)
+            for h in range(H):                                        # no page twice
+                row = [p for j, p in enumerate(idx[i + 1, h]) if p >= 0 and p not in idx[i + 1, h, :j]]
+                idx[i + 1, h] = row + [-1] * (k - len(row))
+    idx[10:20] = idx[10:20, :, ::-1]                                  # holes in front, descending
+    idx[30, :, 0] = positions[30] // T + 1                            # behind the token's own page
+    q = torch.randn(n, H * G, d, generator=gen).to(TYPES[kind]).cuda()
+    out, lse = run_listed(cache, q, idx, positions, requests, 0.02 if kind == "fp16" else 0.0)
+    assert cache.device_error() == (0, 0)
+    check_listed(out, lse, q, raw, table, requests, positions, idx, fmt, kind, T, 0.02 if kind == "fp16" else None)
+    again, _ = run_listed(cache, q, idx, positions, requests, 0.02 if kind == "fp16" else 0.0, with_lse=False)
+    assert torch.equal(out, again)
+    # a few tokens alone take the other way: the same but for the order of the sums
+    few = [i for i in range(60, 70) if positions[i] >= 0]
+    part, _ = run_listed(cache, q[few], idx[few], [positions[i] for i in few], [requests[i] for i in few], 0.02 if kind == "fp16" else 0.0)
+    assert float((part.float() - out[few].float()).abs().max()) <= 2 * ref4.STEP[kind] * float(out[few].float().abs().max())
+
+
+@pytest.mark.parametrize("fmt", ["int4", "bf16", "e4m3"])
+def test_a_neighbours_pages_do_not_reach_a_token(dd, fmt):
+    """Pages that only the other token of a pair lists hold infinities and NaN."""
+    gen = torch.Generator().manual_seed(5)
+    H, G, d, T, k, n = 8, 4, 128, 16, 4, 300
+    cache, raw, table = make(dd, gen, [2000], H, d, T, fmt)
+    bad = [int(table[0, p]) for p in (3, 50)]
+    for blk in bad:
+        if fmt == "int4":
+            _, _, scale, _ = ref4.places(T, d)
+            raw[blk][:, np.unique(scale[1])] = 0x7f
+        elif fmt == "e4m3":
+            raw[blk][:, T * d:2 * T * d] = 0x7f
+        else:
+            raw[blk][:, T * d * 2:] = 0xff
+    cache.data.copy_(torch.from_numpy(raw).cuda())
+    idx = np.tile(np.array([10, 20, 60, 124], dtype=np.int32), (n, H, 1))
+    idx[1::2, :, 0], idx[2::4, :, 2] = 3, 50
+    q = torch.randn(n, H * G, d, generator=gen).to(torch.bfloat16).cuda()
+    out, lse = run_listed(cache, q, idx, [1999] * n, [0] * n)
+    seen = np.zeros(n, bool)
+    seen[1::2] = seen[2::4] = True
+    assert bool(torch.isnan(out[torch.from_numpy(seen)]).all())
+    clean = ~seen
+    check_listed(out[torch.from_numpy(clean)], lse[torch.from_numpy(clean)], q[torch.from_numpy(clean)], raw, table, [0] * int(clean.sum()),
+                 [1999] * int(clean.sum()), idx[clean], fmt, "bf16", T)
+
+
 @pytest.mark.parametrize("fmt", ["int4", "bf16", "e4m3"])
 def test_odd_lists(dd, fmt):
     """No page at all, pages out of order, holes, pages behind the token's own, numbers out of range, one page twice."""
@@ -420,7 +499,7 @@ def test_wrong_memory_and_small_workspaces_are_refused(dd):
     cache, raw, table = make(dd, gen, [64, 64], 2, 128, 16, "int4")
     q, idx, pos = torch.zeros(2, 4, 128, dtype=torch.bfloat16, device="cuda"), torch.zeros(2, 2, 3, dtype=torch.int32, device="cuda"), ints([63, 63])
     lm, out = cache.new_landmarks(), torch.full((2, 4, 128), 7.0, dtype=torch.bfloat16, device="cuda")
-    need = dd.lib.dd_cache_sparse_attn_workspace(4, 2, 128)
+    need = dd.lib.dd_cache_sparse_attn_workspace(2, 4, 2, 128, 3)
     ws = torch.empty(need, dtype=torch.uint8, device="cuda")
     calls = [lambda: cache.sparse_attn(q, idx, pos, out, workspace=ws[:-1]), lambda: cache.sparse_attn(q, idx, pos, out, workspace=ws[8:]),
              lambda: cache.sparse_attn(q.cpu(), idx, pos, out), lambda: cache.sparse_attn(q, idx.cpu(), pos, out), lambda: cache.sparse_attn(q, idx, pos.cpu(), out),

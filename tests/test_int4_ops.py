@@ -21,8 +21,12 @@ def test_sizes(dd):
     assert work(1 << 20, 8, 2048) == (64 << 20) + 1024 * 8 * 128 and work(1 << 20, 8, 1 << 20) == 64 * 8 * ((1 << 22) + 128)
     for bad in [(0, 8, 16), (1, 0, 16), (1, 8, 0), (-1, 8, 16)]:
         assert work(*bad) == 0
-    assert dd.lib.dd_cache_sparse_attn_workspace(32, 8, 128) == dd.lib.dd_cache_decode_attn_workspace(32, 8, 128, 1) > 0
-    for bad in [(32, 5, 128), (32, 8, 96), (0, 8, 128), (4096, 1, 128)]:
+    one = dd.lib.dd_cache_decode_attn_workspace(32, 8, 128, 1)
+    assert dd.lib.dd_cache_sparse_attn_workspace(8, 32, 8, 128, 64) == one > 0
+    # many tokens of up to four heads: room for the pairs' lists and their lengths
+    assert dd.lib.dd_cache_sparse_attn_workspace(2001, 32, 8, 128, 64) == one + 1001 * 8 * 128 * 4 + 4016
+    assert dd.lib.dd_cache_sparse_attn_workspace(2001, 40, 8, 128, 64) == dd.lib.dd_cache_decode_attn_workspace(40, 8, 128, 1)
+    for bad in [(8, 32, 5, 128, 1), (8, 32, 8, 96, 1), (8, 0, 8, 128, 1), (8, 4096, 1, 128, 1), (0, 32, 8, 128, 1), (8, 32, 8, 128, 0)]:
         assert dd.lib.dd_cache_sparse_attn_workspace(*bad) == 0
 
 
