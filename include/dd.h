@@ -446,7 +446,7 @@ int dd_cache_decode_attn(const dd_cache* cache, int n_q_tokens, const dd_rows* q
  * one byte e + 64, 15 bytes of zeros. A landmark is the mean of the valid keys of the page (added in 64 bits), each channel times 2^-e rounded to
  * nearest even, with e the smallest of [-64, 63] that keeps all of them within 127 (beyond 63 they are cut at 127; a channel that is not finite
  * counts as 0). dd_cache_landmarks writes those of the pages that hold any of the last n_last tokens of a request (0: of all its pages).
- * Call it after dd_cache_append; a page's landmark is that of the tokens it held then. */
+ * Call it after dd_cache_append; a page's landmark is that of the tokens it held then. Requests that share a page agree on its tokens. */
 size_t dd_cache_landmark_bytes(int head_dim);
 int dd_cache_landmarks(const dd_cache* cache, const int* ctx_len, int n_last, void* landmarks, void* stream);
 

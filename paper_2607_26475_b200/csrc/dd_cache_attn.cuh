@@ -23,7 +23,7 @@ template <> struct ca_types<5> { using Q = __half; };
 DD_HD constexpr bool ca_quantised(int fmt) { return fmt >= 2; }             // codes as halves, exponents of their own
 DD_HD constexpr bool ca_int4(int fmt) { return fmt >= 4; }
 constexpr float CA_INT4_BACK = 131072.f;                              // 4-bit values enter the products as 2^-17 of themselves
-constexpr int CA_NOWHERE = 0x7fffff00;                                // first token of a tile that is not there
+constexpr int CA_NOWHERE = 0x7ffffff0;                                // first token of a tile that is not there
 
 template <int FMT, int D, int NT, int SP>
 struct ca_geom {
@@ -1197,9 +1197,10 @@ __global__ void __launch_bounds__(CA_THREADS, (ca_geom<FMT, D, NT, SP>::BLOCKS_P
       // this lookup, the last of them left to the careful form
       int n = 0;
       if (SP && PLAIN_LOOP && is.left > 1) {
-        // tiles of the lookup from here on that are there, complete and visible; not the last of the run, of the unit or of the lookup
+        // tiles of the lookup from here on that are there, complete and visible; not the last of the run, of the unit or of the lookup.
+        // Where V of a tile goes with K of the next, the next has to be one too.
         const unsigned odd = __ballot_sync(0xffffffffu, (SP == 2 ? tokens == CA_NOWHERE : (tokens & ~15) > is.s.end - 16) || (unsigned)blocks >= (unsigned)a.c.n_blocks) >> (is.t - blocks_from);
-        n = odd ? __ffs(odd) - 1 : 32 - (is.t - blocks_from);
+        n = (odd ? __ffs(odd) - 1 : 32 - (is.t - blocks_from)) - (V_FIRST ? 1 : 0);
         n = min(min(n, is.left - 1), min(blocks_from + 31 - is.t, is.s.tiles - 1 - is.t));
         n = min(n, n_here - i);
       } else if (PLAIN_LOOP && is.left > 1) {

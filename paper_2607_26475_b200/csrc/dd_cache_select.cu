@@ -44,7 +44,7 @@ constexpr int CS_LM_LEAST = -64, CS_Q_LEAST = -120;
 // ---- landmarks: one warp per page and head, D / 32 channels a lane
 constexpr int CL_THREADS = 256;
 template <int FMT, int D>
-__global__ void __launch_bounds__(CL_THREADS) dd_cache_landmark_kernel(dd_cache_view c, const int* __restrict__ ctx_len, int n_last, int pages, char* landmarks) {
+__global__ void __launch_bounds__(CL_THREADS, 3) dd_cache_landmark_kernel(dd_cache_view c, const int* __restrict__ ctx_len, int n_last, int pages, char* landmarks) {
   constexpr int N = D / 32;
   const int lane = threadIdx.x & 31;
   const long long item = (long long)blockIdx.x * (CL_THREADS / 32) + (threadIdx.x >> 5);
@@ -68,9 +68,10 @@ __global__ void __launch_bounds__(CL_THREADS) dd_cache_landmark_kernel(dd_cache_
     return;
   }
   const char* page = c.data + blk * c.block_stride + h * c.head_stride;
-  double sum[N];
+  constexpr int CHAINS = 4;                            // sums that do not wait for each other
+  double part[CHAINS][N], sum[N];
 #pragma unroll
-  for (int i = 0; i < N; ++i) sum[i] = 0.0;
+  for (int i = 0; i < N; ++i) part[0][i] = part[1][i] = part[2][i] = part[3][i] = 0.0;
   // 16 tokens at a time, all of their loads under way together, however many there are
   for (int t0 = 0; t0 < n; t0 += 16) {
 #pragma unroll
@@ -106,11 +107,11 @@ __global__ void __launch_bounds__(CL_THREADS) dd_cache_landmark_kernel(dd_cache_
         if (N == 4) { v[N - 2] = y.x; v[N - 1] = y.y; }
       }
 #pragma unroll
-      for (int i = 0; i < N; ++i) sum[i] += t0 + j < n ? (double)v[i] : 0.0;
+      for (int i = 0; i < N; ++i) part[j % CHAINS][i] += t0 + j < n ? (double)v[i] : 0.0;
     }
   }
 #pragma unroll
-  for (int i = 0; i < N; ++i) sum[i] = cs_finite(sum[i] / (double)n);
+  for (int i = 0; i < N; ++i) sum[i] = cs_finite(((part[0][i] + part[1][i]) + (part[2][i] + part[3][i])) / (double)n);
   const int e = cs_exponent(sum, CS_LM_LEAST);
   const double down = cs_two_to(-e);
   uint32_t w = 0;

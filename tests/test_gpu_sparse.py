@@ -494,6 +494,60 @@ def test_calls_on_several_streams_at_once(dd):
             assert torch.equal(i, wi) and torch.equal(o, wo)
 
 
+@pytest.mark.parametrize("n,k,ctx", [(2, 30, 2000), (40, 64, 4000), (320, 9, 2000)])      # a cluster a unit, the flat list, pairs
+def test_output_in_place_of_the_queries(dd, n, k, ctx):
+    gen = torch.Generator().manual_seed(n)
+    H, G, d, T = 8, 4, 128, 16
+    cache, raw, table = make(dd, gen, [ctx], H, d, T, "int4")
+    positions = torch.randint(0, ctx, (n,), generator=gen).to(torch.int32)
+    idx = ints(random_lists(gen, positions.tolist(), H, k, T))
+    q = torch.randn(n, H * G, d, generator=gen).to(torch.bfloat16).cuda()
+    out = torch.empty_like(q)
+    cache.sparse_attn(q, idx, positions.cuda(), out)
+    cache.sparse_attn(q, idx, positions.cuda(), q)
+    assert torch.equal(q, out)
+
+
+def test_two_captured_steps_with_workspaces_of_their_own(dd):
+    """Two graphs that replay at the same time on two streams, each with its own workspaces."""
+    gen = torch.Generator().manual_seed(21)
+    H, G, d, T, k, n = 2, 4, 128, 16, 40, 6
+    cache, raw, table = make(dd, gen, [6000], H, d, T, "int4")
+    lm = cache.new_landmarks()
+    cache.update_landmarks(lm, ints([6000]))
+    positions = ints(torch.randint(3000, 6000, (n,), generator=gen))
+    qs = [torch.randn(n, H * G, d, generator=gen).to(torch.bfloat16).cuda() for _ in range(2)]
+    want = []
+    for q in qs:
+        idx, out = torch.empty(n, H, k, dtype=torch.int32, device="cuda"), torch.empty_like(q)
+        cache.select(q, lm, positions, idx)
+        cache.sparse_attn(q, idx, positions, out)
+        want.append((idx, out))
+    torch.cuda.synchronize()
+    graphs, got, spaces = [], [], []
+    for q in qs:
+        ws = torch.empty(dd.lib.dd_cache_select_workspace(n, H, table.shape[1]), dtype=torch.uint8, device="cuda")
+        wa = torch.empty(dd.lib.dd_cache_sparse_attn_workspace(n, H * G, H, d, k), dtype=torch.uint8, device="cuda")
+        idx, out = torch.zeros(n, H, k, dtype=torch.int32, device="cuda"), torch.zeros_like(q)
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            for _ in range(5):
+                cache.select(q, lm, positions, idx, workspace=ws)
+                cache.sparse_attn(q, idx, positions, out, workspace=wa)
+        graphs.append(g)
+        got.append((idx, out))
+        spaces.append((ws, wa))
+    streams = [torch.cuda.Stream() for _ in graphs]
+    torch.cuda.synchronize()
+    for _ in range(4):
+        for g, s in zip(graphs, streams):
+            with torch.cuda.stream(s):
+                g.replay()
+    torch.cuda.synchronize()
+    for (i, o), (wi, wo) in zip(got, want):
+        assert torch.equal(i, wi) and torch.equal(o, wo)
+
+
 def test_wrong_memory_and_small_workspaces_are_refused(dd):
     gen = torch.Generator().manual_seed(12)
     cache, raw, table = make(dd, gen, [64, 64], 2, 128, 16, "int4")
