@@ -258,7 +258,8 @@ __global__ void __launch_bounds__(CR_THREADS) dd_cache_read_kernel(dd_cache_view
 }
 
 // The same for 4-bit pages. A tile is one run of 18 d + 32 bytes; it goes through shared memory, where a lane finds the codes,
-// scales and exponents of the 8 elements it writes in one 16-byte store.
+// scales and exponents of the 8 elements it writes in one 16-byte store. Bound: HBM's writes; 16384 pages of 16 x 128 30.5 us (5.6 TB/s of
+// reads and writes).
 template <typename T, int D>
 __global__ void __launch_bounds__(CR_THREADS) dd_cache_read_int4_kernel(dd_cache_view c, const int* __restrict__ idx,
                                                                        char* __restrict__ out, int k_pages, long long n_tiles) {

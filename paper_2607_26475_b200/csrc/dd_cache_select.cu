@@ -708,48 +708,46 @@ __global__ void __launch_bounds__(CR_ROW_THREADS) dd_cache_topk_rank_kernel(cons
   cs_choose<WARPS, 4, CR_LIST>(each, count, list, [] { __syncthreads(); }, k, out, w, sh_a, sh_b, sh_key, sh_page);
 }
 
-// ---- scores and choice in one, where the keys of a row fit shared memory: TT tokens of one head (16, or 1) against all of their pages.
-// Landmarks come in groups of CF_PAGES, several on their way while one is used; the 16 warps take 8 pages of a group each. Then a
-// warp a token (TT = 16), or all of them (TT = 1), choose; their lists lie where the landmarks were. One block an SM; what bounds it for 16 tokens is the landmarks' way
-// from L2 to every block (2048 pages: 295 KB for 16 tokens) and the choice's instructions. 2048 tokens x 2048 pages x 8 heads: 143 us (two kernels with keys in the workspace: 165).
-constexpr int CF_PAGES = 128, CF_THREADS = 512;
-template <int TT> struct cf_geom {
-  static constexpr int CAP = TT == 1 ? 2048 : 256;                   // of a row's list
-  static constexpr int STAGES = TT == 1 ? 8 : 4;
-};
-constexpr int CF_MOST = 2048;                                        // pages
+// ---- scores and choice in one, where the keys of a row fit shared memory: 16 tokens of one head against all of their pages.
+// A warp brings the landmarks of 8 pages of every group of CF_PAGES, several groups ahead, multiplies them and leaves the keys in shared
+// memory; then it chooses for one of the tokens. The lists of the choice lie where the landmarks were. One block an SM; what
+// bounds it is instructions at four warps a scheduler (0.43 issued a cycle), a third of them the choice's. 2048 tokens x 2048 pages x 8 heads: 143 us (two
+// kernels with the keys in the workspace: 165).
+constexpr int CF_PAGES = 128, CF_THREADS = 512, CF_TOKENS = 16;
+constexpr int CF_STAGES = 4;
+constexpr int CF_LIST = 256;                           // of a row
+constexpr int CF_MOST = 2048;                          // pages
 // Keys of a row in shared memory: a lane's run of pages (a multiple of 8), one word, the next lane's: no bank conflicts.
-template <int TT> __host__ __device__ constexpr int cf_lanes() { return TT == 1 ? CF_THREADS : 32; }
-template <int TT> __host__ __device__ constexpr int cf_run(int pages) { return (pages + 8 * cf_lanes<TT>() - 1) / (8 * cf_lanes<TT>()) * 8; }
-template <int TT> __host__ __device__ constexpr int cf_stride(int max_pages) { return cf_lanes<TT>() * (cf_run<TT>(max_pages) + 1); }
-template <int TT> size_t cf_smem(int d, int max_pages) {
-  return (size_t)cf_geom<TT>::STAGES * CF_PAGES * (d + CS_TAIL) + ((size_t)TT * cf_stride<TT>(max_pages) + max_pages) * 4;
+DD_HD constexpr int cf_run(int pages) { return (pages + 255) / 256 * 8; }
+DD_HD constexpr int cf_stride(int max_pages) { return 32 * (cf_run(max_pages) + 1); }
+size_t cf_smem(int d, int max_pages) {
+  return (size_t)CF_STAGES * CF_PAGES * (d + CS_TAIL) + ((size_t)CF_TOKENS * cf_stride(max_pages) + max_pages) * 4;
 }
-template <typename T, int D, int TT>
+template <typename T, int D>
 __global__ void __launch_bounds__(CF_THREADS) dd_cache_select_kernel(const cs_args a) {
-  constexpr int LM = D + CS_TAIL, STRIDE = D + 16, CAP = cf_geom<TT>::CAP, WARPS = CF_THREADS / 32;
-  constexpr int STAGES = cf_geom<TT>::STAGES;
-  static_assert(TT * CAP * 8 <= STAGES * CF_PAGES * (64 + CS_TAIL), "the lists lie where the landmarks were");
+  constexpr int LM = D + CS_TAIL, STRIDE = D + 16, TT = CF_TOKENS, STAGES = CF_STAGES;
+  static_assert(TT * CF_LIST * 8 <= STAGES * CF_PAGES * LM, "the lists lie where the landmarks were");
+  static_assert(TT == CF_THREADS / 32, "a token a warp");
   extern __shared__ __align__(16) unsigned char cs_smem[];            // landmarks [STAGES][CF_PAGES][LM], keys [TT][stride], a table row
   __shared__ __align__(16) signed char sh_q[TT][STRIDE];
-  __shared__ int sh_own[16], sh_req[16], sh_a[WARPS], sh_b[WARPS];
+  __shared__ int sh_own[TT], sh_req[TT];
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
-  const int h = blockIdx.y, n0 = blockIdx.x * TT, stride = cf_stride<TT>(a.c.max_pages);
+  const int h = blockIdx.y, n0 = blockIdx.x * TT, stride = cf_stride(a.c.max_pages);
   uint32_t* const keys = reinterpret_cast<uint32_t*>(cs_smem + STAGES * CF_PAGES * LM);
   int* const blocks = reinterpret_cast<int*>(keys + TT * stride);
   uint32_t* const list_key = reinterpret_cast<uint32_t*>(cs_smem);
-  unsigned* const list_page = list_key + TT * CAP;
+  unsigned* const list_page = list_key + TT * CF_LIST;
   dd_grid_dependency_wait();
-  if (threadIdx.x < 16) {
+  if (threadIdx.x < TT) {
     int req = -1, own = -1;
-    if (threadIdx.x < TT && n0 + threadIdx.x < a.n_tokens) own = cs_own_page(a, n0 + threadIdx.x, req, h == 0);
+    if (n0 + threadIdx.x < a.n_tokens) own = cs_own_page(a, n0 + threadIdx.x, req, h == 0);
     sh_own[threadIdx.x] = own;
     sh_req[threadIdx.x] = req;
   }
   __syncthreads();
   int furthest = 0;                                    // pages of any token of the tile
   for (int i = 0; i < TT; ++i) furthest = max(furthest, sh_own[i] + 1);
-  const int run = cf_run<TT>(max(furthest, 1));
+  const int run = cf_run(max(furthest, 1));
   const unsigned by_run = 0xffffffffu / run + 1;       // page / run by a multiplication (below 2^16, exact)
   uint32_t qf[D / 32][4];                              // step s: channels D / 4 t + 8 s .. + 7 of tokens g and g + 8
   bool have_q = false;
@@ -792,14 +790,14 @@ __global__ void __launch_bounds__(CF_THREADS) dd_cache_select_kernel(const cs_ar
 #pragma unroll 1
     for (int i = 0; i < STAGES - 1; ++i) fetch(i);
     if (!have_q) {
-      if (warp < TT && n0 + warp < a.n_tokens) cs_query<T, D>(a, n0 + warp, h, sh_q[warp]);
+      if (n0 + warp < a.n_tokens) cs_query<T, D>(a, n0 + warp, h, sh_q[warp]);
       __syncthreads();
       have_q = true;
 #pragma unroll
       for (int i = 0; i < D / 32; ++i) {
         uint2 lo = make_uint2(0u, 0u), hi = make_uint2(0u, 0u);
-        if (g < TT && n0 + g < a.n_tokens) lo = *reinterpret_cast<const uint2*>(&sh_q[g < TT ? g : 0][t * (D / 4) + 8 * i]);
-        if (g + 8 < TT && n0 + g + 8 < a.n_tokens) hi = *reinterpret_cast<const uint2*>(&sh_q[g + 8 < TT ? g + 8 : 0][t * (D / 4) + 8 * i]);
+        if (n0 + g < a.n_tokens) lo = *reinterpret_cast<const uint2*>(&sh_q[g][t * (D / 4) + 8 * i]);
+        if (n0 + g + 8 < a.n_tokens) hi = *reinterpret_cast<const uint2*>(&sh_q[g + 8][t * (D / 4) + 8 * i]);
         qf[i][0] = lo.x; qf[i][1] = hi.x; qf[i][2] = lo.y; qf[i][3] = hi.y;
       }
     }
@@ -822,11 +820,10 @@ __global__ void __launch_bounds__(CF_THREADS) dd_cache_select_kernel(const cs_ar
 #pragma unroll
         for (int c = 0; c < D / 32; ++c) cs_mma(acc, qf[c], r[2 * c], r[2 * c + 1]);
         // pages that all tokens of the run see and none of them keeps anyway
-        const bool plain = TT > 1 && s == 0 && e == TT && p0 >= a.first && p0 + 7 <= least - a.recent;
+        const bool plain = s == 0 && e == TT && p0 >= a.first && p0 + 7 <= least - a.recent;
 #pragma unroll
         for (int x = 0; x < 2; ++x) {
           const int row = g + 8 * x;
-          if (row >= TT) continue;
           uint32_t* to = keys + row * stride + p0 + __umulhi(p0, by_run) + 2 * t;
           const uint32_t k0 = cs_key((float)acc[2 * x] * by0), k1 = cs_key((float)acc[2 * x + 1] * by1);
           if (plain) {
@@ -844,22 +841,20 @@ __global__ void __launch_bounds__(CF_THREADS) dd_cache_select_kernel(const cs_ar
   asm volatile("cp.async.wait_group 0;" ::: "memory");
   __syncthreads();
   // ---- the choice
-  const int row = TT == 1 ? 0 : warp, w = TT == 1 ? warp : 0;
+  const int row = warp;
   if (n0 + row >= a.n_tokens) return;
   const int P = sh_own[row] + 1, k = a.k;
   int* out = a.out + ((long long)(n0 + row) * a.c.n_kv_heads + h) * k;
   if (P <= k) {                                                       // everything visible fits
-    for (int i = w * 32 + lane; i < k; i += (TT == 1 ? CF_THREADS : 32)) out[i] = i < P ? i : -1;
+    for (int i = lane; i < k; i += 32) out[i] = i < P ? i : -1;
     return;
   }
-  constexpr int ROW_WARPS = TT == 1 ? WARPS : 1, NG = 8;
   uint32_t* const mine = keys + row * stride;
-  const int at0 = (w * 32 + lane) * run;
+  const int at0 = lane * run;
   // zeros behind the tiles of 8 pages that were scored for this token (those of its request's furthest one here, at least its own)
-  for (int p = (P + 7) / 8 * 8 + lane + 32 * w; p < cf_lanes<TT>() * run; p += cf_lanes<TT>()) mine[p + __umulhi(p, by_run)] = 0u;
-  if (TT == 1) __syncthreads();
-  else __syncwarp();
-  const uint32_t* const keys_of_lane = mine + at0 + (w * 32 + lane);
+  for (int p = (P + 7) / 8 * 8 + lane; p < 32 * run; p += 32) mine[p + __umulhi(p, by_run)] = 0u;
+  __syncwarp();
+  const uint32_t* const keys_of_lane = mine + at0 + lane;
   auto each = [&](auto&& f) {
     for (int j = 0; j < run; j += 8)
 #pragma unroll
@@ -886,8 +881,7 @@ __global__ void __launch_bounds__(CF_THREADS) dd_cache_select_kernel(const cs_ar
       }
     }
   };
-  if constexpr (TT == 1) cs_choose<ROW_WARPS, NG, CAP>(each, count, list, [] { __syncthreads(); }, k, out, w, sh_a, sh_b, list_key, list_page);
-  else cs_choose<ROW_WARPS, NG, CAP>(each, count, list, [] { __syncwarp(); }, k, out, w, sh_a, sh_b, list_key + row * CAP, list_page + row * CAP);
+  cs_choose<1, 8, CF_LIST>(each, count, list, [] { __syncwarp(); }, k, out, 0, nullptr, nullptr, list_key + row * CF_LIST, list_page + row * CF_LIST);
 }
 
 template <int D> const void* cs_landmark_kernel(int format) {
@@ -1003,17 +997,14 @@ extern "C" int dd_cache_select(const dd_cache* cache, int n_tokens, const int* p
   void* args[] = {&a};
   // One kernel where requests bring more than two tokens each and a row's keys fit shared memory. With one token a block it is the slower way (8 requests x 2048 pages: 22
   // us against 14): few blocks, and every one of them the whole chain.
-  const int ft = each <= 2 ? 1 : 16;
   if (each > 2 && cache->max_pages <= CF_MOST) {
     const bool wide = cache->head_dim == 128, bf16 = q->dtype == DD_BF16;
-    const void* f = ft == 1 ? (wide ? (bf16 ? (const void*)dd_cache_select_kernel<__nv_bfloat16, 128, 1> : (const void*)dd_cache_select_kernel<__half, 128, 1>)
-                                    : (bf16 ? (const void*)dd_cache_select_kernel<__nv_bfloat16, 64, 1> : (const void*)dd_cache_select_kernel<__half, 64, 1>))
-                            : (wide ? (bf16 ? (const void*)dd_cache_select_kernel<__nv_bfloat16, 128, 16> : (const void*)dd_cache_select_kernel<__half, 128, 16>)
-                                    : (bf16 ? (const void*)dd_cache_select_kernel<__nv_bfloat16, 64, 16> : (const void*)dd_cache_select_kernel<__half, 64, 16>));
+    const void* f = wide ? (bf16 ? (const void*)dd_cache_select_kernel<__nv_bfloat16, 128> : (const void*)dd_cache_select_kernel<__half, 128>)
+                         : (bf16 ? (const void*)dd_cache_select_kernel<__nv_bfloat16, 64> : (const void*)dd_cache_select_kernel<__half, 64>);
     a.n_tokens = n_tokens;
-    cfg.dynamicSmemBytes = ft == 1 ? cf_smem<1>(cache->head_dim, cache->max_pages) : cf_smem<16>(cache->head_dim, cache->max_pages);
+    cfg.dynamicSmemBytes = cf_smem(cache->head_dim, cache->max_pages);
     DD_TRY(dd_allow_smem(who, f, (int)cfg.dynamicSmemBytes));
-    cfg.gridDim = dim3((unsigned)((n_tokens + ft - 1) / ft), (unsigned)cache->n_kv_heads);
+    cfg.gridDim = dim3((unsigned)((n_tokens + CF_TOKENS - 1) / CF_TOKENS), (unsigned)cache->n_kv_heads);
     cfg.blockDim = dim3(CF_THREADS);
     return dd_launch(who, &cfg, f, args);
   }

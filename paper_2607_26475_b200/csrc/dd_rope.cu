@@ -11,10 +11,12 @@
 // and a slice of its heads; each lane keeps the two 16-byte chunks of a row whose elements turn with each other (half
 // layout: chunk j and chunk j + rot_dim / 16; interleaved: neighbours), so the rotation needs no exchange between lanes,
 // and the sines and cosines of its eight pairs stay in registers for all heads of the slice. A quantised row's largest
-// magnitude is one reduction over the group. 80 registers (one kind of rows at a time) keep three blocks on an SM.
+// magnitude is one reduction over the group. 80 registers (one kind of rows at a time) keep three blocks on an SM; 4-bit rows take 128
+// and two blocks.
 //
-// Measured on a B200: 32768 tokens of 32 + 8 heads of 128 bf16, rotation 108 us (6.2 TB/s, 0.96 of a copy's rate); the same with
-// 8 + 8 heads of K and V into e4m3 pages 129 us (5.7 TB/s); 8 tokens 2.3 us, one launch.
+// Measured on a B200: 32768 tokens of 32 + 8 heads of 128 bf16, rotation 102.5 us (6.55 TB/s, a copy's rate); the same with
+// 8 + 8 heads of K and V into e4m3 pages 120 us (6.2 TB/s); into 4-bit pages 163 us (4.35 TB/s): instructions and their latencies, 45% of
+// the cycles issue and 14 warps an SM wait for what they loaded; 8 tokens 2.1 us (4-bit 3.6), one launch.
 #include <math.h>
 
 #include <type_traits>
@@ -503,13 +505,13 @@ int rp_launch(rp_args& a, int head_dim, int dtype, int fmt, cudaStream_t st, con
   const int lanes = head_dim / 16, per_warp = 32 / lanes;
   const int n_heads = a.n_q + a.n_k * (fmt >= 0 ? 2 : 1);
   // Heads per group of lanes: 8 (two batches of loads, the token's angles computed once per 8 rows) while that gives half the
-  // groups that fill the device, fewer for fewer tokens. 32768 tokens of 40 heads: 8 heads 108 us, 20 heads 110, 5 heads 128;
-  // 2000 tokens: 8 heads 10.0 us, 4 heads 10.6, 20 heads 12.1.
+  // groups that fill the device, fewer for fewer tokens. 32768 tokens of 40 heads: 8 heads 102.6 us, 16 heads 105.9, 4 heads 114.7; with
+  // rows that are quantised on the way 16: e4m3 8 heads 123.8, 16 heads 120.0, 24 122.8; 4-bit 176.7, 163.3, 163.6.
   int sms = 0;
   cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, device);
   if (sms <= 0) sms = 148;
   const long long fill = (long long)sms * rp_blocks(fmt) * RP_THREADS / lanes;
-  a.slice_heads = 2 * RP_BATCH;
+  a.slice_heads = (fmt >= 0 ? 4 : 2) * RP_BATCH;
   while (a.slice_heads > 1 && (long long)a.n_tokens * ((n_heads + a.slice_heads - 1) / a.slice_heads) < fill / 2) a.slice_heads /= 2;
   a.slices = (n_heads + a.slice_heads - 1) / a.slice_heads;
   const long long per_block = (long long)(RP_THREADS / 32) * per_warp;
