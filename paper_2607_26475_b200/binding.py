@@ -374,7 +374,7 @@ class PagedCache:
                          self.status.data_ptr())
         self._addr = C.addressof(self.c)
         self._batch, self._heads, self._device = batch, n_kv_heads, block_table.device
-        self._workspace_bytes, self._select_bytes = {}, {}
+        self._workspace_bytes = {}
         self._max_pages, self._landmark_shape = max_pages, (n_blocks, n_kv_heads, head_dim + 16)
         # the error word is zeroed on the stream the cache is made on: until that has run, calls on other streams wait for it
         self._made_on = self._made = None
@@ -447,10 +447,7 @@ class PagedCache:
         if out_lse is not None and (out_lse.dtype is not torch.float32 or out_lse.shape != (b, Tq, Hq) or not out_lse.is_contiguous()):
             raise _invalid(f"out_lse must be a dense float32 tensor {(b, Tq, Hq)}")
         if workspace is None:
-            need = self._workspace_bytes.get((Hq, Tq))
-            if need is None:
-                need = max(16, lib.dd_cache_decode_attn_workspace(Hq, self._heads, self.head_dim, Tq))
-                self._workspace_bytes[(Hq, Tq)] = need
+            need = self._bytes((Hq, Tq), lambda: lib.dd_cache_decode_attn_workspace(Hq, self._heads, self.head_dim, Tq))
             workspace = self._take(need, stream)
         else:
             need = self._given(workspace)
@@ -466,6 +463,15 @@ class PagedCache:
             return torch.empty(need, dtype=torch.uint8, device=self._device)
         with torch.cuda.stream(_torch_stream(stream, self._device) if isinstance(stream, int) else stream):
             return torch.empty(need, dtype=torch.uint8, device=self._device)
+
+    def _bytes(self, shape, ask) -> int:
+        """Workspace bytes of a call of this shape, asked for once (and again when very many shapes have come by)."""
+        need = self._workspace_bytes.get(shape)
+        if need is None:
+            if len(self._workspace_bytes) >= 1024:
+                self._workspace_bytes.clear()
+            need = self._workspace_bytes[shape] = max(16, ask())
+        return need
 
     @staticmethod
     def _given(workspace) -> int:
@@ -506,9 +512,7 @@ class PagedCache:
         n, k, p, r, i = self._listed(positions, idx, requests)
         rq = _rows(q, "q", self.head_dim, n)
         if workspace is None:
-            need = self._select_bytes.get(n)
-            if need is None:
-                need = self._select_bytes[n] = max(16, lib.dd_cache_select_workspace(n, self._heads, self._max_pages))
+            need = self._bytes((n,), lambda: lib.dd_cache_select_workspace(n, self._heads, self._max_pages))
             workspace = self._take(need, stream)
         else:
             need = self._given(workspace)
@@ -529,9 +533,7 @@ class PagedCache:
         if out_lse is not None and (out_lse.dtype is not torch.float32 or out_lse.shape != (n, heads) or not out_lse.is_contiguous()):
             raise _invalid(f"out_lse must be a dense float32 tensor {(n, heads)}")
         if workspace is None:
-            need = self._workspace_bytes.get((n, heads, k))
-            if need is None:
-                need = self._workspace_bytes[(n, heads, k)] = max(16, lib.dd_cache_sparse_attn_workspace(n, heads, self._heads, self.head_dim, k))
+            need = self._bytes((n, heads, k), lambda: lib.dd_cache_sparse_attn_workspace(n, heads, self._heads, self.head_dim, k))
             workspace = self._take(need, stream)
         else:
             need = self._given(workspace)

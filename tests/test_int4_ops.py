@@ -150,3 +150,12 @@ def test_python_side_refuses_wrong_shapes_and_types(dd):
         with pytest.raises(dd.DDError) as e:
             call()
         assert e.value.code == dd.DD_ERR_INVALID_ARG
+
+
+def test_calls_without_tokens_do_nothing(dd):
+    c = dd.PagedCache(torch.zeros(4, 2, 2336, dtype=torch.uint8), torch.zeros(2, 2, dtype=torch.int32), cache_format=dd.DD_CACHE_INT4)
+    q, pos, idx = torch.zeros(0, 4, 128, dtype=torch.bfloat16), torch.zeros(0, dtype=torch.int32), torch.zeros(0, 2, 3, dtype=torch.int32)
+    ws = torch.zeros(16, dtype=torch.uint8)
+    c.select(q, c.new_landmarks(), pos, idx, workspace=ws, stream=0)
+    c.sparse_attn(q, idx, pos, torch.empty_like(q), workspace=ws, stream=0)
+    c.append(q[:, :2], q[:, :2], pos, pos, stream=0)
