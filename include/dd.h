@@ -459,7 +459,8 @@ int dd_cache_landmarks(const dd_cache* cache, const int* ctx_len, int n_last, vo
  * its page scores 0.
  *   q          dev [n_tokens][n_q_heads][head_dim], bf16 or half whatever the format of the pages (which are not read)
  *   out_idx    dev int32 [n_tokens][n_kv_heads][k_pages], written
- *   workspace  dev, dd_cache_select_workspace() bytes (up to 64 MiB; more for contexts above 512K pages), 16-byte aligned; one per call that may run at the same time */
+ *   workspace  dev, dd_cache_select_workspace() bytes (4 for each token, head and page: up to 64 MiB or so, or those of 64 tokens where they are
+ *              more), 16-byte aligned; one per call that may run at the same time */
 size_t dd_cache_select_workspace(int n_tokens, int n_kv_heads, int max_pages);
 int dd_cache_select(const dd_cache* cache, int n_tokens, const int* positions, const int* requests, const dd_rows* q,
                     const void* landmarks, int k_pages, int first_pages, int recent_pages, int* out_idx, void* workspace,

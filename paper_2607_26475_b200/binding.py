@@ -510,6 +510,8 @@ class PagedCache:
         """The pages of every query token and KV head into idx [N, Hkv, k] int32 (ascending, -1 behind them): the first first_pages,
         the last recent_pages, and those with the highest scores. q [N, Hq, d]; positions, requests [N] int32 as for append."""
         n, k, p, r, i = self._listed(positions, idx, requests)
+        if not (0 <= first_pages <= k and 1 <= recent_pages <= k):
+            raise _invalid(f"first_pages ({first_pages}) and recent_pages ({recent_pages}, at least 1) must fit the {k} pages of idx")
         rq = _rows(q, "q", self.head_dim, n)
         if workspace is None:
             need = self._bytes((n,), lambda: lib.dd_cache_select_workspace(n, self._heads, self._max_pages))

@@ -898,7 +898,8 @@ template <typename T, int D> const void* cs_score_kernel(int tokens) {
 }
 
 int cs_stride(int max_pages) { return (max_pages + 31) / 32 * 32; }
-// Tokens whose keys go through the workspace at a time: 64 MiB of keys stay in L2, next to the landmarks.
+// Tokens whose keys go through the workspace at a time: 64 MiB of keys stay in L2, next to the landmarks; 64 tokens at least. So a launch
+// has 2^24 rows and fewer blocks than 2^31.
 int cs_tokens_at_once(int n_tokens, int n_kv_heads, int max_pages) {
   const long long row = (long long)n_kv_heads * cs_stride(max_pages) * 4;
   const long long n = (64LL << 20) / row / 64 * 64;
@@ -937,7 +938,7 @@ extern "C" int dd_cache_landmarks(const dd_cache* cache, const int* ctx_len, int
 }
 
 extern "C" size_t dd_cache_select_workspace(int n_tokens, int n_kv_heads, int max_pages) {
-  if (n_tokens < 1 || n_kv_heads < 1 || max_pages < 1) return 0;
+  if (n_tokens < 1 || n_kv_heads < 1 || n_kv_heads > 65535 || max_pages < 1 || max_pages > 0x7fffffff / 16) return 0;      // no such cache
   return (size_t)cs_tokens_at_once(n_tokens, n_kv_heads, max_pages) * n_kv_heads * (cs_stride(max_pages) * 4 + 128);
 }
 
@@ -1015,7 +1016,6 @@ extern "C" int dd_cache_select(const dd_cache* cache, int n_tokens, const int* p
     const long long rows = (long long)a.n_tokens * cache->n_kv_heads, tiles = (a.n_tokens + tt - 1) / tt;
     const int pages = cs_pages(tt);
     a.chunks = (cache->max_pages + pages - 1) / pages;
-    if (tiles * a.chunks > 0x7fffffffLL) return dd_fail(nullptr, DD_ERR_INVALID_ARG, "%s: too many tokens", who);
     if (tt == 64) {
       f = wide ? (bf16 ? (const void*)dd_cache_query_kernel<__nv_bfloat16, 128> : (const void*)dd_cache_query_kernel<__half, 128>)
                : (bf16 ? (const void*)dd_cache_query_kernel<__nv_bfloat16, 64> : (const void*)dd_cache_query_kernel<__half, 64>);
@@ -1044,7 +1044,6 @@ extern "C" int dd_cache_select(const dd_cache* cache, int n_tokens, const int* p
     } else {
       f = (const void*)dd_cache_topk_kernel<32, 0>;
     }
-    if (rows > 0x7fffffffLL) return dd_fail(nullptr, DD_ERR_INVALID_ARG, "%s: too many tokens", who);
     cfg.gridDim = dim3((unsigned)rows);
     cfg.blockDim = dim3(threads);
     DD_TRY(dd_launch(who, &cfg, f, args));

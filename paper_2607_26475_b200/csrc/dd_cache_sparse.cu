@@ -55,6 +55,7 @@ __global__ void __launch_bounds__(CM_THREADS) dd_cache_merge_kernel(const cm_arg
     const int* const from[2] = {a.idx + (2LL * pair * a.c.n_kv_heads + h) * a.k, a.idx + ((2LL * pair + 1) * a.c.n_kv_heads + h) * a.k};
     bool ascending = own[0] >= 0 && own[1] >= 0 && req[0] == req[1] && a.k <= CM_MOST;
     int n[2] = {0, 0}, total = 0;
+    __syncwarp();                                      // the lists of the head before have been read
     for (int i = 0; i < 2; ++i) {
       for (int j0 = 0; j0 < seen[i]; j0 += 32) {
         const int j = j0 + lane, p = j < seen[i] ? from[i][j] : -1;

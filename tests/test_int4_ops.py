@@ -159,3 +159,15 @@ def test_calls_without_tokens_do_nothing(dd):
     c.select(q, c.new_landmarks(), pos, idx, workspace=ws, stream=0)
     c.sparse_attn(q, idx, pos, torch.empty_like(q), workspace=ws, stream=0)
     c.append(q[:, :2], q[:, :2], pos, pos, stream=0)
+
+
+def test_numbers_beyond_31_bits_are_refused(dd):
+    c = dd.PagedCache(torch.zeros(4, 2, 2336, dtype=torch.uint8), torch.zeros(2, 2, dtype=torch.int32), cache_format=dd.DD_CACHE_INT4)
+    q, pos, idx = torch.zeros(2, 4, 128, dtype=torch.bfloat16), torch.zeros(2, dtype=torch.int32), torch.zeros(2, 2, 3, dtype=torch.int32)
+    ws = torch.zeros(4096, dtype=torch.uint8)
+    for more in (dict(first_pages=1 << 32), dict(recent_pages=(1 << 32) + 1), dict(first_pages=-1), dict(recent_pages=0)):
+        with pytest.raises(dd.DDError) as e:
+            c.select(q, c.new_landmarks(), pos, idx, workspace=ws, stream=0, **more)
+        assert e.value.code == dd.DD_ERR_INVALID_ARG
+    assert dd.lib.dd_cache_select_workspace(1, 1, (1 << 31) - 1) == 0
+    assert dd.lib.dd_cache_select_workspace(1, 70000, 16) == 0
