@@ -41,86 +41,101 @@ __device__ __forceinline__ int cs_code(double v, double down) { return (int)fmin
 constexpr int CS_TAIL = 16;                            // bytes behind the codes of a landmark: the exponent + 64, then nothing
 constexpr int CS_LM_LEAST = -64, CS_Q_LEAST = -120;
 
-// ---- landmarks: one warp per page and head, D / 32 channels a lane
-constexpr int CL_THREADS = 256;
+// ---- landmarks: a page and head at a time to a warp, D / 32 channels a lane. A warp takes `per` of them in a row (up to CL_PER): its lanes
+// find the pages together, so that the chain length -> table entry -> keys is waited for once a warp. Bound: instructions (0.62 to 0.7 issued a
+// cycle and scheduler; a widening to 64 bits and an addition for each key's channel), in flight 16 rows a warp. 8 x 2048 pages of 8 heads of
+// 128: bf16 130 us (4.1 TB/s; one a warp 157), e4m3 148 (174), 4 bits 196 (217).
+constexpr int CL_THREADS = 256, CL_PER = 8;            // in a row at most (32: 162 us where 8 took 141, the last warps being alone for too long)
+// Blocks an SM: 16 rows of 16-bit keys of 128 take 32 registers, with four blocks 140 us; the others are the faster for a fourth (e4m3 158 -> 148 us).
+constexpr int cl_blocks(int fmt, int d) { return d == 128 && (fmt == DD_CACHE_BF16 || fmt == DD_CACHE_FP16) ? 3 : 4; }
 template <int FMT, int D>
-__global__ void __launch_bounds__(CL_THREADS, 3) dd_cache_landmark_kernel(dd_cache_view c, const int* __restrict__ ctx_len, int n_last, int pages, char* landmarks) {
+__global__ void __launch_bounds__(CL_THREADS, (cl_blocks(FMT, D))) dd_cache_landmark_kernel(dd_cache_view c, const int* __restrict__ ctx_len, int n_last, int pages, int per, char* landmarks) {
   constexpr int N = D / 32;
   const int lane = threadIdx.x & 31;
-  const long long item = (long long)blockIdx.x * (CL_THREADS / 32) + (threadIdx.x >> 5);
-  const long long bp = item / c.n_kv_heads;
-  const int h = (int)(item - bp * c.n_kv_heads), b = (int)(bp / pages);
+  const long long item0 = ((long long)blockIdx.x * (CL_THREADS / 32) + (threadIdx.x >> 5)) * per;
   dd_grid_dependency_wait();
-  if (b >= c.batch) return;
-  int len = ctx_len[b];
-  const int most = c.max_pages << c.page_shift;
-  if (len < 0 || len > most) {
-    if (lane == 0) dd_status(c.status, len);
-    len = len < 0 ? 0 : most;
-  }
-  const int from = n_last > 0 && n_last < len ? len - n_last : 0;
-  const long long p_ = (from >> c.page_shift) + (bp - (long long)b * pages);
-  if ((p_ << c.page_shift) >= len) return;
-  const int p = (int)p_, n = min(len - (p << c.page_shift), 1 << c.page_shift), T = 1 << c.page_shift;
-  const int blk = c.table[b * c.table_stride + p];
-  if ((unsigned)blk >= (unsigned)c.n_blocks) {
-    if (lane == 0) dd_status(c.status, blk);
-    return;
-  }
-  const char* page = c.data + blk * c.block_stride + h * c.head_stride;
-  constexpr int CHAINS = 4;                            // sums that do not wait for each other
-  double part[CHAINS][N], sum[N];
-#pragma unroll
-  for (int i = 0; i < N; ++i) part[0][i] = part[1][i] = part[2][i] = part[3][i] = 0.0;
-  // 16 tokens at a time, all of their loads under way together, however many there are
-  for (int t0 = 0; t0 < n; t0 += 16) {
-#pragma unroll
-    for (int j = 0; j < 16; ++j) {
-      const int t = min(t0 + j, n - 1);
-      float v[N];
-      if (FMT == DD_CACHE_INT4) {
-        const char* tile = page + (t >> 4) * dd_int4_tile_bytes(D);
-        const int r = t & 15;
-        const uint32_t w = N == 4 ? *reinterpret_cast<const unsigned short*>(tile + r * (D / 2) + lane * 2) : *reinterpret_cast<const unsigned char*>(tile + r * (D / 2) + lane);
-        uint32_t s2, unused;
-        dd_e4m3x4_to_half(*reinterpret_cast<const unsigned char*>(tile + dd_int4_ks_at<D>(r, lane * N / 16)), s2, unused);
-        const float s = dd_unpack2<__half>(s2).x, by = dd_two_to_byte(*reinterpret_cast<const unsigned char*>(tile + 18 * D + r));
-#pragma unroll
-        for (int i = 0; i < N; ++i) v[i] = (float)((int)(w >> (4 * i) & 15u) - 8) * s * by;
-      } else if (FMT == DD_CACHE_E4M3) {
-        const uint32_t w = N == 4 ? *reinterpret_cast<const uint32_t*>(page + t * D + lane * 4) : *reinterpret_cast<const unsigned short*>(page + t * D + lane * 2);
-        const float by = dd_two_to_byte(*reinterpret_cast<const unsigned char*>(page + 2 * T * D + t));
-        uint32_t lo, hi;
-        dd_e4m3x4_to_half(w, lo, hi);
-        const float2 x = dd_unpack2<__half>(lo), y = dd_unpack2<__half>(hi);
-        v[0] = x.x * by;
-        v[1] = x.y * by;
-        if (N == 4) { v[N - 2] = y.x * by; v[N - 1] = y.y * by; }
-      } else {
-        uint2 w = make_uint2(0u, 0u);
-        if (N == 4) w = *reinterpret_cast<const uint2*>(page + t * (2 * D) + lane * 8);
-        else w.x = *reinterpret_cast<const uint32_t*>(page + t * (2 * D) + lane * 4);
-        const float2 x = FMT == DD_CACHE_BF16 ? dd_unpack2<__nv_bfloat16>(w.x) : dd_unpack2<__half>(w.x);
-        const float2 y = FMT == DD_CACHE_BF16 ? dd_unpack2<__nv_bfloat16>(w.y) : dd_unpack2<__half>(w.y);
-        v[0] = x.x;
-        v[1] = x.y;
-        if (N == 4) { v[N - 2] = y.x; v[N - 1] = y.y; }
+  int tokens = 0, block = 0, head = 0;                 // of the lane's page and head, no tokens = nothing to do
+  if (lane < per) {
+    const long long bp = (item0 + lane) / c.n_kv_heads, b = bp / pages;
+    head = (int)(item0 + lane - bp * c.n_kv_heads);
+    if (b < c.batch) {
+      int len = ctx_len[b];
+      const int most = c.max_pages << c.page_shift;
+      if (len < 0 || len > most) {
+        dd_status(c.status, len);
+        len = len < 0 ? 0 : most;
       }
-#pragma unroll
-      for (int i = 0; i < N; ++i) part[j % CHAINS][i] += t0 + j < n ? (double)v[i] : 0.0;
+      const int from = n_last > 0 && n_last < len ? len - n_last : 0;
+      const long long p = (from >> c.page_shift) + (bp - b * pages);
+      if ((p << c.page_shift) < len) {
+        block = c.table[b * c.table_stride + p];
+        if ((unsigned)block < (unsigned)c.n_blocks) tokens = min(len - ((int)p << c.page_shift), 1 << c.page_shift);
+        else dd_status(c.status, block);
+      }
     }
   }
+  const int T = 1 << c.page_shift;
+  for (int item = 0; item < per; ++item) {
+    const int n = __shfl_sync(0xffffffffu, tokens, item), blk = __shfl_sync(0xffffffffu, block, item), h = __shfl_sync(0xffffffffu, head, item);
+    if (n == 0) continue;
+    const char* page = c.data + blk * c.block_stride + h * c.head_stride;
+    constexpr int CHAINS = 4;                            // sums that do not wait for each other
+    double part[CHAINS][N], sum[N];
 #pragma unroll
-  for (int i = 0; i < N; ++i) sum[i] = cs_finite(((part[0][i] + part[1][i]) + (part[2][i] + part[3][i])) / (double)n);
-  const int e = cs_exponent(sum, CS_LM_LEAST);
-  const double down = cs_two_to(-e);
-  uint32_t w = 0;
+    for (int i = 0; i < N; ++i) part[0][i] = part[1][i] = part[2][i] = part[3][i] = 0.0;
+    // 16 tokens at a time, all of their loads under way together, however many there are
+    for (int t0 = 0; t0 < n; t0 += 16) {
 #pragma unroll
-  for (int i = 0; i < N; ++i) w |= (uint32_t)(cs_code(sum[i], down) & 0xff) << (8 * i);
-  char* to = landmarks + ((long long)blk * c.n_kv_heads + h) * (D + CS_TAIL);
-  if (N == 4) *reinterpret_cast<uint32_t*>(to + lane * 4) = w;
-  else *reinterpret_cast<unsigned short*>(to + lane * 2) = (unsigned short)w;
-  if (lane < CS_TAIL / 4) *reinterpret_cast<uint32_t*>(to + D + lane * 4) = lane == 0 ? (uint32_t)(e + 64) : 0u;
+      for (int j = 0; j < 16; ++j) {
+        const int t = min(t0 + j, n - 1);
+        const bool in = t0 + j < n;                    // rows behind the last token are made zeros before they are widened
+        float v[N];
+        if (FMT == DD_CACHE_INT4) {
+          const char* tile = page + (t >> 4) * dd_int4_tile_bytes(D);
+          const int r = t & 15;
+          const uint32_t w = N == 4 ? *reinterpret_cast<const unsigned short*>(tile + r * (D / 2) + lane * 2) : *reinterpret_cast<const unsigned char*>(tile + r * (D / 2) + lane);
+          uint32_t s2, unused;
+          dd_e4m3x4_to_half(*reinterpret_cast<const unsigned char*>(tile + dd_int4_ks_at<D>(r, lane * N / 16)), s2, unused);
+          const float s = in ? dd_unpack2<__half>(s2).x : 0.f, by = !in ? 0.f : dd_two_to_byte(*reinterpret_cast<const unsigned char*>(tile + 18 * D + r));
+#pragma unroll
+          for (int i = 0; i < N; ++i) v[i] = (__uint_as_float((w >> (4 * i) & 15u) | 0x4b000000u) - 8388616.f) * s * by;      // 2^23 + code
+        } else if (FMT == DD_CACHE_E4M3) {
+          uint32_t w = N == 4 ? *reinterpret_cast<const uint32_t*>(page + t * D + lane * 4) : *reinterpret_cast<const unsigned short*>(page + t * D + lane * 2);
+          if (!in) w = 0u;
+          const float by = !in ? 0.f : dd_two_to_byte(*reinterpret_cast<const unsigned char*>(page + 2 * T * D + t));
+          uint32_t lo, hi;
+          dd_e4m3x4_to_half(w, lo, hi);
+          const float2 x = dd_unpack2<__half>(lo), y = dd_unpack2<__half>(hi);
+          v[0] = x.x * by;
+          v[1] = x.y * by;
+          if (N == 4) { v[N - 2] = y.x * by; v[N - 1] = y.y * by; }
+        } else {
+          uint2 w = make_uint2(0u, 0u);
+          if (N == 4) w = *reinterpret_cast<const uint2*>(page + t * (2 * D) + lane * 8);
+          else w.x = *reinterpret_cast<const uint32_t*>(page + t * (2 * D) + lane * 4);
+          if (!in) w = make_uint2(0u, 0u);
+          const float2 x = FMT == DD_CACHE_BF16 ? dd_unpack2<__nv_bfloat16>(w.x) : dd_unpack2<__half>(w.x);
+          const float2 y = FMT == DD_CACHE_BF16 ? dd_unpack2<__nv_bfloat16>(w.y) : dd_unpack2<__half>(w.y);
+          v[0] = x.x;
+          v[1] = x.y;
+          if (N == 4) { v[N - 2] = y.x; v[N - 1] = y.y; }
+        }
+#pragma unroll
+        for (int i = 0; i < N; ++i) part[j % CHAINS][i] += (double)v[i];
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < N; ++i) sum[i] = cs_finite(((part[0][i] + part[1][i]) + (part[2][i] + part[3][i])) / (double)n);
+    const int e = cs_exponent(sum, CS_LM_LEAST);
+    const double down = cs_two_to(-e);
+    uint32_t w = 0;
+#pragma unroll
+    for (int i = 0; i < N; ++i) w |= (uint32_t)(cs_code(sum[i], down) & 0xff) << (8 * i);
+    char* to = landmarks + ((long long)blk * c.n_kv_heads + h) * (D + CS_TAIL);
+    if (N == 4) *reinterpret_cast<uint32_t*>(to + lane * 4) = w;
+    else *reinterpret_cast<unsigned short*>(to + lane * 2) = (unsigned short)w;
+    if (lane < CS_TAIL / 4) *reinterpret_cast<uint32_t*>(to + D + lane * 4) = lane == 0 ? (uint32_t)(e + 64) : 0u;
+  }
 }
 
 // ---- scores
@@ -923,7 +938,14 @@ extern "C" int dd_cache_landmarks(const dd_cache* cache, const int* ctx_len, int
   int pages = cache->max_pages;
   if (n_last > 0 && ((long long)n_last + cache->page_tokens - 2) / cache->page_tokens + 1 < pages)
     pages = (int)(((long long)n_last + cache->page_tokens - 2) / cache->page_tokens + 1);
-  const long long warps = (long long)cache->batch * pages * cache->n_kv_heads, blocks = (warps + CL_THREADS / 32 - 1) / (CL_THREADS / 32);
+  const long long items = (long long)cache->batch * pages * cache->n_kv_heads;
+  int sms = 0;
+  cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, device);
+  if (sms <= 0) sms = 148;
+  // as many to a warp as leave the device full twice over
+  const long long fill = items / ((long long)sms * 2 * 3 * (CL_THREADS / 32));
+  int per = (int)(fill < 1 ? 1 : (fill > CL_PER ? CL_PER : fill));
+  const long long warps = (items + per - 1) / per, blocks = (warps + CL_THREADS / 32 - 1) / (CL_THREADS / 32);
   if (blocks > 0x7fffffffLL) return dd_fail(nullptr, DD_ERR_INVALID_ARG, "%s: too many pages", who);
   cudaLaunchConfig_t cfg = {};
   cudaLaunchAttribute at;
@@ -933,7 +955,7 @@ extern "C" int dd_cache_landmarks(const dd_cache* cache, const int* ctx_len, int
   cfg.gridDim = dim3((unsigned)blocks);
   cfg.blockDim = dim3(CL_THREADS);
   cfg.stream = (cudaStream_t)stream;
-  void* args[] = {&v, &ctx_len, &n_last, &pages, &landmarks};
+  void* args[] = {&v, &ctx_len, &n_last, &pages, &per, &landmarks};
   return dd_launch(who, &cfg, cache->head_dim == 128 ? cs_landmark_kernel<128>(cache->format) : cs_landmark_kernel<64>(cache->format), args);
 }
 

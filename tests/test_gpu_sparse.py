@@ -7,7 +7,7 @@ import torch
 from tests import _int4_ref as ref4
 from tests._cache_ref import f64
 from tests._int4_ref import TYPES, check
-from tests.test_gpu_int4 import dd, make, random_pages, rope_of  # noqa: F401  (dd is the fixture)
+from tests.test_gpu_int4 import dd, format_code, make, random_pages, rope_of  # noqa: F401  (dd is the fixture)
 
 pytestmark = pytest.mark.gpu
 
@@ -41,6 +41,32 @@ def test_landmarks_match_their_definition(dd, fmt, T, d, H, n_last):
                 want[blk, h] = ref4.landmark(ref4.decode_pages(raw[blk, h], fmt, T, d)[0, :min(T, n - p * T)])
     assert np.array_equal(lm.cpu().numpy(), want)
     assert cache.device_error() == (0, 0)
+
+
+@pytest.mark.parametrize("fmt,d,H", [("int4", 64, 8), ("bf16", 128, 7), ("fp16", 64, 3), ("e4m3", 128, 8)])
+def test_landmarks_of_many_pages(dd, fmt, d, H):
+    """More pages than fill the device, so that a warp has several: full ones out of a few blocks, ragged ends, an empty request, a bad entry."""
+    T, M, full = 16, 3001, 40
+    gen = torch.Generator().manual_seed(d + H)
+    lens = [3000 * T + 5, 0, 1200 * T, 2999 * T + 1, 7, 2500 * T + 15, 3001 * T, 17]
+    raw = random_pages(gen, full + len(lens), H, fmt, T, d)
+    table = torch.randint(0, full, (len(lens), M), generator=gen, dtype=torch.int32)
+    for b, n in enumerate(lens):
+        if n % T:
+            table[b, n // T] = full + b
+    table[2, 77] = full + len(lens)                                  # behind the pool
+    table[5, 2501:] = -9                                             # never read
+    cache = dd.PagedCache(torch.from_numpy(raw).cuda(), table.cuda(), cache_format=format_code(dd, fmt), head_dim=d, page_tokens=T)
+    lm = torch.full((raw.shape[0], H, d + 16), 99, dtype=torch.uint8, device="cuda")
+    cache.update_landmarks(lm, ints(lens))
+    torch.cuda.synchronize()
+    want = np.full(lm.shape, 99, dtype=np.uint8)
+    for blk in range(raw.shape[0]):
+        n = T if blk < full else lens[blk - full] % T
+        for h in range(H if n else 0):
+            want[blk, h] = ref4.landmark(ref4.decode_pages(raw[blk, h], fmt, T, d)[0, :n])
+    assert np.array_equal(lm.cpu().numpy(), want)
+    assert cache.device_error()[1] == full + len(lens)
 
 
 # ---------------------------------------------------------------------------------------------- selection
