@@ -290,7 +290,8 @@ __global__ void __launch_bounds__(CR_THREADS) dd_cache_read_int4_kernel(dd_cache
     uint4 r[(CHUNKS + 31) / 32];
 #pragma unroll
     for (int i = 0; i < (CHUNKS + 31) / 32; ++i) {
-      r[i] = make_uint4(0u, 0u, 0u, 0u);             // scales of zero: all zeros
+      const uint32_t none = i * 32 + lane < D ? 0x88888888u : 0u;     // of a page that is not there: codes of zero, then scales and exponents
+      r[i] = make_uint4(none, none, none, none);
       if (blk >= 0 && i * 32 + lane < CHUNKS) r[i] = dd_ld_stream(src + (i * 32 + lane) * 16);
     }
     __syncwarp();
