@@ -400,7 +400,8 @@ int dd_rope_apply(const dd_rope* rope, int head_dim, int n_tokens, const int* po
  * finite magnitude is at most 448 * 2^e, a code is the value times 2^-e (exact) rounded to nearest even; infinities and
  * NaN become the NaN code. DD_CACHE_INT4: the same with 3136 * 2^e (7 * 448); the scale of 16 elements is their largest finite magnitude
  * times 2^-e / 7 rounded to e4m3, at least 2^-4, and the NaN code where one of them is not finite; a code is 8 + the value times 2^-e /
- * scale, rounded to nearest even, within [1, 15]. Codes, scales and exponents of turned keys are those of the 64-bit rotation. With `rope` the keys are turned on the way (32 bits, rounded once, into the page), and with q /
+ * scale, rounded to nearest even, within [1, 15]. Codes, scales and exponents of turned keys are those of the 64-bit rotation, in which
+ * an element beyond the largest 32-bit number counts as infinite. With `rope` the keys are turned on the way (32 bits, rounded once, into the page), and with q /
  * q_out the queries of the same tokens are turned in the same launch. A negative position is padding: nothing of that
  * token is written. A request, page or block out of range is reported in status and the token skipped. Two tokens of one
  * call must not name the same place: which of them the page then holds (in parts) is not defined.

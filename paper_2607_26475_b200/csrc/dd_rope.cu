@@ -69,8 +69,11 @@ __device__ __forceinline__ void rp_angle(double turns, int pos, float amplitude,
 //     RP_KNOWN of the row's largest. Where that leaves a border within reach of the row's exponent, of a scale or of a code (a
 //     few elements in 100,000), it is done again in 64 bits, the element or the row, so that the bytes written are those of the 64-bit
 //     rotation (without a correction otherwise).
-// Rows that are not finite, and rows below 2^-108, take the same 64-bit way.
+// Rows below 2^-108 and rows that are not finite take the same 64-bit way; a turned element beyond what 32 bits hold counts as infinite, so
+// that a row's exponent always fits its byte.
 constexpr float RP_KNOWN = 0x1.8p-21f;
+constexpr double RP_MOST = 0x1.fffffep127;             // the largest 32-bit number
+constexpr unsigned RP_NEAR_MOST = 0x7f7fffe0u;         // bits of 2^128 less 2^-19 of it: further from RP_MOST than RP_KNOWN reaches
 
 // Lane of the group and slot (0 or 1) that hold chunk `chunk` of a row.
 __device__ __forceinline__ void rp_mate(int chunk, int rot16, bool interleaved, int& lane, int& slot) {
@@ -130,7 +133,7 @@ __device__ __noinline__ int rp_int4_slow(const char* row, rp_place at, const dou
   }
   for (int i = 0; i < 16; ++i) {
     const double m = fabs(x[i]);
-    if (m <= 1.7976931348623157e308) top[i >> 3] = fmax(top[i >> 3], m);
+    if (m <= RP_MOST) top[i >> 3] = fmax(top[i >> 3], m);
     else bad[i >> 3] = true;
   }
   double amax = fmax(top[0], top[1]);
@@ -373,7 +376,7 @@ __global__ void __launch_bounds__(RP_THREADS, rp_blocks(FMT)) dd_rope_kernel(rp_
           const bool known = kind == 2 || a.rot16 == 0;        // the row is what was given
           int byte = dd_int4_exponent_byte(__uint_as_float(amax));
           const float up = dd_two_to_byte(254 - byte), whole = __uint_as_float(amax) * up, eps = whole * RP_KNOWN;
-          bool slow = amax >= 0x7f800000u || byte < 8;         // (a scale of 2^-4 * 2^(byte - 127) has an inverse from 8 on)
+          bool slow = amax >= RP_NEAR_MOST || byte < 8;         // (a scale of 2^-4 * 2^(byte - 127) has an inverse from 8 on)
           if (!known) slow |= fabsf(whole - 3136.f) < eps || fabsf(whole - 1568.f) < eps;
           unsigned scale[2];
           uint32_t code[2];
