@@ -83,3 +83,20 @@ def test_keys_turned_beyond_32_bits_count_as_infinite(dd, kind, d, rot, layout, 
     want[beyond] = np.inf
     check_rows(got, want, 0, pos, d)
     check_rows(got, f64(v), 1, pos, d)
+
+
+@pytest.mark.parametrize("d,rot,layout,amplitude", [(128, 128, "half", 2.0 ** -133), (64, 32, "interleaved", 2.0 ** -140), (64, 64, "half", 2.0 ** -101),
+                                                    (128, 48, "half", 0.0)])
+def test_keys_turned_with_the_smallest_amplitudes(dd, d, rot, layout, amplitude):
+    """An amplitude that 32 bits hold as a subnormal times rows near the largest of their type: ordinary keys."""
+    gen = torch.Generator().manual_seed(d + rot)
+    N, H = 512, 2
+    x = torch.randn(N, 2 * H, d, generator=gen)
+    x[:, :H, :rot] *= 2.0 ** 124
+    x = x.to(torch.bfloat16)
+    k, v = x[:, :H], x[:, H:]
+    r, turns = rope_of(dd, d, rot, layout, "none", amplitude)
+    pos = torch.randperm(N, generator=gen).to(torch.int32)
+    got = appended(dd, k, v, pos, r, d)
+    check_rows(got, ref.rotate(f64(k), pos.numpy(), turns, layout, amplitude), 0, pos, d)
+    check_rows(got, f64(v), 1, pos, d)
