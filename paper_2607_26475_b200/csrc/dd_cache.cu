@@ -1,7 +1,4 @@
 // The paged key-value cache: argument checks shared by its calls, and the kernel that reads pages back.
-#include <mutex>
-#include <vector>
-
 #include "dd_cache.cuh"
 
 // ---------------------------------------------------------------------------------------------
@@ -109,29 +106,10 @@ int dd_check_cache_memory(const dd_cache* c, const char* who, int device, bool a
 }
 
 int dd_allow_smem(const char* who, const void* kernel, int bytes) {
-  struct given { const void* kernel; int device, bytes; };
-  static std::mutex lock;
-  static std::vector<given> all;                       // a few dozen kernels at most
-  const int device = dd_current_device();
-  std::lock_guard<std::mutex> guard(lock);
-  given* had = nullptr;
-  for (given& g : all)
-    if (g.kernel == kernel && g.device == device) had = &g;
-  if (had && had->bytes >= bytes) return DD_OK;
   const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
-  if (e != cudaSuccess) {
-    cudaGetLastError();
-    return dd_fail(nullptr, DD_ERR_CUDA, "%s: shared memory: %s", who, cudaGetErrorString(e));
-  }
-  if (had) {
-    had->bytes = bytes;
-  } else {
-    try {
-      all.push_back({kernel, device, bytes});
-    } catch (...) {                                    // not remembered: asked again next time
-    }
-  }
-  return DD_OK;
+  if (e == cudaSuccess) return DD_OK;
+  cudaGetLastError();
+  return dd_fail(nullptr, DD_ERR_CUDA, "%s: shared memory: %s", who, cudaGetErrorString(e));
 }
 
 int dd_launch(const char* who, const cudaLaunchConfig_t* cfg, const void* kernel, void** args) {

@@ -31,10 +31,11 @@ struct dd_cache_view {
   int page_shift;                        // log2 of the tokens per page
 };
 dd_cache_view dd_make_view(const dd_cache* c, const char* data_dev);
-// A launch whose failure is reported here and left behind nowhere (the runtime's last error is cleared).
-// Lets a kernel have `bytes` of dynamic shared memory on the current device: asked of the runtime when a kernel first wants more than it
-// has been given there (0.4 us of host time a call otherwise).
+// Lets a kernel have `bytes` of dynamic shared memory on the current device. Asked at every call: the grant ends with the context, which a
+// caller may end and begin anew (cudaDeviceReset). `bytes` is the most that the kernel is ever launched with, so that calls of two threads do
+// not take from each other.
 int dd_allow_smem(const char* who, const void* kernel, int bytes);
+// A launch whose failure is reported here and left behind nowhere (the runtime's last error is cleared).
 int dd_launch(const char* who, const cudaLaunchConfig_t* cfg, const void* kernel, void** args);
 
 // A tile of a 4-bit page: 16 tokens of one KV head. Offsets within it: codes of K 0, of V 8 d, scales of K 16 d, of V 17 d, exponent

@@ -1026,7 +1026,7 @@ extern "C" int dd_cache_select(const dd_cache* cache, int n_tokens, const int* p
                          : (bf16 ? (const void*)dd_cache_select_kernel<__nv_bfloat16, 64> : (const void*)dd_cache_select_kernel<__half, 64>);
     a.n_tokens = n_tokens;
     cfg.dynamicSmemBytes = cf_smem(cache->head_dim, cache->max_pages);
-    DD_TRY(dd_allow_smem(who, f, (int)cfg.dynamicSmemBytes));
+    DD_TRY(dd_allow_smem(who, f, (int)cf_smem(cache->head_dim, CF_MOST)));
     cfg.gridDim = dim3((unsigned)((n_tokens + CF_TOKENS - 1) / CF_TOKENS), (unsigned)cache->n_kv_heads);
     cfg.blockDim = dim3(CF_THREADS);
     return dd_launch(who, &cfg, f, args);
