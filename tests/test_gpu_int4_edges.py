@@ -100,3 +100,23 @@ def test_keys_turned_with_the_smallest_amplitudes(dd, d, rot, layout, amplitude)
     got = appended(dd, k, v, pos, r, d)
     check_rows(got, ref.rotate(f64(k), pos.numpy(), turns, layout, amplitude), 0, pos, d)
     check_rows(got, f64(v), 1, pos, d)
+
+
+@pytest.mark.parametrize("kind,d,rot,layout", [("bf16", 128, 128, "half"), ("fp16", 64, 32, "interleaved"), ("bf16", 128, 48, "half"), ("bf16", 64, 0, "half")])
+def test_rows_of_zeros(dd, kind, d, rot, layout):
+    """Whole rows of zeros of either sign among others, turned and as they are; rows that vanish in 32 bits."""
+    gen = torch.Generator().manual_seed(rot + d)
+    N, H = 256, 2
+    x = torch.randn(N, 2 * H, d, generator=gen)
+    x[::3] = 0.0
+    x[1::6] = -0.0
+    x[2::9, :, 16:] = 0.0
+    if kind == "bf16":
+        x[4::12] *= 2.0 ** -133
+    x = x.to(TYPES[kind])
+    k, v = x[:, :H], x[:, H:]
+    r, turns = rope_of(dd, d, rot, layout, "none", 1.1) if rot else (None, None)
+    pos = torch.randperm(N, generator=gen).to(torch.int32)
+    got = appended(dd, k, v, pos, r, d)
+    check_rows(got, ref.rotate(f64(k), pos.numpy(), turns, layout, float(np.float32(1.1))) if rot else f64(k), 0, pos, d)
+    check_rows(got, f64(v), 1, pos, d)
