@@ -510,13 +510,14 @@ int rp_launch(rp_args& a, int head_dim, int dtype, int fmt, cudaStream_t st, con
   const int lanes = head_dim / 16, per_warp = 32 / lanes;
   const int n_heads = a.n_q + a.n_k * (fmt >= 0 ? 2 : 1);
   // Heads per group of lanes: 8 (two batches of loads, the token's angles computed once per 8 rows) while that gives half the
-  // groups that fill the device, fewer for fewer tokens. 32768 tokens of 40 heads: 8 heads 102.6 us, 16 heads 105.9, 4 heads 114.7; with
-  // rows that are quantised on the way 16: e4m3 8 heads 123.8, 16 heads 120.0, 24 122.8; 4-bit 176.7, 163.3, 163.6.
+  // groups that fill the device, fewer for fewer tokens. 32768 tokens of 40 heads: 8 heads 102.6 us, 16 heads 105.9, 4 heads 114.7; into
+  // 16-bit pages, unturned, 8 heads 47.5, 16 heads 51.2. Rows that are quantised on the way 16: e4m3 8 heads 123.8, 16 heads 120.0, 24
+  // 122.8; 4-bit 176.7, 163.3, 163.6.
   int sms = 0;
   cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, device);
   if (sms <= 0) sms = 148;
   const long long fill = (long long)sms * rp_blocks(fmt) * RP_THREADS / lanes;
-  a.slice_heads = (fmt >= 0 ? 4 : 2) * RP_BATCH;
+  a.slice_heads = (fmt == DD_CACHE_E4M3 || fmt == DD_CACHE_INT4 ? 4 : 2) * RP_BATCH;
   while (a.slice_heads > 1 && (long long)a.n_tokens * ((n_heads + a.slice_heads - 1) / a.slice_heads) < fill / 2) a.slice_heads /= 2;
   a.slices = (n_heads + a.slice_heads - 1) / a.slice_heads;
   const long long per_block = (long long)(RP_THREADS / 32) * per_warp;
