@@ -1018,9 +1018,16 @@ extern "C" int dd_cache_select(const dd_cache* cache, int n_tokens, const int* p
   cfg.numAttrs = 1;
   cfg.stream = (cudaStream_t)stream;
   void* args[] = {&a};
-  // One kernel where requests bring more than two tokens each and a row's keys fit shared memory. With one token a block it is the slower way (8 requests x 2048 pages: 22
-  // us against 14): few blocks, and every one of them the whole chain.
-  if (each > 2 && cache->max_pages <= CF_MOST) {
+  // One kernel where requests bring more than two tokens each, a row's keys fit shared memory and there are rows enough. A tile of 16 tokens goes
+  // over the pages once for each request that it touches, however few tiles there are: 2048 pages 11 us a pass and 10 for the rest, while the two
+  // kernels take the longer the more rows there are. One kernel | two, us: 8 requests x 3 tokens 72 | 30, 8 x 8 32 | 23,
+  // 1 x 16 22 | 13, 1 x 32 22 | 20, 1 x 40 22 | 23, 32 x 4 53 | 54, 16 x 8 32 | 38, 8 x 16 22 | 38, 1 x 2048 143 | 224; 512 pages: 1 x 32
+  // (head_dim 64) 11.6 | 18.3, 96 x 3 34 | 55, 64 x 4 26 | 39; 256 pages: 1 x 16 10.6 | 12.0. One token a request, 8 of them: 22 | 14.
+  const long long all_rows = (long long)n_tokens * cache->n_kv_heads, passes = (CF_TOKENS + each - 1) / (each < 1 ? 1 : each);
+  int sms = 0;
+  cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, device);
+  if (sms <= 0) sms = 148;
+  if (each > 2 && cache->max_pages <= CF_MOST && all_rows * (CF_MOST / 2) >= sms * passes * cache->max_pages) {
     const bool wide = cache->head_dim == 128, bf16 = q->dtype == DD_BF16;
     const void* f = wide ? (bf16 ? (const void*)dd_cache_select_kernel<__nv_bfloat16, 128> : (const void*)dd_cache_select_kernel<__half, 128>)
                          : (bf16 ? (const void*)dd_cache_select_kernel<__nv_bfloat16, 64> : (const void*)dd_cache_select_kernel<__half, 64>);
