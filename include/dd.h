@@ -456,6 +456,9 @@ int dd_cache_landmarks(const dd_cache* cache, const int* ctx_len, int n_last, vo
  * others; equal scores go to the lower page.
  *   c        = the sum of the group's query rows (in 64 bits), as whole numbers within 127 like a landmark's (e not below -120)
  *   score[p] = <c, codes of the landmark of p> * 2^e: exact in fp32
+ * The set is that of these rounded scores, which is not quite that of the dot products of sum and mean (8 bits a channel, with one power of two: less is left
+ * for the others where a few channels are far larger), and another one than that of the maximum of the heads' probabilities by which
+ * dd_select_topk ranks.
  * Padding, and a token whose request or position is out of range (reported in status), gets -1 throughout; a table entry out of range is reported and
  * its page scores 0.
  *   q          dev [n_tokens][n_q_heads][head_dim], bf16 or half whatever the format of the pages (which are not read)
@@ -468,10 +471,12 @@ int dd_cache_select(const dd_cache* cache, int n_tokens, const int* positions, c
                     size_t workspace_bytes, void* stream);
 
 /* Attention of every query token over the tokens up to its own position in the pages listed for it:
- *   z[i] = <q[n, h, :], K[i, h / G, :]> * scale, i over the tokens of pages idx[n][h / G][0 .. k_pages)   scale 0 = 1 / sqrt(head_dim)
+ *   z[i] = <q[n, h, :], K[i, h / G, :]> * scale, i over the tokens of pages idx[n][h / G][0 .. m)   scale 0 = 1 / sqrt(head_dim)
+ *   m    = min(k_pages, positions[n] / page_tokens + 1): the entries in front, as many as there are pages up to the token's own
  *   out[n, h, :] = sum softmax(z) * V;  out_lse = ln sum exp(z)
- * Entries in any order; -1 is no page, one behind the token's own page has nothing to see, one out of range is reported in status and passed over; a
- * page listed twice counts twice. At most as many entries are looked at as there are pages up to the token's own: those in front. A token
+ * Of these entries, in any order: -1 is no page, one behind the token's own page has nothing to see, one out of range is reported in status and passed
+ * over; a page listed twice counts twice. They count towards m all the same: early in a context, holes and repeats in front keep pages behind them from
+ * being looked at, so a list has its pages in front, as dd_cache_select gives them. A token
  * that sees nothing gives zeros and -inf. The rows of padding, and of a token whose request or position is out of range (reported), stay as they are.
  * A table entry out of range is reported and its page reads as zeros.
  *   q, out     dev [n_tokens][n_q_heads][head_dim], one dtype (that of a 16-bit cache); out may be q itself

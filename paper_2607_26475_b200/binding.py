@@ -508,7 +508,8 @@ class PagedCache:
 
     def select(self, q, landmarks, positions, idx, requests=None, *, first_pages=0, recent_pages=1, workspace=None, stream=None):
         """The pages of every query token and KV head into idx [N, Hkv, k] int32 (ascending, -1 behind them): the first first_pages,
-        the last recent_pages, and those with the highest scores. q [N, Hq, d]; positions, requests [N] int32 as for append."""
+        the last recent_pages, and those with the highest scores (of the summed query heads and the landmarks, both as 8-bit whole
+        numbers). q [N, Hq, d]; positions, requests [N] int32 as for append."""
         n, k, p, r, i = self._listed(positions, idx, requests)
         if not (0 <= first_pages <= k and 1 <= recent_pages <= k):
             raise _invalid(f"first_pages ({first_pages}) and recent_pages ({recent_pages}, at least 1) must fit the {k} pages of idx")
@@ -524,7 +525,9 @@ class PagedCache:
             _raise_last(rc)
 
     def sparse_attn(self, q, idx, positions, out, out_lse=None, requests=None, *, scale=0.0, workspace=None, stream=None):
-        """Attention of every query token over the pages idx [N, Hkv, k] listed for it, up to its own position. q, out [N, Hq, d];
+        """Attention of every query token over the pages idx [N, Hkv, k] listed for it, up to its own position. Only the entries in front are
+        looked at, as many as there are pages up to the token's own, holes (-1) and repeats among them: pages come first, -1 behind
+        them, as select gives them. q, out [N, Hq, d];
         positions, requests [N] int32 as for append; out_lse [N, Hq] float32. Without a workspace the call takes one from torch's
         allocator on the stream it runs on."""
         n, k, p, r, i = self._listed(positions, idx, requests)

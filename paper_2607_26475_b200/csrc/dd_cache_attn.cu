@@ -31,14 +31,17 @@
 // token (8 at head_dim 64: half of that), the MMA's slots take the channels in the order in which the nibbles come out, and the query rows are
 // dealt to match; V lies by token pairs and eighths of the channels, so that a register's two halves are two tokens and nothing is transposed. Row
 // exponents are used as for e4m3, the factor 2^17 comes back with the scores and at the end. A tile is copied whole, two complete ones are taken at a
-// time. Per tile of 2336 bytes 350 instructions, of which 144 turn nibbles into halves: instructions bound it, not bytes.
+// time. Per tile of 2336 bytes 350 instructions, of which 144 turn nibbles into halves. 8 x 32768 tokens are 47 us of bytes and 39 us of
+// issue slots, and take 74.5: four warps a scheduler do not cover the latencies and the pipes' turns between the two.
 //
 // Rounding. A weight enters the second product as two 16-bit parts, its value cut off and the rounded rest (an MMA takes both
 // operands in one type): off by 2^-16 relative at most for bf16 pages, by 2^-22 for half pages and half queries, so that the
 // output's own rounding is the one that shows. One part (2^-8, 2^-11) left an error of 0.0023 relative on 4096 bf16 tokens where
 // the output's rounding alone is 0.00165 (half: 0.00028 for 0.00021). The second part costs 168.1 -> 169.4 us on 8 x 32K tokens
 // of bf16, 9.8 -> 10.1 us on 4096, and the same for half. e4m3 pages with bf16 queries go without: half weights (2^-11) are an
-// eighth of the output's half step (0.00162 against 0.00161), and the part would cost 369 -> 375 us on 1M tokens; so do 4-bit pages. Halves end at
+// eighth of the output's half step (0.00162 against 0.00161), and the part would cost 369 -> 375 us on 1M tokens; so do 4-bit pages with
+// bf16 queries (errors of 0.00167 for 0.00166), where it would cost more: 8 x 32768 tokens 74 -> 84 us, 1M 241 -> 279, 48 ragged requests 60 -> 67, 2048
+// tokens of 64 listed pages 596 -> 677. Halves end at
 // 2^-24: a weight more than 2^31 below the reference is dropped, one above is off by 2^-31 of the reference at most. Queries as
 // said, the output once. Scores, reference, denominators, accumulators and partial results are fp32.
 //
@@ -53,7 +56,7 @@
 // (6.4 TB/s, a copy's rate), e4m3 105 us (5.2 TB/s; twice the instructions per byte, and four warps a scheduler do not cover
 // their latencies), one request of 1M tokens e4m3 370-378 us (5.8 TB/s; 393 in passes that follow one another), 48 requests of 0
 // to 32768 tokens e4m3 78-79 us, one request of 4096 tokens 10.0 us (13.2 where the table is 8192 pages wide). 4-bit pages: 8 x 32768 tokens
-// (2 query tokens) 74.5 us (4.1 TB/s; 58% of the cycles issue, the ALU is busy for 46% of them), 1M tokens 242 us (5.1 TB/s), the ragged 48 60 us, 4096
+// (2 query tokens) 74.5 us (4.1 TB/s; 58% of the cycles issue), 1M tokens 242 us (5.1 TB/s), the ragged 48 60 us, 4096
 // tokens 11.1 us, 100 tokens 7.9 us.
 #include "dd_cache_attn.cuh"
 

@@ -1572,7 +1572,7 @@ inline int ca_cluster_of(long long units, long long tiles, int blocks) {
 // Rows of a unit that go through the MMA together: up to 8 in one column tile, up to 16 in two.
 inline int ca_column_tiles(int rows) { return rows <= 8 ? 1 : 2; }
 
-// The same for 4-bit pages and for listed pages, whose tiles take more instructions than bytes: short units too go to the warps of a block
+// The same for 4-bit pages and for listed pages, whose tiles take longer to work on than to bring: short units too go to the warps of a block
 // (a cluster of one: 7 tiles one after the other in one warp 11.7 us, 7.9 side by side), and clusters as large as all units leave
 // room for, up to two tiles a warp.
 inline int ca_cluster_spread(long long units, long long tiles, int blocks) {
@@ -1593,8 +1593,10 @@ template <int SP> ca_plan ca_pick(int format, int d, int nt) {
   }
 }
 
-// Empty places behind a unit, for what it costs besides its tiles: more where the tiles take less time. 48 requests of 0 to 32K tokens
-// of 4-bit pages: 3 places 68 us, 5 60.7, 8 59.9, 12 61.5; e4m3 pages listed for 481 ragged tokens: 3 41.8, 5 38.1, 8 40.5.
+// Empty places behind a unit, for what it costs besides its tiles, by measurement (us with 3 | 5 | 8 places). 4-bit pages: 48 requests of 0 to 32K
+// tokens 68 | 60.2 | 59.5 (12: 61.5), at head_dim 64 49.7 | 43.2 | 40.1, 100 requests of up to 5000 47.6 | 46.4 | 46.1. Listed pages, 481 ragged
+// tokens at head_dim 64: e4m3 41.8 | 38.2 | 40.5, half 41.7 | 37.7 | 40.7, 4 bits 42.8 | 40.2 | 40.3; 450 at head_dim 128, a group of five: bf16
+// 137.0 | 137.8 | 147.3, e4m3 119.7 | 120.1 | 120.3, 4 bits 134.6 | 124.5 | 122.6.
 inline int ca_unit_cost(int cache_format, bool listed) { return cache_format == DD_CACHE_INT4 ? 8 : (listed ? 5 : 3); }
 
 // Kernel format of a cache's pages and a type of queries.

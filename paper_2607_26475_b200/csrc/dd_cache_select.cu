@@ -7,12 +7,15 @@
 // and with them the chosen set, are defined to the last bit. (Adding up the group's rows orders pages as the product of the heads'
 // soft-max probabilities does: what a head's soft-max divides by is the same for all pages.)
 //
-// Scores: 8-bit whole-number MMAs. Few tokens a request: a block per token, which reads each landmark once (HBM bound: 144 bytes
-// a page and head); many: 64 tokens of a head stay in registers while the pages go by. The keys (scores in an order that
-// compares as unsigned numbers) of a bounded number of tokens go through a workspace that L2 holds.
+// Scores: 8-bit whole-number MMAs. They are kept as keys, numbers that compare as the scores do. Two ways, by the rule in dd_cache_select:
+//   prompt chunks, many tokens   one kernel for scores and choice: 16 tokens of a head a block, the keys of all pages in shared memory
+//   few rows, wide tables        a scoring kernel (1, 8 or 64 tokens a block) leaves the keys of a bounded number of tokens in a workspace that L2
+//                                holds, a second one chooses. One token a block reads each landmark once (HBM: 144 bytes a page and head)
 //
-// Choice: bisection for the k-th largest key: a step counts keys at or above the middle. It stops as soon as exactly k are (about a dozen
-// steps); all the steps come up only with ties, which go to the lower pages.
+// Choice: the k-th largest of the maxima of small groups of keys bounds the k-th largest key from below, and the keys from there on, little more
+// than k, are listed in shared memory. Few rows: every listed key's rank among the listed ones decides. Else one warp finds the k-th
+// largest by bisection, a step counting keys at or above the middle, until exactly k are. Where too many are listed (ties, long lists)
+// the bisection is over all keys. Equal keys go to the lower pages.
 #include "dd_cache.cuh"
 
 namespace {
@@ -42,8 +45,8 @@ constexpr int CS_TAIL = 16;                            // bytes behind the codes
 constexpr int CS_LM_LEAST = -64, CS_Q_LEAST = -120;
 
 // ---- landmarks: a page and head at a time to a warp, D / 32 channels a lane. A warp takes `per` of them in a row (up to CL_PER): its lanes
-// find the pages together, so that the chain length -> table entry -> keys is waited for once a warp. Bound: instructions (0.62 to 0.7 issued a
-// cycle and scheduler; a widening to 64 bits and an addition for each key's channel), in flight 16 rows a warp. 8 x 2048 pages of 8 heads of
+// find the pages together, so that the chain length -> table entry -> keys is waited for once a warp. Bound: the 64-bit
+// pipe (a widening to 64 bits and an addition for each key's channel; 0.62 to 0.7 instructions issued a cycle and scheduler), in flight 16 rows a warp. 8 x 2048 pages of 8 heads of
 // 128: bf16 130 us (4.1 TB/s; one a warp 157), e4m3 148 (174), 4 bits 196 (217).
 constexpr int CL_THREADS = 256, CL_PER = 8;            // in a row at most (32: 162 us where 8 took 141, the last warps being alone for too long)
 // Blocks an SM: 16 rows of 16-bit keys of 128 take 32 registers, with four blocks 140 us; the others are the faster for a fourth (e4m3 158 -> 148 us).
@@ -726,8 +729,8 @@ __global__ void __launch_bounds__(CR_ROW_THREADS) dd_cache_topk_rank_kernel(cons
 // ---- scores and choice in one, where the keys of a row fit shared memory: 16 tokens of one head against all of their pages.
 // A warp brings the landmarks of 8 pages of every group of CF_PAGES, several groups ahead, multiplies them and leaves the keys in shared
 // memory; then it chooses for one of the tokens. The lists of the choice lie where the landmarks were. One block an SM; what
-// bounds it is instructions at four warps a scheduler (0.43 issued a cycle), a third of them the choice's. 2048 tokens x 2048 pages x 8 heads: 143 us (two
-// kernels with the keys in the workspace: 165).
+// bounds it is latency at four warps a scheduler: the 78 M instructions of 2048 tokens x 2048 pages x 8 heads, a third of them the choice's, are 67 us
+// of issue slots and take 143 us (two kernels with the keys in the workspace: 224).
 constexpr int CF_PAGES = 128, CF_THREADS = 512, CF_TOKENS = 16;
 constexpr int CF_STAGES = 4;
 constexpr int CF_LIST = 256;                           // of a row
@@ -1007,7 +1010,9 @@ extern "C" int dd_cache_select(const dd_cache* cache, int n_tokens, const int* p
   a.recent = recent_pages;
   a.stride = cs_stride(cache->max_pages);
   const int each = n_tokens / cache->batch;
-  // Tokens of a block: one where requests bring one or two (every token reads its own landmarks), up to 64 where they bring many.
+  // Tokens of a block: one where requests bring one or two (every token reads its own landmarks), up to 64 where they bring many. 8 requests
+  // x 4096 pages x 8 heads, us with 1 | 8 | 64 tokens a block: 1 token each 20 | 41 | 73, 2 29 | 30 | 73, 3 41 | 35 | 78, 16 169 | 55 | 67, 31 302 | 95 | 73,
+  // 64 616 | 163 | 82; one request of 31 tokens 48 | 20 | 26.
   const int tt = each <= 2 ? 1 : (each < 32 ? 8 : 64);
   const int once = cs_tokens_at_once(n_tokens, cache->n_kv_heads, cache->max_pages);
   a.codes = (signed char*)((char*)workspace + (size_t)once * cache->n_kv_heads * a.stride * 4);

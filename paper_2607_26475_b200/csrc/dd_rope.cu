@@ -15,8 +15,8 @@
 // and two blocks.
 //
 // Measured on a B200: 32768 tokens of 32 + 8 heads of 128 bf16, rotation 102.5 us (6.55 TB/s, a copy's rate); the same with
-// 8 + 8 heads of K and V into e4m3 pages 120 us (6.2 TB/s); into 4-bit pages 163 us (4.35 TB/s): instructions and their latencies, 45% of
-// the cycles issue and 14 warps an SM wait for what they loaded; 8 tokens 2.1 us (4-bit 3.6), one launch.
+// 8 + 8 heads of K and V into e4m3 pages 120 us (6.2 TB/s); into 4-bit pages 163 us (4.35 TB/s): 108 us of bytes and 65 us of
+// issue slots, one after the other, since 14 warps an SM wait for a batch of rows and then work on it; 8 tokens 2.1 us (4-bit 3.6), one launch.
 #include <math.h>
 
 #include <type_traits>
